@@ -48,8 +48,9 @@ typedef enum evospec_status {
     EVOSPEC_INVALID_IDS = 7,        /* evospec_validate_ids only                          */
     EVOSPEC_HIP_ERROR = 8,          /* a launch failed; text via evospec_last_hip_error() */
     EVOSPEC_BAD_LAYOUT = 9,         /* layout is neither EVOSPEC_ROW_MAJOR nor EVOSPEC_PACKED */
-    EVOSPEC_STATIC_SCRATCH_EXCEEDED = 10 /* evospec_active_lmhead_topk_static: the shapes need more
+    EVOSPEC_STATIC_SCRATCH_EXCEEDED = 10, /* evospec_active_lmhead_topk_static: the shapes need more
                                             scratch than EVOSPEC_STATIC_SCRATCH_BYTES             */
+    EVOSPEC_BAD_TYPE = 11           /* an element type or kind of cache that the call does not take */
 } evospec_status;
 
 /*

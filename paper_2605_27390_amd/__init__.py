@@ -32,3 +32,12 @@ from .binding import (  # noqa: F401
     kl_gate_workspace_bytes,
 )
 from .arc import ArcManager, form_candidates, path_a_event, path_a_workspace_bytes  # noqa: F401,E402
+from .decode import (  # noqa: F401,E402
+    KVCache,
+    kv_attention,
+    kv_attention_workspace_bytes,
+    kv_read,
+    kv_write,
+    sample,
+    sample_workspace_bytes,
+)

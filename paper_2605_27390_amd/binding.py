@@ -17,7 +17,7 @@ M_TILE = 64
 STATUS = {
     0: "OK", 1: "NULL_POINTER", 2: "BAD_SHAPE", 3: "BAD_K", 4: "MISALIGNED",
     5: "WORKSPACE_TOO_SMALL", 6: "BAD_SEGMENTS", 7: "INVALID_IDS", 8: "HIP_ERROR", 9: "BAD_LAYOUT",
-    10: "STATIC_SCRATCH_EXCEEDED",
+    10: "STATIC_SCRATCH_EXCEEDED", 11: "BAD_TYPE",
 }
 STATIC_SCRATCH_BYTES = 8 << 20
 ROW_MAJOR = 0

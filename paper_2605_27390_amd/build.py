@@ -10,10 +10,11 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libevospec.so")
-SOURCES = ["kernels.hip", "gemm.hip", "tile.hip", "narrow.hip", "klgate.hip", "noalloc.hip", "api.cpp", "arc.cpp", "path_a.cpp"]
+SOURCES = ["kernels.hip", "gemm.hip", "tile.hip", "narrow.hip", "klgate.hip", "noalloc.hip", "kvcache.hip", "attention.hip", "sample.hip",
+           "api.cpp", "decode.cpp", "arc.cpp", "path_a.cpp"]
 OBJECTS = os.path.join(HERE, "_build")
-HEADERS = ["plan.hpp", "launch.hpp", "common.hpp", "slab.hpp", "slab_epilogue.hpp", os.path.join(ROOT, "include", "evospec.h"),
-           os.path.join(ROOT, "include", "evospec_arc.h")]
+HEADERS = ["plan.hpp", "launch.hpp", "common.hpp", "slab.hpp", "slab_epilogue.hpp", "decode.hpp", os.path.join(ROOT, "include", "evospec.h"),
+           os.path.join(ROOT, "include", "evospec_arc.h"), os.path.join(ROOT, "include", "evospec_decode.h")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

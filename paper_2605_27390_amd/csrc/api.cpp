@@ -7,6 +7,7 @@
 #include <cstdio>
 #include <cstring>
 
+#include "decode.hpp"
 #include "evospec.h"
 #include "launch.hpp"
 #include "plan.hpp"
@@ -76,6 +77,7 @@ const char* evospec_status_string(int status) {
         case EVOSPEC_BAD_LAYOUT: return "layout must be EVOSPEC_ROW_MAJOR or EVOSPEC_PACKED";
         case EVOSPEC_STATIC_SCRATCH_EXCEEDED:
             return "shapes need more scratch than EVOSPEC_STATIC_SCRATCH_BYTES (use the workspace variant)";
+        case EVOSPEC_BAD_TYPE: return "an element type or kind of cache that the call does not take";
         default: return "unknown status";
     }
 }
@@ -248,6 +250,7 @@ int head_impl(const void* h, int M, int d, const void* W_act, const int32_t* ids
 }
 
 int record_hip_error(hipError_t e) { return hip_fail(e); }
+int device_compute_units(int* out) { return device_num_cu(out); }
 }  // namespace evospec
 
 extern "C" {

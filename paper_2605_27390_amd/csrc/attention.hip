@@ -1,0 +1,468 @@
+// Attention over the 8-bit cache: o = sum softmax(scale q.k) v for the rows of single tokens, draft trees and chunks.
+//
+// The query heads that share a key/value head are rows side by side (row r = token r / group, head r % group), in tiles of
+// 32: the score tile S^T = K Q^T of a block of 32 tokens is one accumulator of v_mfma_f32_32x32x16, in which a lane holds 16
+// tokens of one row.  What a lane needs of a row's maximum and sum is therefore its own registers and one exchange between
+// the halves of the wavefront; the same 16 probabilities, rounded to fp16, are the second operand of O^T += V^T P^T as they are,
+// because the cache keeps V's tokens in that order; and a row's rescaling is one factor per lane.  K and V come from
+// memory as 16-byte pieces that are operands after conversion (8 bits to the query's type, or to fp16: exact), so
+// nothing of them goes through LDS.
+//
+// One pass over the tokens (running maximum and sum).  With s_k, s_v the scales of a block, t = x log2(e) + log2(s_v)
+// has the running reference M (of the lane's row), p = 2^(t - M) is at most 2^kSlack whatever the scales are, and
+//   l += sum p / s_v,   O += sum p code_v,   so out = O / l,   lse = (M + log2 l) ln 2.
+// p is rounded to fp16 (2^-11 of itself): the smallest normal fp16 is 2^-14 of the reference, and what is below keeps an
+// absolute error of 2^-25 of it.
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "common.hpp"
+#include "decode.hpp"
+
+namespace evospec {
+namespace {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kNone = -3.0e38f;                 // the reference of a row that has seen nothing
+constexpr float kSlack = 6.f;                     // a row's reference moves when a score passes it by more than that
+
+// 8 codes of two dwords as an operand of fp16 or bf16 elements
+template <int KIND, bool HALF>
+__device__ __forceinline__ u32x4 widen(uint32_t lo, uint32_t hi) {
+    u32x4 out;
+    const uint32_t in[2] = {lo, hi};
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        if constexpr (KIND == EVOSPEC_KV_E4M3 && HALF) {
+            out[2 * j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(in[j], 1.f, false));
+            out[2 * j + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(in[j], 1.f, true));
+        } else if constexpr (KIND == EVOSPEC_KV_E4M3) {
+            out[2 * j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(in[j], 1.f, false));
+            out[2 * j + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(in[j], 1.f, true));
+        } else if constexpr (HALF) {
+            // fp16 0x6400 + u is 1024 + u: the code with its sign bit flipped, 1,152 too much
+            const uint32_t u = in[j] ^ 0x80808080u;
+            const f16x2 off = {(_Float16)1152.f, (_Float16)1152.f};
+            const f16x2 a = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) - off;
+            const f16x2 b = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) - off;
+            out[2 * j] = __builtin_bit_cast(uint32_t, a);
+            out[2 * j + 1] = __builtin_bit_cast(uint32_t, b);
+        } else {
+            // a whole number below 256 has its bits in the upper half of a float
+            uint32_t f[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[i] = __float_as_uint((float)(int8_t)(in[j] >> (8 * i)));
+            out[2 * j] = __builtin_amdgcn_perm(f[1], f[0], 0x07060302u);
+            out[2 * j + 1] = __builtin_amdgcn_perm(f[3], f[2], 0x07060302u);
+        }
+    }
+    return out;
+}
+// The same with the NaN code's values: NaN for int8 (e4m3 has it already).
+template <int KIND, bool HALF>
+__device__ __forceinline__ u32x4 widen_nan(uint32_t lo, uint32_t hi) {
+    u32x4 out = widen<KIND, HALF>(lo, hi);
+    if constexpr (KIND == EVOSPEC_KV_INT8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t code = ((i < 4 ? lo : hi) >> (8 * (i & 3))) & 255u;
+            if (code == 0x80u) out[i >> 1] |= 0x7fffu << (16 * (i & 1));       // NaN in both types
+        }
+    }
+    return out;
+}
+
+template <bool HALF>
+__device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
+    if constexpr (HALF)
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+__device__ __forceinline__ float other_half(float x, int lane) { return __uint_as_float(xor_lane<32>(__float_as_uint(x), lane)); }
+
+// 0xff in every byte of x that is a NaN code
+template <int KIND>
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t x) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t c = (x >> (8 * i)) & 255u;
+        if (KIND == EVOSPEC_KV_E4M3 ? (c & 0x7fu) == 0x7fu : c == 0x80u) m |= 255u << (8 * i);
+    }
+    return m;
+}
+
+// NQ: dim / 32.  RT: tiles of 32 rows of a wavefront.  WR x WT wavefronts over rows and tokens.
+template <int NQ, int KIND, bool HALF, int RT, int WR, int WT>
+__global__ __launch_bounds__(64 * WR * WT) void kv_attention_kernel(AttnArgs A) {
+    constexpr int kDim = 32 * NQ, kRows = 32 * RT * WR, kWaves = WR * WT;
+    constexpr int kPad = 36;                                     // floats of a row of 32 in LDS
+    __shared__ __align__(16) float s_o[2][kWaves][32 * kPad];
+    __shared__ float2 s_ml[kWaves][RT * 32];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, half = lane >> 5;
+    const int wr = wave / WT, wt = wave % WT;
+    int id = blockIdx.x;
+    const int split = id % A.splits;
+    id /= A.splits;
+    const int tile = id % A.tiles;
+    id /= A.tiles;
+    const int head = id % A.c.heads, s = id / A.c.heads;
+    const Rows& R = A.r;
+    const int n0 = min(max(R.row_off[s], 0), R.T), n1 = min(max(R.row_off[s + 1], n0), R.T);
+    const int n_all = n1 - n0, n = min(n_all, R.max_rows);
+    const int rows = n * A.group, r0 = tile * kRows;
+    if (r0 >= rows) return;
+    const int len = (int)min((long long)max(R.at[s], 0), (long long)R.width << (A.c.shift + 5));
+    const int base = len - n_all;                                // the position of row 0 (may be negative)
+    // tokens [0, full) are seen by every row of the workgroup, tokens [hi, len) by none
+    const int i_first = r0 / A.group, i_last = (min(rows, r0 + kRows) - 1) / A.group;
+    const int full = max(0, A.tree ? base : base + i_first + 1);
+    const int hi = max(0, A.tree ? len : base + i_last + 1);
+    const int blocks = (hi + kBlock - 1) / kBlock;
+    const int b_lo = (int)((long long)blocks * split / A.splits), b_hi = (int)((long long)blocks * (split + 1) / A.splits);
+
+    // the rows' queries, as second operands
+    u32x4 qf[RT][NQ][2];
+    int last_seen[RT];                                           // causal: the row's own position
+    uint64_t bits[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int r = r0 + (wr * RT + rt) * 32 + col;
+        const bool ok = r < rows;
+        const int i = ok ? r / A.group : 0, a = ok ? r % A.group : 0;
+        last_seen[rt] = ok ? base + i : -1;
+        bits[rt] = ok && A.tree ? A.tree[n0 + i] : 0;
+        const uint16_t* q = static_cast<const uint16_t*>(A.q) + (long long)(n0 + i) * A.q_stride + (long long)(head * A.group + a) * kDim + 16 * half;
+#pragma unroll
+        for (int k = 0; k < NQ; ++k)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                qf[rt][k][j] = ok ? *reinterpret_cast<const u32x4*>(q + 32 * k + 8 * j) : u32x4{0, 0, 0, 0};
+    }
+
+    f32x16 o[RT][NQ];
+    float m[RT], l[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        m[rt] = kNone;
+        l[rt] = 0.f;
+#pragma unroll
+        for (int k = 0; k < NQ; ++k)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[rt][k][e] = 0.f;
+    }
+
+    const int mask = (1 << A.c.shift) - 1;
+    for (int b = b_lo + wt; b < b_hi; b += WT) {
+        const int page = __builtin_amdgcn_readfirstlane(R.table[(long long)s * R.width + (b >> A.c.shift)]);
+        if ((unsigned)page >= (unsigned)A.c.pages) continue;     // (uniform)
+        const long long at = (((long long)page * A.c.heads + head) << A.c.shift) + (b & mask);
+        const uint8_t* data = A.c.data + at * (2 * kBlock * kDim) + lane * 16;
+        const float2 sc = *reinterpret_cast<const float2*>(A.c.scales + at * 2);
+        u32x4 kr[NQ], vr[NQ];
+#pragma unroll
+        for (int k = 0; k < NQ; ++k) kr[k] = *reinterpret_cast<const u32x4*>(data + k * 1024);
+#pragma unroll
+        for (int k = 0; k < NQ; ++k) vr[k] = *reinterpret_cast<const u32x4*>(data + kBlock * kDim + k * 1024);
+
+        const bool has_nan = (__float_as_uint(sc.x) | __float_as_uint(sc.y)) >> 31;   // (uniform)
+        const float ck = fmaxf(fabsf(sc.x) * (A.scale * kLog2e), 0x1p-126f);       // (not zero: -inf stays what it is)
+        const float sv = fabsf(sc.y), lv = __log2f(sv), iv = 1.f / sv;
+
+        f32x16 x[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[rt][e] = 0.f;
+#pragma unroll
+        for (int k = 0; k < NQ; ++k)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const u32x4 a = has_nan ? widen_nan<KIND, HALF>(kr[k][2 * j], kr[k][2 * j + 1]) : widen<KIND, HALF>(kr[k][2 * j], kr[k][2 * j + 1]);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) x[rt] = mfma<HALF>(a, qf[rt][k][j], x[rt]);
+            }
+
+        const int t0 = b * kBlock;
+        uint32_t seen[RT];                                       // bit e: the lane's row sees token 8 (e / 4) + 4 half + e % 4
+        const bool whole = t0 + kBlock <= full;                  // (uniform)
+        if (!whole) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                seen[rt] = 0;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int t = t0 + 8 * (e / 4) + 4 * half + e % 4;
+                    bool ok;
+                    if (A.tree) {
+                        const int j = t - base;
+                        ok = t < len && (j < 0 || (j < 64 && ((bits[rt] >> j) & 1)));
+                        ok = ok && last_seen[rt] >= base && j < n_all;
+                    } else {
+                        ok = t <= last_seen[rt];
+                    }
+                    seen[rt] |= (uint32_t)ok << e;
+                    x[rt][e] = ok ? x[rt][e] : -__builtin_inff();
+                }
+            }
+        }
+        u32x4 pf[RT][2];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            float top = x[rt][0];
+#pragma unroll
+            for (int e = 1; e < 16; ++e) top = fmaxf(top, x[rt][e]);
+            top = fmaxf(top, other_half(top, lane));
+            const float t = top * ck + lv;
+            if (__ballot(t > m[rt] + kSlack)) {
+                const float next = fmaxf(m[rt], t);
+                const float f = __builtin_amdgcn_exp2f(m[rt] - next);
+                m[rt] = next;
+                l[rt] *= f;
+#pragma unroll
+                for (int k = 0; k < NQ; ++k)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[rt][k][e] *= f;
+            }
+            const float c0 = lv - m[rt];
+            float sum = 0.f;
+            f16x8 p[2];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const float y = __builtin_amdgcn_exp2f(x[rt][e] * ck + c0);
+                sum += y;
+                p[e >> 3][e & 7] = (_Float16)y;
+            }
+            l[rt] += sum * iv;
+            pf[rt][0] = __builtin_bit_cast(u32x4, p[0]);
+            pf[rt][1] = __builtin_bit_cast(u32x4, p[1]);
+        }
+        if (t0 + kBlock > len) {                                 // bytes behind the last token may be anything
+#pragma unroll
+            for (int k = 0; k < NQ; ++k)
+#pragma unroll
+                for (int a = 0; a < 4; ++a) {
+                    const int left = len - (t0 + 8 * a + 4 * half);
+                    vr[k][a] &= left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
+                }
+        }
+        if (has_nan) {
+            // A NaN reaches the rows that see its token, and no others: rows by tokens that are seen (0 or 1) against
+            // tokens by dims that are NaN (0 or 1); what is not zero in that product becomes NaN.
+#pragma unroll
+            for (int k = 0; k < NQ; ++k) {
+                u32x4 nb;
+#pragma unroll
+                for (int a = 0; a < 4; ++a) {
+                    nb[a] = nan_bytes<KIND>(vr[k][a]);
+                    vr[k][a] &= ~nb[a];
+                }
+                if (!__ballot((nb[0] | nb[1] | nb[2] | nb[3]) != 0)) continue;
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    f32x16 hit;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) hit[e] = 0.f;
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        f16x8 is, sees;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            is[e] = (nb[2 * y + (e >> 2)] >> (8 * (e & 3))) & 1 ? (_Float16)1.f : (_Float16)0.f;
+                            sees[e] = whole || ((seen[rt] >> (8 * y + e)) & 1) ? (_Float16)1.f : (_Float16)0.f;
+                        }
+                        hit = mfma<true>(__builtin_bit_cast(u32x4, is), __builtin_bit_cast(u32x4, sees), hit);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[rt][k][e] = hit[e] > 0.f ? __uint_as_float(0x7fc00000u) : o[rt][k][e];
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < NQ; ++k)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const u32x4 a = widen<KIND, true>(vr[k][2 * y], vr[k][2 * y + 1]);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) o[rt][k] = mfma<true>(a, pf[rt][y], o[rt][k]);
+            }
+    }
+
+    // the wavefronts that share rows: one reference, and their shares of it
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        l[rt] += other_half(l[rt], lane);
+        if (half == 0) s_ml[wave][rt * 32 + col] = make_float2(m[rt], l[rt]);
+    }
+    __syncthreads();
+    float mm[RT], ll[RT], f[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        mm[rt] = kNone;
+#pragma unroll
+        for (int w = 0; w < WT; ++w) mm[rt] = fmaxf(mm[rt], s_ml[wr * WT + w][rt * 32 + col].x);
+        ll[rt] = 0.f;
+#pragma unroll
+        for (int w = 0; w < WT; ++w) {
+            const float2 ml = s_ml[wr * WT + w][rt * 32 + col];
+            ll[rt] += ml.y * __builtin_amdgcn_exp2f(ml.x - mm[rt]);
+        }
+        f[rt] = __builtin_amdgcn_exp2f(m[rt] - mm[rt]);
+        if (ll[rt] > 0.f) f[rt] /= ll[rt];                       // (NaN sums divide as well, below)
+        else if (ll[rt] != ll[rt]) f[rt] = ll[rt];
+        const int r = r0 + (wr * RT + rt) * 32 + col;
+        if (wt == 0 && half == 0 && r < rows) {
+            const long long row = (long long)(n0 + r / A.group) * (A.c.heads * A.group) + head * A.group + r % A.group;
+            if (A.splits > 1) A.part_ml[(long long)split * R.T * A.c.heads * A.group + row] = make_float2(mm[rt], ll[rt]);
+            else if (A.lse) A.lse[row] = ll[rt] == 0.f ? -__builtin_inff() : (mm[rt] + __log2f(ll[rt])) * kLn2;
+        }
+    }
+    // O, 32 dims at a time: every wavefront's share to LDS, summed in a fixed order on the way out
+    int buf = 0;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int k = 0; k < NQ; ++k) {
+            float* mine = s_o[buf][wave] + col * kPad + 4 * half;
+#pragma unroll
+            for (int a = 0; a < 4; ++a)
+                *reinterpret_cast<float4*>(mine + 8 * a) = make_float4(o[rt][k][4 * a] * f[rt], o[rt][k][4 * a + 1] * f[rt],
+                                                                       o[rt][k][4 * a + 2] * f[rt], o[rt][k][4 * a + 3] * f[rt]);
+            __syncthreads();
+            for (int e = tid; e < WR * 32 * 8; e += 64 * kWaves) {
+                const int g = e >> 8, c = (e >> 3) & 31, d4 = e & 7;
+                const int r = r0 + (g * RT + rt) * 32 + c;
+                if (r >= rows) continue;
+                float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int w = 0; w < WT; ++w) {
+                    const float4 v = *reinterpret_cast<const float4*>(s_o[buf][g * WT + w] + c * kPad + 4 * d4);
+                    sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+                }
+                const long long row = (long long)(n0 + r / A.group) * (A.c.heads * A.group) + head * A.group + r % A.group;
+                const int d = 32 * k + 4 * d4;
+                if (A.splits > 1) {
+                    *reinterpret_cast<float4*>(A.part_o + ((long long)split * R.T * A.c.heads * A.group + row) * kDim + d) = sum;
+                } else if constexpr (HALF) {
+                    typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+                    *reinterpret_cast<f16x4*>(static_cast<_Float16*>(A.out) + row * kDim + d) = f16x4{(_Float16)sum.x, (_Float16)sum.y, (_Float16)sum.z, (_Float16)sum.w};
+                } else {
+                    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+                    *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(A.out) + row * kDim + d) = bf16x4{(__bf16)sum.x, (__bf16)sum.y, (__bf16)sum.z, (__bf16)sum.w};
+                }
+            }
+            buf ^= 1;
+        }
+}
+
+// The shares of a row's splits, each a mean over its tokens with a reference and a sum, in their order: one wavefront a row.
+template <int NQ, bool HALF>
+__global__ __launch_bounds__(256) void kv_attention_merge_kernel(AttnArgs A) {
+    constexpr int kDim = 32 * NQ;
+    const int lane = threadIdx.x & 63;
+    const int heads = A.c.heads * A.group;
+    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6), all = (long long)A.r.T * heads;
+    if (row >= all) return;
+    // a row of no sequence has no shares
+    const int token = (int)(row / heads);
+    bool mine = false;
+    for (int s = lane; s < A.r.S; s += 64) {
+        const int n0 = min(max(A.r.row_off[s], 0), A.r.T), n1 = min(max(A.r.row_off[s + 1], n0), A.r.T);
+        mine |= token >= n0 && token < min(n1, n0 + A.r.max_rows);
+    }
+    if (!__ballot(mine)) return;
+    float m = kNone;
+    for (int j = lane; j < A.splits; j += 64) m = fmaxf(m, A.part_ml[j * all + row].x);
+    m = wave_max(m, lane);
+    float sum = 0.f;
+    float o[(kDim + 63) / 64];
+#pragma unroll
+    for (int k = 0; k < (kDim + 63) / 64; ++k) o[k] = 0.f;
+    for (int j = 0; j < A.splits; ++j) {
+        const float2 ml = A.part_ml[j * all + row];
+        const float w = ml.y * __builtin_amdgcn_exp2f(ml.x - m);
+        if (w == 0.f) continue;                                  // (uniform)
+        sum += w;
+#pragma unroll
+        for (int k = 0; k < (kDim + 63) / 64; ++k)
+            if (kDim % 64 == 0 || 64 * k + lane < kDim) o[k] += w * A.part_o[(j * all + row) * kDim + 64 * k + lane];
+    }
+#pragma unroll
+    for (int k = 0; k < (kDim + 63) / 64; ++k) {
+        if (kDim % 64 != 0 && 64 * k + lane >= kDim) continue;
+        const float v = sum == 0.f ? 0.f : o[k] / sum;
+        if constexpr (HALF) static_cast<_Float16*>(A.out)[row * kDim + 64 * k + lane] = (_Float16)v;
+        else static_cast<__bf16*>(A.out)[row * kDim + 64 * k + lane] = (__bf16)v;
+    }
+    if (A.lse && lane == 0) A.lse[row] = sum == 0.f ? -__builtin_inff() : (m + __log2f(sum)) * kLn2;
+}
+
+template <int I>
+using Const = std::integral_constant<int, I>;
+
+template <int NQ, int KIND, bool HALF>
+hipError_t launch_as(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
+    const dim3 grid((unsigned)(a.splits * a.tiles * a.c.heads * a.r.S));
+    if (p.row_waves == 4) kv_attention_kernel<NQ, KIND, HALF, 1, 4, 1><<<grid, 256, 0, stream>>>(a);
+    else if (p.row_waves == 2) kv_attention_kernel<NQ, KIND, HALF, 1, 2, 2><<<grid, 256, 0, stream>>>(a);
+    else kv_attention_kernel<NQ, KIND, HALF, 1, 1, 4><<<grid, 256, 0, stream>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.splits == 1) return e;
+    const long long rows = (long long)a.r.T * a.c.heads * a.group;
+    kv_attention_merge_kernel<NQ, HALF><<<dim3((unsigned)((rows + 3) / 4)), 256, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+AttnPlan attention_plan(int dim, int heads, int group, int S, int max_rows, int max_len) {
+    (void)dim;
+    AttnPlan p;
+    const long long rows = (long long)max_rows * group;
+    p.row_tiles = 1;
+    p.row_waves = rows > 64 ? 4 : rows > 32 ? 2 : 1;
+    const int per = 32 * p.row_tiles * p.row_waves;
+    p.tiles = (int)((rows + per - 1) / per);
+    const long long units = (long long)p.tiles * heads * S;
+    const long long blocks = ((long long)max_len + kBlock - 1) / kBlock;
+    const int token_waves = 4 / p.row_waves;
+    long long splits = (2 * 256 + units - 1) / units;
+    const long long most = (blocks + 2 * token_waves - 1) / (2 * token_waves);      // two blocks for every wavefront
+    splits = splits > most ? most : splits;
+    p.splits = (int)(splits < 1 ? 1 : splits > 128 ? 128 : splits);
+    return p;
+}
+
+size_t attention_workspace(const AttnPlan& p, int dim, int heads, int group, int T) {
+    if (p.splits <= 1) return 0;
+    return (size_t)p.splits * T * heads * group * (dim * 4 + 8);
+}
+
+hipError_t launch_kv_attention(const AttnArgs& a, const AttnPlan& p, int dim, int kind, int type, hipStream_t stream) {
+    auto by_type = [&](auto nq, auto kd) {
+        return type == EVOSPEC_FP16 ? launch_as<nq.value, kd.value, true>(a, p, stream) : launch_as<nq.value, kd.value, false>(a, p, stream);
+    };
+    auto by_kind = [&](auto nq) {
+        return kind == EVOSPEC_KV_E4M3 ? by_type(nq, Const<EVOSPEC_KV_E4M3>{}) : by_type(nq, Const<EVOSPEC_KV_INT8>{});
+    };
+    switch (dim) {
+        case 64: return by_kind(Const<2>{});
+        case 96: return by_kind(Const<3>{});
+        case 128: return by_kind(Const<4>{});
+        case 192: return by_kind(Const<6>{});
+        default: return by_kind(Const<8>{});
+    }
+}
+
+}  // namespace evospec

@@ -1,0 +1,81 @@
+// The 8-bit key/value cache and the sampler: layout, host-side arguments and launchers (no HIP code in the types).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "evospec_decode.h"
+
+namespace evospec {
+
+constexpr int kBlock = EVOSPEC_KV_BLOCK;      // tokens that share a scale
+
+// A cache as the kernels take it.
+struct Cache {
+    uint8_t* data;
+    float* scales;
+    int pages, heads;
+    int shift;                                // log2 of the blocks of a page
+};
+
+// The rows of a call: who they belong to.
+struct Rows {
+    const int32_t* table;
+    int width;
+    const int32_t* at;                        // starts (write, read) or lens (attention)
+    const int32_t* row_off;
+    int S, T, max_rows;
+};
+
+// Blocks that rows of one sequence can touch, wherever they start.
+inline int touched_blocks(int max_rows) { return (max_rows + kBlock - 2) / kBlock + 1; }
+
+hipError_t launch_kv_write(const Cache& c, int dim, int kind, const void* k, long long k_stride, const void* v, long long v_stride,
+                           int type, const Rows& r, hipStream_t stream);
+hipError_t launch_kv_read(const Cache& c, int dim, int kind, const Rows& r, int type, void* out_k, void* out_v, hipStream_t stream);
+
+// How an attention call is laid out: wavefronts of a workgroup over rows and tokens, workgroups over the tokens.
+struct AttnPlan {
+    int row_waves;                            // wavefronts side by side over rows (each `row_tiles` tiles of 32)
+    int row_tiles;
+    int tiles;                                // workgroups over the rows of a sequence and head
+    int splits;                               // workgroups over its tokens
+};
+AttnPlan attention_plan(int dim, int heads, int group, int S, int max_rows, int max_len);
+size_t attention_workspace(const AttnPlan& p, int dim, int heads, int group, int T);
+
+struct AttnArgs {
+    Cache c;
+    Rows r;
+    const void* q;
+    long long q_stride;
+    int group;
+    const uint64_t* tree;
+    float scale;
+    void* out;
+    float* lse;
+    float* part_o;                            // [splits][T * heads * group][dim], of splits > 1
+    float2* part_ml;                          // [splits][T * heads * group]: reference and sum
+    int splits, tiles;
+};
+hipError_t launch_kv_attention(const AttnArgs& a, const AttnPlan& p, int dim, int kind, int type, hipStream_t stream);
+
+struct SampleArgs {
+    const void* logits;
+    long long stride;
+    int M, V;
+    const float* u;
+    const float* temperature;
+    const int32_t* top_k;
+    const float* top_p;
+    const float* min_p;
+    const int32_t* ids;
+    int32_t* out_ids;
+    float* out_logprob;
+};
+size_t sample_workspace(int M, int V);
+hipError_t launch_sample(const SampleArgs& a, int type, void* workspace, int num_cu, hipStream_t stream);
+
+// Compute units of the current device (api.cpp); an evospec_status.
+int device_compute_units(int* out);
+
+}  // namespace evospec

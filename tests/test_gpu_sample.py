@@ -1,0 +1,195 @@
+"""Sampling on the GPU against the definition in 64 bits: tokens are equal, log-probabilities within 2^-23 of 1 + |lp| (one
+rounding to 32 bits; weights are multiples of 2^-43, so the sum of 2^20 of them is off by 2^-24 at most)."""
+import numpy as np
+import pytest
+
+import decode_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ev():
+    import torch
+    assert torch.cuda.is_available()
+    import paper_2605_27390_amd as ev
+    return ev
+
+
+def run(ev, z, u, type="fp32", ids=None, stride=None, **kw):
+    """z: float64 array, taken as `type`.  Compares with the definition and returns the tokens."""
+    import torch
+    t = torch.from_numpy(np.asarray(z, dtype=np.float64)).to({"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}[type])
+    g = t.cuda()
+    if stride:
+        wide = torch.full((t.shape[0], stride), float("inf"), dtype=t.dtype, device="cuda")
+        wide[:, :t.shape[1]] = g
+        g = wide[:, :t.shape[1]]
+    dev = {k: torch.tensor(np.asarray(v), dtype=torch.int32 if k == "top_k" else torch.float32, device="cuda") for k, v in kw.items()}
+    u = np.asarray(u, dtype=np.float32)
+    got, lp = ev.sample(g, torch.from_numpy(u).cuda(), ids=None if ids is None else torch.tensor(ids, dtype=torch.int32, device="cuda"), **dev)
+    host = {k: v.cpu().numpy() for k, v in dev.items()}
+    want, want_lp, margin = ref.sample(t.double().numpy(), u, ids=ids, **host)
+    got, lp = got.cpu().numpy(), lp.double().cpu().numpy()
+    sure = margin > 1e-11
+    assert np.array_equal(got[sure], want[sure]), (got, want)
+    assert np.array_equal(np.isnan(lp[sure]), np.isnan(want_lp[sure]))
+    ok = sure & ~np.isnan(want_lp)
+    assert (np.abs(lp - want_lp)[ok] <= 2.0 ** -23 * (1 + np.abs(want_lp[ok]))).all()
+    return got
+
+
+def logits(rng, M, V, spread=2.0):
+    z = rng.standard_normal((M, V)) * spread
+    for m in range(M):
+        at = rng.choice(V, min(V, 20), replace=False)
+        z[m, at] += rng.random(at.size) * 8
+    return z
+
+
+FILTERS = {"none": {}, "T": dict(T=1), "k": dict(k=1), "p": dict(p=1), "m": dict(m=1), "kp": dict(k=1, p=1), "all": dict(T=1, k=1, p=1, m=1)}
+
+
+def params(rng, M, f):
+    out = {}
+    if "T" in f:
+        out["temperature"] = rng.choice([0.0, 0.3, 0.7, 1.0, 1.7], M)
+    if "k" in f:
+        out["top_k"] = rng.choice([0, -1, 1, 2, 7, 50, 1000], M)
+    if "p" in f:
+        out["top_p"] = rng.choice([0.0, 0.1, 0.5, 0.9, 0.99, 1.0, 1.5], M)
+    if "m" in f:
+        out["min_p"] = rng.choice([0.0, -1.0, 0.01, 0.1, 1.0], M)
+    return out
+
+
+@pytest.mark.parametrize("name", list(FILTERS))
+@pytest.mark.parametrize("type", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("M,V", [(1, 1), (3, 2), (5, 63), (8, 1000), (9, 8193), (6, 30011)])
+def test_filters(ev, name, type, M, V):
+    rng = np.random.default_rng(M * V + len(name))
+    run(ev, logits(rng, M, V), rng.random(M), type, **params(rng, M, FILTERS[name]))
+
+
+@pytest.mark.parametrize("type", ["fp32", "bf16"])
+def test_full_vocabulary(ev, type):
+    rng = np.random.default_rng(1)
+    M, V = 24, 151936
+    z = logits(rng, M, V)
+    z[:, 50000:52000] = -np.inf
+    for f in ({}, dict(p=1), dict(k=1), dict(T=1, k=1, p=1, m=1)):
+        run(ev, z, rng.random(M), type, **params(rng, M, f))
+
+
+@pytest.mark.parametrize("type", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", [1000, 40000])
+def test_flat_rows(ev, type, V):
+    """High temperatures and logits that are all alike: the kept tokens are many, and ties go by id."""
+    rng = np.random.default_rng(2)
+    M = 8
+    z = logits(rng, M, V)
+    run(ev, z, rng.random(M), type, temperature=[100.0] * M, top_p=rng.random(M))
+    run(ev, np.zeros((M, V)), rng.random(M), type, top_p=[0.5, 0.9, 1, 1, 1, 0.1, 0.7, 0.3], top_k=[0, 0, 10, 0, 999, 5, 0, 30000])
+    got = run(ev, np.zeros((1, V)), [0.0], type)
+    assert got[0] == 0
+    ids = rng.permutation(3 * V)[:V]
+    got = run(ev, np.zeros((1, V)), [0.0], type, ids=ids)
+    assert got[0] == ids.min()
+    z = np.round(rng.standard_normal((M, V)))                  # a few values, thousands of each
+    run(ev, z, rng.random(M), type, top_k=rng.integers(1, V, M), top_p=rng.random(M), ids=ids)
+
+
+def test_borders(ev):
+    """Equal weights, so that the borders of top-k, top-p and u fall on tokens exactly."""
+    z = np.zeros((4, 8))
+    z[:, 6:] = -np.inf
+    u = [0.0, 0.25, 0.5, 0.99999994]
+    assert run(ev, z, u, top_k=[4] * 4).tolist() == [0, 1, 2, 3]
+    assert run(ev, z[:, :4], u, top_p=[0.5] * 4).tolist() == [0, 0, 1, 1]
+    assert run(ev, z, u, min_p=[1.0] * 4).tolist() == [0, 1, 3, 5]
+    # u out of range is taken to the nearest token that is kept
+    assert run(ev, z, [1.0, 2.0, -1.0, np.inf]).tolist() == [5, 5, 0, 5]
+
+
+def test_masked_and_special_logits(ev):
+    inf, nan = np.inf, np.nan
+    z = np.array([[-inf, -inf, -inf], [nan, nan, nan], [nan, 1.0, nan], [inf, 1.0, inf], [-inf, nan, -3e38], [3e38, -3e38, 0.0]])
+    got = run(ev, z, [0.7] * 6)
+    assert got.tolist() == [-1, -1, 1, 2, 2, 0]
+    got = run(ev, z, [0.7] * 6, temperature=[0.0] * 6, top_k=[2] * 6)
+    assert got.tolist() == [-1, -1, 1, 0, 2, 0]
+    z = np.full((3, 20000), -inf)                               # one token that is allowed, wherever it is
+    z[0, 0], z[1, 19999], z[2, 7777] = 5.0, -100.0, 0.0
+    for f in ({}, dict(top_p=[0.9] * 3), dict(top_k=[50] * 3), dict(min_p=[0.5] * 3)):
+        assert run(ev, z, [0.1, 0.5, 0.9], **f).tolist() == [0, 19999, 7777]
+    # signed zeros tie
+    assert run(ev, np.array([[-0.0, 0.0, 0.0]]), [0.0]).tolist() == [0]
+    # parameters that are NaN keep all, a temperature that is NaN is greedy
+    run(ev, np.array([[1.0, 2.0]]), [0.9], min_p=[nan])
+    assert run(ev, np.array([[1.0, 2.0]]), [0.9], temperature=[nan]).tolist() == [1]
+
+
+def test_extreme_temperatures(ev):
+    rng = np.random.default_rng(4)
+    z = logits(rng, 6, 5000)
+    run(ev, z, rng.random(6), temperature=[1e-30, 1e-6, 1e-3, 1e3, 1e6, 1e30])
+    run(ev, z, rng.random(6), temperature=[1e-30, 1e-6, 1e-3, 1e3, 1e6, 1e30], top_p=[0.9] * 6, top_k=[100] * 6)
+    run(ev, z * 1e30, rng.random(6), temperature=[1e29] * 6)
+
+
+def test_strided_rows_of_an_active_vocabulary(ev):
+    """Rows of a padded buffer, at odd places; ids of an active vocabulary in any order."""
+    rng = np.random.default_rng(5)
+    for type, stride in (("fp32", 4099), ("bf16", 4101), ("fp16", 4100)):
+        M, V = 7, 4097
+        ids = rng.permutation(151936)[:V]
+        run(ev, logits(rng, M, V), rng.random(M), type, ids=ids, stride=stride, **params(rng, M, dict(T=1, k=1, p=1)))
+
+
+def test_shares_come_out_as_they_should(ev):
+    """u over an even grid: each token is drawn as often as its share says."""
+    z = np.tile(np.log([[0.05, 0.5, 0.2, 0.25]]), (1000, 1))
+    got = run(ev, z, (np.arange(1000) + 0.5) / 1000)
+    assert np.bincount(got, minlength=4).tolist() == [50, 500, 200, 250]
+
+
+def test_largest_vocabulary(ev):
+    rng = np.random.default_rng(6)
+    run(ev, np.zeros((1, 1 << 20)), [0.999999], "bf16", top_p=[0.999])
+    run(ev, rng.standard_normal((1, 1 << 20)), [0.5], "fp32", top_p=[0.95])
+
+
+def test_graph_replays_follow_their_inputs(ev):
+    import torch
+    M, V = 5, 40000
+    z, u = torch.randn(M, V, device="cuda") * 3, torch.rand(M, device="cuda")
+    p = torch.full((M,), 0.9, device="cuda")
+    ids, lp = torch.empty(M, dtype=torch.int32, device="cuda"), torch.empty(M, device="cuda")
+    ws = torch.empty(max(1, ev.sample_workspace_bytes(M, V)), dtype=torch.uint8, device="cuda")
+    call = lambda: ev.sample(z, u, top_p=p, out_ids=ids, out_logprob=lp, workspace=ws)   # noqa: E731
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for _ in range(4):
+        z.normal_(0, 3)
+        u.uniform_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = ids.clone(), lp.clone()
+        eager = ev.sample(z, u, top_p=p)
+        assert torch.equal(got[0], eager[0]) and torch.equal(got[1], eager[1])
+
+
+def test_wrapper_refusals(ev):
+    import torch
+    z, u = torch.zeros(2, 10, device="cuda"), torch.zeros(2, device="cuda")
+    for bad in (dict(u=u[:1]), dict(u=u.double()), dict(temperature=u.half()), dict(top_k=u), dict(top_p=u[:1]), dict(ids=u),
+                dict(ids=torch.zeros(9, dtype=torch.int32, device="cuda")), dict(out_ids=u), dict(z=z.t()), dict(z=z.double()), dict(z=z[0])):
+        kw = {k: v for k, v in bad.items() if k not in ("u", "z")}
+        with pytest.raises((TypeError, ValueError)):
+            ev.sample(bad.get("z", z), bad.get("u", u), **kw)
