@@ -99,7 +99,7 @@ int evospec_kv_attention(const evospec_kv_cache *cache, const void *q, long long
  *   4. the token drawn is the first whose cumulative w, in that order, exceeds u times the sum of the kept ones (the last
  *      kept one if none does).
  * out_logprob = log of the drawn token's share in the kept ones.  temperature that is not > 0 draws the first token.
- * Tokens with w below 2^-44 are not drawn, and weigh nothing.  A row without a number above -inf gives id -1, logprob NaN.
+ * Tokens with w below 2^-42 may be left out of 4.  A row without a number above -inf gives id -1, logprob NaN.
  *   logits dev `type` [M, V], rows `stride` elements apart; V <= 2^20
  *   u, temperature, top_p, min_p dev fp32 [M]; top_k dev int32 [M]; each of the last four may be NULL (1, all, all, all)
  *   ids dev int32 [V] or NULL: the id of column i (distinct, not negative); NULL: i

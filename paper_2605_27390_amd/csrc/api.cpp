@@ -7,7 +7,6 @@
 #include <cstdio>
 #include <cstring>
 
-#include "decode.hpp"
 #include "evospec.h"
 #include "launch.hpp"
 #include "plan.hpp"
@@ -250,7 +249,6 @@ int head_impl(const void* h, int M, int d, const void* W_act, const int32_t* ids
 }
 
 int record_hip_error(hipError_t e) { return hip_fail(e); }
-int device_compute_units(int* out) { return device_num_cu(out); }
 }  // namespace evospec
 
 extern "C" {

@@ -142,7 +142,7 @@ int evospec_kv_attention(const evospec_kv_cache* cache, const void* q, long long
 
 int evospec_sample_workspace_bytes(int M, int V, size_t* out_bytes) {
     if (!out_bytes) return EVOSPEC_NULL_POINTER;
-    if (M < 0 || V < 1 || V > (1 << 20)) return EVOSPEC_BAD_SHAPE;
+    if (M < 0 || M > (1 << 24) || V < 1 || V > (1 << 20)) return EVOSPEC_BAD_SHAPE;
     *out_bytes = sample_workspace(M, V);
     return EVOSPEC_OK;
 }
@@ -151,18 +151,15 @@ int evospec_sample(const void* logits, long long stride, int type, int M, int V,
                    const int32_t* top_k, const float* top_p, const float* min_p, const int32_t* ids, int32_t* out_ids,
                    float* out_logprob, void* workspace, size_t workspace_bytes, void* stream) {
     if (type < EVOSPEC_BF16 || type > EVOSPEC_FP32) return EVOSPEC_BAD_TYPE;
-    if (M < 0 || V < 1 || V > (1 << 20) || stride < V) return EVOSPEC_BAD_SHAPE;
+    if (M < 0 || M > (1 << 24) || V < 1 || V > (1 << 20) || stride < V) return EVOSPEC_BAD_SHAPE;
     if (M == 0) return EVOSPEC_OK;
     if (!logits || !u || !out_ids) return EVOSPEC_NULL_POINTER;
     if (!aligned(logits, type_bytes(type)) || !aligned(workspace, 16)) return EVOSPEC_MISALIGNED;
     const size_t need = sample_workspace(M, V);
     if (need && !workspace) return EVOSPEC_NULL_POINTER;
     if (workspace_bytes < need) return EVOSPEC_WORKSPACE_TOO_SMALL;
-    int num_cu = 0;
-    const int rc = device_compute_units(&num_cu);
-    if (rc) return rc;
     const SampleArgs a{logits, stride, M, V, u, temperature, top_k, top_p, min_p, ids, out_ids, out_logprob};
-    return failed(launch_sample(a, type, workspace, num_cu, static_cast<hipStream_t>(stream)));
+    return failed(launch_sample(a, type, workspace, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -73,9 +73,6 @@ struct SampleArgs {
     float* out_logprob;
 };
 size_t sample_workspace(int M, int V);
-hipError_t launch_sample(const SampleArgs& a, int type, void* workspace, int num_cu, hipStream_t stream);
-
-// Compute units of the current device (api.cpp); an evospec_status.
-int device_compute_units(int* out);
+hipError_t launch_sample(const SampleArgs& a, int type, void* workspace, hipStream_t stream);
 
 }  // namespace evospec

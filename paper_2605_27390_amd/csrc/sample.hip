@@ -45,6 +45,27 @@ __device__ __forceinline__ double weight(float z, float z_max, double c) {
 }
 __device__ __forceinline__ u64 fixed(double w) { return (u64)(w * kOne + 0.5); }
 
+// Products of a sum of weights with a fraction, exact: a float is a whole number of 24 bits over a power of two.
+// floor(f x), f in [0, 1)
+__device__ __forceinline__ u64 share(float f, u64 x, bool up) {
+    const uint32_t bits = __float_as_uint(f), e = bits >> 23, man = e ? (bits & 0x7fffffu) | 0x800000u : bits & 0x7fffffu;
+    const int down = 150 - (int)(e ? e : 1);                     // f = man / 2^down, down >= 24
+    const unsigned __int128 y = (unsigned __int128)man * x;
+    if (down >= 127) return up && y != 0 ? 1 : 0;
+    const u64 q = (u64)(y >> down);
+    return q + (up && ((unsigned __int128)q << down) != y ? 1 : 0);
+}
+// the least whole number >= f x, at least 1 and at most x (f < 1)
+__device__ __forceinline__ u64 share_up(float f, u64 x) {
+    const u64 s = f > 0.f ? share(f, x, true) : 0;
+    return s < 1 ? 1 : s;
+}
+// the least whole number > f x, at most x
+__device__ __forceinline__ u64 share_past(float f, u64 x) {
+    if (f >= 1.f) return x;
+    return f > 0.f ? share(f, x, false) + 1 : 1;
+}
+
 template <int TYPE>
 __device__ __forceinline__ float logit(const void* row, int i) {
     if constexpr (TYPE == EVOSPEC_FP32) return static_cast<const float*>(row)[i];
@@ -98,11 +119,9 @@ __device__ u64 find_key(u64 low, u64 target, u64* s_hist, u64* s_pick, EachKey e
     return prefix;
 }
 
-// One workgroup a row; the row is read again for every digit.
+// A row by one workgroup, read again for every digit of a key: for rows whose tokens the bins below do not separate.
 template <int TYPE>
-__global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs A) {
-    __shared__ u64 s_hist[256], s_part[kThreads / 64], s_pick[2];
-    const int m = blockIdx.x;
+__device__ __noinline__ void sample_by_digits(const SampleArgs& A, int m, u64* s_hist, u64* s_part, u64* s_pick) {
     const char* row = static_cast<const char*>(A.logits) + (long long)m * A.stride * (TYPE == EVOSPEC_FP32 ? 4 : 2);
     const float T = A.temperature ? A.temperature[m] : 1.f;
     auto each = [&](auto f) {
@@ -143,9 +162,7 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs A) {
     const float p = A.top_p ? A.top_p[m] : 1.f;
     if (p < 1.f) {
         const u64 all = mass_from(low);
-        const double t = ceil((double)p * (double)all);
-        const u64 target = t >= 1.0 ? (u64)t : 1;
-        low = find_key(low, target < all ? target : all, s_hist, s_pick, masses);
+        low = find_key(low, share_up(p, all), s_hist, s_pick, masses);
     }
     const float least = A.min_p ? A.min_p[m] : 0.f;
     if (least > 0.f) {
@@ -154,10 +171,7 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs A) {
         low = reduce_all(first, s_part, [](u64 a, u64 b) { return a < b ? a : b; });
     }
     const u64 total = mass_from(low);
-    const float u = A.u[m];
-    const double t = floor((double)u * (double)total);
-    const u64 target = t >= 0.0 ? (t < (double)total ? (u64)t + 1 : total) : 1;
-    const u64 key = find_key(low, target < total ? target : total, s_hist, s_pick, masses);
+    const u64 key = find_key(low, share_past(A.u[m], total), s_hist, s_pick, masses);
     if (threadIdx.x == 0) {
         A.out_ids[m] = key_id(key);
         if (A.out_logprob) {
@@ -167,16 +181,727 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs A) {
     }
 }
 
+
+// ---------------------------------------------------------------------------------------
+// The fast way, three launches.
+//
+// 1. sample_bins_kernel, a workgroup for each slice of a row (kSlice logits at most, which stay in registers): the slice's
+//    largest logit, and the weights of its tokens, summed in bins of 1 / kBins of a power of two below e = the next power of two
+//    above that logit.  References are whole powers of two, so that slices' bins lie on one grid and their sums are joined by shifts.
+// 2. sample_row_kernel, a workgroup for each row: the bins of all slices, joined; in which bins top-k, top-p and min-p cut, and in which
+//    the draw falls (a range of them where one depends on a cut inside a bin).  Greedy rows end here.
+// 3. sample_pick_kernel, a workgroup for each slice again: tokens of those bins are put on the row's list; the last workgroup of
+//    the row to come sorts the list, and goes through the filters with the list's tokens and the bins' sums.
+// Lists that are full (thousands of tokens within 1 / kBins of a power of two) leave the row to sample_by_digits.
+constexpr int kBins = 32;                         // to a factor of 2
+constexpr int kRange = 44;                        // factors of 2 that are kept,
+constexpr int kAll = kBins * 28;                  // those behind the 28th in the last bin
+constexpr int kGroups = 5;                        // of 4 logits of a thread
+constexpr int kSlice = kThreads * 4 * kGroups;
+constexpr int kList = 4096;
+constexpr int kMostK = 512;                       // top-k up to this goes by lists alone
+constexpr int kSteps = 128;                       // of the table of powers of two
+
+struct RowState {
+    double ref;                                   // exponent of the row's reference
+    float z_max;
+    int state;                                    // kOpen, kDone, kDigits
+    int lo[3], hi[3];                             // bins lo[i] .. hi[i] are on the list
+    int end_bin;                                  // the last bin in which the kept tokens can end
+    int least_bin;                                // the last bin that can hold a weight of min-p
+    int k_bin, k_left;                            // the bin that top-k cuts, and how many of it are kept; -1: none
+};
+enum { kOpen = 0, kDone = 1, kDigits = 2 };
+
+// A row's part of the workspace.
+struct RowSpace {
+    u64* mass;                                    // [slices][kAll]
+    uint32_t* count;                              // [slices][kAll], where top-k asks for it
+    double* ref;                                  // [slices]
+    u64* top;                                     // [slices]: greedy rows' largest key
+    u64* before;                                  // [kAll + 1]: what the bins in front weigh
+    RowState* row;
+    uint32_t* ticket;                             // tokens on the list, workgroups that came
+    u64* list;                                    // [kList]
+};
+__host__ __device__ inline size_t row_bytes(int slices) {
+    const size_t n = (size_t)slices * (kAll * 12 + 16) + (kAll + 1) * 8 + sizeof(RowState) + 8 + kList * 8;
+    return (n + 255) / 256 * 256;
+}
+__device__ __forceinline__ RowSpace row_space(char* ws, int m, int slices) {
+    char* p = ws + (size_t)m * row_bytes(slices);
+    RowSpace r;
+    r.mass = reinterpret_cast<u64*>(p);           p += (size_t)slices * kAll * 8;
+    r.ref = reinterpret_cast<double*>(p);         p += (size_t)slices * 8;
+    r.top = reinterpret_cast<u64*>(p);            p += (size_t)slices * 8;
+    r.before = reinterpret_cast<u64*>(p);         p += (kAll + 1) * 8;
+    r.list = reinterpret_cast<u64*>(p);           p += kList * 8;
+    r.row = reinterpret_cast<RowState*>(p);       p += sizeof(RowState);
+    r.ticket = reinterpret_cast<uint32_t*>(p);    p += 8;
+    r.count = reinterpret_cast<uint32_t*>(p);
+    return r;
+}
+
+// Powers 2^(j / kSteps), for weights by table: x = n + j / kSteps + r, |r| <= 1 / (2 kSteps); the series of 2^r to the fourth
+// power is off by 1e-15.
+__device__ __forceinline__ void fill_table(double* table) {
+    if (threadIdx.x < kSteps) table[threadIdx.x] = 2.0 * exp2_series((double)threadIdx.x / kSteps - 1.0);
+}
+// -x in steps of 1 / kSteps, to the nearest (x in (-2^20, 0]); r = what is left
+__device__ __forceinline__ int steps_of(double x, double& r) {
+    const double magic = 6755399441055744.0 / kSteps;            // 1.5 * 2^52 / kSteps
+    const double t = x + magic;
+    r = x - (t - magic);
+    return -(int)(uint32_t)__double_as_longlong(t);
+}
+__device__ __forceinline__ u64 weight_of(int steps, double r, const double* table) {
+    double p = 0.0096181291076284772;                            // ln(2)^4 / 4!
+    p = fma(p, r, 0.055504108664821580);
+    p = fma(p, r, 0.24022650695910071);
+    p = fma(p, r, 0.69314718055994531);
+    p = fma(p, r, 1.0);
+    const int n = (-steps) >> 7, j = (-steps) & (kSteps - 1);
+    const double s = __longlong_as_double((long long)(1023 + 43 + n) << 52);
+    const double d = fma(table[j] * p, s, 4503599627370496.0);   // 2^52 + the weight, rounded to a whole number
+    return (u64)__double_as_longlong(d) & 0xfffffffffffffull;
+}
+static_assert(kSteps == 128 && kSteps % kBins == 0, "shifts");
+__device__ __forceinline__ int bin_of(int steps) { return min(steps / (kSteps / kBins), kAll - 1); }
+
+struct Slice {
+    int first, last;
+    // the logit that is the thread's e-th of group g: 4 in a row, the next group kThreads * 4 further on; short slices are dealt
+    // out one by one, so that all wavefronts have a share of them
+    __device__ __forceinline__ bool small() const { return last - first <= 4 * kThreads; }
+    __device__ __forceinline__ int at(int g, int e) const {
+        return small() ? first + (4 * g + e) * kThreads + (int)threadIdx.x : first + (g * kThreads + (int)threadIdx.x) * 4 + e;
+    }
+};
+__device__ __forceinline__ Slice slice_of(int V, int slices, int j) {
+    const int per = ((V + slices - 1) / slices + 3) / 4 * 4;     // (<= kSlice)
+    return Slice{min(V, j * per), min(V, (j + 1) * per)};
+}
+template <int TYPE>
+__device__ __forceinline__ void load_slice(const char* row, Slice S, float (&z)[kGroups][4]) {
+    constexpr int kBytes = TYPE == EVOSPEC_FP32 ? 4 : 2;
+    const bool whole = (reinterpret_cast<uintptr_t>(row) & (4 * kBytes - 1)) == 0 && !S.small();
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+        const int i = S.at(g, 0);
+        if (whole && i + 4 <= S.last) {
+            if constexpr (TYPE == EVOSPEC_FP32) {
+                const float4 v = *reinterpret_cast<const float4*>(row + (size_t)i * 4);
+                z[g][0] = v.x; z[g][1] = v.y; z[g][2] = v.z; z[g][3] = v.w;
+            } else {
+                const uint2 v = *reinterpret_cast<const uint2*>(row + (size_t)i * 2);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint16_t b = (uint16_t)((e < 2 ? v.x : v.y) >> (16 * (e & 1)));
+                    if constexpr (TYPE == EVOSPEC_FP16) z[g][e] = (float)__builtin_bit_cast(_Float16, b);
+                    else z[g][e] = __uint_as_float((uint32_t)b << 16);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z[g][e] = S.at(g, e) < S.last ? logit<TYPE>(row, S.at(g, e)) : -__builtin_inff();
+        }
+    }
+}
+
+__device__ __forceinline__ bool regular(float T, float z_max) {
+    const double c = 1.4426950408889634074 / (double)T;
+    return c < 0x1p60 && c > 0x1p-60 && fabs((double)z_max * c) < 0x1p40;
+}
+
+// Rows of a small top-k: tokens of the slice that can be among the row's k largest, as keys in the place of its bins, and a
+// bound that k of them reach.  Of every wavefront's 64 largest logits of a lane the q-th largest is taken, q times the wavefronts >= k, and
+// the least of these: k logits reach it.  (k = 50 of 19,000: some 150 tokens pass.)
+template <int TYPE>
+__device__ __forceinline__ void list_largest(const SampleArgs& A, const float (&z)[kGroups][4], Slice S, int k, float top, const RowSpace& R,
+                                             int j, u64* s_key, float* s_bound) {
+    __shared__ uint32_t s_n;
+    const int tid = threadIdx.x;
+    float mine = -__builtin_inff();
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mine = fmaxf(mine, z[g][e]);
+    // (short slices have none for some wavefronts)
+    const int waves = min(kThreads, S.last - S.first) / 64, q = waves > 0 ? (k + waves - 1) / waves : 65;
+    const float b = q <= 64 ? ordered_to_f32(wave_kth_largest(f32_to_ordered(mine), q)) : -__builtin_inff();
+    __syncthreads();                                             // (s_bound held the maxima)
+    if ((tid & 63) == 0) s_bound[tid >> 6] = b;
+    if (tid == 0) s_n = 0;
+    __syncthreads();
+    float bound = s_bound[0];
+    for (int w = 1; w < waves; ++w) bound = fminf(bound, s_bound[w]);
+    if (top > -__builtin_inff()) {
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (z[g][e] >= bound && z[g][e] > -__builtin_inff()) {
+                    const uint32_t at = atomicAdd(&s_n, 1u);
+                    const int i = S.at(g, e);
+                    if (at < kAll) s_key[at] = make_key(z[g][e], A.ids ? A.ids[i] : i);
+                }
+    }
+    __syncthreads();
+    const uint32_t n = s_n;
+    for (int i = tid; i < (int)min(n, (uint32_t)kAll); i += kThreads) R.mass[(size_t)j * kAll + i] = s_key[i];
+    if (tid == 0) {
+        R.count[(size_t)j * kAll] = n;
+        R.top[j] = top > -__builtin_inff() ? make_key(top, 0) : 0;
+        R.ref[j] = (double)bound;
+    }
+}
+
+template <int TYPE>
+__global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs A, char* ws, int slices) {
+    __shared__ u64 s_mass[kAll];
+    __shared__ uint32_t s_count[kAll];
+    __shared__ double s_table[kSteps];
+    __shared__ float s_max[kThreads / 64];
+    __shared__ u64 s_part[kThreads / 64];
+    const int m = blockIdx.x / slices, j = blockIdx.x % slices, tid = threadIdx.x, lane = tid & 63;
+    const char* row = static_cast<const char*>(A.logits) + (long long)m * A.stride * (TYPE == EVOSPEC_FP32 ? 4 : 2);
+    const Slice S = slice_of(A.V, slices, j);
+    const RowSpace R = row_space(ws, m, slices);
+    float z[kGroups][4];
+    load_slice<TYPE>(row, S, z);
+    const float T = A.temperature ? A.temperature[m] : 1.f;
+    const bool counts = A.top_k && A.top_k[m] > 0;
+    fill_table(s_table);
+    for (int b = tid; b < kAll; b += kThreads) {
+        s_mass[b] = 0;
+        s_count[b] = 0;
+    }
+    if (j == 0 && tid < 2) R.ticket[tid] = 0;
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, z[g][e]);
+    top = wave_max(top, lane);
+    if (lane == 0) s_max[tid >> 6] = top;
+    __syncthreads();
+    top = s_max[lane & (kThreads / 64 - 1)];
+    top = wave_max(top, lane);
+    if (!(T > 0.f)) {                                            // greedy: the largest key
+        u64 best = 0;
+        if (top > -__builtin_inff()) {
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (z[g][e] == top) {
+                        const int i = S.at(g, e);
+                        const u64 key = make_key(top, A.ids ? A.ids[i] : i);
+                        best = key > best ? key : best;
+                    }
+        }
+        best = reduce_all(best, s_part, [](u64 a, u64 b) { return a > b ? a : b; });
+        if (tid == 0) {
+            R.top[j] = best;
+            R.ref[j] = 0.0;
+        }
+        return;
+    }
+    if (counts && A.top_k[m] <= kMostK) {                        // (uniform)
+        list_largest<TYPE>(A, z, S, A.top_k[m], top, R, j, s_mass, s_max);
+        return;
+    }
+    const double c = 1.4426950408889634074 / (double)T;
+    const bool ok = top > -__builtin_inff() && regular(T, top);
+    const double ref = ok ? ceil((double)top * c) : 0.0;
+    if (tid == 0) {
+        R.top[j] = top > -__builtin_inff() ? make_key(top, 0) : 0;
+        R.ref[j] = ref;
+    }
+    if (!ok) return;                                             // (uniform) nothing here, or a row for the digits
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const double x = fma((double)z[g][e], c, -ref);
+            if (x > -(double)kRange) {                           // (not NaN)
+                double r;
+                const int steps = steps_of(x, r), b = bin_of(steps);
+                atomicAdd(&s_mass[b], weight_of(steps, r, s_table));
+                if (counts) atomicAdd(&s_count[b], 1u);
+            }
+        }
+    __syncthreads();
+    for (int b = tid; b < kAll; b += kThreads) {
+        R.mass[(size_t)j * kAll + b] = s_mass[b];
+        if (counts) R.count[(size_t)j * kAll + b] = s_count[b];
+    }
+}
+
+// Sorts s_key[0, n), descending, n <= the array's power of two of places; what is behind n becomes 0.
+template <int THREADS>
+__device__ __forceinline__ void sort_keys(u64* s_key, int n) {
+    int size = 64;
+    while (size < n) size *= 2;
+    for (int i = n + threadIdx.x; i < size; i += THREADS) s_key[i] = 0;
+    __syncthreads();
+    for (int w = 2; w <= size; w *= 2)
+        for (int d = w / 2; d > 0; d /= 2) {
+            for (int i = threadIdx.x; i < size / 2; i += THREADS) {
+                const int a = (i & ~(d - 1)) * 2 + (i & (d - 1)), b = a + d;
+                const u64 x = s_key[a], y = s_key[b];
+                if ((x < y) == ((a & w) == 0)) {
+                    s_key[a] = y;
+                    s_key[b] = x;
+                }
+            }
+            __syncthreads();
+        }
+}
+__device__ __forceinline__ u64 shfl_up64(u64 x, int s) {
+    return (u64)(uint32_t)__shfl_up((int)(uint32_t)x, s) | (u64)(uint32_t)__shfl_up((int)(uint32_t)(x >> 32), s) << 32;
+}
+// s_sum[i] = sum of the weights of s_key[0, i]; `each` places in a row to a thread, each * THREADS >= n.
+template <int THREADS, int EACH>
+__device__ __forceinline__ void sum_weights(const u64* s_key, u64* s_sum, int n, double c, double ref, const double* table, u64* s_part) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    u64 w[EACH], sum = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int at = tid * EACH + i;
+        w[i] = 0;
+        if (at < n) {
+            const double x = fmin(fma((double)key_value(s_key[at]), c, -ref), 0.0);
+            double r;
+            const int steps = steps_of(fmax(x, -60.0), r);
+            w[i] = x > -(double)kRange ? weight_of(steps, r, table) : 0;
+        }
+        sum += w[i];
+    }
+    u64 run = sum;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+        const u64 x = shfl_up64(run, s);
+        if (lane >= s) run += x;
+    }
+    if (lane == 63) s_part[tid >> 6] = run;
+    __syncthreads();
+    run -= sum;
+    for (int v = 0; v < tid >> 6; ++v) run += s_part[v];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        run += w[i];
+        if (tid * EACH + i < n) s_sum[tid * EACH + i] = run;
+    }
+    __syncthreads();
+}
+// The first of [lo, hi) for which f holds (and holds from there on), hi if there is none; a wavefront tries 64 at a time.
+template <class F>
+__device__ __forceinline__ int search(int lo, int hi, int lane, F f) {
+    while (lo < hi) {
+        const int step = (hi - lo + 63) / 64, i = lo + lane * step;
+        const u64 yes = __ballot(i >= hi || f(i < hi ? i : hi - 1));
+        const int first = yes ? __ffsll((long long)yes) - 1 : 64;
+        if (first == 0) return lo;
+        hi = min(hi, lo + first * step);
+        lo += (first - 1) * step + 1;
+    }
+    return hi;
+}
+__device__ __forceinline__ void give(const SampleArgs& A, int m, u64 key, u64 kept, double c, double ref) {
+    A.out_ids[m] = key_id(key);
+    if (A.out_logprob)
+        A.out_logprob[m] = (float)((fma((double)key_value(key), c, -ref) - log2((double)kept / kOne)) * 0.69314718055994530942);
+}
+
+constexpr int kRowThreads = 512;
+constexpr int kRowList = 2048;
+
+// A row of a small top-k, from its slices' lists.  False if they do not hold what is needed.
+__device__ bool finish_largest(const SampleArgs& A, int m, int k, const RowSpace& R, int slices, double c, double ref, float z_max, u64* s_key,
+                               u64* s_sum, double* s_table, u64* s_part, uint32_t* s_n) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    fill_table(s_table);
+    if (tid == 0) *s_n = 0;
+    // k logits of one slice reach its bound: the largest bound is one for the row
+    float bound = -__builtin_inff();
+    bool full = false;
+    for (int j = 0; j < slices; ++j) {
+        bound = fmaxf(bound, (float)R.ref[j]);
+        full |= R.count[(size_t)j * kAll] > (uint32_t)kAll;
+    }
+    if (full) return false;                                      // (uniform)
+    __syncthreads();
+    for (int j = 0; j < slices; ++j) {
+        const int n = (int)R.count[(size_t)j * kAll];
+        for (int i = tid; i < n; i += kRowThreads) {
+            const u64 key = R.mass[(size_t)j * kAll + i];
+            if (key_value(key) >= bound) {
+                const uint32_t at = atomicAdd(s_n, 1u);
+                if (at < kRowList) s_key[at] = key;
+            }
+        }
+    }
+    __syncthreads();
+    int n = (int)*s_n;
+    if (n > kRowList) return false;
+    sort_keys<kRowThreads>(s_key, n);
+    n = min(n, k);
+    sum_weights<kRowThreads, 1>(s_key, s_sum, n, c, ref, s_table, s_part);     // (n <= k <= kMostK)
+    if (tid >= 64) return true;
+    int last = n - 1;
+    const float p = A.top_p ? A.top_p[m] : 1.f;
+    if (p < 1.f) {
+        const u64 target = share_up(p, s_sum[last]);
+        last = min(last, search(0, n, lane, [&](int i) { return s_sum[i] >= target; }));
+    }
+    const float least = A.min_p ? A.min_p[m] : 0.f;
+    if (least > 0.f) {
+        const int first = search(0, n, lane, [&](int i) {
+            const float z = key_value(s_key[i]);
+            return z != z_max && weight(z, z_max, c) < (double)least;
+        });
+        last = max(min(last, first - 1), 0);
+    }
+    const u64 kept = s_sum[last], target = share_past(A.u[m], kept);
+    const int at = min(search(0, n, lane, [&](int i) { return s_sum[i] >= target; }), last);
+    if (tid == 0) give(A, m, s_key[at], kept, c, ref);
+    return true;
+}
+static_assert(kMostK <= kRowThreads, "one token a thread");
+constexpr int kPer = (kAll + kRowThreads - 1) / kRowThreads;     // bins of a thread
+
+__global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs A, char* ws, int slices) {
+    __shared__ u64 s_before[kAll + 1];
+    __shared__ uint32_t s_first[kAll + 1];
+    __shared__ u64 s_sum[kRowThreads / 64];
+    __shared__ uint32_t s_num[kRowThreads / 64];
+    __shared__ int s_found[8];
+    const int m = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+    const RowSpace R = row_space(ws, m, slices);
+    const float T = A.temperature ? A.temperature[m] : 1.f;
+    u64 top = 0;
+    for (int j = 0; j < slices; ++j) top = R.top[j] > top ? R.top[j] : top;
+    const float z_max = key_value(top);
+    const int k = A.top_k ? A.top_k[m] : 0;
+    if (top == 0 || !(T > 0.f)) {
+        if (tid == 0) {
+            A.out_ids[m] = top == 0 ? -1 : key_id(top);
+            if (A.out_logprob) A.out_logprob[m] = top == 0 ? __uint_as_float(0x7fc00000u) : 0.f;
+            R.row->state = kDone;
+        }
+        return;
+    }
+    if (!regular(T, z_max)) {
+        if (tid == 0) R.row->state = kDigits;
+        return;
+    }
+    const double c = 1.4426950408889634074 / (double)T;
+    const double ref = ceil((double)z_max * c);
+    if (k > 0 && k <= kMostK) {
+        __shared__ u64 s_key[kRowList], s_weight[kRowList];
+        __shared__ double s_table[kSteps];
+        __shared__ uint32_t s_n;
+        const bool done = finish_largest(A, m, k, R, slices, c, ref, z_max, s_key, s_weight, s_table, s_sum, &s_n);
+        if (tid == 0) R.row->state = done ? kDone : kDigits;
+        return;
+    }
+    // the slices' bins, joined: bin b of a slice whose reference is `shift` factors of 2 lower goes to b + shift kBins, or the last
+    for (int b = tid; b <= kAll; b += kRowThreads) {
+        s_before[b] = 0;
+        s_first[b] = 0;
+    }
+    __syncthreads();
+    for (int j = 0; j < slices; ++j) {
+        if (R.top[j] == 0 || !regular(T, key_value(R.top[j]))) continue;
+        const double gap = ref - R.ref[j];                       // (a whole number >= 0)
+        if (gap >= kRange) continue;
+        const int shift = (int)gap;
+        for (int b = tid; b < kAll; b += kRowThreads) {
+            const u64 w = R.mass[(size_t)j * kAll + b];
+            const int to = min(b + shift * kBins, kAll - 1);
+            if (w) atomicAdd(&s_before[to], shift ? (w + (1ull << (shift - 1))) >> shift : w);
+            if (k > 0) atomicAdd(&s_first[to], R.count[(size_t)j * kAll + b]);
+        }
+    }
+    __syncthreads();
+    u64 mass[kPer];
+    uint32_t count[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int b = tid * kPer + i;
+        mass[i] = b < kAll ? s_before[b] : 0;
+        count[i] = b < kAll ? s_first[b] : 0;
+    }
+    __syncthreads();
+    // what lies in front of each bin
+    u64 sum = 0;
+    uint32_t num = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        sum += mass[i];
+        num += count[i];
+    }
+    u64 run = sum;
+    uint32_t runs = num;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+        const u64 x = (u64)(uint32_t)__shfl_up((int)(uint32_t)run, s) | (u64)(uint32_t)__shfl_up((int)(uint32_t)(run >> 32), s) << 32;
+        const uint32_t y = (uint32_t)__shfl_up((int)runs, s);
+        if (lane >= s) {
+            run += x;
+            runs += y;
+        }
+    }
+    if (lane == 63) {
+        s_sum[tid >> 6] = run;
+        s_num[tid >> 6] = runs;
+    }
+    __syncthreads();
+    run -= sum;
+    runs -= num;
+    for (int w = 0; w < tid >> 6; ++w) {
+        run += s_sum[w];
+        runs += s_num[w];
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int b = tid * kPer + i;
+        if (b > kAll) break;
+        s_before[b] = run;
+        s_first[b] = runs;
+        if (b < kAll) {
+            run += mass[i];
+            runs += count[i];
+        }
+    }
+    if (tid == kRowThreads - 1) {
+        s_before[kAll] = run;
+        s_first[kAll] = runs;
+    }
+    __syncthreads();
+    for (int b = tid; b <= kAll; b += kRowThreads) R.before[b] = s_before[b];
+    const u64 total = s_before[kAll];
+    // the bin at which the sum over the bins reaches target (1 <= target <= total)
+    auto bin_at = [&](u64 target, int slot) {
+        target = target < 1 ? 1 : target > total ? total : target;
+        for (int b = tid; b < kAll; b += kRowThreads)
+            if (s_before[b] < target && s_before[b + 1] >= target) s_found[slot] = b;
+        __syncthreads();
+        return s_found[slot];
+    };
+    int k_bin = -1, k_left = 0;
+    u64 lo = total, hi = total;                                  // bounds of what is kept
+    int end_lo = kAll, end_hi = kAll;                            // and of the bin where that ends (kAll: all are kept)
+    if (k > 0 && (uint32_t)k < s_first[kAll]) {
+        for (int b = tid; b < kAll; b += kRowThreads)
+            if (s_first[b] < (uint32_t)k && s_first[b + 1] >= (uint32_t)k) s_found[0] = b;
+        __syncthreads();
+        k_bin = s_found[0];
+        k_left = k - (int)s_first[k_bin];
+        lo = s_before[k_bin];
+        hi = s_before[k_bin + 1];
+        end_lo = end_hi = k_bin;
+    }
+    const float p = A.top_p ? A.top_p[m] : 1.f;
+    if (p < 1.f) {
+        end_lo = bin_at(share_up(p, lo), 1);
+        end_hi = bin_at(share_up(p, hi), 2);
+    }
+    const float least = A.min_p ? A.min_p[m] : 0.f;
+    int least_bin = kAll - 1;
+    if (least > 0.f) {
+        // the bin of w = least, give or take two
+        const double x = fma((double)z_max, c, -ref) + (least < 1.f ? (double)__log2f(least) : 0.0);
+        const int b = (int)fmin(-x * kBins, (double)kAll + 4);
+        if (b - 2 < end_lo) end_lo = max(b - 2, 0);
+        if (b + 2 < end_hi) end_hi = b + 2;
+        least_bin = min(b + 2, kAll - 1);
+    }
+    int n = 0;
+    int bins[3][2];
+    if (end_hi < kAll) {
+        lo = s_before[end_lo];
+        hi = s_before[end_hi + 1];
+        bins[n][0] = end_lo;
+        bins[n++][1] = end_hi;
+    } else if (end_lo < kAll) {                                  // min-p cuts among the last bins, or behind them
+        lo = s_before[end_lo];
+        hi = total;
+        bins[n][0] = end_lo;
+        bins[n++][1] = end_hi = kAll - 1;
+    }
+    const float u = A.u[m];
+    const int draw_lo = bin_at(share_past(u, lo), 3), draw_hi = bin_at(share_past(u, hi), 4);
+    bins[n][0] = draw_lo;
+    bins[n++][1] = draw_hi;
+    if (k_bin >= 0) {
+        bins[n][0] = k_bin;
+        bins[n++][1] = k_bin;
+    }
+    if (tid == 0) {
+        RowState st;
+        st.ref = ref;
+        st.z_max = z_max;
+        st.state = kOpen;
+        for (int i = 0; i < 3; ++i) {
+            st.lo[i] = i < n ? bins[i][0] : kAll;
+            st.hi[i] = i < n ? bins[i][1] : -1;
+        }
+        st.end_bin = min(end_hi, kAll - 1);
+        st.least_bin = least_bin;
+        st.k_bin = k_bin;
+        st.k_left = k_left;
+        *R.row = st;
+    }
+}
+
+template <int TYPE>
+__global__ __launch_bounds__(kThreads) void sample_pick_kernel(SampleArgs A, char* ws, int slices) {
+    __shared__ u64 s_key[kList], s_sum[kList], s_before[kAll + 1];
+    __shared__ double s_table[kSteps];
+    __shared__ u64 s_part[kThreads / 64], s_pick[2];
+    __shared__ uint32_t s_last, s_n, s_at;
+    const int m = blockIdx.x / slices, j = blockIdx.x % slices, tid = threadIdx.x, lane = tid & 63;
+    const RowSpace R = row_space(ws, m, slices);
+    const int state = R.row->state;
+    if (state == kDone) return;
+    const float T = A.temperature ? A.temperature[m] : 1.f;
+    if (state == kDigits) {
+        if (j == 0) sample_by_digits<TYPE>(A, m, s_key, s_part, s_pick);
+        return;
+    }
+    const RowState st = *R.row;
+    const double c = 1.4426950408889634074 / (double)T;
+    const char* row = static_cast<const char*>(A.logits) + (long long)m * A.stride * (TYPE == EVOSPEC_FP32 ? 4 : 2);
+    const int b_min = min(st.lo[0], min(st.lo[1], st.lo[2])), b_max = max(st.hi[0], max(st.hi[1], st.hi[2]));
+    const u64 mine = R.top[j];
+    const double ref = R.ref[j];
+    const int shift = (int)fmin(st.ref - ref, 64.0) * kBins;
+    fill_table(s_table);
+    if (tid == 0) s_n = 0;
+    __syncthreads();
+    if (mine != 0 && regular(T, key_value(mine)) && st.ref - ref < kRange) {    // (uniform)
+        const Slice S = slice_of(A.V, slices, j);
+        float z[kGroups][4];
+        load_slice<TYPE>(row, S, z);
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const double x = fma((double)z[g][e], c, -ref);
+                bool on = false;
+                if (x > -(double)kRange) {
+                    double r;
+                    const int b = min(bin_of(steps_of(x, r)) + shift, kAll - 1);
+                    on = b >= b_min && b <= b_max &&
+                         ((b >= st.lo[0] && b <= st.hi[0]) || (b >= st.lo[1] && b <= st.hi[1]) || (b >= st.lo[2] && b <= st.hi[2]));
+                }
+                if (on) {
+                    const uint32_t at = atomicAdd(&s_n, 1u);
+                    const int i = S.at(g, e);
+                    if (at < kList) s_key[at] = make_key(z[g][e], A.ids ? A.ids[i] : i);
+                }
+            }
+        __syncthreads();
+        // (a list that is too long for one workgroup is too long for the row)
+        if (tid == 0) s_at = atomicAdd(&R.ticket[0], s_n);
+        __syncthreads();
+        const uint32_t at = s_at;
+        for (int i = tid; i < (int)min(s_n, (uint32_t)kList); i += kThreads)
+            if (at + i < kList) R.list[at + i] = s_key[i];
+    }
+    __threadfence();
+    __syncthreads();
+    if (tid == 0) s_last = atomicAdd(&R.ticket[1], 1u) == (uint32_t)slices - 1;
+    __syncthreads();
+    if (!s_last) return;
+    __threadfence();
+    const int n = (int)__hip_atomic_load(&R.ticket[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (n > kList) {
+        __syncthreads();
+        sample_by_digits<TYPE>(A, m, s_key, s_part, s_pick);
+        return;
+    }
+    for (int b = tid; b <= kAll; b += kThreads) s_before[b] = R.before[b];
+    for (int i = tid; i < n; i += kThreads) s_key[i] = __hip_atomic_load(&R.list[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    sort_keys<kThreads>(s_key, n);
+    sum_weights<kThreads, kList / kThreads>(s_key, s_sum, n, c, st.ref, s_table, s_part);
+    if (tid >= 64) return;
+    // One wavefront goes through the filters.  Every place is an index into the sorted list.
+    auto bin_at = [&](int i) {
+        double r;
+        return bin_of(steps_of(fmax(fmin(fma((double)key_value(s_key[i]), c, -st.ref), 0.0), -60.0), r));
+    };
+    // the first place of the list in bin b or behind
+    auto place_of = [&](int b) { return search(0, n, lane, [&](int i) { return bin_at(i) >= b; }); };
+    auto sum_to = [&](int i) { return i > 0 ? s_sum[i - 1] : 0ull; };
+    // the weight of the row's tokens in front of the list's place i
+    auto before = [&](int i) {
+        const int b = bin_at(i);
+        return s_before[b] + sum_to(i) - sum_to(place_of(b));
+    };
+    auto upto = [&](int i) { return before(i) + s_sum[i] - sum_to(i); };
+    // the place where that reaches target: its bin from the row's sums, then within the bin
+    auto place_at = [&](u64 target) {
+        const int bin = min(search(0, kAll, lane, [&](int b) { return s_before[b + 1] >= target; }), kAll - 1);
+        const int first = place_of(bin), end = place_of(bin + 1);
+        const u64 rest = target - s_before[bin] + sum_to(first);
+        const int i = search(first, end, lane, [&](int i) { return s_sum[i] >= rest; });
+        return max(min(i, min(end, n) - 1), 0);                  // (the last of the bin if rounding leaves it short)
+    };
+    int last = n;                                                // the place of the last token that is kept; n: all of the row are
+    u64 kept = s_before[kAll];
+    if (st.k_bin >= 0) {
+        last = min(place_of(st.k_bin) + st.k_left, n) - 1;
+        kept = upto(last);
+    }
+    const float p = A.top_p ? A.top_p[m] : 1.f;
+    if (p < 1.f) {
+        kept = share_up(p, kept);
+        if (s_before[st.end_bin + 1] >= kept) {                  // (otherwise min-p cuts in front of that)
+            last = min(last, place_at(kept));
+            kept = upto(last);
+        }
+    }
+    const float least = A.min_p ? A.min_p[m] : 0.f;
+    if (least > 0.f) {
+        // the first place whose weight is too small; if that is not on the list, the last bin that may hold larger ones ends there
+        const int first = search(0, n, lane, [&](int i) {
+            const float z = key_value(s_key[i]);
+            return z != st.z_max && weight(z, st.z_max, c) < (double)least;
+        });
+        const bool on = first < n && bin_at(min(first, n - 1)) <= st.least_bin;
+        const u64 mass = on ? before(first) : s_before[st.least_bin + 1];
+        if (mass < kept) {
+            kept = mass;
+            last = max((on ? first : place_of(st.least_bin + 1)) - 1, 0);
+        }
+    }
+    int at = place_at(share_past(A.u[m], kept));
+    if (last < n) at = min(at, last);
+    if (tid == 0) give(A, m, s_key[at], kept, c, st.ref);
+}
+
 }  // namespace
 
-size_t sample_workspace(int M, int V) { return 0; }
+static int slices_of(int V) { return (V + kSlice - 1) / kSlice; }
 
-hipError_t launch_sample(const SampleArgs& a, int type, void* workspace, int num_cu, hipStream_t stream) {
-    const dim3 grid((unsigned)a.M);
-    if (type == EVOSPEC_FP32) sample_row_kernel<EVOSPEC_FP32><<<grid, kThreads, 0, stream>>>(a);
-    else if (type == EVOSPEC_FP16) sample_row_kernel<EVOSPEC_FP16><<<grid, kThreads, 0, stream>>>(a);
-    else sample_row_kernel<EVOSPEC_BF16><<<grid, kThreads, 0, stream>>>(a);
+size_t sample_workspace(int M, int V) { return (size_t)M * row_bytes(slices_of(V)); }
+
+template <int TYPE>
+static hipError_t sample_as(const SampleArgs& a, char* ws, hipStream_t stream) {
+    const int slices = slices_of(a.V);
+    sample_bins_kernel<TYPE><<<dim3((unsigned)(a.M * slices)), kThreads, 0, stream>>>(a, ws, slices);
+    sample_row_kernel<<<dim3((unsigned)a.M), kRowThreads, 0, stream>>>(a, ws, slices);
+    sample_pick_kernel<TYPE><<<dim3((unsigned)(a.M * slices)), kThreads, 0, stream>>>(a, ws, slices);
     return hipGetLastError();
+}
+
+hipError_t launch_sample(const SampleArgs& a, int type, void* workspace, hipStream_t stream) {
+    char* ws = static_cast<char*>(workspace);
+    return type == EVOSPEC_FP32 ? sample_as<EVOSPEC_FP32>(a, ws, stream)
+                                : type == EVOSPEC_FP16 ? sample_as<EVOSPEC_FP16>(a, ws, stream) : sample_as<EVOSPEC_BF16>(a, ws, stream);
 }
 
 }  // namespace evospec

@@ -99,6 +99,31 @@ def test_flat_rows(ev, type, V):
     run(ev, z, rng.random(M), type, top_k=rng.integers(1, V, M), top_p=rng.random(M), ids=ids)
 
 
+def test_filters_that_cut_in_turn(ev):
+    """Each of the three filters in front of, near and far behind the others."""
+    rng = np.random.default_rng(7)
+    M = 48
+    for V in (300, 60000):
+        z = logits(rng, M, V)
+        run(ev, z, rng.random(M), temperature=rng.choice([0.5, 1.0, 1.5], M), top_k=rng.choice([0, 3, 30, V - 1], M),
+            top_p=rng.choice([0.3, 0.9, 0.999, 0.999999], M), min_p=rng.choice([0.0, 0.9, 0.1, 1e-3, 1e-6, 1e-12], M))
+        run(ev, z, rng.random(M), top_p=[0.999999] * M, min_p=rng.random(M) ** 3)
+        run(ev, z, rng.random(M), top_k=[V - 1] * M, min_p=10.0 ** -rng.integers(0, 14, M))
+
+
+@pytest.mark.parametrize("V", [65, 700, 897, 1000, 1024, 4096, 4097, 20480, 20481, 41000])
+def test_lists_of_the_largest(ev, V):
+    """top-k up to and past what is kept in lists, of slices of every size; ties at the border; most tokens masked."""
+    rng = np.random.default_rng(V)
+    M = 12
+    k = rng.choice([1, 2, 15, 16, 17, 64, 100, 511, 512, 513], M)
+    z = logits(rng, M, V)
+    run(ev, z, rng.random(M), top_k=k)
+    run(ev, np.round(z), rng.random(M), "bf16", top_k=k, top_p=rng.random(M), ids=rng.permutation(V))
+    z[rng.random((M, V)) < 0.99] = -np.inf
+    run(ev, z, rng.random(M), top_k=k, min_p=rng.random(M) / 10)
+
+
 def test_borders(ev):
     """Equal weights, so that the borders of top-k, top-p and u fall on tokens exactly."""
     z = np.zeros((4, 8))
