@@ -198,6 +198,7 @@ constexpr int kRange = 44;                        // factors of 2 that are kept,
 constexpr int kAll = kBins * 28;                  // those behind the 28th in the last bin
 constexpr int kGroups = 5;                        // of 4 logits of a thread
 constexpr int kSlice = kThreads * 4 * kGroups;
+constexpr int kMostSlices = ((1 << 20) + kSlice - 1) / kSlice;
 constexpr int kList = 4096;
 constexpr int kMostK = 512;                       // top-k up to this goes by lists alone
 constexpr int kSteps = 128;                       // of the table of powers of two
@@ -213,27 +214,31 @@ struct RowState {
 };
 enum { kOpen = 0, kDone = 1, kDigits = 2 };
 
+struct SliceState {
+    double ref;                                   // exponent of its reference; with lists the bound that they reach
+    u64 top;                                      // its largest logit as a key, greedy rows with its id; 0: no number there
+    uint32_t n, pad;                              // tokens on its list
+};
+
 // A row's part of the workspace.
 struct RowSpace {
     u64* mass;                                    // [slices][kAll]
     uint32_t* count;                              // [slices][kAll], where top-k asks for it
-    double* ref;                                  // [slices]
-    u64* top;                                     // [slices]: greedy rows' largest key
+    SliceState* slice;                            // [slices]
     u64* before;                                  // [kAll + 1]: what the bins in front weigh
     RowState* row;
     uint32_t* ticket;                             // tokens on the list, workgroups that came
     u64* list;                                    // [kList]
 };
 __host__ __device__ inline size_t row_bytes(int slices) {
-    const size_t n = (size_t)slices * (kAll * 12 + 16) + (kAll + 1) * 8 + sizeof(RowState) + 8 + kList * 8;
+    const size_t n = (size_t)slices * (kAll * 12 + sizeof(SliceState)) + (kAll + 1) * 8 + sizeof(RowState) + 8 + kList * 8;
     return (n + 255) / 256 * 256;
 }
 __device__ __forceinline__ RowSpace row_space(char* ws, int m, int slices) {
     char* p = ws + (size_t)m * row_bytes(slices);
     RowSpace r;
     r.mass = reinterpret_cast<u64*>(p);           p += (size_t)slices * kAll * 8;
-    r.ref = reinterpret_cast<double*>(p);         p += (size_t)slices * 8;
-    r.top = reinterpret_cast<u64*>(p);            p += (size_t)slices * 8;
+    r.slice = reinterpret_cast<SliceState*>(p);   p += (size_t)slices * sizeof(SliceState);
     r.before = reinterpret_cast<u64*>(p);         p += (kAll + 1) * 8;
     r.list = reinterpret_cast<u64*>(p);           p += kList * 8;
     r.row = reinterpret_cast<RowState*>(p);       p += sizeof(RowState);
@@ -254,11 +259,18 @@ __device__ __forceinline__ int steps_of(double x, double& r) {
     r = x - (t - magic);
     return -(int)(uint32_t)__double_as_longlong(t);
 }
+// x y + c with c in scalar registers (the compiler's choice copies c to vector registers first, 2 more instructions of 3)
+__device__ __forceinline__ double fma_to(double x, double y, double c) {
+    double d;
+    asm("v_fma_f64 %0, %1, %2, %3" : "=v"(d) : "v"(x), "v"(y), "s"(c));
+    return d;
+}
 __device__ __forceinline__ u64 weight_of(int steps, double r, const double* table) {
-    double p = 0.0096181291076284772;                            // ln(2)^4 / 4!
-    p = fma(p, r, 0.055504108664821580);
-    p = fma(p, r, 0.24022650695910071);
-    p = fma(p, r, 0.69314718055994531);
+    double first = 0.0096181291076284772;                        // ln(2)^k / k!
+    asm("" : "+v"(first));                                     // (one vector register pair for all calls)
+    double p = fma_to(r, first, 0.055504108664821580);
+    p = fma_to(p, r, 0.24022650695910071);
+    p = fma_to(p, r, 0.69314718055994531);
     p = fma(p, r, 1.0);
     const int n = (-steps) >> 7, j = (-steps) & (kSteps - 1);
     const double s = __longlong_as_double((long long)(1023 + 43 + n) << 52);
@@ -266,7 +278,7 @@ __device__ __forceinline__ u64 weight_of(int steps, double r, const double* tabl
     return (u64)__double_as_longlong(d) & 0xfffffffffffffull;
 }
 static_assert(kSteps == 128 && kSteps % kBins == 0, "shifts");
-__device__ __forceinline__ int bin_of(int steps) { return min(steps / (kSteps / kBins), kAll - 1); }
+__device__ __forceinline__ int bin_of(int steps) { return min((int)((uint32_t)steps / (kSteps / kBins)), kAll - 1); }
 
 struct Slice {
     int first, last;
@@ -350,9 +362,7 @@ __device__ __forceinline__ void list_largest(const SampleArgs& A, const float (&
     const uint32_t n = s_n;
     for (int i = tid; i < (int)min(n, (uint32_t)kAll); i += kThreads) R.mass[(size_t)j * kAll + i] = s_key[i];
     if (tid == 0) {
-        R.count[(size_t)j * kAll] = n;
-        R.top[j] = top > -__builtin_inff() ? make_key(top, 0) : 0;
-        R.ref[j] = (double)bound;
+        R.slice[j] = SliceState{(double)bound, top > -__builtin_inff() ? make_key(top, 0) : 0, n, 0};
     }
 }
 
@@ -401,10 +411,7 @@ __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs A, cha
                     }
         }
         best = reduce_all(best, s_part, [](u64 a, u64 b) { return a > b ? a : b; });
-        if (tid == 0) {
-            R.top[j] = best;
-            R.ref[j] = 0.0;
-        }
+        if (tid == 0) R.slice[j] = SliceState{0.0, best, 0, 0};
         return;
     }
     if (counts && A.top_k[m] <= kMostK) {                        // (uniform)
@@ -414,17 +421,15 @@ __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs A, cha
     const double c = 1.4426950408889634074 / (double)T;
     const bool ok = top > -__builtin_inff() && regular(T, top);
     const double ref = ok ? ceil((double)top * c) : 0.0;
-    if (tid == 0) {
-        R.top[j] = top > -__builtin_inff() ? make_key(top, 0) : 0;
-        R.ref[j] = ref;
-    }
+    if (tid == 0) R.slice[j] = SliceState{ref, top > -__builtin_inff() ? make_key(top, 0) : 0, 0, 0};
     if (!ok) return;                                             // (uniform) nothing here, or a row for the digits
+    const float cut = (float)((ref - kRange) / c);
 #pragma unroll
     for (int g = 0; g < kGroups; ++g)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const double x = fma((double)z[g][e], c, -ref);
-            if (x > -(double)kRange) {                           // (not NaN)
+            if (z[g][e] >= cut) {                                // (not NaN)
+                const double x = fma((double)z[g][e], c, -ref);
                 double r;
                 const int steps = steps_of(x, r), b = bin_of(steps);
                 atomicAdd(&s_mass[b], weight_of(steps, r, s_table));
@@ -438,25 +443,50 @@ __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs A, cha
     }
 }
 
-// Sorts s_key[0, n), descending, n <= the array's power of two of places; what is behind n becomes 0.
-template <int THREADS>
+// x of lane ^ d, d a power of two below 64
+__device__ __forceinline__ u64 xor_lane64(u64 x, int d, int lane) {
+    const uint32_t lo = (uint32_t)x, hi = (uint32_t)(x >> 32);
+#define EVOSPEC_XOR(D) \
+    case D: return (u64)xor_lane<D>(hi, lane) << 32 | xor_lane<D>(lo, lane);
+    switch (d) {
+        EVOSPEC_XOR(1) EVOSPEC_XOR(2) EVOSPEC_XOR(4) EVOSPEC_XOR(8) EVOSPEC_XOR(16)
+        default: return (u64)xor_lane<32>(hi, lane) << 32 | xor_lane<32>(lo, lane);
+    }
+#undef EVOSPEC_XOR
+}
+// Sorts s_key[0, n), descending, n <= THREADS * EACH (its size).  Bitonic, place i in register i / THREADS of thread i % THREADS, so
+// that exchanges of up to 32 places stay within a wavefront's registers (300 keys by 512 threads: 6 of 45 steps go through LDS).
+template <int THREADS, int EACH>
 __device__ __forceinline__ void sort_keys(u64* s_key, int n) {
+    const int tid = threadIdx.x, lane = tid & 63;
     int size = 64;
     while (size < n) size *= 2;
-    for (int i = n + threadIdx.x; i < size; i += THREADS) s_key[i] = 0;
+    u64 v[EACH];
+#pragma unroll
+    for (int r = 0; r < EACH; ++r) v[r] = r * THREADS + tid < n ? s_key[r * THREADS + tid] : 0;
     __syncthreads();
     for (int w = 2; w <= size; w *= 2)
         for (int d = w / 2; d > 0; d /= 2) {
-            for (int i = threadIdx.x; i < size / 2; i += THREADS) {
-                const int a = (i & ~(d - 1)) * 2 + (i & (d - 1)), b = a + d;
-                const u64 x = s_key[a], y = s_key[b];
-                if ((x < y) == ((a & w) == 0)) {
-                    s_key[a] = y;
-                    s_key[b] = x;
-                }
+            if (d >= 64) {
+#pragma unroll
+                for (int r = 0; r < EACH; ++r)
+                    if (r * THREADS + tid < size) s_key[r * THREADS + tid] = v[r];
+                __syncthreads();
             }
-            __syncthreads();
+#pragma unroll
+            for (int r = 0; r < EACH; ++r) {
+                const int i = r * THREADS + tid;
+                if (r * THREADS >= size) break;                  // (uniform)
+                const u64 y = d >= 64 ? (i < size ? s_key[i ^ d] : 0) : xor_lane64(v[r], d, lane);
+                const bool larger = ((i & d) == 0) == ((i & w) == 0);
+                v[r] = (y > v[r]) == larger ? y : v[r];
+            }
+            if (d >= 64) __syncthreads();
         }
+#pragma unroll
+    for (int r = 0; r < EACH; ++r)
+        if (r * THREADS + tid < size) s_key[r * THREADS + tid] = v[r];
+    __syncthreads();
 }
 __device__ __forceinline__ u64 shfl_up64(u64 x, int s) {
     return (u64)(uint32_t)__shfl_up((int)(uint32_t)x, s) | (u64)(uint32_t)__shfl_up((int)(uint32_t)(x >> 32), s) << 32;
@@ -518,8 +548,8 @@ constexpr int kRowThreads = 512;
 constexpr int kRowList = 2048;
 
 // A row of a small top-k, from its slices' lists.  False if they do not hold what is needed.
-__device__ bool finish_largest(const SampleArgs& A, int m, int k, const RowSpace& R, int slices, double c, double ref, float z_max, u64* s_key,
-                               u64* s_sum, double* s_table, u64* s_part, uint32_t* s_n) {
+__device__ bool finish_largest(const SampleArgs& A, int m, int k, const RowSpace& R, const SliceState* s_slice, int slices, double c, double ref,
+                               float z_max, u64* s_key, u64* s_sum, double* s_table, u64* s_part, uint32_t* s_n) {
     const int tid = threadIdx.x, lane = tid & 63;
     fill_table(s_table);
     if (tid == 0) *s_n = 0;
@@ -527,14 +557,14 @@ __device__ bool finish_largest(const SampleArgs& A, int m, int k, const RowSpace
     float bound = -__builtin_inff();
     bool full = false;
     for (int j = 0; j < slices; ++j) {
-        bound = fmaxf(bound, (float)R.ref[j]);
-        full |= R.count[(size_t)j * kAll] > (uint32_t)kAll;
+        bound = fmaxf(bound, (float)s_slice[j].ref);
+        full |= s_slice[j].n > (uint32_t)kAll;
     }
     if (full) return false;                                      // (uniform)
     __syncthreads();
-    for (int j = 0; j < slices; ++j) {
-        const int n = (int)R.count[(size_t)j * kAll];
-        for (int i = tid; i < n; i += kRowThreads) {
+    for (int j = tid >> 6; j < slices; j += kRowThreads / 64) {
+        const int n = (int)s_slice[j].n;
+        for (int i = lane; i < n; i += 64) {
             const u64 key = R.mass[(size_t)j * kAll + i];
             if (key_value(key) >= bound) {
                 const uint32_t at = atomicAdd(s_n, 1u);
@@ -545,7 +575,7 @@ __device__ bool finish_largest(const SampleArgs& A, int m, int k, const RowSpace
     __syncthreads();
     int n = (int)*s_n;
     if (n > kRowList) return false;
-    sort_keys<kRowThreads>(s_key, n);
+    sort_keys<kRowThreads, kRowList / kRowThreads>(s_key, n);
     n = min(n, k);
     sum_weights<kRowThreads, 1>(s_key, s_sum, n, c, ref, s_table, s_part);     // (n <= k <= kMostK)
     if (tid >= 64) return true;
@@ -577,11 +607,14 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs A, c
     __shared__ u64 s_sum[kRowThreads / 64];
     __shared__ uint32_t s_num[kRowThreads / 64];
     __shared__ int s_found[8];
+    __shared__ SliceState s_slice[kMostSlices];
     const int m = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
     const RowSpace R = row_space(ws, m, slices);
     const float T = A.temperature ? A.temperature[m] : 1.f;
+    for (int j = tid; j < slices; j += kRowThreads) s_slice[j] = R.slice[j];
+    __syncthreads();
     u64 top = 0;
-    for (int j = 0; j < slices; ++j) top = R.top[j] > top ? R.top[j] : top;
+    for (int j = 0; j < slices; ++j) top = s_slice[j].top > top ? s_slice[j].top : top;
     const float z_max = key_value(top);
     const int k = A.top_k ? A.top_k[m] : 0;
     if (top == 0 || !(T > 0.f)) {
@@ -602,7 +635,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs A, c
         __shared__ u64 s_key[kRowList], s_weight[kRowList];
         __shared__ double s_table[kSteps];
         __shared__ uint32_t s_n;
-        const bool done = finish_largest(A, m, k, R, slices, c, ref, z_max, s_key, s_weight, s_table, s_sum, &s_n);
+        const bool done = finish_largest(A, m, k, R, s_slice, slices, c, ref, z_max, s_key, s_weight, s_table, s_sum, &s_n);
         if (tid == 0) R.row->state = done ? kDone : kDigits;
         return;
     }
@@ -613,8 +646,8 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs A, c
     }
     __syncthreads();
     for (int j = 0; j < slices; ++j) {
-        if (R.top[j] == 0 || !regular(T, key_value(R.top[j]))) continue;
-        const double gap = ref - R.ref[j];                       // (a whole number >= 0)
+        if (s_slice[j].top == 0 || !regular(T, key_value(s_slice[j].top))) continue;
+        const double gap = ref - s_slice[j].ref;                       // (a whole number >= 0)
         if (gap >= kRange) continue;
         const int shift = (int)gap;
         for (int b = tid; b < kAll; b += kRowThreads) {
@@ -775,26 +808,29 @@ __global__ __launch_bounds__(kThreads) void sample_pick_kernel(SampleArgs A, cha
     const double c = 1.4426950408889634074 / (double)T;
     const char* row = static_cast<const char*>(A.logits) + (long long)m * A.stride * (TYPE == EVOSPEC_FP32 ? 4 : 2);
     const int b_min = min(st.lo[0], min(st.lo[1], st.lo[2])), b_max = max(st.hi[0], max(st.hi[1], st.hi[2]));
-    const u64 mine = R.top[j];
-    const double ref = R.ref[j];
+    const SliceState mine = R.slice[j];
+    const double ref = mine.ref;
     const int shift = (int)fmin(st.ref - ref, 64.0) * kBins;
     fill_table(s_table);
     if (tid == 0) s_n = 0;
     __syncthreads();
-    if (mine != 0 && regular(T, key_value(mine)) && st.ref - ref < kRange) {    // (uniform)
+    if (mine.top != 0 && regular(T, key_value(mine.top)) && st.ref - ref < kRange) {    // (uniform)
         const Slice S = slice_of(A.V, slices, j);
         float z[kGroups][4];
         load_slice<TYPE>(row, S, z);
+        // logits that can be in those bins, a little generously: bin b ends where x = -(b + 1) / kBins, to half a step
+        const double far = (st.ref - (double)(b_max + 2) / kBins) / c;
+        const float least = b_max == kAll - 1 ? -__builtin_inff() : (float)(far - fabs(far) * 0x1p-20);
 #pragma unroll
         for (int g = 0; g < kGroups; ++g)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const double x = fma((double)z[g][e], c, -ref);
                 bool on = false;
-                if (x > -(double)kRange) {
+                if (z[g][e] >= least) {
+                    const double x = fma((double)z[g][e], c, -ref);
                     double r;
-                    const int b = min(bin_of(steps_of(x, r)) + shift, kAll - 1);
-                    on = b >= b_min && b <= b_max &&
+                    const int b = min(bin_of(steps_of(fmax(x, -60.0), r)) + shift, kAll - 1);
+                    on = x > -(double)kRange && b >= b_min && b <= b_max &&
                          ((b >= st.lo[0] && b <= st.hi[0]) || (b >= st.lo[1] && b <= st.hi[1]) || (b >= st.lo[2] && b <= st.hi[2]));
                 }
                 if (on) {
@@ -805,18 +841,19 @@ __global__ __launch_bounds__(kThreads) void sample_pick_kernel(SampleArgs A, cha
             }
         __syncthreads();
         // (a list that is too long for one workgroup is too long for the row)
-        if (tid == 0) s_at = atomicAdd(&R.ticket[0], s_n);
+        if (tid == 0) s_at = __hip_atomic_fetch_add(&R.ticket[0], s_n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __syncthreads();
         const uint32_t at = s_at;
         for (int i = tid; i < (int)min(s_n, (uint32_t)kList); i += kThreads)
-            if (at + i < kList) R.list[at + i] = s_key[i];
+            if (at + i < kList) __hip_atomic_store(&R.list[at + i], s_key[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    __threadfence();
+    // The list is written and read past the caches that are not shared (agent scope), and every store has arrived before the
+    // workgroup's ticket is taken: a fence instead would write back all of an L2 for each workgroup (960 rows: 5.5 ms).
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (tid == 0) s_last = atomicAdd(&R.ticket[1], 1u) == (uint32_t)slices - 1;
+    if (tid == 0) s_last = __hip_atomic_fetch_add(&R.ticket[1], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)slices - 1;
     __syncthreads();
     if (!s_last) return;
-    __threadfence();
     const int n = (int)__hip_atomic_load(&R.ticket[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (n > kList) {
         __syncthreads();
@@ -825,7 +862,7 @@ __global__ __launch_bounds__(kThreads) void sample_pick_kernel(SampleArgs A, cha
     }
     for (int b = tid; b <= kAll; b += kThreads) s_before[b] = R.before[b];
     for (int i = tid; i < n; i += kThreads) s_key[i] = __hip_atomic_load(&R.list[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    sort_keys<kThreads>(s_key, n);
+    sort_keys<kThreads, kList / kThreads>(s_key, n);
     sum_weights<kThreads, kList / kThreads>(s_key, s_sum, n, c, st.ref, s_table, s_part);
     if (tid >= 64) return;
     // One wavefront goes through the filters.  Every place is an index into the sorted list.
