@@ -183,24 +183,27 @@ __device__ __noinline__ void sample_by_digits(const SampleArgs& A, int m, u64* s
 
 
 // ---------------------------------------------------------------------------------------
-// The fast way, three launches.
+// The fast way, four launches.
 //
 // 1. sample_bins_kernel, a workgroup for each slice of a row (kSlice logits at most, which stay in registers): the slice's
 //    largest logit, and the weights of its tokens, summed in bins of 1 / kBins of a power of two below e = the next power of two
 //    above that logit.  References are whole powers of two, so that slices' bins lie on one grid and their sums are joined by shifts.
 // 2. sample_row_kernel, a workgroup for each row: the bins of all slices, joined; in which bins top-k, top-p and min-p cut, and in which
 //    the draw falls (a range of them where one depends on a cut inside a bin).  Greedy rows end here.
-// 3. sample_pick_kernel, a workgroup for each slice again: tokens of those bins are put on the row's list; the last workgroup of
-//    the row to come sorts the list, and goes through the filters with the list's tokens and the bins' sums.
-// Lists that are full (thousands of tokens within 1 / kBins of a power of two) leave the row to sample_by_digits.
+// 3. sample_pick_kernel, a workgroup for each slice again: tokens of those bins are put on the row's list.
+// 4. sample_finish_kernel, a workgroup for each row: sorts the list, and goes through the filters with the list's tokens and the bins'
+//    sums.
+// Rows of a top-k up to kMostK need no weights but those of their k largest tokens: 1. lists the tokens that can be among them, and 2.
+// ends the row.  Lists that are full (thousands of tokens within 1 / kBins of a power of two) leave the row to sample_by_digits.
 constexpr int kBins = 32;                         // to a factor of 2
 constexpr int kRange = 44;                        // factors of 2 that are kept,
 constexpr int kAll = kBins * 28;                  // those behind the 28th in the last bin
 constexpr int kGroups = 5;                        // of 4 logits of a thread
 constexpr int kSlice = kThreads * 4 * kGroups;
 constexpr int kMostSlices = ((1 << 20) + kSlice - 1) / kSlice;
-constexpr int kList = 4096;
-constexpr int kMostK = 512;                       // top-k up to this goes by lists alone
+constexpr int kList = 4096;                       // tokens of a row that are looked at one by one
+constexpr int kStage = 1024;                      // of a slice that go to that list at once
+constexpr int kMostK = 256;                       // top-k up to this goes by lists alone
 constexpr int kSteps = 128;                       // of the table of powers of two
 
 struct RowState {
@@ -227,8 +230,8 @@ struct RowSpace {
     SliceState* slice;                            // [slices]
     u64* before;                                  // [kAll + 1]: what the bins in front weigh
     RowState* row;
-    uint32_t* ticket;                             // tokens on the list, workgroups that came
-    u64* list;                                    // [kList]
+    uint32_t* ticket;                             // tokens on the list
+    u64* list;                                    // [kList], in any order
 };
 __host__ __device__ inline size_t row_bytes(int slices) {
     const size_t n = (size_t)slices * (kAll * 12 + sizeof(SliceState)) + (kAll + 1) * 8 + sizeof(RowState) + 8 + kList * 8;
@@ -386,7 +389,7 @@ __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs A, cha
         s_mass[b] = 0;
         s_count[b] = 0;
     }
-    if (j == 0 && tid < 2) R.ticket[tid] = 0;
+    if (j == 0 && tid == 0) *R.ticket = 0;
     float top = -__builtin_inff();
 #pragma unroll
     for (int g = 0; g < kGroups; ++g)
@@ -443,50 +446,55 @@ __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs A, cha
     }
 }
 
-// x of lane ^ d, d a power of two below 64
-__device__ __forceinline__ u64 xor_lane64(u64 x, int d, int lane) {
-    const uint32_t lo = (uint32_t)x, hi = (uint32_t)(x >> 32);
-#define EVOSPEC_XOR(D) \
-    case D: return (u64)xor_lane<D>(hi, lane) << 32 | xor_lane<D>(lo, lane);
-    switch (d) {
-        EVOSPEC_XOR(1) EVOSPEC_XOR(2) EVOSPEC_XOR(4) EVOSPEC_XOR(8) EVOSPEC_XOR(16)
-        default: return (u64)xor_lane<32>(hi, lane) << 32 | xor_lane<32>(lo, lane);
-    }
-#undef EVOSPEC_XOR
+// One step of a bitonic sort within a wavefront: the larger of lane and lane ^ D goes to the one that is to have it.
+template <int D>
+__device__ __forceinline__ void exchange(u64& v, bool descending, int lane) {
+    const u64 y = (u64)xor_lane<D>((uint32_t)(v >> 32), lane) << 32 | xor_lane<D>((uint32_t)v, lane);
+    const bool larger = ((lane & D) == 0) == descending;
+    v = (y > v) == larger ? y : v;
 }
-// Sorts s_key[0, n), descending, n <= THREADS * EACH (its size).  Bitonic, place i in register i / THREADS of thread i % THREADS, so
-// that exchanges of up to 32 places stay within a wavefront's registers (300 keys by 512 threads: 6 of 45 steps go through LDS).
-template <int THREADS, int EACH>
+template <int D>
+__device__ __forceinline__ void exchange_from(u64& v, bool descending, int lane) {
+    exchange<D>(v, descending, lane);
+    if constexpr (D > 1) exchange_from<D / 2>(v, descending, lane);
+}
+// Sorts s_key[0, n), descending; places up to the next power of two are there.  Exchanges of up to 32 places are made in the
+// registers of a wavefront that holds 64 keys in a row, the others (10 of the 55 steps of 1,024 keys) in LDS.
+template <int THREADS>
 __device__ __forceinline__ void sort_keys(u64* s_key, int n) {
     const int tid = threadIdx.x, lane = tid & 63;
     int size = 64;
     while (size < n) size *= 2;
-    u64 v[EACH];
-#pragma unroll
-    for (int r = 0; r < EACH; ++r) v[r] = r * THREADS + tid < n ? s_key[r * THREADS + tid] : 0;
+    for (int i = tid; i < size; i += THREADS) {
+        u64 v = i < n ? s_key[i] : 0;
+        exchange_from<1>(v, (lane & 2) == 0, lane);
+        exchange_from<2>(v, (lane & 4) == 0, lane);
+        exchange_from<4>(v, (lane & 8) == 0, lane);
+        exchange_from<8>(v, (lane & 16) == 0, lane);
+        exchange_from<16>(v, (lane & 32) == 0, lane);
+        exchange_from<32>(v, (i & 64) == 0, lane);
+        s_key[i] = v;
+    }
     __syncthreads();
-    for (int w = 2; w <= size; w *= 2)
-        for (int d = w / 2; d > 0; d /= 2) {
-            if (d >= 64) {
-#pragma unroll
-                for (int r = 0; r < EACH; ++r)
-                    if (r * THREADS + tid < size) s_key[r * THREADS + tid] = v[r];
-                __syncthreads();
+    for (int w = 128; w <= size; w *= 2) {
+        for (int d = w / 2; d >= 64; d /= 2) {
+            for (int i = tid; i < size / 2; i += THREADS) {
+                const int a = (i & ~(d - 1)) * 2 + (i & (d - 1)), b = a + d;
+                const u64 x = s_key[a], y = s_key[b];
+                if ((x < y) == ((a & w) == 0)) {
+                    s_key[a] = y;
+                    s_key[b] = x;
+                }
             }
-#pragma unroll
-            for (int r = 0; r < EACH; ++r) {
-                const int i = r * THREADS + tid;
-                if (r * THREADS >= size) break;                  // (uniform)
-                const u64 y = d >= 64 ? (i < size ? s_key[i ^ d] : 0) : xor_lane64(v[r], d, lane);
-                const bool larger = ((i & d) == 0) == ((i & w) == 0);
-                v[r] = (y > v[r]) == larger ? y : v[r];
-            }
-            if (d >= 64) __syncthreads();
+            __syncthreads();
         }
-#pragma unroll
-    for (int r = 0; r < EACH; ++r)
-        if (r * THREADS + tid < size) s_key[r * THREADS + tid] = v[r];
-    __syncthreads();
+        for (int i = tid; i < size; i += THREADS) {
+            u64 v = s_key[i];
+            exchange_from<32>(v, (i & w) == 0, lane);
+            s_key[i] = v;
+        }
+        __syncthreads();
+    }
 }
 __device__ __forceinline__ u64 shfl_up64(u64 x, int s) {
     return (u64)(uint32_t)__shfl_up((int)(uint32_t)x, s) | (u64)(uint32_t)__shfl_up((int)(uint32_t)(x >> 32), s) << 32;
@@ -547,6 +555,44 @@ __device__ __forceinline__ void give(const SampleArgs& A, int m, u64 key, u64 ke
 constexpr int kRowThreads = 512;
 constexpr int kRowList = 2048;
 
+// Of n keys in LDS, logits in [bound, top], those that can be among the k largest, k <= n: by their numbers in kRowThreads even steps
+// of the range.  Gives how many are left.
+__device__ int keep_front(u64* s_key, int n, int k, float bound, float top, uint32_t* s_n) {
+    __shared__ uint32_t s_num[kRowThreads + 1], s_wave[kRowThreads / 64];
+    __shared__ int s_cut;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const float per = (float)kRowThreads / fmaxf(top - bound, 1e-30f);
+    auto step_of = [&](u64 key) { return min(max((int)((top - key_value(key)) * per), 0), kRowThreads - 1); };
+    s_num[tid] = 0;
+    if (tid == 0) *s_n = 0;
+    __syncthreads();
+    u64 mine[kRowList / kRowThreads];
+#pragma unroll
+    for (int r = 0; r < kRowList / kRowThreads; ++r) {
+        mine[r] = r * kRowThreads + tid < n ? s_key[r * kRowThreads + tid] : 0;
+        if (mine[r]) atomicAdd(&s_num[step_of(mine[r])], 1u);
+    }
+    __syncthreads();
+    const uint32_t num = s_num[tid];
+    uint32_t run = num;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+        const uint32_t x = (uint32_t)__shfl_up((int)run, s);
+        if (lane >= s) run += x;
+    }
+    if (lane == 63) s_wave[tid >> 6] = run;
+    __syncthreads();
+    for (int w = 0; w < tid >> 6; ++w) run += s_wave[w];
+    if (run >= (uint32_t)k && run - num < (uint32_t)k) s_cut = tid;
+    __syncthreads();
+    const int cut = s_cut;
+#pragma unroll
+    for (int r = 0; r < kRowList / kRowThreads; ++r)
+        if (mine[r] && step_of(mine[r]) <= cut) s_key[atomicAdd(s_n, 1u)] = mine[r];
+    __syncthreads();
+    return (int)*s_n;
+}
+
 // A row of a small top-k, from its slices' lists.  False if they do not hold what is needed.
 __device__ bool finish_largest(const SampleArgs& A, int m, int k, const RowSpace& R, const SliceState* s_slice, int slices, double c, double ref,
                                float z_max, u64* s_key, u64* s_sum, double* s_table, u64* s_part, uint32_t* s_n) {
@@ -575,7 +621,8 @@ __device__ bool finish_largest(const SampleArgs& A, int m, int k, const RowSpace
     __syncthreads();
     int n = (int)*s_n;
     if (n > kRowList) return false;
-    sort_keys<kRowThreads, kRowList / kRowThreads>(s_key, n);
+    if (n > 2 * k) n = keep_front(s_key, n, k, bound, z_max, s_n);
+    sort_keys<kRowThreads>(s_key, n);
     n = min(n, k);
     sum_weights<kRowThreads, 1>(s_key, s_sum, n, c, ref, s_table, s_part);     // (n <= k <= kMostK)
     if (tid >= 64) return true;
@@ -791,19 +838,12 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs A, c
 
 template <int TYPE>
 __global__ __launch_bounds__(kThreads) void sample_pick_kernel(SampleArgs A, char* ws, int slices) {
-    __shared__ u64 s_key[kList], s_sum[kList], s_before[kAll + 1];
-    __shared__ double s_table[kSteps];
-    __shared__ u64 s_part[kThreads / 64], s_pick[2];
-    __shared__ uint32_t s_last, s_n, s_at;
-    const int m = blockIdx.x / slices, j = blockIdx.x % slices, tid = threadIdx.x, lane = tid & 63;
+    __shared__ u64 s_key[kStage];
+    __shared__ uint32_t s_n, s_at;
+    const int m = blockIdx.x / slices, j = blockIdx.x % slices, tid = threadIdx.x;
     const RowSpace R = row_space(ws, m, slices);
-    const int state = R.row->state;
-    if (state == kDone) return;
+    if (R.row->state != kOpen) return;
     const float T = A.temperature ? A.temperature[m] : 1.f;
-    if (state == kDigits) {
-        if (j == 0) sample_by_digits<TYPE>(A, m, s_key, s_part, s_pick);
-        return;
-    }
     const RowState st = *R.row;
     const double c = 1.4426950408889634074 / (double)T;
     const char* row = static_cast<const char*>(A.logits) + (long long)m * A.stride * (TYPE == EVOSPEC_FP32 ? 4 : 2);
@@ -811,7 +851,6 @@ __global__ __launch_bounds__(kThreads) void sample_pick_kernel(SampleArgs A, cha
     const SliceState mine = R.slice[j];
     const double ref = mine.ref;
     const int shift = (int)fmin(st.ref - ref, 64.0) * kBins;
-    fill_table(s_table);
     if (tid == 0) s_n = 0;
     __syncthreads();
     if (mine.top != 0 && regular(T, key_value(mine.top)) && st.ref - ref < kRange) {    // (uniform)
@@ -836,33 +875,50 @@ __global__ __launch_bounds__(kThreads) void sample_pick_kernel(SampleArgs A, cha
                 if (on) {
                     const uint32_t at = atomicAdd(&s_n, 1u);
                     const int i = S.at(g, e);
-                    if (at < kList) s_key[at] = make_key(z[g][e], A.ids ? A.ids[i] : i);
+                    const u64 key = make_key(z[g][e], A.ids ? A.ids[i] : i);
+                    if (at < kStage) {
+                        s_key[at] = key;
+                    } else {                                     // (rare: places of the row's list one by one)
+                        const uint32_t far = atomicAdd(R.ticket, 1u);
+                        if (far < kList) R.list[far] = key;
+                    }
                 }
             }
         __syncthreads();
-        // (a list that is too long for one workgroup is too long for the row)
-        if (tid == 0) s_at = __hip_atomic_fetch_add(&R.ticket[0], s_n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const uint32_t n = min(s_n, (uint32_t)kStage);
+        if (tid == 0) s_at = atomicAdd(R.ticket, n);
         __syncthreads();
-        const uint32_t at = s_at;
-        for (int i = tid; i < (int)min(s_n, (uint32_t)kList); i += kThreads)
-            if (at + i < kList) __hip_atomic_store(&R.list[at + i], s_key[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        for (uint32_t i = tid; i < n; i += kThreads)
+            if (s_at + i < kList) R.list[s_at + i] = s_key[i];
     }
-    // The list is written and read past the caches that are not shared (agent scope), and every store has arrived before the
-    // workgroup's ticket is taken: a fence instead would write back all of an L2 for each workgroup (960 rows: 5.5 ms).
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (tid == 0) s_last = __hip_atomic_fetch_add(&R.ticket[1], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)slices - 1;
-    __syncthreads();
-    if (!s_last) return;
-    const int n = (int)__hip_atomic_load(&R.ticket[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// What the bins leave open, a workgroup for each row.
+template <int TYPE>
+__global__ __launch_bounds__(kThreads) void sample_finish_kernel(SampleArgs A, char* ws, int slices) {
+    __shared__ u64 s_key[kList], s_sum[kList], s_before[kAll + 1];
+    __shared__ double s_table[kSteps];
+    __shared__ u64 s_part[kThreads / 64], s_pick[2];
+    const int m = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+    const RowSpace R = row_space(ws, m, slices);
+    const RowState st = *R.row;
+    if (st.state == kDone) return;
+    const float T = A.temperature ? A.temperature[m] : 1.f;
+    const double c = 1.4426950408889634074 / (double)T;
+    const int n = (int)*R.ticket;
+    fill_table(s_table);
+    if (st.state == kDigits) {
+        sample_by_digits<TYPE>(A, m, s_key, s_part, s_pick);
+        return;
+    }
     if (n > kList) {
-        __syncthreads();
         sample_by_digits<TYPE>(A, m, s_key, s_part, s_pick);
         return;
     }
     for (int b = tid; b <= kAll; b += kThreads) s_before[b] = R.before[b];
-    for (int i = tid; i < n; i += kThreads) s_key[i] = __hip_atomic_load(&R.list[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    sort_keys<kThreads, kList / kThreads>(s_key, n);
+    for (int i = tid; i < n; i += kThreads) s_key[i] = R.list[i];
+    __syncthreads();
+    sort_keys<kThreads>(s_key, n);
     sum_weights<kThreads, kList / kThreads>(s_key, s_sum, n, c, st.ref, s_table, s_part);
     if (tid >= 64) return;
     // One wavefront goes through the filters.  Every place is an index into the sorted list.
@@ -932,6 +988,7 @@ static hipError_t sample_as(const SampleArgs& a, char* ws, hipStream_t stream) {
     sample_bins_kernel<TYPE><<<dim3((unsigned)(a.M * slices)), kThreads, 0, stream>>>(a, ws, slices);
     sample_row_kernel<<<dim3((unsigned)a.M), kRowThreads, 0, stream>>>(a, ws, slices);
     sample_pick_kernel<TYPE><<<dim3((unsigned)(a.M * slices)), kThreads, 0, stream>>>(a, ws, slices);
+    sample_finish_kernel<TYPE><<<dim3((unsigned)a.M), kThreads, 0, stream>>>(a, ws, slices);
     return hipGetLastError();
 }
 
