@@ -65,20 +65,6 @@ __device__ __forceinline__ u32x4 widen(uint32_t lo, uint32_t hi) {
     }
     return out;
 }
-// The same with the NaN code's values: NaN for int8 (e4m3 has it already).
-template <int KIND, bool HALF>
-__device__ __forceinline__ u32x4 widen_nan(uint32_t lo, uint32_t hi) {
-    u32x4 out = widen<KIND, HALF>(lo, hi);
-    if constexpr (KIND == EVOSPEC_KV_INT8) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t code = ((i < 4 ? lo : hi) >> (8 * (i & 3))) & 255u;
-            if (code == 0x80u) out[i >> 1] |= 0x7fffu << (16 * (i & 1));       // NaN in both types
-        }
-    }
-    return out;
-}
-
 template <bool HALF>
 __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
     if constexpr (HALF)
@@ -103,7 +89,7 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t x) {
 
 // NQ: dim / 32.  RT: tiles of 32 rows of a wavefront.  WR x WT wavefronts over rows and tokens.
 template <int NQ, int KIND, bool HALF, int RT, int WR, int WT>
-__global__ __launch_bounds__(64 * WR * WT) void kv_attention_kernel(AttnArgs A) {
+__global__ __launch_bounds__(64 * WR * WT, NQ >= 6 ? 1 : 2) void kv_attention_kernel(AttnArgs A) {
     constexpr int kDim = 32 * NQ, kRows = 32 * RT * WR, kWaves = WR * WT;
     constexpr int kPad = 36;                                     // floats of a row of 32 in LDS
     __shared__ __align__(16) float s_o[2][kWaves][32 * kPad];
@@ -112,11 +98,13 @@ __global__ __launch_bounds__(64 * WR * WT) void kv_attention_kernel(AttnArgs A) 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
     const int wr = wave / WT, wt = wave % WT;
-    int id = blockIdx.x;
-    const int split = id % A.splits;
-    id /= A.splits;
+    // workgroups go round the 8 dies in turn: each die gets neighbours, which read the same tokens, for its cache
+    const int die = blockIdx.x & 7, most = gridDim.x >> 3, rest = gridDim.x & 7;
+    int id = die * most + min(die, rest) + (blockIdx.x >> 3);
     const int tile = id % A.tiles;
     id /= A.tiles;
+    const int split = id % A.splits;
+    id /= A.splits;
     const int head = id % A.c.heads, s = id / A.c.heads;
     const Rows& R = A.r;
     const int n0 = min(max(R.row_off[s], 0), R.T), n1 = min(max(R.row_off[s + 1], n0), R.T);
@@ -163,23 +151,52 @@ __global__ __launch_bounds__(64 * WR * WT) void kv_attention_kernel(AttnArgs A) 
             for (int e = 0; e < 16; ++e) o[rt][k][e] = 0.f;
     }
 
+    // Tokens come in blocks.  K of the next block is asked for when this one's scores are there, and V when it has been added, so that
+    // both are under way during half of a block's work; the page table runs a block further ahead.
     const int mask = (1 << A.c.shift) - 1;
-    for (int b = b_lo + wt; b < b_hi; b += WT) {
-        const int page = __builtin_amdgcn_readfirstlane(R.table[(long long)s * R.width + (b >> A.c.shift)]);
-        if ((unsigned)page >= (unsigned)A.c.pages) continue;     // (uniform)
-        const long long at = (((long long)page * A.c.heads + head) << A.c.shift) + (b & mask);
+    const int32_t* table = R.table + (long long)s * R.width;
+    auto page_of = [&](int b) { return __builtin_amdgcn_readfirstlane(table[min(b, b_hi - 1) >> A.c.shift]); };
+    // Blocks without a page are read from page 0, and no row sees them.
+    auto is_page = [&](int page) { return (unsigned)page < (unsigned)A.c.pages; };
+    auto place = [&](int b, int page) { return (((long long)(is_page(page) ? page : 0) * A.c.heads + head) << A.c.shift) + (b & mask); };
+    u32x4 kr[NQ], vr[NQ];
+    float2 sc = make_float2(1.f, 1.f);
+    auto load_k = [&](long long at) {
         const uint8_t* data = A.c.data + at * (2 * kBlock * kDim) + lane * 16;
-        const float2 sc = *reinterpret_cast<const float2*>(A.c.scales + at * 2);
-        u32x4 kr[NQ], vr[NQ];
+        sc = *reinterpret_cast<const float2*>(A.c.scales + at * 2);
 #pragma unroll
         for (int k = 0; k < NQ; ++k) kr[k] = *reinterpret_cast<const u32x4*>(data + k * 1024);
+    };
+    auto load_v = [&](long long at) {
+        const uint8_t* data = A.c.data + at * (2 * kBlock * kDim) + kBlock * kDim + lane * 16;
 #pragma unroll
-        for (int k = 0; k < NQ; ++k) vr[k] = *reinterpret_cast<const u32x4*>(data + kBlock * kDim + k * 1024);
-
+        for (int k = 0; k < NQ; ++k) vr[k] = *reinterpret_cast<const u32x4*>(data + k * 1024);
+    };
+    int b = b_lo + wt, page = 0, page_next = 0;
+    if (b < b_hi) {
+        page = page_of(b);
+        page_next = page_of(b + WT);
+        load_k(place(b, page));
+        load_v(place(b, page));
+    }
+    for (; b < b_hi; b += WT) {
+        // (the last block's next is a block that is there, read for nothing)
+        const long long at_next = place(b + WT, page_next);
+        const bool there = is_page(page);
+        page = page_next;
+        page_next = page_of(b + 2 * WT);
         const bool has_nan = (__float_as_uint(sc.x) | __float_as_uint(sc.y)) >> 31;   // (uniform)
         const float ck = fmaxf(fabsf(sc.x) * (A.scale * kLog2e), 0x1p-126f);       // (not zero: -inf stays what it is)
         const float sv = fabsf(sc.y), lv = __log2f(sv), iv = 1.f / sv;
 
+        uint32_t nan_tokens = 0;                                 // of K (e4m3's NaN code is one for the matrix cores)
+        if (KIND == EVOSPEC_KV_INT8 && has_nan) {
+            uint32_t any = 0;
+#pragma unroll
+            for (int k = 0; k < NQ; ++k) any |= nan_bytes<KIND>(kr[k][0]) | nan_bytes<KIND>(kr[k][1]) | nan_bytes<KIND>(kr[k][2]) | nan_bytes<KIND>(kr[k][3]);
+            const u64 who = __ballot(any != 0);
+            nan_tokens = (uint32_t)who | (uint32_t)(who >> 32);
+        }
         f32x16 x[RT];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
@@ -189,14 +206,25 @@ __global__ __launch_bounds__(64 * WR * WT) void kv_attention_kernel(AttnArgs A) 
         for (int k = 0; k < NQ; ++k)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const u32x4 a = has_nan ? widen_nan<KIND, HALF>(kr[k][2 * j], kr[k][2 * j + 1]) : widen<KIND, HALF>(kr[k][2 * j], kr[k][2 * j + 1]);
+                const u32x4 a = widen<KIND, HALF>(kr[k][2 * j], kr[k][2 * j + 1]);
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) x[rt] = mfma<HALF>(a, qf[rt][k][j], x[rt]);
             }
 
+        if (KIND == EVOSPEC_KV_INT8 && nan_tokens) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if ((nan_tokens >> (8 * (e / 4) + 4 * half + e % 4)) & 1) x[rt][e] = __uint_as_float(0x7fc00000u);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        load_k(at_next);
+        __builtin_amdgcn_sched_barrier(0);
+
         const int t0 = b * kBlock;
         uint32_t seen[RT];                                       // bit e: the lane's row sees token 8 (e / 4) + 4 half + e % 4
-        const bool whole = t0 + kBlock <= full;                  // (uniform)
+        const bool whole = there && t0 + kBlock <= full;         // (uniform)
         if (!whole) {
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
@@ -212,6 +240,7 @@ __global__ __launch_bounds__(64 * WR * WT) void kv_attention_kernel(AttnArgs A) 
                     } else {
                         ok = t <= last_seen[rt];
                     }
+                    ok = ok && there;
                     seen[rt] |= (uint32_t)ok << e;
                     x[rt][e] = ok ? x[rt][e] : -__builtin_inff();
                 }
@@ -248,6 +277,7 @@ __global__ __launch_bounds__(64 * WR * WT) void kv_attention_kernel(AttnArgs A) 
             pf[rt][0] = __builtin_bit_cast(u32x4, p[0]);
             pf[rt][1] = __builtin_bit_cast(u32x4, p[1]);
         }
+        __builtin_amdgcn_sched_barrier(0);
         if (t0 + kBlock > len) {                                 // bytes behind the last token may be anything
 #pragma unroll
             for (int k = 0; k < NQ; ++k)
@@ -262,6 +292,7 @@ __global__ __launch_bounds__(64 * WR * WT) void kv_attention_kernel(AttnArgs A) 
             // tokens by dims that are NaN (0 or 1); what is not zero in that product becomes NaN.
 #pragma unroll
             for (int k = 0; k < NQ; ++k) {
+                __builtin_amdgcn_sched_barrier(0);               // (one after the other: fewer registers)
                 u32x4 nb;
 #pragma unroll
                 for (int a = 0; a < 4; ++a) {
@@ -276,16 +307,18 @@ __global__ __launch_bounds__(64 * WR * WT) void kv_attention_kernel(AttnArgs A) 
                     for (int e = 0; e < 16; ++e) hit[e] = 0.f;
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
-                        f16x8 is, sees;
+                        u32x4 is, sees;                          // fp16 1 or 0
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            is[e] = (nb[2 * y + (e >> 2)] >> (8 * (e & 3))) & 1 ? (_Float16)1.f : (_Float16)0.f;
-                            sees[e] = whole || ((seen[rt] >> (8 * y + e)) & 1) ? (_Float16)1.f : (_Float16)0.f;
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t pair = (nb[2 * y + (e >> 1)] >> (16 * (e & 1))) & 0x0101u, bits2 = (seen[rt] >> (8 * y + 2 * e)) & 3u;
+                            is[e] = ((pair & 1u) | (pair & 0x100u) << 8) * 0x3c00u;
+                            sees[e] = whole ? 0x3c003c00u : ((bits2 & 1u) | (bits2 & 2u) << 15) * 0x3c00u;
                         }
-                        hit = mfma<true>(__builtin_bit_cast(u32x4, is), __builtin_bit_cast(u32x4, sees), hit);
+                        hit = mfma<true>(is, sees, hit);
                     }
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) o[rt][k][e] = hit[e] > 0.f ? __uint_as_float(0x7fc00000u) : o[rt][k][e];
+                    for (int e = 0; e < 16; ++e)
+                        if (hit[e] > 0.f) o[rt][k][e] = __uint_as_float(0x7fc00000u);
                 }
             }
         }
@@ -297,6 +330,8 @@ __global__ __launch_bounds__(64 * WR * WT) void kv_attention_kernel(AttnArgs A) 
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) o[rt][k] = mfma<true>(a, pf[rt][y], o[rt][k]);
             }
+        __builtin_amdgcn_sched_barrier(0);
+        load_v(at_next);
     }
 
     // the wavefronts that share rows: one reference, and their shares of it
