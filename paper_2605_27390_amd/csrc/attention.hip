@@ -31,6 +31,8 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kNone = -3.0e38f;                 // the reference of a row that has seen nothing
+constexpr int kMostSplits = 128;
+constexpr int kWaves = 4;                         // of a workgroup
 constexpr float kSlack = 6.f;                     // a row's reference moves when a score passes it by more than that
 
 // 8 codes of two dwords as an operand of fp16 or bf16 elements
@@ -75,6 +77,15 @@ __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
 
 __device__ __forceinline__ float other_half(float x, int lane) { return __uint_as_float(xor_lane<32>(__float_as_uint(x), lane)); }
 
+template <bool ONCE>
+__device__ __forceinline__ u32x4 load_piece(const uint8_t* p) {
+    if constexpr (ONCE) return load_once((gvec_ptr)(uintptr_t)p);
+    else return *reinterpret_cast<const u32x4*>(p);
+}
+
+// the first n bits of 32
+__device__ __forceinline__ uint32_t first_bits(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1; }
+
 // 0xff in every byte of x that is a NaN code
 template <int KIND>
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t x) {
@@ -87,17 +98,17 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t x) {
     return m;
 }
 
-// NQ: dim / 32.  RT: tiles of 32 rows of a wavefront.  WR x WT wavefronts over rows and tokens.
-template <int NQ, int KIND, bool HALF, int RT, int WR, int WT>
-__global__ __launch_bounds__(64 * WR * WT, NQ >= 6 ? 1 : 2) void kv_attention_kernel(AttnArgs A) {
-    constexpr int kDim = 32 * NQ, kRows = 32 * RT * WR, kWaves = WR * WT;
+// NQ: dim / 32.  RT: tiles of 32 rows; the kWaves wavefronts of a workgroup have all of them, and every kWaves-th block of tokens.
+// ONCE: K and V are loaded past the caches.
+template <int NQ, int KIND, bool HALF, int RT, bool ONCE>
+__global__ __launch_bounds__(64 * kWaves, NQ >= 6 ? 1 : 2) void kv_attention_kernel(AttnArgs A) {
+    constexpr int kDim = 32 * NQ, kRows = 32 * RT;
     constexpr int kPad = 36;                                     // floats of a row of 32 in LDS
     __shared__ __align__(16) float s_o[2][kWaves][32 * kPad];
     __shared__ float2 s_ml[kWaves][RT * 32];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
-    const int wr = wave / WT, wt = wave % WT;
     // workgroups go round the 8 dies in turn: each die gets neighbours, which read the same tokens, for its cache
     const int die = blockIdx.x & 7, most = gridDim.x >> 3, rest = gridDim.x & 7;
     int id = die * most + min(die, rest) + (blockIdx.x >> 3);
@@ -121,22 +132,31 @@ __global__ __launch_bounds__(64 * WR * WT, NQ >= 6 ? 1 : 2) void kv_attention_ke
     const int b_lo = (int)((long long)blocks * split / A.splits), b_hi = (int)((long long)blocks * (split + 1) / A.splits);
 
     // the rows' queries, as second operands
-    u32x4 qf[RT][NQ][2];
-    int last_seen[RT];                                           // causal: the row's own position
+    constexpr bool kShared = RT > 1;                             // from LDS, where the registers hold more tiles
+    __shared__ __align__(16) u32x4 s_q[kShared ? RT * NQ * 2 * 64 : 1];
+    u32x4 qf[kShared ? 1 : RT][NQ][2];
+    int last_seen[RT];                                           // the last token the row can see: its own, or the last of the tree
     uint64_t bits[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        const int r = r0 + (wr * RT + rt) * 32 + col;
+        const int r = r0 + rt * 32 + col;
         const bool ok = r < rows;
         const int i = ok ? r / A.group : 0, a = ok ? r % A.group : 0;
-        last_seen[rt] = ok ? base + i : -1;
+        last_seen[rt] = !ok ? -1 : A.tree ? len - 1 : base + i;
         bits[rt] = ok && A.tree ? A.tree[n0 + i] : 0;
         const uint16_t* q = static_cast<const uint16_t*>(A.q) + (long long)(n0 + i) * A.q_stride + (long long)(head * A.group + a) * kDim + 16 * half;
 #pragma unroll
         for (int k = 0; k < NQ; ++k)
 #pragma unroll
             for (int j = 0; j < 2; ++j)
-                qf[rt][k][j] = ok ? *reinterpret_cast<const u32x4*>(q + 32 * k + 8 * j) : u32x4{0, 0, 0, 0};
+            {
+                if constexpr (kShared) {
+                    if ((rt * NQ * 2 + 2 * k + j) % kWaves != wave) continue;
+                    s_q[(rt * NQ * 2 + 2 * k + j) * 64 + lane] = ok ? *reinterpret_cast<const u32x4*>(q + 32 * k + 8 * j) : u32x4{0, 0, 0, 0};
+                } else {
+                    qf[rt][k][j] = ok ? *reinterpret_cast<const u32x4*>(q + 32 * k + 8 * j) : u32x4{0, 0, 0, 0};
+                }
+            }
     }
 
     f32x16 o[RT][NQ];
@@ -153,6 +173,15 @@ __global__ __launch_bounds__(64 * WR * WT, NQ >= 6 ? 1 : 2) void kv_attention_ke
 
     // Tokens come in blocks.  K of the next block is asked for when this one's scores are there, and V when it has been added, so that
     // both are under way during half of a block's work; the page table runs a block further ahead.
+    // bit 8 a + i: the lane's row sees token 8 a + 4 half + i of the block at t0
+    auto sees = [&](int rt, int t0, bool there) {
+        uint32_t w = there ? first_bits(min(len, last_seen[rt] + 1) - t0) : 0;
+        if (A.tree) {                                            // its own bits behind the context
+            const int j = t0 - base;
+            w &= j >= 64 ? 0u : j >= 0 ? (uint32_t)(bits[rt] >> j) : j > -kBlock ? (uint32_t)(bits[rt] << -j) | first_bits(-j) : ~0u;
+        }
+        return w >> (4 * half);
+    };
     const int mask = (1 << A.c.shift) - 1;
     const int32_t* table = R.table + (long long)s * R.width;
     auto page_of = [&](int b) { return __builtin_amdgcn_readfirstlane(table[min(b, b_hi - 1) >> A.c.shift]); };
@@ -165,32 +194,42 @@ __global__ __launch_bounds__(64 * WR * WT, NQ >= 6 ? 1 : 2) void kv_attention_ke
         const uint8_t* data = A.c.data + at * (2 * kBlock * kDim) + lane * 16;
         sc = *reinterpret_cast<const float2*>(A.c.scales + at * 2);
 #pragma unroll
-        for (int k = 0; k < NQ; ++k) kr[k] = *reinterpret_cast<const u32x4*>(data + k * 1024);
+        for (int k = 0; k < NQ; ++k) kr[k] = load_piece<ONCE>(data + k * 1024);
     };
     auto load_v = [&](long long at) {
         const uint8_t* data = A.c.data + at * (2 * kBlock * kDim) + kBlock * kDim + lane * 16;
 #pragma unroll
-        for (int k = 0; k < NQ; ++k) vr[k] = *reinterpret_cast<const u32x4*>(data + k * 1024);
+        for (int k = 0; k < NQ; ++k) vr[k] = load_piece<ONCE>(data + k * 1024);
     };
-    int b = b_lo + wt, page = 0, page_next = 0;
+    bool nan_blocks = false;
+    int b = b_lo + wave, page = 0, page_next = 0;
     if (b < b_hi) {
         page = page_of(b);
-        page_next = page_of(b + WT);
+        page_next = page_of(b + kWaves);
         load_k(place(b, page));
         load_v(place(b, page));
     }
-    for (; b < b_hi; b += WT) {
+    // The queries are waited for here: a wait in the loop would be one for everything that is under way.
+    if constexpr (kShared) {
+        __syncthreads();
+    } else {
+#pragma unroll
+        for (int k = 0; k < NQ; ++k)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) asm("" : "+v"(qf[0][k][j]));
+    }
+    for (; b < b_hi; b += kWaves) {
         // (the last block's next is a block that is there, read for nothing)
-        const long long at_next = place(b + WT, page_next);
+        const long long at_next = place(b + kWaves, page_next);
         const bool there = is_page(page);
         page = page_next;
-        page_next = page_of(b + 2 * WT);
-        const bool has_nan = (__float_as_uint(sc.x) | __float_as_uint(sc.y)) >> 31;   // (uniform)
+        page_next = page_of(b + 2 * kWaves);
+        const float sc_y = sc.y;
         const float ck = fmaxf(fabsf(sc.x) * (A.scale * kLog2e), 0x1p-126f);       // (not zero: -inf stays what it is)
-        const float sv = fabsf(sc.y), lv = __log2f(sv), iv = 1.f / sv;
+        const float sv = fabsf(sc.y), lv = __log2f(sv), iv = __builtin_amdgcn_rcpf(sv);
 
         uint32_t nan_tokens = 0;                                 // of K (e4m3's NaN code is one for the matrix cores)
-        if (KIND == EVOSPEC_KV_INT8 && has_nan) {
+        if (KIND == EVOSPEC_KV_INT8 && __float_as_uint(sc.x) >> 31) {
             uint32_t any = 0;
 #pragma unroll
             for (int k = 0; k < NQ; ++k) any |= nan_bytes<KIND>(kr[k][0]) | nan_bytes<KIND>(kr[k][1]) | nan_bytes<KIND>(kr[k][2]) | nan_bytes<KIND>(kr[k][3]);
@@ -208,7 +247,7 @@ __global__ __launch_bounds__(64 * WR * WT, NQ >= 6 ? 1 : 2) void kv_attention_ke
             for (int j = 0; j < 2; ++j) {
                 const u32x4 a = widen<KIND, HALF>(kr[k][2 * j], kr[k][2 * j + 1]);
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) x[rt] = mfma<HALF>(a, qf[rt][k][j], x[rt]);
+                for (int rt = 0; rt < RT; ++rt) x[rt] = mfma<HALF>(a, kShared ? s_q[(rt * NQ * 2 + 2 * k + j) * 64 + lane] : qf[kShared ? 0 : rt][k][j], x[rt]);
             }
 
         if (KIND == EVOSPEC_KV_INT8 && nan_tokens) {
@@ -223,32 +262,18 @@ __global__ __launch_bounds__(64 * WR * WT, NQ >= 6 ? 1 : 2) void kv_attention_ke
         __builtin_amdgcn_sched_barrier(0);
 
         const int t0 = b * kBlock;
-        uint32_t seen[RT];                                       // bit e: the lane's row sees token 8 (e / 4) + 4 half + e % 4
-        const bool whole = there && t0 + kBlock <= full;         // (uniform)
-        if (!whole) {
+        if (!(there && t0 + kBlock <= full)) {                   // (uniform)
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
-                seen[rt] = 0;
+                const uint32_t seen = sees(rt, t0, there);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int t = t0 + 8 * (e / 4) + 4 * half + e % 4;
-                    bool ok;
-                    if (A.tree) {
-                        const int j = t - base;
-                        ok = t < len && (j < 0 || (j < 64 && ((bits[rt] >> j) & 1)));
-                        ok = ok && last_seen[rt] >= base && j < n_all;
-                    } else {
-                        ok = t <= last_seen[rt];
-                    }
-                    ok = ok && there;
-                    seen[rt] |= (uint32_t)ok << e;
-                    x[rt][e] = ok ? x[rt][e] : -__builtin_inff();
-                }
+                for (int e = 0; e < 16; ++e) x[rt][e] = (seen >> (8 * (e / 4) + e % 4)) & 1 ? x[rt][e] : -__builtin_inff();
             }
         }
         u32x4 pf[RT][2];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
+            if (RT > 1) __builtin_amdgcn_sched_barrier(0);       // (one tile after the other: fewer registers)
             float top = x[rt][0];
 #pragma unroll
             for (int e = 1; e < 16; ++e) top = fmaxf(top, x[rt][e]);
@@ -287,40 +312,12 @@ __global__ __launch_bounds__(64 * WR * WT, NQ >= 6 ? 1 : 2) void kv_attention_ke
                     vr[k][a] &= left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
                 }
         }
-        if (has_nan) {
-            // A NaN reaches the rows that see its token, and no others: rows by tokens that are seen (0 or 1) against
-            // tokens by dims that are NaN (0 or 1); what is not zero in that product becomes NaN.
+        if (__float_as_uint(sc_y) >> 31) {                       // (uniform) NaN is left out, and looked at behind the loop
+            nan_blocks = true;
 #pragma unroll
-            for (int k = 0; k < NQ; ++k) {
-                __builtin_amdgcn_sched_barrier(0);               // (one after the other: fewer registers)
-                u32x4 nb;
+            for (int k = 0; k < NQ; ++k)
 #pragma unroll
-                for (int a = 0; a < 4; ++a) {
-                    nb[a] = nan_bytes<KIND>(vr[k][a]);
-                    vr[k][a] &= ~nb[a];
-                }
-                if (!__ballot((nb[0] | nb[1] | nb[2] | nb[3]) != 0)) continue;
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    f32x16 hit;
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) hit[e] = 0.f;
-#pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        u32x4 is, sees;                          // fp16 1 or 0
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const uint32_t pair = (nb[2 * y + (e >> 1)] >> (16 * (e & 1))) & 0x0101u, bits2 = (seen[rt] >> (8 * y + 2 * e)) & 3u;
-                            is[e] = ((pair & 1u) | (pair & 0x100u) << 8) * 0x3c00u;
-                            sees[e] = whole ? 0x3c003c00u : ((bits2 & 1u) | (bits2 & 2u) << 15) * 0x3c00u;
-                        }
-                        hit = mfma<true>(is, sees, hit);
-                    }
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (hit[e] > 0.f) o[rt][k][e] = __uint_as_float(0x7fc00000u);
-                }
-            }
+                for (int a = 0; a < 4; ++a) vr[k][a] &= ~nan_bytes<KIND>(vr[k][a]);
         }
 #pragma unroll
         for (int k = 0; k < NQ; ++k)
@@ -332,6 +329,40 @@ __global__ __launch_bounds__(64 * WR * WT, NQ >= 6 ? 1 : 2) void kv_attention_ke
             }
         __builtin_amdgcn_sched_barrier(0);
         load_v(at_next);
+    }
+    if (nan_blocks) {
+        // A NaN in V reaches the rows that see its token, and no others: tokens that are seen (0 or 1) against dims that are NaN (0
+        // or 1); what is not zero in that product becomes NaN.
+        for (b = b_lo + wave; b < b_hi; b += kWaves) {
+            const int page = page_of(b);
+            const long long at = place(b, page);
+            if (!is_page(page) || !(__float_as_uint(A.c.scales[at * 2 + 1]) >> 31)) continue;
+            load_v(at);
+#pragma unroll
+            for (int k = 0; k < NQ; ++k)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    const uint32_t seen = sees(rt, b * kBlock, true);
+                    f32x16 hit;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) hit[e] = 0.f;
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        u32x4 is, see;                           // fp16 1 or 0
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t nb = nan_bytes<KIND>(vr[k][2 * y + (e >> 1)]);
+                            const uint32_t pair = (nb >> (16 * (e & 1))) & 0x0101u, two = (seen >> (16 * y + 8 * (e >> 1) + 2 * (e & 1))) & 3u;
+                            is[e] = ((pair & 1u) | (pair & 0x100u) << 8) * 0x3c00u;
+                            see[e] = ((two & 1u) | (two & 2u) << 15) * 0x3c00u;
+                        }
+                        hit = mfma<true>(is, see, hit);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (hit[e] > 0.f) o[rt][k][e] = __uint_as_float(0x7fc00000u);
+                }
+        }
     }
 
     // the wavefronts that share rows: one reference, and their shares of it
@@ -346,18 +377,18 @@ __global__ __launch_bounds__(64 * WR * WT, NQ >= 6 ? 1 : 2) void kv_attention_ke
     for (int rt = 0; rt < RT; ++rt) {
         mm[rt] = kNone;
 #pragma unroll
-        for (int w = 0; w < WT; ++w) mm[rt] = fmaxf(mm[rt], s_ml[wr * WT + w][rt * 32 + col].x);
+        for (int w = 0; w < kWaves; ++w) mm[rt] = fmaxf(mm[rt], s_ml[w][rt * 32 + col].x);
         ll[rt] = 0.f;
 #pragma unroll
-        for (int w = 0; w < WT; ++w) {
-            const float2 ml = s_ml[wr * WT + w][rt * 32 + col];
+        for (int w = 0; w < kWaves; ++w) {
+            const float2 ml = s_ml[w][rt * 32 + col];
             ll[rt] += ml.y * __builtin_amdgcn_exp2f(ml.x - mm[rt]);
         }
         f[rt] = __builtin_amdgcn_exp2f(m[rt] - mm[rt]);
         if (ll[rt] > 0.f) f[rt] /= ll[rt];                       // (NaN sums divide as well, below)
         else if (ll[rt] != ll[rt]) f[rt] = ll[rt];
-        const int r = r0 + (wr * RT + rt) * 32 + col;
-        if (wt == 0 && half == 0 && r < rows) {
+        const int r = r0 + rt * 32 + col;
+        if (wave == 0 && half == 0 && r < rows) {
             const long long row = (long long)(n0 + r / A.group) * (A.c.heads * A.group) + head * A.group + r % A.group;
             if (A.splits > 1) A.part_ml[(long long)split * R.T * A.c.heads * A.group + row] = make_float2(mm[rt], ll[rt]);
             else if (A.lse) A.lse[row] = ll[rt] == 0.f ? -__builtin_inff() : (mm[rt] + __log2f(ll[rt])) * kLn2;
@@ -375,14 +406,16 @@ __global__ __launch_bounds__(64 * WR * WT, NQ >= 6 ? 1 : 2) void kv_attention_ke
                 *reinterpret_cast<float4*>(mine + 8 * a) = make_float4(o[rt][k][4 * a] * f[rt], o[rt][k][4 * a + 1] * f[rt],
                                                                        o[rt][k][4 * a + 2] * f[rt], o[rt][k][4 * a + 3] * f[rt]);
             __syncthreads();
-            for (int e = tid; e < WR * 32 * 8; e += 64 * kWaves) {
-                const int g = e >> 8, c = (e >> 3) & 31, d4 = e & 7;
-                const int r = r0 + (g * RT + rt) * 32 + c;
+            {
+                static_assert(64 * kWaves == 32 * 8, "4 elements of a row a thread");
+                const int c = tid >> 3, d4 = tid & 7;
+                const int r = r0 + rt * 32 + c;
+                buf ^= 1;
                 if (r >= rows) continue;
                 float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                for (int w = 0; w < WT; ++w) {
-                    const float4 v = *reinterpret_cast<const float4*>(s_o[buf][g * WT + w] + c * kPad + 4 * d4);
+                for (int w = 0; w < kWaves; ++w) {
+                    const float4 v = *reinterpret_cast<const float4*>(s_o[buf ^ 1][w] + c * kPad + 4 * d4);
                     sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
                 }
                 const long long row = (long long)(n0 + r / A.group) * (A.c.heads * A.group) + head * A.group + r % A.group;
@@ -397,18 +430,19 @@ __global__ __launch_bounds__(64 * WR * WT, NQ >= 6 ? 1 : 2) void kv_attention_ke
                     *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(A.out) + row * kDim + d) = bf16x4{(__bf16)sum.x, (__bf16)sum.y, (__bf16)sum.z, (__bf16)sum.w};
                 }
             }
-            buf ^= 1;
         }
 }
 
-// The shares of a row's splits, each a mean over its tokens with a reference and a sum, in their order: one wavefront a row.
-template <int NQ, bool HALF>
+// The shares of a row's splits, each a mean over its tokens with a reference and a sum, in a fixed order: WAVES wavefronts a row,
+// each with every WAVES-th split; 4 / WAVES rows a workgroup.
+template <int NQ, bool HALF, int WAVES>
 __global__ __launch_bounds__(256) void kv_attention_merge_kernel(AttnArgs A) {
-    constexpr int kDim = 32 * NQ;
-    const int lane = threadIdx.x & 63;
+    constexpr int kDim = 32 * NQ, kPer = (kDim + 63) / 64;
+    __shared__ float s_o[WAVES > 1 ? WAVES : 1][kPer * 64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = wave % WAVES;
     const int heads = A.c.heads * A.group;
-    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6), all = (long long)A.r.T * heads;
-    if (row >= all) return;
+    const long long row = (long long)blockIdx.x * (4 / WAVES) + wave / WAVES, all = (long long)A.r.T * heads;
+    if (row >= all) return;                                      // (a workgroup as a whole where its wavefronts share a row)
     // a row of no sequence has no shares
     const int token = (int)(row / heads);
     bool mine = false;
@@ -417,24 +451,40 @@ __global__ __launch_bounds__(256) void kv_attention_merge_kernel(AttnArgs A) {
         mine |= token >= n0 && token < min(n1, n0 + A.r.max_rows);
     }
     if (!__ballot(mine)) return;
-    float m = kNone;
-    for (int j = lane; j < A.splits; j += 64) m = fmaxf(m, A.part_ml[j * all + row].x);
-    m = wave_max(m, lane);
-    float sum = 0.f;
-    float o[(kDim + 63) / 64];
+    static_assert(kMostSplits <= 128, "two splits a lane");
+    float2 ml[2];
 #pragma unroll
-    for (int k = 0; k < (kDim + 63) / 64; ++k) o[k] = 0.f;
-    for (int j = 0; j < A.splits; ++j) {
-        const float2 ml = A.part_ml[j * all + row];
-        const float w = ml.y * __builtin_amdgcn_exp2f(ml.x - m);
-        if (w == 0.f) continue;                                  // (uniform)
-        sum += w;
+    for (int i = 0; i < 2; ++i) ml[i] = lane + 64 * i < A.splits ? A.part_ml[(lane + 64 * i) * all + row] : make_float2(kNone, 0.f);
+    const float m = wave_max(fmaxf(ml[0].x, ml[1].x), lane);
+    float w[2];
 #pragma unroll
-        for (int k = 0; k < (kDim + 63) / 64; ++k)
-            if (kDim % 64 == 0 || 64 * k + lane < kDim) o[k] += w * A.part_o[(j * all + row) * kDim + 64 * k + lane];
+    for (int i = 0; i < 2; ++i) w[i] = ml[i].y == 0.f ? 0.f : ml[i].y * __builtin_amdgcn_exp2f(ml[i].x - m);
+    const float sum = wave_sum(w[0] + w[1], lane);
+    float o[kPer];
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) o[k] = 0.f;
+#pragma unroll 4
+    for (int j = part; j < A.splits; j += WAVES) {
+        const float wj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(j < 64 ? w[0] : w[1]), j & 63));
+        const float* from = A.part_o + (j * all + row) * kDim + lane;
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            const float v = kDim % 64 == 0 || 64 * k + lane < kDim ? from[64 * k] : 0.f;
+            o[k] += wj == 0.f ? 0.f : wj * v;                    // (a share of nothing was not written)
+        }
+    }
+    if constexpr (WAVES > 1) {
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) s_o[part][64 * k + lane] = o[k];
+        __syncthreads();
+        if (part != 0) return;
+#pragma unroll
+        for (int k = 0; k < kPer; ++k)
+#pragma unroll
+            for (int p = 1; p < WAVES; ++p) o[k] += s_o[p][64 * k + lane];
     }
 #pragma unroll
-    for (int k = 0; k < (kDim + 63) / 64; ++k) {
+    for (int k = 0; k < kPer; ++k) {
         if (kDim % 64 != 0 && 64 * k + lane >= kDim) continue;
         const float v = sum == 0.f ? 0.f : o[k] / sum;
         if constexpr (HALF) static_cast<_Float16*>(A.out)[row * kDim + 64 * k + lane] = (_Float16)v;
@@ -449,33 +499,39 @@ using Const = std::integral_constant<int, I>;
 template <int NQ, int KIND, bool HALF>
 hipError_t launch_as(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
     const dim3 grid((unsigned)(a.splits * a.tiles * a.c.heads * a.r.S));
-    if (p.row_waves == 4) kv_attention_kernel<NQ, KIND, HALF, 1, 4, 1><<<grid, 256, 0, stream>>>(a);
-    else if (p.row_waves == 2) kv_attention_kernel<NQ, KIND, HALF, 1, 2, 2><<<grid, 256, 0, stream>>>(a);
-    else kv_attention_kernel<NQ, KIND, HALF, 1, 1, 4><<<grid, 256, 0, stream>>>(a);
+    if (p.row_tiles == 2) {
+        if constexpr (NQ <= 4) kv_attention_kernel<NQ, KIND, HALF, 2, false><<<grid, 64 * kWaves, 0, stream>>>(a);
+    } else if (p.once) {
+        kv_attention_kernel<NQ, KIND, HALF, 1, true><<<grid, 64 * kWaves, 0, stream>>>(a);
+    } else {
+        kv_attention_kernel<NQ, KIND, HALF, 1, false><<<grid, 64 * kWaves, 0, stream>>>(a);
+    }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
+    // (few rows of many splits: one of 131,072 tokens and 32 heads 23 us by a wavefront a row)
     const long long rows = (long long)a.r.T * a.c.heads * a.group;
-    kv_attention_merge_kernel<NQ, HALF><<<dim3((unsigned)((rows + 3) / 4)), 256, 0, stream>>>(a);
+    if (a.splits >= 8) kv_attention_merge_kernel<NQ, HALF, 4><<<dim3((unsigned)rows), 256, 0, stream>>>(a);
+    else kv_attention_merge_kernel<NQ, HALF, 1><<<dim3((unsigned)((rows + 3) / 4)), 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 
 }  // namespace
 
+constexpr int kSlots = 512;                      // workgroups that run at the same time
+
 AttnPlan attention_plan(int dim, int heads, int group, int S, int max_rows, int max_len) {
-    (void)dim;
     AttnPlan p;
     const long long rows = (long long)max_rows * group;
-    p.row_tiles = 1;
-    p.row_waves = rows > 64 ? 4 : rows > 32 ? 2 : 1;
-    const int per = 32 * p.row_tiles * p.row_waves;
+    p.row_tiles = dim <= 128 && rows > 32 && (rows + 63) / 64 * heads * S >= kSlots ? 2 : 1;
+    const int per = 32 * p.row_tiles;
     p.tiles = (int)((rows + per - 1) / per);
-    const long long units = (long long)p.tiles * heads * S;
+    const long long groups = (long long)p.tiles * heads * S;
     const long long blocks = ((long long)max_len + kBlock - 1) / kBlock;
-    const int token_waves = 4 / p.row_waves;
-    long long splits = (2 * 256 + units - 1) / units;
-    const long long most = (blocks + 2 * token_waves - 1) / (2 * token_waves);      // two blocks for every wavefront
+    long long splits = (kSlots + groups - 1) / groups;
+    const long long most = (blocks + 8 * kWaves - 1) / (8 * kWaves);      // eight blocks for every wavefront
     splits = splits > most ? most : splits;
-    p.splits = (int)(splits < 1 ? 1 : splits > 128 ? 128 : splits);
+    p.once = p.tiles == 1;
+    p.splits = (int)(splits < 1 ? 1 : splits > kMostSplits ? kMostSplits : splits);
     return p;
 }
 

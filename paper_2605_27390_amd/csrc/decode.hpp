@@ -33,12 +33,12 @@ hipError_t launch_kv_write(const Cache& c, int dim, int kind, const void* k, lon
                            int type, const Rows& r, hipStream_t stream);
 hipError_t launch_kv_read(const Cache& c, int dim, int kind, const Rows& r, int type, void* out_k, void* out_v, hipStream_t stream);
 
-// How an attention call is laid out: wavefronts of a workgroup over rows and tokens, workgroups over the tokens.
+// How an attention call is laid out.
 struct AttnPlan {
-    int row_waves;                            // wavefronts side by side over rows (each `row_tiles` tiles of 32)
-    int row_tiles;
+    int row_tiles;                            // tiles of 32 rows of a workgroup
     int tiles;                                // workgroups over the rows of a sequence and head
     int splits;                               // workgroups over its tokens
+    bool once;                                // K and V past the caches
 };
 AttnPlan attention_plan(int dim, int heads, int group, int S, int max_rows, int max_len);
 size_t attention_workspace(const AttnPlan& p, int dim, int heads, int group, int T);

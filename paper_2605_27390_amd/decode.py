@@ -3,13 +3,15 @@ Argument marshalling only; tensors are torch tensors on the GPU, work goes to to
 from __future__ import annotations
 
 import ctypes
+import functools
 
 import torch
 
-from .binding import _check, _expect, _ptr, _stream, lib
+from .binding import _check, _expect, _get_device, _ptr, _raw_stream, lib
 
 _TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 _KINDS = {"e4m3": 0, "int8": 1}
+_i32, _f32 = torch.int32, torch.float32
 
 
 class _Cache(ctypes.Structure):
@@ -33,6 +35,30 @@ for _name, _args in {
     getattr(lib, _name).argtypes = _args
 
 
+# The sizes that the library reports depend on few numbers, which are the same from call to call.
+@functools.lru_cache(maxsize=256)
+def _cache_bytes(pages, page, heads, dim, kind):
+    nd, ns = _sz(0), _sz(0)
+    _check(lib.evospec_kv_cache_bytes(ctypes.byref(_Cache(None, None, pages, page, heads, dim, kind)), ctypes.byref(nd),
+                                      ctypes.byref(ns)), "evospec_kv_cache_bytes")
+    return nd.value, ns.value
+
+
+@functools.lru_cache(maxsize=256)
+def _attention_bytes(pages, page, heads, dim, kind, group, S, T, max_rows, max_len):
+    out = _sz(0)
+    _check(lib.evospec_kv_attention_workspace_bytes(ctypes.byref(_Cache(None, None, pages, page, heads, dim, kind)), group, S, T,
+                                                    max_rows, max_len, ctypes.byref(out)), "evospec_kv_attention_workspace_bytes")
+    return out.value
+
+
+@functools.lru_cache(maxsize=256)
+def _sample_bytes(M, V):
+    out = _sz(0)
+    _check(lib.evospec_sample_workspace_bytes(M, V, ctypes.byref(out)), "evospec_sample_workspace_bytes")
+    return out.value
+
+
 class KVCache:
     """A paged key/value cache of one layer in 8 bits: `pages` pages of `page` tokens (32, 64, 128, 256) for `heads` heads
     of `dim` elements (64, 96, 128, 192, 256), `kind` "e4m3" or "int8".  32 tokens of a head are a block; K and V of a block
@@ -48,15 +74,14 @@ class KVCache:
         self.pages, self.page, self.heads, self.dim, self.kind = int(pages), int(page), int(heads), int(dim), kind
         self._c = _Cache(None, None, self.pages, self.page, self.heads, self.dim, _KINDS[kind])
         self._ref = ctypes.byref(self._c)
-        nd, ns = _sz(0), _sz(0)
-        _check(lib.evospec_kv_cache_bytes(self._ref, ctypes.byref(nd), ctypes.byref(ns)), "evospec_kv_cache_bytes")
+        n_data, n_scales = _cache_bytes(self.pages, self.page, self.heads, self.dim, self._c.kind)
         if data is None:
-            data = torch.empty(nd.value, dtype=torch.uint8, device=device)
+            data = torch.empty(n_data, dtype=torch.uint8, device=device)
         if scales is None:
-            scales = torch.empty(ns.value // 4, dtype=torch.float32, device=device)
+            scales = torch.empty(n_scales // 4, dtype=torch.float32, device=device)
         _expect(data, torch.uint8, "data")
         _expect(scales, torch.float32, "scales")
-        if data.numel() < nd.value or scales.numel() * 4 < ns.value:
+        if data.numel() < n_data or scales.numel() * 4 < n_scales:
             raise ValueError("data or scales is smaller than evospec_kv_cache_bytes reports")
         self.data, self.scales = data, scales
         self._c.data, self._c.scales = data.data_ptr(), scales.data_ptr()
@@ -64,38 +89,40 @@ class KVCache:
 
 def _rows(page_table, at, name, row_off):
     """(width, S) of the index tensors of a call."""
-    _expect(page_table, torch.int32, "page_table", 2)
-    _expect(at, torch.int32, name, 1)
-    _expect(row_off, torch.int32, "row_off", 1)
+    for x, what, ndim in ((page_table, "page_table", 2), (at, name, 1), (row_off, "row_off", 1)):
+        if not (isinstance(x, torch.Tensor) and x.dtype is _i32 and x.is_cuda and x.dim() == ndim and x.is_contiguous()):
+            _expect(x, _i32, what, ndim)
     S, width = page_table.shape
-    if at.shape[0] != S or row_off.shape[0] != S + 1:
+    if at.numel() != S or row_off.numel() != S + 1:
         raise ValueError(f"page_table, {name} and row_off disagree about the number of sequences")
     return width, S
 
 
-def _strided(x, shape, name):
+def _strided(x, heads, dim, name):
     """Row stride in elements of a GPU tensor [T, heads, dim] whose rows are contiguous in themselves."""
     if not isinstance(x, torch.Tensor) or not x.is_cuda:
         raise TypeError(f"{name} must be a GPU torch tensor")
-    if x.dim() != 3 or tuple(x.shape[1:]) != shape:
-        raise ValueError(f"{name} must be [rows, {shape[0]}, {shape[1]}], got {tuple(x.shape)}")
-    if x.stride(2) != 1 or (x.stride(1) != shape[1] and shape[0] > 1):
+    if x.dim() != 3 or x.size(1) != heads or x.size(2) != dim:
+        raise ValueError(f"{name} must be [rows, {heads}, {dim}], got {tuple(x.shape)}")
+    s = x.stride()
+    if s[2] != 1 or (s[1] != dim and heads > 1):
         raise ValueError(f"{name}: heads and elements of a row must be contiguous")
-    return x.stride(0) if x.shape[0] > 1 else shape[0] * shape[1]
+    return s[0] if x.size(0) > 1 else heads * dim
 
 
 def kv_write(cache: KVCache, k, v, page_table, starts, row_off, max_rows: int) -> None:
     """Quantise rows row_off[s] .. row_off[s + 1] of k and v [T, heads, dim] into the cache as the tokens starts[s],
     starts[s] + 1, ... of sequence s.  No sequence may have more than max_rows of them."""
     width, S = _rows(page_table, starts, "starts", row_off)
-    shape = (cache.heads, cache.dim)
-    ks, vs = _strided(k, shape, "k"), _strided(v, shape, "v")
-    if k.dtype not in _TYPES or v.dtype != k.dtype:
+    ks, vs = _strided(k, cache.heads, cache.dim, "k"), _strided(v, cache.heads, cache.dim, "v")
+    type_ = _TYPES.get(k.dtype)
+    if type_ is None or v.dtype != k.dtype:
         raise TypeError(f"k and v must share one of {list(_TYPES)}")
-    if v.shape[0] != k.shape[0]:
+    T = k.size(0)
+    if v.size(0) != T:
         raise ValueError("k and v differ in length")
-    _check(lib.evospec_kv_write(cache._ref, k.data_ptr(), ks, v.data_ptr(), vs, _TYPES[k.dtype], k.shape[0], page_table.data_ptr(),
-                                width, starts.data_ptr(), row_off.data_ptr(), S, max_rows, _stream()), "evospec_kv_write")
+    _check(lib.evospec_kv_write(cache._ref, k.data_ptr(), ks, v.data_ptr(), vs, type_, T, page_table.data_ptr(),
+                                width, starts.data_ptr(), row_off.data_ptr(), S, max_rows, _raw_stream(_get_device())), "evospec_kv_write")
 
 
 def kv_read(cache: KVCache, page_table, starts, row_off, max_rows: int, rows: int, dtype=torch.bfloat16, out_k=None, out_v=None):
@@ -104,23 +131,22 @@ def kv_read(cache: KVCache, page_table, starts, row_off, max_rows: int, rows: in
     width, S = _rows(page_table, starts, "starts", row_off)
     if dtype not in _TYPES:
         raise TypeError(f"dtype must be one of {list(_TYPES)}")
-    shape = (int(rows), cache.heads, cache.dim)
+    rows = int(rows)
+    shape = (rows, cache.heads, cache.dim)
+    for t, name in ((out_k, "out_k"), (out_v, "out_v")):
+        if t is not None:
+            _expect(t, dtype, name, 3)
+            if tuple(t.shape) != shape:
+                raise ValueError(f"{name} must be {shape}, got {tuple(t.shape)}")
     out_k = torch.empty(shape, dtype=dtype, device=cache.data.device) if out_k is None else out_k
     out_v = torch.empty(shape, dtype=dtype, device=cache.data.device) if out_v is None else out_v
-    for t, name in ((out_k, "out_k"), (out_v, "out_v")):
-        _expect(t, dtype, name, 3)
-        if tuple(t.shape) != shape:
-            raise ValueError(f"{name} must be {shape}, got {tuple(t.shape)}")
-    _check(lib.evospec_kv_read(cache._ref, page_table.data_ptr(), width, starts.data_ptr(), row_off.data_ptr(), S, max_rows, shape[0],
-                               _TYPES[dtype], out_k.data_ptr(), out_v.data_ptr(), _stream()), "evospec_kv_read")
+    _check(lib.evospec_kv_read(cache._ref, page_table.data_ptr(), width, starts.data_ptr(), row_off.data_ptr(), S, max_rows, rows,
+                               _TYPES[dtype], out_k.data_ptr(), out_v.data_ptr(), _raw_stream(_get_device())), "evospec_kv_read")
     return out_k, out_v
 
 
 def kv_attention_workspace_bytes(cache: KVCache, group: int, S: int, T: int, max_rows: int, max_len: int) -> int:
-    out = _sz(0)
-    _check(lib.evospec_kv_attention_workspace_bytes(cache._ref, int(group), int(S), int(T), int(max_rows), int(max_len),
-                                                    ctypes.byref(out)), "evospec_kv_attention_workspace_bytes")
-    return int(out.value)
+    return _attention_bytes(cache.pages, cache.page, cache.heads, cache.dim, cache._c.kind, group, S, T, max_rows, max_len)
 
 
 def kv_attention(q, cache: KVCache, page_table, lens, row_off, max_rows: int, max_len=None, tree=None, scale=None, out=None,
@@ -131,11 +157,12 @@ def kv_attention(q, cache: KVCache, page_table, lens, row_off, max_rows: int, ma
     come before the sequence's rows, and those of its bits.  `scale` is 1 / sqrt(dim) if not given; max_len (a bound of lens)
     only decides how the work is split."""
     width, S = _rows(page_table, lens, "lens", row_off)
-    if q.dim() != 3 or q.shape[1] % cache.heads:
+    if q.dim() != 3 or q.size(1) % cache.heads:
         raise ValueError("q must be [rows, a multiple of the cache's heads, dim]")
     T, heads, dim = q.shape
-    qs = _strided(q, (heads, cache.dim), "q")
-    if q.dtype not in (torch.bfloat16, torch.float16):
+    qs = _strided(q, heads, cache.dim, "q")
+    type_ = _TYPES.get(q.dtype, 2)
+    if type_ == 2:
         raise TypeError(f"q must be bfloat16 or float16, got {q.dtype}")
     if tree is not None:
         _expect(tree, torch.int64, "tree", 1)
@@ -158,17 +185,15 @@ def kv_attention(q, cache: KVCache, page_table, lens, row_off, max_rows: int, ma
     if workspace is None:
         need = kv_attention_workspace_bytes(cache, group, S, T, max_rows, max_len)
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-    _check(lib.evospec_kv_attention(cache._ref, q.data_ptr(), qs, _TYPES[q.dtype], T, group, page_table.data_ptr(), width,
+    _check(lib.evospec_kv_attention(cache._ref, q.data_ptr(), qs, type_, T, group, page_table.data_ptr(), width,
                                     lens.data_ptr(), row_off.data_ptr(), S, max_rows, max_len, _ptr(tree),
                                     dim ** -0.5 if scale is None else scale, out.data_ptr(), out_lse.data_ptr(), _ptr(workspace),
-                                    0 if workspace is None else workspace.numel(), _stream()), "evospec_kv_attention")
+                                    0 if workspace is None else workspace.numel(), _raw_stream(_get_device())), "evospec_kv_attention")
     return out, out_lse
 
 
 def sample_workspace_bytes(M: int, V: int) -> int:
-    out = _sz(0)
-    _check(lib.evospec_sample_workspace_bytes(int(M), int(V), ctypes.byref(out)), "evospec_sample_workspace_bytes")
-    return int(out.value)
+    return _sample_bytes(M, V)
 
 
 def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, ids=None, out_ids=None, out_logprob=None,
@@ -187,24 +212,26 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, ids=
     for t, dtype, name in ((u, torch.float32, "u"), (temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
                            (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p")):
         if t is not None or name == "u":
-            _expect(t, dtype, name, 1)
-            if t.shape[0] != M:
+            if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.dim() == 1 and t.is_contiguous()):
+                _expect(t, dtype, name, 1)
+            if t.numel() != M:
                 raise ValueError(f"{name} needs a value for every row")
     if ids is not None:
         _expect(ids, torch.int32, "ids", 1)
         if ids.shape[0] != V:
             raise ValueError("ids needs an id for every column")
-    out_ids = torch.empty(M, dtype=torch.int32, device=logits.device) if out_ids is None else out_ids
-    out_logprob = torch.empty(M, dtype=torch.float32, device=logits.device) if out_logprob is None else out_logprob
-    for t, dtype, name in ((out_ids, torch.int32, "out_ids"), (out_logprob, torch.float32, "out_logprob")):
-        _expect(t, dtype, name, 1)
-        if t.shape[0] != M:
-            raise ValueError(f"{name} needs a place for every row")
+    for t, dtype, name in ((out_ids, _i32, "out_ids"), (out_logprob, _f32, "out_logprob")):
+        if t is not None:
+            _expect(t, dtype, name, 1)
+            if t.numel() != M:
+                raise ValueError(f"{name} needs a place for every row")
+    out_ids = torch.empty(M, dtype=_i32, device=logits.device) if out_ids is None else out_ids
+    out_logprob = torch.empty(M, dtype=_f32, device=logits.device) if out_logprob is None else out_logprob
     if workspace is None:
-        need = sample_workspace_bytes(M, V)
+        need = _sample_bytes(M, V)
         workspace = torch.empty(need, dtype=torch.uint8, device=logits.device) if need else None
     _check(lib.evospec_sample(logits.data_ptr(), logits.stride(0) if M > 1 else V, _TYPES[logits.dtype], M, V, u.data_ptr(),
                               _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(ids), out_ids.data_ptr(),
-                              out_logprob.data_ptr(), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream()),
+                              out_logprob.data_ptr(), _ptr(workspace), 0 if workspace is None else workspace.numel(), _raw_stream(_get_device())),
            "evospec_sample")
     return out_ids, out_logprob
