@@ -152,20 +152,6 @@ __device__ __forceinline__ void piece_to_rows(uint8_t* rows, int p, u32x4 x) {
     }
 }
 
-// 8 elements of a row as floats
-template <int TYPE>
-__device__ __forceinline__ void load8(const typename Element<TYPE>::type* p, float* x) {
-    if constexpr (TYPE == EVOSPEC_FP32) {
-        const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-        x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-    } else {
-        typedef typename Element<TYPE>::type vec __attribute__((ext_vector_type(8)));
-        const vec v = *reinterpret_cast<const vec*>(p);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
-    }
-}
 template <int TYPE>
 __device__ __forceinline__ void store8(typename Element<TYPE>::type* p, const float* x) {
     if constexpr (TYPE == EVOSPEC_FP32) {
@@ -180,97 +166,205 @@ __device__ __forceinline__ void store8(typename Element<TYPE>::type* p, const fl
     }
 }
 
-// Quantises the new tokens of one block (K or V) and writes the block.
-template <int DIM, int KIND, int TYPE, bool V>
-__device__ __forceinline__ void write_half(const Task& t, const typename Element<TYPE>::type* x, long long stride, uint8_t* data,
-                                           float* scale, uint8_t* rows, float* reduce) {
-    constexpr int kChunks = kBlock * DIM / 8;                    // of 8 elements
-    constexpr int kPer = (kChunks + kThreads - 1) / kThreads;
-    constexpr int kPieces = 2 * DIM;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    float y[kPer][8];
-    float amax = 0.f;
-    bool nan = false;
-#pragma unroll
-    for (int c = 0; c < kPer; ++c) {
-        const int chunk = c * kThreads + tid, m = chunk / (DIM / 8), d = chunk % (DIM / 8) * 8;
-        if (m >= t.first && m < t.last && (kChunks % kThreads == 0 || chunk < kChunks)) {
-            load8<TYPE>(x + (long long)(t.row + m) * stride + (long long)t.head * DIM + d, y[c]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[c][i] = 0.f;
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float a = fabsf(y[c][i]);
-            nan |= a != a;
-            amax = fmaxf(amax, a < __builtin_inff() ? a : 0.f);
-        }
+// 8 elements of a row as they come, and as floats
+template <int TYPE>
+struct Raw {
+    u32x4 a, b;                                                  // (b: fp32 only)
+    __device__ __forceinline__ void load(const typename Element<TYPE>::type* p) {
+        a = reinterpret_cast<const u32x4*>(p)[0];
+        if constexpr (TYPE == EVOSPEC_FP32) b = reinterpret_cast<const u32x4*>(p)[1];
     }
-    amax = wave_max(amax, lane);
-    const bool any = __ballot(nan) != 0;
-    if (lane == 0) reduce[wave] = any ? -amax : amax;            // (the sign bit, also of a zero)
-    __syncthreads();
-    amax = 0.f;
-    nan = false;
-#pragma unroll
-    for (int w = 0; w < kThreads / 64; ++w) {
-        const float a = reduce[w];
-        nan |= __float_as_uint(a) >> 31;
-        amax = fmaxf(amax, fabsf(a));
+    __device__ __forceinline__ void clear() { a = b = u32x4{0, 0, 0, 0}; }
+    __device__ __forceinline__ float at(int i) const {
+        if constexpr (TYPE == EVOSPEC_FP32) return __uint_as_float(i < 4 ? a[i] : b[i - 4]);
+        else if constexpr (TYPE == EVOSPEC_BF16) return __uint_as_float(i & 1 ? a[i >> 1] & 0xffff0000u : a[i >> 1] << 16);
+        else return (float)__builtin_bit_cast(_Float16, (uint16_t)(a[i >> 1] >> (16 * (i & 1))));
     }
-    float s = scale_of<KIND>(amax), s_old = 0.f;
-    if (!t.fresh) {
-        const float o = *scale;
-        nan |= __float_as_uint(o) >> 31;
-        s_old = fabsf(o);
-        s = fmaxf(s, s_old);
+    // the largest magnitude so far as bits, whose order is that of the magnitudes; 16-bit types two at a time
+    __device__ __forceinline__ u32x4 larger(u32x4 m) const {
+        typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+        if constexpr (TYPE == EVOSPEC_FP32)
+            return __builtin_elementwise_max(m, __builtin_elementwise_max(a & 0x7fffffffu, b & 0x7fffffffu));
+        else
+            return __builtin_bit_cast(u32x4, __builtin_elementwise_max(__builtin_bit_cast(u16x8, m), __builtin_bit_cast(u16x8, a & 0x7fff7fffu)));
     }
-    const bool keep = !t.fresh;                                  // (uniform)
-    __syncthreads();                                             // every thread has read the scale and `reduce`
-    if (keep) {                                                  // the block's bytes first, as rows
-        for (int p = tid; p < kPieces; p += kThreads) {
-            const u32x4 b = *reinterpret_cast<const u32x4*>(data + p * 16);
-            piece_to_rows<DIM, V>(rows, p, b);
-        }
-        __syncthreads();
+};
+// of four words of such bits, as a float (infinity and NaN as they are)
+template <int TYPE>
+__device__ __forceinline__ float magnitude(u32x4 m) {
+    uint32_t x = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (TYPE == EVOSPEC_FP32) x = max(x, m[i]);
+        else x = max(x, max(m[i] & 0xffffu, m[i] >> 16));
     }
-#pragma unroll
-    for (int c = 0; c < kPer; ++c) {
-        const int chunk = c * kThreads + tid, m = chunk / (DIM / 8), d = chunk % (DIM / 8) * 8;
-        if (kChunks % kThreads != 0 && chunk >= kChunks) break;
-        uint2* at = reinterpret_cast<uint2*>(rows + m * kRow<DIM> + d);
-        if (m < t.old) {
-            if (s == s_old) continue;                            // (uniform)
-            const uint2 b = *at;
-            decode4<KIND>(b.x, y[c]);
-            decode4<KIND>(b.y, y[c] + 4);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[c][i] = y[c][i] * s_old;
-        } else if (m >= t.last && keep) {
-            continue;                                            // what is behind the new tokens stays
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[c][i] = y[c][i] / s;
-        *at = make_uint2(encode4<KIND>(y[c]), encode4<KIND>(y[c] + 4));
-    }
-    __syncthreads();
-    for (int p = tid; p < kPieces; p += kThreads) *reinterpret_cast<u32x4*>(data + p * 16) = piece_from_rows<DIM, V>(rows, p);
-    if (tid == 0) *scale = nan ? -s : s;
+    if constexpr (TYPE == EVOSPEC_FP32) return __uint_as_float(x);
+    else if constexpr (TYPE == EVOSPEC_BF16) return __uint_as_float(x << 16);
+    else return (float)__builtin_bit_cast(_Float16, (uint16_t)x);
 }
 
+// Codes of 8 values that are finite and no larger than the largest code times s.  e4m3's s is a power of two, whose reciprocal is
+// exact; int8 multiplies too, and divides only where the quotient lies so near to the middle between two codes that the
+// product may be on the other side of it.  x / s + 1.5 * 2^23 has the rounded quotient in its low bits.
+template <int KIND, int TYPE>
+__device__ __forceinline__ uint2 encode_plain(const Raw<TYPE>& x, float s, float inv) {
+    uint32_t out[2];
+    if constexpr (KIND == EVOSPEC_KV_E4M3) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int p = __builtin_amdgcn_cvt_pk_fp8_f32(x.at(4 * j) * inv, x.at(4 * j + 1) * inv, 0, false);
+            out[j] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x.at(4 * j + 2) * inv, x.at(4 * j + 3) * inv, p, true);
+        }
+    } else {
+        constexpr float kMagic = 12582912.f;
+        uint32_t f[8];
+        float far = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float v = x.at(i), y = fmaf(v, inv, kMagic);
+            far = fmaxf(far, fabsf(fmaf(v, inv, kMagic - y)));
+            f[i] = __float_as_uint(y);
+        }
+        if (far > 0.5f - 0x1p-12f) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = __float_as_uint(x.at(i) / s + kMagic);
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            out[j] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(f[4 * j + 3], f[4 * j + 2], 0x0c0c0400u),
+                                           __builtin_amdgcn_perm(f[4 * j + 1], f[4 * j], 0x0c0c0400u), 0x05040100u);
+    }
+    return make_uint2(out[0], out[1]);
+}
+// Codes of any 8 values.
+template <int KIND>
+__device__ __forceinline__ uint2 encode_any(float* y, float s) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = y[i] / s;
+    return make_uint2(encode4<KIND>(y), encode4<KIND>(y + 4));
+}
+
+// Quantises the new tokens of one block, K and V side by side, and writes the block.  What is rare (a NaN, an infinity, older codes
+// that have to be scaled) has code of its own: with it in the way of all, 64 elements of a thread took 1,600 instructions, and
+// 12,000 tokens of 8 heads 28 us.
 template <int DIM, int KIND, int TYPE>
 __global__ __launch_bounds__(kThreads) void kv_write_kernel(Cache c, Rows r, int per, const typename Element<TYPE>::type* k,
                                                             long long k_stride, const typename Element<TYPE>::type* v,
                                                             long long v_stride) {
     __shared__ __align__(16) uint8_t rows[2][kBlock * kRow<DIM>];
-    __shared__ float reduce[2][kThreads / 64];
+    __shared__ float reduce[2][2][kThreads / 64];
+    constexpr int kChunks = kBlock * DIM / 8;                    // of 8 elements
+    constexpr int kPer = (kChunks + kThreads - 1) / kThreads;
+    constexpr int kPieces = 2 * DIM;
     const Task t = task_of(c, r, per, blockIdx.x);
     if (t.at < 0) return;
     uint8_t* data = c.data + t.at * (2 * kBlock * DIM);
     float* scale = c.scales + t.at * 2;
-    write_half<DIM, KIND, TYPE, false>(t, k, k_stride, data, scale, rows[0], reduce[0]);
-    write_half<DIM, KIND, TYPE, true>(t, v, v_stride, data + kBlock * DIM, scale + 1, rows[1], reduce[1]);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    Raw<TYPE> x[2][kPer];
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+#pragma unroll
+        for (int p = 0; p < kPer; ++p) {
+            const int chunk = p * kThreads + tid, m = chunk / (DIM / 8), d = chunk % (DIM / 8) * 8;
+            if (m >= t.first && m < t.last && (kChunks % kThreads == 0 || chunk < kChunks))
+                x[w][p].load((w ? v : k) + (long long)(t.row + m) * (w ? v_stride : k_stride) + (long long)t.head * DIM + d);
+            else
+                x[w][p].clear();
+        }
+    const bool keep = !t.fresh;                                  // (uniform)
+    float old[2] = {0.f, 0.f};
+    if (keep) {                                                  // the block's bytes first, as rows
+        for (int p = tid; p < kPieces; p += kThreads) {
+            piece_to_rows<DIM, false>(rows[0], p, *reinterpret_cast<const u32x4*>(data + p * 16));
+            piece_to_rows<DIM, true>(rows[1], p, *reinterpret_cast<const u32x4*>(data + kBlock * DIM + p * 16));
+        }
+        old[0] = scale[0];
+        old[1] = scale[1];
+    }
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        u32x4 m = {0, 0, 0, 0};
+#pragma unroll
+        for (int p = 0; p < kPer; ++p) m = x[w][p].larger(m);
+        // (as numbers of bits: a NaN is larger than all)
+        uint32_t top = __float_as_uint(magnitude<TYPE>(m));
+        top = max(top, xor_lane<1>(top, lane));
+        top = max(top, xor_lane<2>(top, lane));
+        top = max(top, xor_lane<4>(top, lane));
+        top = max(top, xor_lane<8>(top, lane));
+        top = max(top, xor_lane<16>(top, lane));
+        top = max(top, xor_lane<32>(top, lane));
+        if (lane == 0) reduce[0][w][wave] = __uint_as_float(top);
+    }
+    __syncthreads();
+    float final[2];
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        uint32_t bits = 0;
+#pragma unroll
+        for (int i = 0; i < kThreads / 64; ++i) bits = max(bits, __float_as_uint(reduce[0][w][i]));
+        float amax = __uint_as_float(bits);
+        bool nan = __float_as_uint(old[w]) >> 31;
+        const bool special = bits >= 0x7f800000u;                // (uniform) a NaN or an infinity: the largest of the others
+        if (special) {
+            amax = 0.f;
+            bool mine = false;
+#pragma unroll
+            for (int p = 0; p < kPer; ++p)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float a = fabsf(x[w][p].at(i));
+                    mine |= a != a;
+                    amax = fmaxf(amax, a < __builtin_inff() ? a : 0.f);
+                }
+            amax = wave_max(amax, lane);
+            mine = __ballot(mine) != 0;
+            if (lane == 0) reduce[1][w][wave] = mine ? -amax : amax;         // (the sign bit, also of a zero)
+            __syncthreads();
+            amax = 0.f;
+#pragma unroll
+            for (int i = 0; i < kThreads / 64; ++i) {
+                const float a = reduce[1][w][i];
+                nan |= __float_as_uint(a) >> 31;
+                amax = fmaxf(amax, fabsf(a));
+            }
+        }
+        const float s_old = fabsf(old[w]), s = fmaxf(scale_of<KIND>(amax), s_old);
+        const bool plain = !special && (KIND == EVOSPEC_KV_INT8 || amax <= 448.f * s);
+        const float inv = 1.f / s;
+        final[w] = nan ? -s : s;
+#pragma unroll
+        for (int p = 0; p < kPer; ++p) {
+            const int chunk = p * kThreads + tid, m = chunk / (DIM / 8), d = chunk % (DIM / 8) * 8;
+            if (kChunks % kThreads != 0 && chunk >= kChunks) break;
+            uint2* at = reinterpret_cast<uint2*>(rows[w] + m * kRow<DIM> + d);
+            float y[8];
+            if (m < t.old) {
+                if (s == s_old) continue;                        // (uniform)
+                const uint2 b = *at;
+                decode4<KIND>(b.x, y);
+                decode4<KIND>(b.y, y + 4);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] = y[i] * s_old;
+                *at = encode_any<KIND>(y, s);
+            } else if (m < t.last || !keep) {                    // (what is behind the new tokens of an older block stays)
+                if (plain) {
+                    *at = encode_plain<KIND, TYPE>(x[w][p], s, inv);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) y[i] = x[w][p].at(i);
+                    *at = encode_any<KIND>(y, s);
+                }
+            }
+        }
+    }
+    __syncthreads();
+    for (int p = tid; p < kPieces; p += kThreads) {
+        *reinterpret_cast<u32x4*>(data + p * 16) = piece_from_rows<DIM, false>(rows[0], p);
+        *reinterpret_cast<u32x4*>(data + kBlock * DIM + p * 16) = piece_from_rows<DIM, true>(rows[1], p);
+    }
+    if (tid < 2) scale[tid] = final[tid];
 }
 
 template <int DIM, int KIND, int TYPE>
