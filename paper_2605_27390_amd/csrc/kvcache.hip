@@ -90,7 +90,6 @@ struct Task {
     int row;                    // row of the block's token 0 (may be negative; only tokens in [first, last) are rows)
     bool fresh;                 // token 0 of the block is among them, or no token is older
     int old;                    // tokens [0, old) of the block are older
-    long long at;               // its place: (page * heads + head) blocks in, -1 if it has none
 };
 __device__ __forceinline__ Task task_of(const Cache& c, const Rows& r, int per, int id) {
     Task t;
@@ -108,13 +107,14 @@ __device__ __forceinline__ Task task_of(const Cache& c, const Rows& r, int per, 
     t.old = t.first;
     t.fresh = t.old == 0;
     t.row = n0 + (int)(token - start);
-    t.at = -1;
-    if (t.last > t.first && (t.block >> c.shift) < r.width) {
-        const int page = r.table[(long long)t.s * r.width + (t.block >> c.shift)];
-        if ((unsigned)page < (unsigned)c.pages)
-            t.at = ((((long long)page * c.heads + t.head) << c.shift) + (t.block & ((1 << c.shift) - 1)));
-    }
     return t;
+}
+// A task's place: (page * heads + head) blocks in, -1 if it has none.
+__device__ __forceinline__ long long place_of(const Cache& c, const Rows& r, const Task& t) {
+    if ((t.block >> c.shift) >= r.width) return -1;
+    const int page = r.table[(long long)t.s * r.width + (t.block >> c.shift)];
+    if ((unsigned)page >= (unsigned)c.pages) return -1;
+    return (((long long)page * c.heads + t.head) << c.shift) + (t.block & ((1 << c.shift) - 1));
 }
 
 // Bytes of a block's tokens in LDS: a row of dim bytes, 16 more so that pieces of neighbouring tokens lie in other banks.
@@ -257,9 +257,7 @@ __global__ __launch_bounds__(kThreads) void kv_write_kernel(Cache c, Rows r, int
     constexpr int kPer = (kChunks + kThreads - 1) / kThreads;
     constexpr int kPieces = 2 * DIM;
     const Task t = task_of(c, r, per, blockIdx.x);
-    if (t.at < 0) return;
-    uint8_t* data = c.data + t.at * (2 * kBlock * DIM);
-    float* scale = c.scales + t.at * 2;
+    if (t.last <= t.first) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     Raw<TYPE> x[2][kPer];
 #pragma unroll
@@ -272,6 +270,10 @@ __global__ __launch_bounds__(kThreads) void kv_write_kernel(Cache c, Rows r, int
             else
                 x[w][p].clear();
         }
+    const long long place = place_of(c, r, t);                   // (while the new tokens are under way)
+    if (place < 0) return;
+    uint8_t* data = c.data + place * (2 * kBlock * DIM);
+    float* scale = c.scales + place * 2;
     const bool keep = !t.fresh;                                  // (uniform)
     float old[2] = {0.f, 0.f};
     if (keep) {                                                  // the block's bytes first, as rows
@@ -376,10 +378,11 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(Cache c, Rows r, int 
     constexpr int kChunks = kBlock * DIM / 8, kPieces = 2 * DIM;
     const int tid = threadIdx.x;
     float s[2] = {0.f, 0.f};
-    if (t.at >= 0) {
-        const uint8_t* data = c.data + t.at * (2 * kBlock * DIM);
-        s[0] = fabsf(c.scales[t.at * 2]);
-        s[1] = fabsf(c.scales[t.at * 2 + 1]);
+    const long long place = place_of(c, r, t);
+    if (place >= 0) {
+        const uint8_t* data = c.data + place * (2 * kBlock * DIM);
+        s[0] = fabsf(c.scales[place * 2]);
+        s[1] = fabsf(c.scales[place * 2 + 1]);
         for (int p = tid; p < kPieces; p += kThreads) {
             piece_to_rows<DIM, false>(rows[0], p, *reinterpret_cast<const u32x4*>(data + p * 16));
             piece_to_rows<DIM, true>(rows[1], p, *reinterpret_cast<const u32x4*>(data + kBlock * DIM + p * 16));
@@ -393,7 +396,7 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(Cache c, Rows r, int 
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
             float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if (t.at >= 0) {                                     // (uniform)
+            if (place >= 0) {                                    // (uniform)
                 const uint2 b = *reinterpret_cast<const uint2*>(rows[w] + m * kRow<DIM> + d);
                 decode4<KIND>(b.x, y);
                 decode4<KIND>(b.y, y + 4);
