@@ -71,27 +71,37 @@ class KVCache:
     def __init__(self, pages: int, page: int, heads: int, dim: int, kind: str = "e4m3", device="cuda", data=None, scales=None):
         if kind not in _KINDS:
             raise ValueError(f"kind must be one of {sorted(_KINDS)}, got {kind!r}")
-        self.pages, self.page, self.heads, self.dim, self.kind = int(pages), int(page), int(heads), int(dim), kind
-        self._c = _Cache(None, None, self.pages, self.page, self.heads, self.dim, _KINDS[kind])
-        self._ref = ctypes.byref(self._c)
-        n_data, n_scales = _cache_bytes(self.pages, self.page, self.heads, self.dim, self._c.kind)
+        pages, page, heads, dim = int(pages), int(page), int(heads), int(dim)
+        self.pages, self.page, self.heads, self.dim, self.kind = pages, page, heads, dim, kind
+        n_data, n_scales = _cache_bytes(pages, page, heads, dim, _KINDS[kind])
         if data is None:
             data = torch.empty(n_data, dtype=torch.uint8, device=device)
         if scales is None:
             scales = torch.empty(n_scales // 4, dtype=torch.float32, device=device)
-        _expect(data, torch.uint8, "data")
-        _expect(scales, torch.float32, "scales")
+        if not (data.dtype is torch.uint8 and scales.dtype is _f32 and data.is_cuda and scales.is_cuda and data.is_contiguous()
+                and scales.is_contiguous()):
+            _expect(data, torch.uint8, "data")
+            _expect(scales, _f32, "scales")
         if data.numel() < n_data or scales.numel() * 4 < n_scales:
             raise ValueError("data or scales is smaller than evospec_kv_cache_bytes reports")
         self.data, self.scales = data, scales
-        self._c.data, self._c.scales = data.data_ptr(), scales.data_ptr()
+        self._c = _Cache(data.data_ptr(), scales.data_ptr(), pages, page, heads, dim, _KINDS[kind])
+        self._ref = ctypes.byref(self._c)
 
 
 def _rows(page_table, at, name, row_off):
-    """(width, S) of the index tensors of a call."""
-    for x, what, ndim in ((page_table, "page_table", 2), (at, name, 1), (row_off, "row_off", 1)):
-        if not (isinstance(x, torch.Tensor) and x.dtype is _i32 and x.is_cuda and x.dim() == ndim and x.is_contiguous()):
-            _expect(x, _i32, what, ndim)
+    """(width, S) of the index tensors of a call.  (Checks here and below are written out: a call is about 4 us of launch, and
+    a function for each check cost another 3.)"""
+    try:
+        ok = (page_table.dtype is at.dtype is row_off.dtype is _i32 and page_table.is_cuda and at.is_cuda and row_off.is_cuda
+              and page_table.dim() == 2 and at.dim() == row_off.dim() == 1
+              and page_table.is_contiguous() and at.is_contiguous() and row_off.is_contiguous())
+    except AttributeError:
+        ok = False
+    if not ok:
+        _expect(page_table, _i32, "page_table", 2)
+        _expect(at, _i32, name, 1)
+        _expect(row_off, _i32, "row_off", 1)
     S, width = page_table.shape
     if at.numel() != S or row_off.numel() != S + 1:
         raise ValueError(f"page_table, {name} and row_off disagree about the number of sequences")
@@ -157,9 +167,12 @@ def kv_attention(q, cache: KVCache, page_table, lens, row_off, max_rows: int, ma
     come before the sequence's rows, and those of its bits.  `scale` is 1 / sqrt(dim) if not given; max_len (a bound of lens)
     only decides how the work is split."""
     width, S = _rows(page_table, lens, "lens", row_off)
-    if q.dim() != 3 or q.size(1) % cache.heads:
-        raise ValueError("q must be [rows, a multiple of the cache's heads, dim]")
+    if q.dim() != 3:
+        raise ValueError("q must be [rows, query heads, dim]")
     T, heads, dim = q.shape
+    group = heads // cache.heads
+    if group * cache.heads != heads:
+        raise ValueError("q must have a multiple of the cache's heads")
     qs = _strided(q, heads, cache.dim, "q")
     type_ = _TYPES.get(q.dtype, 2)
     if type_ == 2:
@@ -168,10 +181,9 @@ def kv_attention(q, cache: KVCache, page_table, lens, row_off, max_rows: int, ma
         _expect(tree, torch.int64, "tree", 1)
         if tree.shape[0] != T:
             raise ValueError("tree needs a word for every row of q")
-    group = heads // cache.heads
     max_len = width * cache.page if max_len is None else int(max_len)
     if out is None:
-        out = torch.empty((T, heads, dim), dtype=q.dtype, device=q.device)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     else:
         _expect(out, q.dtype, "out", 3)
         if out.shape != q.shape:
@@ -183,7 +195,7 @@ def kv_attention(q, cache: KVCache, page_table, lens, row_off, max_rows: int, ma
         if tuple(out_lse.shape) != (T, heads):
             raise ValueError("out_lse must be [rows, query heads]")
     if workspace is None:
-        need = kv_attention_workspace_bytes(cache, group, S, T, max_rows, max_len)
+        need = _attention_bytes(cache.pages, cache.page, cache.heads, cache.dim, cache._c.kind, group, S, T, max_rows, max_len)
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
     _check(lib.evospec_kv_attention(cache._ref, q.data_ptr(), qs, type_, T, group, page_table.data_ptr(), width,
                                     lens.data_ptr(), row_off.data_ptr(), S, max_rows, max_len, _ptr(tree),
