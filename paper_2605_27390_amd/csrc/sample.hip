@@ -213,7 +213,7 @@ constexpr int kMostSlices = ((1 << 20) + kSlice - 1) / kSlice;
 constexpr int kList = 4096;                       // tokens of a row that are looked at one by one
 constexpr int kStage = 1024;                      // of a slice that go to that list at once
 constexpr int kMostK = 256;                       // top-k up to this goes by lists alone
-constexpr int kSteps = 128;                       // of the table of powers of two
+constexpr int kSteps = 32;                        // to a factor of 2 in the table of powers: each has its own banks of LDS
 
 struct RowState {
     double ref;                                   // exponent of the row's reference
@@ -259,38 +259,49 @@ __device__ __forceinline__ RowSpace row_space(char* ws, int m, int slices) {
     return r;
 }
 
-// Powers 2^(j / kSteps), for weights by table: x = n + j / kSteps + r, |r| <= 1 / (2 kSteps); the series of 2^r to the fourth
-// power is off by 1e-15.
-__device__ __forceinline__ void fill_table(double* table) {
-    if (threadIdx.x < kSteps) table[threadIdx.x] = 2.0 * exp2_series((double)threadIdx.x / kSteps - 1.0);
-}
-// -x in steps of 1 / kSteps, to the nearest (x in (-2^20, 0]); r = what is left
-__device__ __forceinline__ int steps_of(double x, double& r) {
-    const double magic = 6755399441055744.0 / kSteps;            // 1.5 * 2^52 / kSteps
-    const double t = x + magic;
-    r = x - (t - magic);
-    return -(int)(uint32_t)__double_as_longlong(t);
-}
+// Weights by table: with y = z log2(e) / T = k / kSteps + r, |r| <= 1 / (2 kSteps), and `ref` a whole power of two above the row's or
+// slice's largest, w = 2^(y - ref) = 2^(-m / kSteps) 2^r, m = kSteps ref - k >= 0.  2^r by its series to the fourth power is off by
+// 2^-39.  What bounds the bins is LDS, an addition to a bin for each logit; a table of 128 steps, whose reads meet in its banks,
+// made it 183 us for 146 million logits.
+struct Steps {
+    int m;
+    double r;
+};
 // x y + c with c in scalar registers (the compiler's choice copies c to vector registers first, 2 more instructions of 3)
 __device__ __forceinline__ double fma_to(double x, double y, double c) {
     double d;
     asm("v_fma_f64 %0, %1, %2, %3" : "=v"(d) : "v"(x), "v"(y), "s"(c));
     return d;
 }
-__device__ __forceinline__ u64 weight_of(int steps, double r, const double* table) {
-    double first = 0.0096181291076284772;                        // ln(2)^k / k!
-    asm("" : "+v"(first));                                     // (one vector register pair for all calls)
-    double p = fma_to(r, first, 0.055504108664821580);
-    p = fma_to(p, r, 0.24022650695910071);
-    p = fma_to(p, r, 0.69314718055994531);
-    p = fma(p, r, 1.0);
-    const int n = (-steps) >> 7, j = (-steps) & (kSteps - 1);
-    const double s = __longlong_as_double((long long)(1023 + 43 + n) << 52);
-    const double d = fma(table[j] * p, s, 4503599627370496.0);   // 2^52 + the weight, rounded to a whole number
-    return (u64)__double_as_longlong(d) & 0xfffffffffffffull;
+__device__ __forceinline__ Steps locate(float z, double c, int ref_steps) {
+    const double magic = 6755399441055744.0 / kSteps;            // 1.5 * 2^52 / kSteps: k in the low bits
+    const double zd = (double)z, t = fma_to(zd, c, magic);
+    Steps s;
+    s.r = fma(zd, c, -(t - magic));
+    s.m = ref_steps - (int)(uint32_t)__double_as_longlong(t);
+    return s;
 }
-static_assert(kSteps == 128 && kSteps % kBins == 0, "shifts");
-__device__ __forceinline__ int bin_of(int steps) { return min((int)((uint32_t)steps / (kSteps / kBins)), kAll - 1); }
+__device__ __forceinline__ void fill_table(double* table) {
+    if (threadIdx.x < kSteps) table[threadIdx.x] = kOne * exp2_series(-(double)threadIdx.x / kSteps);
+}
+// m < kRange kSteps
+__device__ __forceinline__ u64 weight_of(Steps s, const double* table) {
+    double first = 0.0096181291076284772;                        // ln(2)^k / k!
+    asm("" : "+v"(first));                                       // (one vector register pair for all calls)
+    double p = fma_to(s.r, first, 0.055504108664821580);
+    p = fma_to(p, s.r, 0.24022650695910071);
+    p = fma_to(p, s.r, 0.69314718055994531);
+    p = fma(p, s.r, 1.0);
+    const long long power = __double_as_longlong(table[s.m & (kSteps - 1)]);
+    const uint32_t hi = (uint32_t)(power >> 32) - ((uint32_t)s.m / kSteps << 20);
+    const double d = fma_to(__longlong_as_double((long long)((u64)hi << 32 | (uint32_t)power)), p, 4503599627370496.0);
+    return (u64)__double_as_longlong(d) & 0xfffffffffffffull;    // 2^52 + the weight, rounded to a whole number
+}
+static_assert(kSteps == kBins, "a step is a bin");
+__device__ __forceinline__ int bin_of(int m) { return min(m, kAll - 1); }
+// logits below this have no weight
+__device__ __forceinline__ float cut_of(double ref, float T) { return (float)((ref - kRange) * ((double)T * 0.69314718055994530942)); }
+__device__ __forceinline__ bool has_weight(float z, float cut, Steps s) { return z >= cut && (uint32_t)s.m < (uint32_t)(kRange * kSteps); }
 
 struct Slice {
     int first, last;
@@ -333,7 +344,7 @@ __device__ __forceinline__ void load_slice(const char* row, Slice S, float (&z)[
 }
 
 __device__ __forceinline__ bool regular(float T, float z_max) {
-    return T < 0x1p60f && T > 0x1p-60f && fabsf(z_max) < T * 0x1p40f;
+    return T < 0x1p60f && T > 0x1p-60f && fabsf(z_max) < T * 0x1p22f;
 }
 
 // Rows of a small top-k: tokens of the slice that can be among the row's k largest, as keys in the place of its bins, and a
@@ -434,16 +445,17 @@ __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs A, cha
     const double ref = ok ? ceil((double)top * c) : 0.0;
     if (tid == 0) R.slice[j] = SliceState{ref, top > -__builtin_inff() ? make_key(top, 0) : 0, 0, 0};
     if (!ok) return;                                             // (uniform) nothing here, or a row for the digits
-    const float cut = (float)((ref - kRange) * ((double)T * 0.69314718055994530942));
+    const float cut = cut_of(ref, T);
+    const int ref_steps = (int)ref * kSteps;
 #pragma unroll
     for (int g = 0; g < kGroups; ++g)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             if (z[g][e] >= cut) {                                // (not NaN)
-                const double x = fma((double)z[g][e], c, -ref);
-                double r;
-                const int steps = steps_of(x, r), b = bin_of(steps);
-                atomicAdd(&s_mass[b], weight_of(steps, r, s_table));
+                const Steps s = locate(z[g][e], c, ref_steps);
+                if ((uint32_t)s.m >= (uint32_t)(kRange * kSteps)) continue;
+                const int b = bin_of(s.m);
+                atomicAdd(&s_mass[b], weight_of(s, s_table));
                 if (counts) atomicAdd(&s_count[b], 1u);
             }
         }
@@ -509,7 +521,9 @@ __device__ __forceinline__ u64 shfl_up64(u64 x, int s) {
 }
 // s_sum[i] = sum of the weights of s_key[0, i]; `each` places in a row to a thread, each * THREADS >= n.
 template <int THREADS, int EACH>
-__device__ __forceinline__ void sum_weights(const u64* s_key, u64* s_sum, int n, double c, double ref, const double* table, u64* s_part) {
+__device__ __forceinline__ void sum_weights(const u64* s_key, u64* s_sum, int n, float T, double ref, const double* table, u64* s_part) {
+    const double c = log2e_over(T);
+    const float cut = cut_of(ref, T);
     const int tid = threadIdx.x, lane = tid & 63;
     u64 w[EACH], sum = 0;
 #pragma unroll
@@ -517,10 +531,9 @@ __device__ __forceinline__ void sum_weights(const u64* s_key, u64* s_sum, int n,
         const int at = tid * EACH + i;
         w[i] = 0;
         if (at < n) {
-            const double x = fmin(fma((double)key_value(s_key[at]), c, -ref), 0.0);
-            double r;
-            const int steps = steps_of(fmax(x, -60.0), r);
-            w[i] = x > -(double)kRange ? weight_of(steps, r, table) : 0;
+            const float z = key_value(s_key[at]);
+            const Steps s = locate(z, c, (int)ref * kSteps);
+            w[i] = has_weight(z, cut, s) ? weight_of(s, table) : 0;
         }
         sum += w[i];
     }
@@ -632,7 +645,7 @@ __device__ bool finish_largest(const SampleArgs& A, int m, int k, const RowSpace
     if (n > 2 * k) n = keep_front(s_key, n, k, bound, z_max, s_n);
     sort_keys<kRowThreads>(s_key, n);
     n = min(n, k);
-    sum_weights<kRowThreads, 1>(s_key, s_sum, n, c, ref, s_table, s_part);     // (n <= k <= kMostK)
+    sum_weights<kRowThreads, 1>(s_key, s_sum, n, A.temperature ? A.temperature[m] : 1.f, ref, s_table, s_part);     // (n <= k <= kMostK)
     if (tid >= 64) return true;
     int last = n - 1;
     const float p = A.top_p ? A.top_p[m] : 1.f;
@@ -673,16 +686,16 @@ __device__ __forceinline__ void pick_tokens(const SampleArgs& A, Slice S, const 
     const int shift = (int)(st.ref - ref) * kBins;
     // logits that can be in those bins, a little generously: bin b ends where x = -(b + 1) / kBins, to half a step
     const double far = (st.ref - (double)(b_max + 2) * (1.0 / kBins)) * ((double)T * 0.69314718055994530942);
-    const float least = b_max == kAll - 1 ? -__builtin_inff() : (float)(far - fabs(far) * 0x1p-20);
+    const float cut = cut_of(ref, T), least = b_max == kAll - 1 ? cut : fmaxf(cut, (float)(far - fabs(far) * 0x1p-20));
+    const int ref_steps = (int)ref * kSteps;
 #pragma unroll
     for (int g = 0; g < kGroups; ++g)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if (z[g][e] >= least) {
-                const double x = fma((double)z[g][e], c, -ref);
-                double r;
-                const int b = min(bin_of(steps_of(fmax(x, -60.0), r)) + shift, kAll - 1);
-                if (x > -(double)kRange && b >= b_min && b <= b_max &&
+                const Steps s = locate(z[g][e], c, ref_steps);
+                const int b = min(bin_of(s.m) + shift, kAll - 1);
+                if ((uint32_t)s.m < (uint32_t)(kRange * kSteps) && b >= b_min && b <= b_max &&
                     ((b >= st.lo[0] && b <= st.hi[0]) || (b >= st.lo[1] && b <= st.hi[1]) || (b >= st.lo[2] && b <= st.hi[2]))) {
                     const int i = S.at(g, e);
                     put(make_key(z[g][e], A.ids ? A.ids[i] : i));
@@ -696,13 +709,10 @@ __device__ void finish_row(const SampleArgs& A, int m, const RowState& st, u64* 
     const int tid = threadIdx.x, lane = tid & 63;
     const double c = log2e_over(A.temperature ? A.temperature[m] : 1.f);
     sort_keys<kThreads>(s_key, n);
-    sum_weights<kThreads, kList / kThreads>(s_key, s_sum, n, c, st.ref, s_table, s_part);
+    sum_weights<kThreads, kList / kThreads>(s_key, s_sum, n, A.temperature ? A.temperature[m] : 1.f, st.ref, s_table, s_part);
     if (tid >= 64) return;
     // One wavefront goes through the filters.  Every place is an index into the sorted list.
-    auto bin_at = [&](int i) {
-        double r;
-        return bin_of(steps_of(fmax(fmin(fma((double)key_value(s_key[i]), c, -st.ref), 0.0), -60.0), r));
-    };
+    auto bin_at = [&](int i) { return bin_of(locate(key_value(s_key[i]), c, (int)st.ref * kSteps).m); };
     // the first place of the list in bin b or behind
     auto place_of = [&](int b) { return search(0, n, lane, [&](int i) { return bin_at(i) >= b; }); };
     auto sum_to = [&](int i) { return i > 0 ? s_sum[i - 1] : 0ull; };
@@ -919,7 +929,7 @@ __global__ __launch_bounds__(kRowThreads, 8) void sample_row_kernel(SampleArgs A
     __shared__ uint32_t s_n;
     __shared__ int s_found[8];
     __shared__ SliceState s_slice[kMostSlices];
-    const int m = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+    const int m = blockIdx.x, tid = threadIdx.x;
     const RowSpace R = row_space(ws, m, slices);
     const float T = A.temperature ? A.temperature[m] : 1.f;
     for (int j = tid; j < slices; j += kRowThreads) s_slice[j] = R.slice[j];
