@@ -517,21 +517,27 @@ hipError_t launch_as(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
 
 }  // namespace
 
-constexpr int kSlots = 512;                      // workgroups that run at the same time
-
+// Two tiles of rows a wavefront halve what is loaded and converted for a row, and leave half as many workgroups: taken where these still
+// fill 256 compute units twice (2,048 rows of 8 x 4 heads on 10,240 tokens 324 us with one tile, 298 with two; 60 rows of 8
+// sequences, 256 workgroups of two tiles, 31 and 40).  From 160 elements on there are no registers for them.
+// The tokens are split over workgroups where there are fewer of these than compute units, and enough to split: 131,072 tokens of 8
+// heads over 16, 32 and 64 workgroups a head 62 + 4.5, 44 + 5.1 and 46 + 7.5 us (attention + joining the shares), 16 x 4,096 tokens
+// over 1, 2 and 4 30, 22 + 4 and 22 + 4; 4,096 tokens over 1, 4, 8 and 16 23, 11 + 3.6, 8.6 + 3.6 and 7.3 + 4.2, but 1,000 of 64
+// elements over 1 and 4 9.0 and 6.3 + 3.4, and another launch.
+// K and V are loaded past the caches where one workgroup reads them once (64 x 4,096 tokens 75 and 66.6 us, 16 x 4,096 24 and 22).
 AttnPlan attention_plan(int dim, int heads, int group, int S, int max_rows, int max_len) {
+    constexpr long long kUnits = 256, kLeast = 48, kShare = 4;   // compute units; blocks that are worth a split, and of a wavefront then
     AttnPlan p;
     const long long rows = (long long)max_rows * group;
-    p.row_tiles = dim <= 128 && rows > 32 && (rows + 63) / 64 * heads * S >= kSlots ? 2 : 1;
+    p.row_tiles = dim <= 128 && rows > 32 && (rows + 63) / 64 * heads * S >= 2 * kUnits ? 2 : 1;
     const int per = 32 * p.row_tiles;
     p.tiles = (int)((rows + per - 1) / per);
-    const long long groups = (long long)p.tiles * heads * S;
-    const long long blocks = ((long long)max_len + kBlock - 1) / kBlock;
-    long long splits = (kSlots + groups - 1) / groups;
-    const long long most = (blocks + 8 * kWaves - 1) / (8 * kWaves);      // eight blocks for every wavefront
+    const long long groups = (long long)p.tiles * heads * S, blocks = ((long long)max_len + kBlock - 1) / kBlock;
+    long long splits = (kUnits + groups - 1) / groups;
+    const long long most = blocks < kLeast ? 1 : blocks / (kShare * kWaves);
     splits = splits > most ? most : splits;
+    p.splits = (int)(splits > kMostSplits ? kMostSplits : splits);
     p.once = p.tiles == 1;
-    p.splits = (int)(splits < 1 ? 1 : splits > kMostSplits ? kMostSplits : splits);
     return p;
 }
 
