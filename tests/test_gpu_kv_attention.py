@@ -118,6 +118,44 @@ def test_chunks(ev, kind, type, dim, heads, group, page, lens, rows):
     case(ev, dim + sum(rows), kind, type, dim, heads, group, page, lens, rows)
 
 
+@pytest.mark.parametrize("kind,type,dim", [("e4m3", "bf16", 64), ("int8", "fp16", 64), ("e4m3", "fp16", 96), ("int8", "bf16", 128)])
+@pytest.mark.parametrize("tree", [False, True])
+def test_many_rows(ev, kind, type, dim, tree):
+    """Enough rows of enough heads that a wavefront takes two tiles of them; the last tile is ragged, some sequences are short."""
+    rows = [33 + (5 * i) % 32 for i in range(32)]
+    rows[3], rows[7], rows[31] = 64, 1, 40
+    lens = [r + (7 * i) % 50 for i, r in enumerate(rows)]
+    case(ev, dim, kind, type, dim, 16, 1, 32, lens, rows, tree=tree)
+
+
+def test_nan_with_many_rows(ev):
+    """As below, where a wavefront has two tiles: a NaN in V of one node of one sequence."""
+    import torch
+    rng = np.random.default_rng(42)
+    S, n, ctx, heads, dim = 32, 40, 30, 16, 64
+    width = 3
+    kv = torch.from_numpy(rng.standard_normal((2, S * (ctx + n), heads, dim))).to(torch.bfloat16).cuda()
+    q = torch.from_numpy(rng.standard_normal((S * n, heads, dim))).to(torch.bfloat16).cuda()
+    bits = sum([random_tree(rng, n) for _ in range(S)], [])
+    at, zero = i32(np.arange(S * width).reshape(S, width)), i32([0] * S)
+    off, whole = i32(np.arange(S + 1) * n), i32(np.arange(S + 1) * (ctx + n))
+    s, node, h = 5, 17, 9
+    got = []
+    for bad in (False, True):
+        x = kv.clone()
+        if bad:
+            x[1, s * (ctx + n) + ctx + node, h, 50] = float("nan")
+        c = ev.KVCache(S * width, 32, heads, dim)
+        ev.kv_write(c, x[0], x[1], at, zero, whole, ctx + n)
+        got.append(ev.kv_attention(q, c, at, i32([ctx + n] * S), off, n, tree=as_words(bits)))
+    nan = torch.isnan(got[1][0])
+    sees = [s * n + j for j in range(n) if bits[s * n + j] >> node & 1]
+    want = torch.zeros_like(nan)
+    want[sees, h, 50] = True
+    assert sees and torch.equal(nan, want)
+    assert torch.equal(got[0][0][~want], got[1][0][~want]) and torch.equal(got[0][1], got[1][1])
+
+
 @pytest.mark.parametrize("rows", [1, 9, 17, 33])
 def test_split_over_long_sequences(ev, rows):
     """Long and short sequences in one call: several workgroups share the tokens of a row, some of them find none."""
