@@ -97,36 +97,56 @@ __device__ __forceinline__ u64 reduce_all(u64 x, u64* s_part, F f) {
     return x;
 }
 
+__device__ __forceinline__ u64 shfl_up64(u64 x, int s) {
+    return (u64)(uint32_t)__shfl_up((int)(uint32_t)x, s) | (u64)(uint32_t)__shfl_up((int)(uint32_t)(x >> 32), s) << 32;
+}
+
 // The key of the row at which the cumulative measure of the keys from the largest down reaches `target` (>= 1; no more than
-// the measure of all keys >= low): f(key index) calls back with (key, measure) of every key.
-template <class EachKey>
-__device__ u64 find_key(u64 low, u64 target, u64* s_hist, u64* s_pick, EachKey each) {
+// the measure of all keys >= low), 11 bits of it at a time.  each(f) calls f(key, logit) for every key of the row; measure(logit)
+// is asked for those alone that agree with what is known.
+constexpr int kDigit = 11, kDigits2 = 1 << kDigit;
+template <class EachKey, class Measure>
+__device__ __forceinline__ u64 find_key(u64 low, u64 target, u64* s_hist, u64* s_part, u64* s_pick, EachKey each, Measure measure) {
+    const int tid = threadIdx.x, lane = tid & 63;
     u64 prefix = 0, mask = 0;
-    for (int shift = 56; shift >= 0; shift -= 8) {
-        for (int i = threadIdx.x; i < 256; i += kThreads) s_hist[i] = 0;
+    for (int top = 64; top > 0; top -= kDigit) {
+        const int shift = top > kDigit ? top - kDigit : 0, width = top - shift;
+        for (int i = tid; i < kDigits2; i += kThreads) s_hist[i] = 0;
         __syncthreads();
-        each([&](u64 key, u64 measure) {
-            if (key >= low && (key & mask) == prefix && measure) atomicAdd(&s_hist[(key >> shift) & 255], measure);
+        each([&](u64 key, float z) {
+            if (key >= low && (key & mask) == prefix) {
+                const u64 w = measure(z);
+                if (w) atomicAdd(&s_hist[(key >> shift) & ((1u << width) - 1)], w);
+            }
         });
         __syncthreads();
-        if (threadIdx.x == 0) {
-            u64 sum = 0;
-            int d = 255;
-            for (; d > 0; --d) {
-                if (sum + s_hist[d] >= target) break;
-                sum += s_hist[d];
-            }
-            s_pick[0] = (u64)d;
-            s_pick[1] = target - sum;
+        // two digits a thread, the largest first
+        const int d = kDigits2 - 1 - 2 * tid;
+        const u64 a = s_hist[d], b = s_hist[d - 1];
+        u64 run = a + b;
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) {
+            const u64 x = shfl_up64(run, s);
+            if (lane >= s) run += x;
+        }
+        if (lane == 63) s_part[tid >> 6] = run;
+        __syncthreads();
+        run -= a + b;
+        for (int w = 0; w < tid >> 6; ++w) run += s_part[w];
+        if (run < target && run + a + b >= target) {
+            const bool first = run + a >= target;
+            s_pick[0] = (u64)(first ? d : d - 1);
+            s_pick[1] = target - run - (first ? 0 : a);
         }
         __syncthreads();
         prefix |= s_pick[0] << shift;
         target = s_pick[1];
-        mask |= 255ull << shift;
+        mask |= (u64)((1u << width) - 1) << shift;
         __syncthreads();
     }
     return prefix;
 }
+static_assert(2 * kThreads == kDigits2, "two digits a thread");
 
 // A row by one workgroup, read again for every digit of a key: for rows whose tokens the bins below do not separate.
 template <int TYPE>
@@ -134,9 +154,19 @@ __device__ __forceinline__ void sample_by_digits(const SampleArgs& A, int m, u64
     const char* row = static_cast<const char*>(A.logits) + (long long)m * A.stride * (TYPE == EVOSPEC_FP32 ? 4 : 2);
     const float T = A.temperature ? A.temperature[m] : 1.f;
     auto each = [&](auto f) {
-        for (int i = threadIdx.x; i < A.V; i += kThreads) {
-            const float z = logit<TYPE>(row, i);
-            if (z > -__builtin_inff()) f(make_key(z, A.ids ? A.ids[i] : i), z);
+        // (eight loads at a time: one after the other a pass over 151,936 logits took 56 us)
+        for (int first = threadIdx.x; first < A.V; first += 8 * kThreads) {
+            float z[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) z[j] = first + j * kThreads < A.V ? logit<TYPE>(row, first + j * kThreads) : -__builtin_inff();
+#pragma unroll 1
+            for (int j = 0; j < 8; ++j) {
+                const float v = z[0];
+#pragma unroll
+                for (int e = 0; e < 7; ++e) z[e] = z[e + 1];     // (a loop, not eight copies of what is called)
+                const int i = first + j * kThreads;
+                if (v > -__builtin_inff()) f(make_key(v, A.ids ? A.ids[i] : i), v);
+            }
         }
     };
     u64 top = 0, n = 0;
@@ -158,20 +188,20 @@ __device__ __forceinline__ void sample_by_digits(const SampleArgs& A, int m, u64
         }
         return;
     }
-    const double c = log2e_over(T);
-    auto masses = [&](auto f) { each([&](u64 key, float z) { f(key, fixed(weight(z, z_max, c))); }); };
+    const double c = 1.4426950408889634074 / (double)T;          // (any temperature: rows that are not regular come here)
+    auto mass = [&](float z) { return fixed(weight(z, z_max, c)); };
     auto mass_from = [&](u64 low) {
         u64 sum = 0;
-        masses([&](u64 key, u64 w) { sum += key >= low ? w : 0; });
+        each([&](u64 key, float z) { if (key >= low) sum += mass(z); });
         return reduce_all(sum, s_part, [](u64 a, u64 b) { return a + b; });
     };
     u64 low = 0;
     const int k = A.top_k ? A.top_k[m] : 0;
-    if (k > 0 && (u64)k < n) low = find_key(low, (u64)k, s_hist, s_pick, [&](auto f) { each([&](u64 key, float) { f(key, 1); }); });
+    if (k > 0 && (u64)k < n) low = find_key(low, (u64)k, s_hist, s_part, s_pick, each, [](float) { return (u64)1; });
     const float p = A.top_p ? A.top_p[m] : 1.f;
     if (p < 1.f) {
         const u64 all = mass_from(low);
-        low = find_key(low, share_up(p, all), s_hist, s_pick, masses);
+        low = find_key(low, share_up(p, all), s_hist, s_part, s_pick, each, mass);
     }
     const float least = A.min_p ? A.min_p[m] : 0.f;
     if (least > 0.f) {
@@ -180,7 +210,7 @@ __device__ __forceinline__ void sample_by_digits(const SampleArgs& A, int m, u64
         low = reduce_all(first, s_part, [](u64 a, u64 b) { return a < b ? a : b; });
     }
     const u64 total = mass_from(low);
-    const u64 key = find_key(low, share_past(A.u[m], total), s_hist, s_pick, masses);
+    const u64 key = find_key(low, share_past(A.u[m], total), s_hist, s_part, s_pick, each, mass);
     if (threadIdx.x == 0) {
         A.out_ids[m] = key_id(key);
         if (A.out_logprob) {
@@ -515,9 +545,6 @@ __device__ __forceinline__ void sort_keys(u64* s_key, int n) {
         }
         __syncthreads();
     }
-}
-__device__ __forceinline__ u64 shfl_up64(u64 x, int s) {
-    return (u64)(uint32_t)__shfl_up((int)(uint32_t)x, s) | (u64)(uint32_t)__shfl_up((int)(uint32_t)(x >> 32), s) << 32;
 }
 // s_sum[i] = sum of the weights of s_key[0, i]; `each` places in a row to a thread, each * THREADS >= n.
 template <int THREADS, int EACH>

@@ -160,6 +160,8 @@ def test_extreme_temperatures(ev):
     run(ev, z, rng.random(6), temperature=[1e-30, 1e-6, 1e-3, 1e3, 1e6, 1e30])
     run(ev, z, rng.random(6), temperature=[1e-30, 1e-6, 1e-3, 1e3, 1e6, 1e30], top_p=[0.9] * 6, top_k=[100] * 6)
     run(ev, z * 1e30, rng.random(6), temperature=[1e29] * 6)
+    run(ev, z, rng.random(6), temperature=[np.inf] * 6, top_p=rng.random(6))
+    run(ev, z * 1e-40, rng.random(6), temperature=[1e-41, 1e-40, 1e-39, 1e-38, 1e-37, 1e-45])
 
 
 def test_strided_rows_of_an_active_vocabulary(ev):
