@@ -187,7 +187,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ >= 6 ? 1 : 2) void kv_attention_ker
     const int mask = (1 << A.c.shift) - 1;
     const int32_t* table = R.table + (long long)s * R.width;
     auto page_of = [&](int b) { return __builtin_amdgcn_readfirstlane(table[min(b, b_hi - 1) >> A.c.shift]); };
-    // Blocks without a page are read from page 0, and no row sees them.
+    // Blocks without a page are read from page 0, and no row sees them: their scales count as 1 and their V as zero, whatever is there.
     auto is_page = [&](int page) { return (unsigned)page < (unsigned)A.c.pages; };
     auto place = [&](int b, int page) { return (((long long)(is_page(page) ? page : 0) * A.c.heads + head) << A.c.shift) + (b & mask); };
     u32x4 kr[NQ], vr[NQ];
@@ -226,12 +226,12 @@ __global__ __launch_bounds__(64 * kWaves, NQ >= 6 ? 1 : 2) void kv_attention_ker
         const bool there = is_page(page);
         page = page_next;
         page_next = page_of(b + 2 * kWaves);
-        const float sc_y = sc.y;
-        const float ck = fmaxf(fabsf(sc.x) * (A.scale * kLog2e), 0x1p-126f);       // (not zero: -inf stays what it is)
-        const float sv = fabsf(sc.y), lv = __log2f(sv), iv = __builtin_amdgcn_rcpf(sv);
+        const float sc_x = there ? sc.x : 1.f, sc_y = there ? sc.y : 1.f;
+        const float ck = fmaxf(fabsf(sc_x) * (A.scale * kLog2e), 0x1p-126f);       // (not zero: -inf stays what it is)
+        const float sv = fabsf(sc_y), lv = __log2f(sv), iv = __builtin_amdgcn_rcpf(sv);
 
         uint32_t nan_tokens = 0;                                 // of K (e4m3's NaN code is one for the matrix cores)
-        if (KIND == EVOSPEC_KV_INT8 && __float_as_uint(sc.x) >> 31) {
+        if (KIND == EVOSPEC_KV_INT8 && __float_as_uint(sc_x) >> 31) {
             uint32_t any = 0;
 #pragma unroll
             for (int k = 0; k < NQ; ++k) any |= nan_bytes<KIND>(kr[k][0]) | nan_bytes<KIND>(kr[k][1]) | nan_bytes<KIND>(kr[k][2]) | nan_bytes<KIND>(kr[k][3]);
@@ -305,12 +305,13 @@ __global__ __launch_bounds__(64 * kWaves, NQ >= 6 ? 1 : 2) void kv_attention_ker
             pf[rt][1] = __builtin_bit_cast(u32x4, p[1]);
         }
         __builtin_amdgcn_sched_barrier(0);
-        if (t0 + kBlock > len) {                                 // bytes behind the last token may be anything
+        const int end = there ? len : t0;
+        if (t0 + kBlock > end) {                                 // bytes behind the last token may be anything
 #pragma unroll
             for (int k = 0; k < NQ; ++k)
 #pragma unroll
                 for (int a = 0; a < 4; ++a) {
-                    const int left = len - (t0 + 8 * a + 4 * half);
+                    const int left = end - (t0 + 8 * a + 4 * half);
                     vr[k][a] &= left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
                 }
         }

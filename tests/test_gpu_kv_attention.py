@@ -250,6 +250,27 @@ def test_pages_that_are_not_there(ev):
     check(out.double().cpu().numpy(), lse.double().cpu().numpy(), c, *want, 200.0, 96, "bf16")
 
 
+def test_pages_that_are_not_there_read_nothing_else(ev):
+    """Whatever page 0 holds, codes and scales of NaN among it: a page that is not there has no share in the result."""
+    import torch
+    rng = np.random.default_rng(43)
+    for kind in ("e4m3", "int8"):
+        c = ref.Cache(4, 32, 2, 64, kind, rng)
+        table = np.array([[2, -1, 3]])
+        q = torch.from_numpy(rng.standard_normal((3, 4, 64))).to(torch.bfloat16)
+        want = ref.attention(c, q.double().numpy(), table, [90], [0, 3], 2, None, 0.125)
+        for scale in (np.nan, -np.nan, np.inf, 0.0, -1.0):
+            c.data[0] = 0x7F if kind == "e4m3" else 0x80
+            c.scales[0] = scale
+            out, lse = ev.kv_attention(q.cuda(), to_gpu(ev, c), i32(table), i32([90]), i32([0, 3]), 3)
+            check(out.double().cpu().numpy(), lse.double().cpu().numpy(), c, *want, 200.0, 96, "bf16")
+
+
+def test_trees_larger_than_their_sequence(ev):
+    """Rows whose tokens lie before the first one: their nodes are not in the cache."""
+    case(ev, 44, "e4m3", "bf16", 64, 1, 2, 32, [10, 3, 40], [12, 9, 20], tree=True)
+
+
 def test_rows_past_max_rows_stay(ev):
     import torch
     rng = np.random.default_rng(39)
