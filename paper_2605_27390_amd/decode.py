@@ -167,8 +167,8 @@ def kv_attention(q, cache: KVCache, page_table, lens, row_off, max_rows: int, ma
     come before the sequence's rows, and those of its bits.  `scale` is 1 / sqrt(dim) if not given; max_len (a bound of lens)
     only decides how the work is split."""
     width, S = _rows(page_table, lens, "lens", row_off)
-    if q.dim() != 3:
-        raise ValueError("q must be [rows, query heads, dim]")
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q must be a tensor [rows, query heads, dim]")
     T, heads, dim = q.shape
     group = heads // cache.heads
     if group * cache.heads != heads:
@@ -194,7 +194,9 @@ def kv_attention(q, cache: KVCache, page_table, lens, row_off, max_rows: int, ma
         _expect(out_lse, torch.float32, "out_lse", 2)
         if tuple(out_lse.shape) != (T, heads):
             raise ValueError("out_lse must be [rows, query heads]")
-    if workspace is None:
+    if workspace is not None:
+        _expect(workspace, torch.uint8, "workspace")
+    else:
         need = _attention_bytes(cache.pages, cache.page, cache.heads, cache.dim, cache._c.kind, group, S, T, max_rows, max_len)
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
     _check(lib.evospec_kv_attention(cache._ref, q.data_ptr(), qs, type_, T, group, page_table.data_ptr(), width,
@@ -239,7 +241,9 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, ids=
                 raise ValueError(f"{name} needs a place for every row")
     out_ids = torch.empty(M, dtype=_i32, device=logits.device) if out_ids is None else out_ids
     out_logprob = torch.empty(M, dtype=_f32, device=logits.device) if out_logprob is None else out_logprob
-    if workspace is None:
+    if workspace is not None:
+        _expect(workspace, torch.uint8, "workspace")
+    else:
         need = _sample_bytes(M, V)
         workspace = torch.empty(need, dtype=torch.uint8, device=logits.device) if need else None
     _check(lib.evospec_sample(logits.data_ptr(), logits.stride(0) if M > 1 else V, _TYPES[logits.dtype], M, V, u.data_ptr(),

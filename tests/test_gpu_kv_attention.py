@@ -336,3 +336,15 @@ def test_wrapper_refusals(ev):
     with pytest.raises(ev.EvospecError) as e:
         ev.kv_attention(q, c, t, n, o, 3, scale=-1.0)
     assert e.value.status == 2
+
+
+def test_workspace_refusals(ev):
+    """Scratch that is not bytes on the GPU."""
+    import torch
+    c = ev.KVCache(4, 32, 2, 64)
+    t, n, o = i32([[0, 1]]), i32([5]), i32([0, 3])
+    q = torch.zeros(3, 4, 64, dtype=torch.bfloat16, device="cuda")
+    need = max(ev.kv_attention_workspace_bytes(c, 2, 1, 3, 3, 64), 1024)
+    for bad in (torch.zeros(need, dtype=torch.uint8), torch.zeros(need, device="cuda"), torch.zeros(2 * need, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises((TypeError, ValueError)):
+            ev.kv_attention(q, c, t, n, o, 3, workspace=bad)

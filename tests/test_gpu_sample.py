@@ -220,3 +220,13 @@ def test_wrapper_refusals(ev):
         kw = {k: v for k, v in bad.items() if k not in ("u", "z")}
         with pytest.raises((TypeError, ValueError)):
             ev.sample(bad.get("z", z), bad.get("u", u), **kw)
+
+
+def test_workspace_refusals(ev):
+    """Scratch that is not bytes on the GPU."""
+    import torch
+    z, u = torch.zeros(2, 10, device="cuda"), torch.zeros(2, device="cuda")
+    need = ev.sample_workspace_bytes(2, 10)
+    for bad in (torch.zeros(need, dtype=torch.uint8), torch.zeros(need, device="cuda"), torch.zeros(2 * need, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises((TypeError, ValueError)):
+            ev.sample(z, u, workspace=bad)
