@@ -100,7 +100,7 @@ int evospec_kv_attention(const evospec_kv_cache *cache, const void *q, long long
  *      kept one if none does).
  * out_logprob = log of the drawn token's share in the kept ones.  temperature that is not > 0 draws the first token.
  * Tokens with w below 2^-42 may be left out of 4.  A row without a number above -inf gives id -1, logprob NaN.
- *   logits dev `type` [M, V], rows `stride` elements apart; V <= 2^20
+ *   logits dev `type` [M, V], rows `stride` elements apart; V <= 2^20, M * ceil(V / 20480) < 2^22
  *   u, temperature, top_p, min_p dev fp32 [M]; top_k dev int32 [M]; each of the last four may be NULL (1, all, all, all)
  *   ids dev int32 [V] or NULL: the id of column i (distinct, not negative); NULL: i
  *   out_ids dev int32 [M]      out_logprob dev fp32 [M] or NULL

@@ -40,10 +40,12 @@ int check_stride(long long stride, long long least, int type) {
 int check_rows(int width, int S, int max_rows, int T) {
     return width < 1 || S < 0 || max_rows < 0 || T < 0 || max_rows > (1 << 28) || width > (1 << 24) ? EVOSPEC_BAD_SHAPE : EVOSPEC_OK;
 }
-bool grid_fits(long long a, long long b, long long c, long long d = 1) {
-    const long long most = 2147483647ll;
-    return a * b <= most && a * b * c <= most && a * b * c * d <= most;
+bool grid_fits(long long a, long long b, long long c) {
+    const long long most = (1ll << 24) - 1024;                   // workgroups: a launch takes fewer than 2^32 threads, of 256 here
+    return a * b <= most && a * b * c <= most;
 }
+
+bool sample_fits(int M, int V) { return M >= 0 && V >= 1 && V <= (1 << 20) && (long long)M * sample_slices(V) < (1 << 22); }
 
 }  // namespace
 
@@ -97,9 +99,12 @@ static int check_attention(const evospec_kv_cache* cache, int group, int S, int 
     if (rc) return rc;
     if (group < 1 || group > 1024 || max_len < 0 || max_len > (1 << 30)) return EVOSPEC_BAD_SHAPE;
     if ((rc = check_rows(1, S, max_rows, T))) return rc;
-    // rows of a head, workgroups and rows of the merge
-    if ((long long)max_rows * group > (1 << 30) || !grid_fits(T, cache->heads, group)) return EVOSPEC_BAD_SHAPE;
-    return grid_fits(((long long)max_rows * group + 31) / 32, cache->heads, S, 128) ? EVOSPEC_OK : EVOSPEC_BAD_SHAPE;
+    if ((long long)max_rows * group > (1 << 30) || (long long)T * cache->heads > (1 << 30) / group) return EVOSPEC_BAD_SHAPE;
+    // (splits come to no more than 256 workgroups beyond the tiles)
+    if (!grid_fits(((long long)max_rows * group + 31) / 32, cache->heads, S)) return EVOSPEC_BAD_SHAPE;
+    if (S == 0 || T == 0 || max_rows == 0) return EVOSPEC_OK;    // (nothing to plan)
+    const AttnPlan p = attention_plan(cache->dim, cache->heads, group, S, max_rows, max_len);
+    return p.splits == 1 || grid_fits(T, cache->heads, group) ? EVOSPEC_OK : EVOSPEC_BAD_SHAPE;      // rows of the merge
 }
 
 int evospec_kv_attention_workspace_bytes(const evospec_kv_cache* cache, int group, int S, int T, int max_rows, int max_len,
@@ -142,7 +147,7 @@ int evospec_kv_attention(const evospec_kv_cache* cache, const void* q, long long
 
 int evospec_sample_workspace_bytes(int M, int V, size_t* out_bytes) {
     if (!out_bytes) return EVOSPEC_NULL_POINTER;
-    if (M < 0 || M > (1 << 24) || V < 1 || V > (1 << 20)) return EVOSPEC_BAD_SHAPE;
+    if (!sample_fits(M, V)) return EVOSPEC_BAD_SHAPE;
     *out_bytes = sample_workspace(M, V);
     return EVOSPEC_OK;
 }
@@ -151,7 +156,7 @@ int evospec_sample(const void* logits, long long stride, int type, int M, int V,
                    const int32_t* top_k, const float* top_p, const float* min_p, const int32_t* ids, int32_t* out_ids,
                    float* out_logprob, void* workspace, size_t workspace_bytes, void* stream) {
     if (type < EVOSPEC_BF16 || type > EVOSPEC_FP32) return EVOSPEC_BAD_TYPE;
-    if (M < 0 || M > (1 << 24) || V < 1 || V > (1 << 20) || stride < V) return EVOSPEC_BAD_SHAPE;
+    if (!sample_fits(M, V) || stride < V) return EVOSPEC_BAD_SHAPE;
     if (M == 0) return EVOSPEC_OK;
     if (!logits || !u || !out_ids) return EVOSPEC_NULL_POINTER;
     if (!aligned(logits, type_bytes(type)) || !aligned(workspace, 16)) return EVOSPEC_MISALIGNED;

@@ -72,6 +72,7 @@ struct SampleArgs {
     int32_t* out_ids;
     float* out_logprob;
 };
+int sample_slices(int V);                     // workgroups of 1,024 threads of a row
 size_t sample_workspace(int M, int V);
 hipError_t launch_sample(const SampleArgs& a, int type, void* workspace, hipStream_t stream);
 

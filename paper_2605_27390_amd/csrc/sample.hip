@@ -1077,13 +1077,13 @@ __global__ __launch_bounds__(kThreads, 8) void sample_finish_kernel(SampleArgs A
 
 constexpr int kManyRows = 512;
 
-static int slices_of(int V) { return (V + kSlice - 1) / kSlice; }
+int sample_slices(int V) { return (V + kSlice - 1) / kSlice; }
 
-size_t sample_workspace(int M, int V) { return (size_t)M * row_bytes(slices_of(V)); }
+size_t sample_workspace(int M, int V) { return (size_t)M * row_bytes(sample_slices(V)); }
 
 template <int TYPE>
 static hipError_t sample_as(const SampleArgs& a, char* ws, hipStream_t stream) {
-    const int slices = slices_of(a.V);
+    const int slices = sample_slices(a.V);
     sample_bins_kernel<TYPE><<<dim3((unsigned)(a.M * slices)), kThreads, 0, stream>>>(a, ws, slices);
     // Who ends the rows: a workgroup for each, with less to launch and to pass on, where top-k leaves little, rows are one slice, or there
     // are enough of them; otherwise its slices side by side (one row of 151,936 41.5 us against 56.7, 256 rows 147 and 153, 512 rows 242

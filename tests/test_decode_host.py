@@ -125,6 +125,20 @@ def test_sample_refusals(ev):
     assert w(3, 100, None) == 1 and w(-1, 100, ctypes.byref(n)) == 2 and w(3, 0, ctypes.byref(n)) == 2
 
 
+def test_more_threads_than_a_launch_takes(ev):
+    """2^32 threads of a launch and more are refused here."""
+    c = cache(ev, heads=4)
+    assert write(ev, c=c, S=1 << 22, most=1, ks=512, vs=512) == 2 and read(ev, c=c, S=1 << 22, most=1) == 2
+    assert attend(ev, c=c, S=1 << 22, most=1, qs=2048) == 2 and attend(ev, T=1 << 21, most=1, max_len=1 << 20, S=1) == 2
+    n = ctypes.c_size_t(0)
+    w = ev.lib.evospec_sample_workspace_bytes
+    assert draw(ev, M=1 << 22) == 2 and w(1 << 22, 100, ctypes.byref(n)) == 2 and w((1 << 22) - 1, 100, ctypes.byref(n)) == 0
+    assert w(1 << 21, 20481, ctypes.byref(n)) == 2 and w(1 << 21, 20480, ctypes.byref(n)) == 0
+    # what is just below is not (the null pointer is what it stops at)
+    assert write(ev, c=c, S=(1 << 22) - 256, most=1, ks=512, vs=512, k=None) == 1
+    assert attend(ev, c=c, S=(1 << 22) - 256, most=1, qs=2048, q=None) == 1
+
+
 def test_wrapper_refusals_need_no_gpu(ev):
     import torch
     with pytest.raises(ValueError):
