@@ -124,7 +124,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ >= 6 ? 1 : 2) void kv_attention_ker
     const int n_all = n1 - n0, n = min(n_all, R.max_rows);
     const int rows = n * A.group, r0 = tile * kRows;
     if (r0 >= rows) return;
-    const int len = (int)min((long long)max(R.at[s], 0), (long long)R.width << (A.c.shift + 5));
+    const int len = (int)min((long long)min(max(R.at[s], 0), 1 << 30), (long long)R.width << (A.c.shift + 5));
     const int base = len - n_all;                                // the position of row 0 (may be negative)
     // tokens [0, full) are seen by every row of the workgroup, tokens [hi, len) by none
     const int i_first = r0 / A.group, i_last = (min(rows, r0 + kRows) - 1) / A.group;

@@ -69,9 +69,9 @@ __device__ __forceinline__ u64 share_up(float f, u64 x) {
     const u64 s = f > 0.f ? share(f, x, true) : 0;
     return s < 1 ? 1 : s;
 }
-// the least whole number > f x, at most x
+// the least whole number > f x, at most x (which NaN does not pass either)
 __device__ __forceinline__ u64 share_past(float f, u64 x) {
-    if (f >= 1.f) return x;
+    if (!(f < 1.f)) return x;
     return f > 0.f ? share(f, x, false) + 1 : 1;
 }
 

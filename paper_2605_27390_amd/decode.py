@@ -181,7 +181,7 @@ def kv_attention(q, cache: KVCache, page_table, lens, row_off, max_rows: int, ma
         _expect(tree, torch.int64, "tree", 1)
         if tree.shape[0] != T:
             raise ValueError("tree needs a word for every row of q")
-    max_len = width * cache.page if max_len is None else int(max_len)
+    max_len = min(width * cache.page, 1 << 30) if max_len is None else int(max_len)
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
     else:

@@ -348,3 +348,31 @@ def test_workspace_refusals(ev):
     for bad in (torch.zeros(need, dtype=torch.uint8), torch.zeros(need, device="cuda"), torch.zeros(2 * need, dtype=torch.uint8, device="cuda")[::2]):
         with pytest.raises((TypeError, ValueError)):
             ev.kv_attention(q, c, t, n, o, 3, workspace=bad)
+
+
+def test_pages_past_32_bits(ev):
+    """Pages behind the first 4 GiB of a cache: the same bits as from a cache of these pages alone."""
+    import torch
+    rng = np.random.default_rng(45)
+    heads, dim, page, pages, T = 8, 256, 256, 4500, 600          # 1 MiB a page
+    far, near = ev.KVCache(pages, page, heads, dim), ev.KVCache(3, page, heads, dim)
+    k, v = (torch.from_numpy(rng.standard_normal((T, heads, dim))).to(torch.bfloat16).cuda() for _ in range(2))
+    q = torch.from_numpy(rng.standard_normal((5, heads, dim))).to(torch.bfloat16).cuda()
+    got = []
+    for c, table in ((far, [[pages - 1, 4200, 4400]]), (near, [[2, 0, 1]])):
+        ev.kv_write(c, k, v, i32(table), i32([0]), i32([0, T]), T)
+        got.append(ev.kv_attention(q, c, i32(table), i32([T]), i32([0, 5]), 5))
+    assert all(torch.equal(a, b) for a, b in zip(*got)) and torch.isfinite(got[0][0]).all()
+
+
+def test_lengths_past_the_page_table(ev):
+    """Lengths beyond what the page table has are cut to it."""
+    import torch
+    rng = np.random.default_rng(46)
+    c = ref.Cache(4, 32, 2, 64, "int8", rng)
+    g, table = to_gpu(ev, c), i32([[2, 0, 3]])
+    q = torch.from_numpy(rng.standard_normal((3, 4, 64))).to(torch.bfloat16).cuda()
+    want = ev.kv_attention(q, g, table, i32([96]), i32([0, 3]), 3)
+    for n in (97, 5000, 2 ** 31 - 1):
+        got = ev.kv_attention(q, g, table, i32([n]), i32([0, 3]), 3)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])

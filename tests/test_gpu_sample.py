@@ -230,3 +230,21 @@ def test_workspace_refusals(ev):
     for bad in (torch.zeros(need, dtype=torch.uint8), torch.zeros(need, device="cuda"), torch.zeros(2 * need, dtype=torch.uint8, device="cuda")[::2]):
         with pytest.raises((TypeError, ValueError)):
             ev.sample(z, u, workspace=bad)
+
+
+def test_random_numbers_outside_their_range(ev):
+    """u of 1 and above, or NaN, exceeds every sum: the last token kept.  Below 0: the first."""
+    import torch
+    rng = np.random.default_rng(77)
+    for V in (300, 30000):
+        z = torch.from_numpy(rng.standard_normal((5, V)).astype(np.float32)).cuda()
+        u = torch.tensor([1.0, 2.0, float("inf"), float("nan"), -1.0], device="cuda")
+        k = torch.full((5,), 7, dtype=torch.int32, device="cuda")
+        p = torch.full((5,), 0.5, device="cuda")
+        order = z.double().sort(dim=1, descending=True)
+        w = (order.values - order.values[:, :1]).exp().cumsum(1)
+        last = (w < 0.5 * w[:, -1:]).sum(1)                    # the place where the sum reaches the half
+        for kw, place in ((dict(top_k=k), torch.full((5,), 6)), (dict(top_p=p), last.cpu())):
+            ids, _ = ev.sample(z, u, **kw)
+            want = [int(order.indices[r, place[r] if r < 4 else 0]) for r in range(5)]
+            assert ids.tolist() == want
