@@ -8,6 +8,7 @@
 // atomics, and 2^20 of them fit 64 bits.  Measured on rows of 151,936: one in 17 us, 60 with top-k in 26, 960 of bf16 with top-p in 385.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "common.hpp"
@@ -84,6 +85,14 @@ __device__ __forceinline__ float logit(const void* row, int i) {
 
 __device__ __forceinline__ u64 shfl_xor64(u64 x, int s) {
     return (u64)(uint32_t)__shfl_xor((int)(uint32_t)x, s) | (u64)(uint32_t)__shfl_xor((int)(uint32_t)(x >> 32), s) << 32;
+}
+__device__ __forceinline__ u64 sum_lanes(u64 x) {
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) x += shfl_xor64(x, s);
+    return x;
+}
+__device__ __forceinline__ u64 first_lane(u64 x) {
+    return (u64)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x) | (u64)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(x >> 32)) << 32;
 }
 template <class F>
 __device__ __forceinline__ u64 reduce_all(u64 x, u64* s_part, F f) {
@@ -227,7 +236,7 @@ __device__ __forceinline__ void sample_by_digits(const SampleArgs& A, int m, u64
 // 1. sample_bins_kernel, a workgroup for each slice of a row (kSlice logits at most, which stay in registers): the slice's
 //    largest logit, and the weights of its tokens, summed in bins of 1 / kBins of a power of two below e = the next power of two
 //    above that logit.  References are whole powers of two, so that slices' bins lie on one grid and their sums are joined by shifts.
-// 2. sample_row_kernel, a workgroup for each row: the bins of all slices, joined; in which bins top-k, top-p and min-p cut, and in which
+// 2. sample_row_kernel, a workgroup for each row: the bins of all slices, joined (eight slices' loads at a time); in which bins top-k, top-p and min-p cut, and in which
 //    the draw falls (a range of them where one depends on a cut inside a bin).  Greedy rows end here.
 // 3. sample_pick_kernel, a workgroup for each slice again: tokens of those bins are put on the row's list.
 // 4. sample_finish_kernel, a workgroup for each row: sorts the list, and goes through the filters with the list's tokens and the bins'
@@ -796,21 +805,47 @@ __device__ __forceinline__ RowState plan_row(const SampleArgs& A, int m, const R
                                              uint32_t* s_num, int* s_found) {
     const int tid = threadIdx.x, lane = tid & 63;
     // the slices' bins, joined: bin b of a slice whose reference is `shift` factors of 2 lower goes to b + shift kBins, or the last
-    for (int b = tid; b <= kAll; b += kRowThreads) {
-        s_before[b] = 0;
-        s_first[b] = 0;
+    static_assert(kAll <= kRowThreads, "a bin a thread");
+    __shared__ int s_shift[kMostSlices];
+    if (tid < slices) {
+        const SliceState s = s_slice[tid];
+        const double gap = s.top != 0 && regular(T, key_value(s.top)) ? ref - s.ref : kRange;      // (a whole number >= 0)
+        s_shift[tid] = gap < kRange ? (int)gap : -1;
+    }
+    if (tid <= kAll) {
+        s_before[tid] = 0;
+        s_first[tid] = 0;
     }
     __syncthreads();
-    for (int j = 0; j < slices; ++j) {
-        if (s_slice[j].top == 0 || !regular(T, key_value(s_slice[j].top))) continue;
-        const double gap = ref - s_slice[j].ref;                       // (a whole number >= 0)
-        if (gap >= kRange) continue;
-        const int shift = (int)gap;
-        for (int b = tid; b < kAll; b += kRowThreads) {
-            const u64 w = R.mass[(size_t)j * kAll + b];
-            const int to = min(b + shift * kBins, kAll - 1);
-            if (w) atomicAdd(&s_before[to], shift ? (w + (1ull << (shift - 1))) >> shift : w);
-            if (k > 0) atomicAdd(&s_first[to], R.count[(size_t)j * kAll + b]);
+    u64 past = 0;                                                // of bins behind the last
+    uint32_t num_past = 0;
+    constexpr int kAtOnce = 8;
+    for (int first = 0; first < slices; first += kAtOnce) {
+        u64 w[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) w[i] = R.mass[(size_t)min(first + i, slices - 1) * kAll + min(tid, kAll - 1)];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const int j = first + i, shift = __builtin_amdgcn_readfirstlane(j < slices ? s_shift[j] : -1), to = tid + shift * kBins;
+            if (shift < 0) continue;                             // (uniform)
+            const u64 x = shift ? (w[i] + (1ull << (shift - 1))) >> shift : w[i];
+            const uint32_t n = k > 0 && tid < kAll ? R.count[(size_t)j * kAll + tid] : 0;
+            if (to < kAll) {
+                atomicAdd(&s_before[to], x);
+                if (k > 0) atomicAdd(&s_first[to], n);
+            } else if (tid < kAll) {
+                past += x;
+                num_past += n;
+            }
+        }
+    }
+    // (lanes that add to one place of LDS go one by one: 2 us a slice)
+    if (__ballot(past != 0)) {
+        past = sum_lanes(past);
+        if (lane == 0) atomicAdd(&s_before[kAll - 1], past);
+        if (k > 0) {
+            num_past = (uint32_t)sum_lanes(num_past);
+            if (lane == 0) atomicAdd(&s_first[kAll - 1], num_past);
         }
     }
     __syncthreads();
@@ -959,12 +994,19 @@ __global__ __launch_bounds__(kRowThreads, 8) void sample_row_kernel(SampleArgs A
     const int m = blockIdx.x, tid = threadIdx.x;
     const RowSpace R = row_space(ws, m, slices);
     const float T = A.temperature ? A.temperature[m] : 1.f;
-    for (int j = tid; j < slices; j += kRowThreads) s_slice[j] = R.slice[j];
+    static_assert(kMostSlices <= 64, "a slice a lane");
+    const SliceState of_lane = R.slice[min(tid & 63, slices - 1)];
+    if (tid < slices) s_slice[tid] = of_lane;
+    u64 top = of_lane.top;
+    for (int s = 32; s >= 1; s >>= 1) {
+        if (s >= slices) continue;                               // (uniform; lanes from there on repeat the last slice)
+        const u64 x = shfl_xor64(top, s);
+        top = x > top ? x : top;
+    }
+    if (slices > 1) top = first_lane(top);
     __syncthreads();
-    u64 top = 0;
-    for (int j = 0; j < slices; ++j) top = s_slice[j].top > top ? s_slice[j].top : top;
     const float z_max = key_value(top);
-    const int k = A.top_k ? A.top_k[m] : 0;
+    const int k = REST && A.top_k ? A.top_k[m] : 0;              // (with a top-k rows are ended here)
     if (top == 0 || !(T > 0.f)) {
         if (tid == 0) {
             A.out_ids[m] = top == 0 ? -1 : key_id(top);
@@ -991,12 +1033,12 @@ __global__ __launch_bounds__(kRowThreads, 8) void sample_row_kernel(SampleArgs A
             if (tid == 0) s_n = 0;
             __syncthreads();
             const char* row = row_of<TYPE>(A, m);
-            for (int j = 0; j < slices; ++j) {
-                if (!has_any(s_slice[j], st, T)) continue;       // (uniform)
-                const Slice S = slice_of(A.V, slices, j);
+            const int parts = (A.V + kSlice - 1) / kSlice;       // (few and large, whatever the slices of the bins were)
+            for (int j = 0; j < parts; ++j) {
+                const Slice S = slice_of(A.V, parts, j);
                 float z[kGroups][4];
                 load_slice<TYPE>(row, S, z);
-                pick_tokens(A, S, z, st, s_slice[j].ref, T, [&](u64 key) {
+                pick_tokens(A, S, z, st, st.ref, T, [&](u64 key) {
                     const uint32_t at = atomicAdd(&s_n, 1u);
                     if (at < kList) s_key[at] = key;
                 });
@@ -1077,18 +1119,34 @@ __global__ __launch_bounds__(kThreads, 8) void sample_finish_kernel(SampleArgs A
 
 constexpr int kManyRows = 512;
 
-int sample_slices(int V) { return (V + kSlice - 1) / kSlice; }
+// Slices of a row: as few as there can be, or, where no row asks for a top-k, as many as give each compute unit one, of kLeastSlice
+// logits at least (lists of a top-k get longer with more slices).  8 rows of 151,936 with a top-p 55 and 46 us, 60 rows of 20,000 41 and
+// 35, one row of 151,936 34 and 33.
+constexpr int kLeastSlice = 4096, kUnits = 256;
+static int whole_slices(int V) { return (V + kSlice - 1) / kSlice; }
+static int many_slices(int M, int V) {
+    const int most = std::min(std::max(V / kLeastSlice, 1), kMostSlices);
+    return std::max(whole_slices(V), std::min((kUnits + M - 1) / M, most));
+}
+int sample_slices(int V) { return whole_slices(V); }
 
-size_t sample_workspace(int M, int V) { return (size_t)M * row_bytes(sample_slices(V)); }
+// What any M' <= M rows take: M' many_slices(M') is M' whole_slices at most, or less than kUnits + M'.
+size_t sample_workspace(int M, int V) {
+    if (M == 0) return 0;
+    const size_t n = whole_slices(V), most = (size_t)M * std::max((size_t)many_slices(1, V), n);
+    const size_t slices = std::max((size_t)M * n, std::min((size_t)kUnits + M, most));
+    return slices * (row_bytes(2) - row_bytes(1) + 256) + (size_t)M * row_bytes(1);
+}
 
 template <int TYPE>
 static hipError_t sample_as(const SampleArgs& a, char* ws, hipStream_t stream) {
-    const int slices = sample_slices(a.V);
+    // Who ends the rows: a workgroup for each, with less to launch and to pass on, where top-k leaves little, rows would fit one
+    // slice, or there are enough of them; otherwise its slices side by side.  By itself against side by side: one row of 151,936 57 and
+    // 41 us, 256 rows 153 and 147, 512 rows 232 and 242; 30 rows of 60,000 50 and 40, of 40,000 41 and 36.5; 60 rows of 20,000 41 and 46.
+    const bool rest = a.top_k || whole_slices(a.V) == 1 || a.M >= kManyRows;
+    const int slices = a.top_k ? whole_slices(a.V) : many_slices(a.M, a.V);
     sample_bins_kernel<TYPE><<<dim3((unsigned)(a.M * slices)), kThreads, 0, stream>>>(a, ws, slices);
-    // Who ends the rows: a workgroup for each, with less to launch and to pass on, where top-k leaves little, rows are one slice, or there
-    // are enough of them; otherwise its slices side by side (one row of 151,936 41.5 us against 56.7, 256 rows 147 and 153, 512 rows 242
-    // and 232; 60 rows of 20,000 46 and 41).
-    if (a.top_k || slices == 1 || a.M >= kManyRows) {
+    if (rest) {
         sample_row_kernel<TYPE, true><<<dim3((unsigned)a.M), kRowThreads, 0, stream>>>(a, ws, slices);
     } else {
         sample_row_kernel<TYPE, false><<<dim3((unsigned)a.M), kRowThreads, 0, stream>>>(a, ws, slices);

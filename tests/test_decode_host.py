@@ -139,6 +139,13 @@ def test_more_threads_than_a_launch_takes(ev):
     assert attend(ev, c=c, S=(1 << 22) - 256, most=1, qs=2048, q=None) == 1
 
 
+def test_sample_workspace_of_fewer_rows(ev):
+    """Scratch for M rows is enough for fewer."""
+    for V in (1, 4096, 20480, 20481, 50000, 151936, 1 << 20):
+        sizes = [ev.sample_workspace_bytes(M, V) for M in list(range(0, 300)) + [511, 512, 513, 960]]
+        assert sizes == sorted(sizes) and sizes[0] == 0
+
+
 def test_wrapper_refusals_need_no_gpu(ev):
     import torch
     with pytest.raises(ValueError):

@@ -248,3 +248,25 @@ def test_random_numbers_outside_their_range(ev):
             ids, _ = ev.sample(z, u, **kw)
             want = [int(order.indices[r, place[r] if r < 4 else 0]) for r in range(5)]
             assert ids.tolist() == want
+
+
+def test_few_rows_of_many_slices(ev):
+    """From one row on, whose slices are the more the fewer rows there are; all in one buffer, that of the most rows."""
+    import torch
+    rng = np.random.default_rng(78)
+    V = 60001
+    ws = torch.empty(ev.sample_workspace_bytes(90, V), dtype=torch.uint8, device="cuda")
+    z = torch.from_numpy((rng.standard_normal((90, V)) * 2).astype(np.float32)).cuda()
+    z[3, 30000:] -= 40.0                                       # slices far below the others
+    z[5, 1000:] = -float("inf")                                # slices of nothing
+    z[7] -= torch.arange(V, device="cuda") * 1e-3
+    u = torch.from_numpy(rng.random(90).astype(np.float32)).cuda()
+    p = torch.full((90,), 0.9, device="cuda")
+    least = torch.full((90,), 0.01, device="cuda")
+    for kw in (dict(), dict(top_p=p), dict(min_p=least)):
+        ids, lp = ev.sample(z, u, workspace=ws, **kw)
+        for M in (1, 2, 3, 7, 8, 17, 64):
+            part = {k: v[:M] for k, v in kw.items()}
+            got, lq = ev.sample(z[:M], u[:M], workspace=ws, **part)
+            assert torch.equal(got, ids[:M]), M
+            assert (lq - lp[:M]).abs().max() <= 1e-6
