@@ -5,7 +5,7 @@
 // cumulative weight of the kept ones passes u times their sum.  Such keys are found digit by digit from a histogram of the
 // keys that agree so far, of numbers (top-k) or of weights (top-p, the draw).  Weights w = exp((z - z_max) / T) are computed
 // in 64 bits and kept as whole multiples of 2^-43: their sums do not depend on an order, so that a histogram may be filled by
-// atomics, and 2^20 of them fit 64 bits.  Measured on rows of 151,936: one in 17 us, 60 with top-k in 26, 960 of bf16 with top-p in 385.
+// atomics, and 2^20 of them fit 64 bits.  Measured on rows of 151,936: one in 17 us, 60 with top-k in 26, 960 of bf16 with top-p in 302.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -355,31 +355,61 @@ __device__ __forceinline__ Slice slice_of(int V, int slices, int j) {
     const int per = ((V + slices - 1) / slices + 3) / 4 * 4;     // (<= kSlice)
     return Slice{min(V, j * per), min(V, (j + 1) * per)};
 }
+// A thread's logits as they come: 16-bit types two to a word.
 template <int TYPE>
-__device__ __forceinline__ void load_slice(const char* row, Slice S, float (&z)[kGroups][4]) {
-    constexpr int kBytes = TYPE == EVOSPEC_FP32 ? 4 : 2;
-    const bool whole = (reinterpret_cast<uintptr_t>(row) & (4 * kBytes - 1)) == 0 && !S.small();
+struct RawSlice {
+    static constexpr int kWords = TYPE == EVOSPEC_FP32 ? 4 : 2;
+    uint32_t w[kGroups][kWords];
+    __device__ __forceinline__ void load(const char* row, Slice S) {
+        constexpr int kBytes = TYPE == EVOSPEC_FP32 ? 4 : 2;
+        constexpr uint32_t kInf = TYPE == EVOSPEC_FP32 ? 0xff800000u : TYPE == EVOSPEC_FP16 ? 0xfc00u : 0xff80u;       // -inf
+        const bool whole = (reinterpret_cast<uintptr_t>(row) & (4 * kBytes - 1)) == 0 && !S.small();
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-        const int i = S.at(g, 0);
-        if (whole && i + 4 <= S.last) {
-            if constexpr (TYPE == EVOSPEC_FP32) {
-                const float4 v = *reinterpret_cast<const float4*>(row + (size_t)i * 4);
-                z[g][0] = v.x; z[g][1] = v.y; z[g][2] = v.z; z[g][3] = v.w;
+        for (int g = 0; g < kGroups; ++g) {
+            const int i = S.at(g, 0);
+            if (whole && i + 4 <= S.last) {
+                if constexpr (TYPE == EVOSPEC_FP32) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(row + (size_t)i * 4);
+                    w[g][0] = v.x; w[g][1] = v.y; w[g][2] = v.z; w[g][3] = v.w;
+                } else {
+                    const uint2 v = *reinterpret_cast<const uint2*>(row + (size_t)i * 2);
+                    w[g][0] = v.x; w[g][1] = v.y;
+                }
             } else {
-                const uint2 v = *reinterpret_cast<const uint2*>(row + (size_t)i * 2);
+                uint32_t x[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const uint16_t b = (uint16_t)((e < 2 ? v.x : v.y) >> (16 * (e & 1)));
-                    if constexpr (TYPE == EVOSPEC_FP16) z[g][e] = (float)__builtin_bit_cast(_Float16, b);
-                    else z[g][e] = __uint_as_float((uint32_t)b << 16);
+                    x[e] = kInf;
+                    if (S.at(g, e) < S.last) {
+                        if constexpr (TYPE == EVOSPEC_FP32) x[e] = reinterpret_cast<const uint32_t*>(row)[S.at(g, e)];
+                        else x[e] = reinterpret_cast<const uint16_t*>(row)[S.at(g, e)];
+                    }
                 }
-            }
-        } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) z[g][e] = S.at(g, e) < S.last ? logit<TYPE>(row, S.at(g, e)) : -__builtin_inff();
+                for (int e = 0; e < kWords; ++e) w[g][e] = TYPE == EVOSPEC_FP32 ? x[e] : x[2 * e & 3] | x[(2 * e + 1) & 3] << 16;
+            }
         }
     }
+    __device__ __forceinline__ void give(float (&z)[kGroups][4]) const {
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (TYPE == EVOSPEC_FP32) {
+                    z[g][e] = __uint_as_float(w[g][e]);
+                } else {
+                    const uint32_t x = w[g][e >> 1];
+                    if constexpr (TYPE == EVOSPEC_BF16) z[g][e] = __uint_as_float(e & 1 ? x & 0xffff0000u : x << 16);
+                    else z[g][e] = (float)__builtin_bit_cast(_Float16, (uint16_t)(x >> (16 * (e & 1))));
+                }
+            }
+    }
+};
+template <int TYPE>
+__device__ __forceinline__ void load_slice(const char* row, Slice S, float (&z)[kGroups][4]) {
+    RawSlice<TYPE> raw;
+    raw.load(row, S);
+    raw.give(z);
 }
 
 __device__ __forceinline__ bool regular(float T, float z_max) {
@@ -427,10 +457,17 @@ __device__ __forceinline__ void list_largest(const SampleArgs& A, const float (&
     }
 }
 
-template <int TYPE>
-__global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs A, char* ws, int slices) {
+// bf16 has 128 values to a factor of 2: a slice's logits between 2^-12 and 2^6, of either sign, are counted by value, and each value is
+// weighed once, times its number (whole numbers: the sums are the same).  960 rows of 151,936 183 us one by one, 132 so, 64 rows 29 and 13.
+constexpr int kLeastByValue = 8192;               // logits of a slice (8 rows of 50,000 in slices of 4,168 8.9 us by value, 7.4 one by one)
+constexpr int kLowCode = 0x3980, kCodes = 0x4280 - kLowCode;    // upper halves of 2^-12 and 2^6
+
+template <int TYPE, bool BY_VALUE>
+__global__ __launch_bounds__(kThreads, 8) void sample_bins_kernel(SampleArgs A, char* ws, int slices) {
     __shared__ u64 s_mass[kAll];
     __shared__ uint32_t s_count[kAll];
+    static_assert(!BY_VALUE || TYPE == EVOSPEC_BF16, "");
+    __shared__ uint32_t s_num[BY_VALUE ? 2 * kCodes : 1];
     __shared__ double s_table[kSteps];
     __shared__ float s_max[kThreads / 64];
     __shared__ u64 s_part[kThreads / 64];
@@ -447,6 +484,8 @@ __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs A, cha
         s_mass[b] = 0;
         s_count[b] = 0;
     }
+    if constexpr (BY_VALUE)
+        for (int i = tid; i < 2 * kCodes; i += kThreads) s_num[i] = 0;
     if (j == 0 && tid == 0) *R.ticket = 0;
     float top = -__builtin_inff();
 #pragma unroll
@@ -486,18 +525,35 @@ __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs A, cha
     if (!ok) return;                                             // (uniform) nothing here, or a row for the digits
     const float cut = cut_of(ref, T);
     const int ref_steps = (int)ref * kSteps;
+    auto add = [&](float x, uint32_t n) {
+        if (x >= cut) {                                          // (not NaN)
+            const Steps s = locate(x, c, ref_steps);
+            if ((uint32_t)s.m >= (uint32_t)(kRange * kSteps)) return;
+            const int b = bin_of(s.m);
+            atomicAdd(&s_mass[b], n * weight_of(s, s_table));
+            if (counts) atomicAdd(&s_count[b], n);
+        }
+    };
 #pragma unroll
     for (int g = 0; g < kGroups; ++g)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            if (z[g][e] >= cut) {                                // (not NaN)
-                const Steps s = locate(z[g][e], c, ref_steps);
-                if ((uint32_t)s.m >= (uint32_t)(kRange * kSteps)) continue;
-                const int b = bin_of(s.m);
-                atomicAdd(&s_mass[b], weight_of(s, s_table));
-                if (counts) atomicAdd(&s_count[b], 1u);
+            if constexpr (BY_VALUE) {
+                const uint32_t u = __float_as_uint(z[g][e]), code = ((u >> 16) & 0x7fffu) - kLowCode;
+                if (code < (uint32_t)kCodes) {
+                    atomicAdd(&s_num[code + (u >> 31) * kCodes], 1u);
+                    continue;
+                }
             }
+            add(z[g][e], 1);
         }
+    if constexpr (BY_VALUE) {
+        __syncthreads();
+        for (int i = tid; i < 2 * kCodes; i += kThreads) {
+            const uint32_t n = s_num[i], code = (uint32_t)(i < kCodes ? i : i - kCodes) + kLowCode;
+            if (n) add(__uint_as_float((code | (i < kCodes ? 0u : 0x8000u)) << 16), n);
+        }
+    }
     __syncthreads();
     for (int b = tid; b < kAll; b += kThreads) {
         R.mass[(size_t)j * kAll + b] = s_mass[b];
@@ -1034,10 +1090,14 @@ __global__ __launch_bounds__(kRowThreads, 8) void sample_row_kernel(SampleArgs A
             __syncthreads();
             const char* row = row_of<TYPE>(A, m);
             const int parts = (A.V + kSlice - 1) / kSlice;       // (few and large, whatever the slices of the bins were)
+            RawSlice<TYPE> raw;                                  // (16-bit types: the next part is under way meanwhile)
+            if (TYPE != EVOSPEC_FP32) raw.load(row, slice_of(A.V, parts, 0));
             for (int j = 0; j < parts; ++j) {
                 const Slice S = slice_of(A.V, parts, j);
                 float z[kGroups][4];
-                load_slice<TYPE>(row, S, z);
+                if (TYPE == EVOSPEC_FP32) raw.load(row, S);
+                raw.give(z);
+                if (TYPE != EVOSPEC_FP32 && j + 1 < parts) raw.load(row, slice_of(A.V, parts, j + 1));
                 pick_tokens(A, S, z, st, st.ref, T, [&](u64 key) {
                     const uint32_t at = atomicAdd(&s_n, 1u);
                     if (at < kList) s_key[at] = key;
@@ -1145,12 +1205,14 @@ static hipError_t sample_as(const SampleArgs& a, char* ws, hipStream_t stream) {
     // 41 us, 256 rows 153 and 147, 512 rows 232 and 242; 30 rows of 60,000 50 and 40, of 40,000 41 and 36.5; 60 rows of 20,000 41 and 46.
     const bool rest = a.top_k || whole_slices(a.V) == 1 || a.M >= kManyRows;
     const int slices = a.top_k ? whole_slices(a.V) : many_slices(a.M, a.V);
-    sample_bins_kernel<TYPE><<<dim3((unsigned)(a.M * slices)), kThreads, 0, stream>>>(a, ws, slices);
+    const dim3 parts((unsigned)(a.M * slices));
+    if (TYPE == EVOSPEC_BF16 && a.V / slices >= kLeastByValue) sample_bins_kernel<TYPE, TYPE == EVOSPEC_BF16><<<parts, kThreads, 0, stream>>>(a, ws, slices);
+    else sample_bins_kernel<TYPE, false><<<parts, kThreads, 0, stream>>>(a, ws, slices);
     if (rest) {
         sample_row_kernel<TYPE, true><<<dim3((unsigned)a.M), kRowThreads, 0, stream>>>(a, ws, slices);
     } else {
         sample_row_kernel<TYPE, false><<<dim3((unsigned)a.M), kRowThreads, 0, stream>>>(a, ws, slices);
-        sample_pick_kernel<TYPE><<<dim3((unsigned)(a.M * slices)), kThreads, 0, stream>>>(a, ws, slices);
+        sample_pick_kernel<TYPE><<<parts, kThreads, 0, stream>>>(a, ws, slices);
         sample_finish_kernel<TYPE><<<dim3((unsigned)a.M), kThreads, 0, stream>>>(a, ws, slices);
     }
     return hipGetLastError();

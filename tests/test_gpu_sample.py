@@ -270,3 +270,18 @@ def test_few_rows_of_many_slices(ev):
             got, lq = ev.sample(z[:M], u[:M], workspace=ws, **part)
             assert torch.equal(got, ids[:M]), M
             assert (lq - lp[:M]).abs().max() <= 1e-6
+
+
+def test_values_of_every_magnitude(ev):
+    """Long rows of bf16: magnitudes from 2^-20 to 2^9 and zeros of either sign, few values or many, masked ones between."""
+    rng = np.random.default_rng(79)
+    M, V = 24, 100000
+    z = rng.standard_normal((M, V)) * 2.0 ** rng.integers(-20, 2, (M, V))
+    z[:4] = rng.standard_normal((4, V)) * 300
+    z[4:8] = rng.choice([-0.0, 0.0, 2.0 ** -12, -2.0 ** -12, 2.0 ** -13, 63.75, 64.0, -64.0, 1.0], (4, V))
+    z[8:12] = rng.choice([0.5, 0.50390625, -3.0], (4, V))
+    z[::3, rng.random(V) < 0.5] = -np.inf
+    z[1::3, 5000:70000] = np.nan
+    t = rng.choice([0.5, 1.0, 30.0], M)
+    for f in ({}, dict(top_p=rng.random(M)), dict(min_p=rng.random(M) * 0.1), dict(top_k=rng.choice([300, 5000, 40000], M), top_p=rng.random(M))):
+        run(ev, z, rng.random(M), "bf16", temperature=t, **f)
