@@ -5,7 +5,7 @@
 // cumulative weight of the kept ones passes u times their sum.  Such keys are found digit by digit from a histogram of the
 // keys that agree so far, of numbers (top-k) or of weights (top-p, the draw).  Weights w = exp((z - z_max) / T) are computed
 // in 64 bits and kept as whole multiples of 2^-43: their sums do not depend on an order, so that a histogram may be filled by
-// atomics, and 2^20 of them fit 64 bits.  Measured on rows of 151,936: one in 17 us, 60 with top-k in 26, 960 of bf16 with top-p in 302.
+// atomics, and 2^20 of them fit 64 bits.  Measured on rows of 151,936: one in 17 us, 60 with top-k in 26, 960 of bf16 with top-p in 262.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -231,14 +231,14 @@ __device__ __forceinline__ void sample_by_digits(const SampleArgs& A, int m, u64
 
 
 // ---------------------------------------------------------------------------------------
-// The fast way, four launches.
+// The fast way, four launches or two.
 //
 // 1. sample_bins_kernel, a workgroup for each slice of a row (kSlice logits at most, which stay in registers): the slice's
 //    largest logit, and the weights of its tokens, summed in bins of 1 / kBins of a power of two below e = the next power of two
 //    above that logit.  References are whole powers of two, so that slices' bins lie on one grid and their sums are joined by shifts.
 // 2. sample_row_kernel, a workgroup for each row: the bins of all slices, joined (eight slices' loads at a time); in which bins top-k, top-p and min-p cut, and in which
 //    the draw falls (a range of them where one depends on a cut inside a bin).  Greedy rows end here.
-// 3. sample_pick_kernel, a workgroup for each slice again: tokens of those bins are put on the row's list.
+// 3. sample_pick_kernel, a workgroup for each part of a row again: tokens of those bins are put on the row's list.
 // 4. sample_finish_kernel, a workgroup for each row: sorts the list, and goes through the filters with the list's tokens and the bins'
 //    sums.
 // Rows of a top-k up to kMostK need no weights but those of their k largest tokens: 1. lists the tokens that can be among them, and 2.
@@ -561,6 +561,98 @@ __global__ __launch_bounds__(kThreads, 8) void sample_bins_kernel(SampleArgs A, 
     }
 }
 
+// The same by value for many rows of bf16 without a top-k: a slice is `parts` times as long, taken in parts with the next one under way,
+// and its values are weighed once.  The window goes down to 2^-22, and what lies outside of it is read again at the end, when the
+// slice's largest logit is known.  960 rows of 151,936 in slices of 75,968: 132 and 91 us; 128 rows 38 and 19.
+constexpr int kWideLow = 0x3480, kWideCodes = 0x4280 - kWideLow;
+__global__ __launch_bounds__(kThreads, 8) void sample_wide_bins_kernel(SampleArgs A, char* ws, int slices, int parts) {
+    __shared__ u64 s_mass[kAll];
+    __shared__ uint32_t s_num[2 * kWideCodes];
+    __shared__ double s_table[kSteps];
+    __shared__ float s_max[kThreads / 64];
+    __shared__ u64 s_part[kThreads / 64];
+    __shared__ uint32_t s_outside;
+    const int m = blockIdx.x / slices, j = blockIdx.x % slices, tid = threadIdx.x, lane = tid & 63;
+    const char* row = static_cast<const char*>(A.logits) + (long long)m * A.stride * 2;
+    const Slice S = slice_of(A.V, slices, j);
+    const int per = ((S.last - S.first + parts - 1) / parts + 3) / 4 * 4;      // (<= kSlice)
+    auto part = [&](int p) { return Slice{min(S.last, S.first + p * per), min(S.last, S.first + (p + 1) * per)}; };
+    // f(logit, where it is: part, group, element) for all of the slice's
+    auto each = [&](auto f) {
+        RawSlice<EVOSPEC_BF16> raw;
+        raw.load(row, part(0));
+        for (int p = 0; p < parts; ++p) {
+            float z[kGroups][4];
+            raw.give(z);
+            if (p + 1 < parts) raw.load(row, part(p + 1));
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f(z[g][e], p, g, e);
+        }
+    };
+    auto code_of = [](float z) { return ((__float_as_uint(z) >> 16) & 0x7fffu) - kWideLow; };
+    const RowSpace R = row_space(ws, m, slices);
+    const float T = A.temperature ? A.temperature[m] : 1.f;
+    fill_table(s_table);
+    for (int b = tid; b < kAll; b += kThreads) s_mass[b] = 0;
+    for (int i = tid; i < 2 * kWideCodes; i += kThreads) s_num[i] = 0;
+    if (tid == 0) s_outside = 0;
+    if (j == 0 && tid == 0) *R.ticket = 0;
+    __syncthreads();
+    float top = -__builtin_inff();
+    bool outside = false;
+    each([&](float z, int, int, int) {
+        top = fmaxf(top, z);
+        const uint32_t code = code_of(z);
+        if (code < (uint32_t)kWideCodes) atomicAdd(&s_num[code + (__float_as_uint(z) >> 31) * kWideCodes], 1u);
+        else outside |= z > -__builtin_inff();
+    });
+    top = wave_max(top, lane);
+    if (lane == 0) s_max[tid >> 6] = top;
+    if (__ballot(outside) && lane == 0) s_outside = 1;
+    __syncthreads();
+    top = s_max[lane & (kThreads / 64 - 1)];
+    top = wave_max(top, lane);
+    if (!(T > 0.f)) {                                            // greedy: the largest key
+        u64 best = 0;
+        if (top > -__builtin_inff())
+            each([&](float z, int p, int g, int e) {
+                if (z == top) {
+                    const int i = part(p).at(g, e);
+                    const u64 key = make_key(top, A.ids ? A.ids[i] : i);
+                    best = key > best ? key : best;
+                }
+            });
+        best = reduce_all(best, s_part, [](u64 a, u64 b) { return a > b ? a : b; });
+        if (tid == 0) R.slice[j] = SliceState{0.0, best, 0, 0};
+        return;
+    }
+    const double c = log2e_over(T);
+    const bool ok = top > -__builtin_inff() && regular(T, top);
+    const double ref = ok ? ceil((double)top * c) : 0.0;
+    if (tid == 0) R.slice[j] = SliceState{ref, top > -__builtin_inff() ? make_key(top, 0) : 0, 0, 0};
+    if (!ok) return;                                             // (uniform) nothing here, or a row for the digits
+    const float cut = cut_of(ref, T);
+    const int ref_steps = (int)ref * kSteps;
+    auto add = [&](float x, uint32_t n) {
+        if (x >= cut) {                                          // (not NaN)
+            const Steps s = locate(x, c, ref_steps);
+            if ((uint32_t)s.m < (uint32_t)(kRange * kSteps)) atomicAdd(&s_mass[bin_of(s.m)], n * weight_of(s, s_table));
+        }
+    };
+    for (int i = tid; i < 2 * kWideCodes; i += kThreads) {
+        const uint32_t n = s_num[i], code = (uint32_t)(i < kWideCodes ? i : i - kWideCodes) + kWideLow;
+        if (n) add(__uint_as_float((code | (i < kWideCodes ? 0u : 0x8000u)) << 16), n);
+    }
+    if (s_outside)
+        each([&](float z, int, int, int) {
+            if (code_of(z) >= (uint32_t)kWideCodes) add(z, 1);
+        });
+    __syncthreads();
+    for (int b = tid; b < kAll; b += kThreads) R.mass[(size_t)j * kAll + b] = s_mass[b];
+}
+
 // One step of a bitonic sort within a wavefront: the larger of lane and lane ^ D goes to the one that is to have it.
 template <int D>
 __device__ __forceinline__ void exchange(u64& v, bool descending, int lane) {
@@ -765,28 +857,23 @@ template <int TYPE>
 __device__ __forceinline__ const char* row_of(const SampleArgs& A, int m) {
     return static_cast<const char*>(A.logits) + (long long)m * A.stride * (TYPE == EVOSPEC_FP32 ? 4 : 2);
 }
-// Whether a slice has weights at all next to the row's.
-__device__ __forceinline__ bool has_any(const SliceState& s, const RowState& st, float T) {
-    return s.top != 0 && regular(T, key_value(s.top)) && st.ref - s.ref < kRange;
-}
 // Calls put(key) for the slice's tokens whose bins are to be on the list.
 template <class Put>
-__device__ __forceinline__ void pick_tokens(const SampleArgs& A, Slice S, const float (&z)[kGroups][4], const RowState& st, double ref, float T,
+__device__ __forceinline__ void pick_tokens(const SampleArgs& A, Slice S, const float (&z)[kGroups][4], const RowState& st, float T,
                                             Put put) {
     const double c = log2e_over(T);
     const int b_min = min(st.lo[0], min(st.lo[1], st.lo[2])), b_max = max(st.hi[0], max(st.hi[1], st.hi[2]));
-    const int shift = (int)(st.ref - ref) * kBins;
     // logits that can be in those bins, a little generously: bin b ends where x = -(b + 1) / kBins, to half a step
     const double far = (st.ref - (double)(b_max + 2) * (1.0 / kBins)) * ((double)T * 0.69314718055994530942);
-    const float cut = cut_of(ref, T), least = b_max == kAll - 1 ? cut : fmaxf(cut, (float)(far - fabs(far) * 0x1p-20));
-    const int ref_steps = (int)ref * kSteps;
+    const float cut = cut_of(st.ref, T), least = b_max == kAll - 1 ? cut : fmaxf(cut, (float)(far - fabs(far) * 0x1p-20));
+    const int ref_steps = (int)st.ref * kSteps;
 #pragma unroll
     for (int g = 0; g < kGroups; ++g)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if (z[g][e] >= least) {
                 const Steps s = locate(z[g][e], c, ref_steps);
-                const int b = min(bin_of(s.m) + shift, kAll - 1);
+                const int b = bin_of(s.m);
                 if ((uint32_t)s.m < (uint32_t)(kRange * kSteps) && b >= b_min && b <= b_max &&
                     ((b >= st.lo[0] && b <= st.hi[0]) || (b >= st.lo[1] && b <= st.hi[1]) || (b >= st.lo[2] && b <= st.hi[2]))) {
                     const int i = S.at(g, e);
@@ -1098,7 +1185,7 @@ __global__ __launch_bounds__(kRowThreads, 8) void sample_row_kernel(SampleArgs A
                 if (TYPE == EVOSPEC_FP32) raw.load(row, S);
                 raw.give(z);
                 if (TYPE != EVOSPEC_FP32 && j + 1 < parts) raw.load(row, slice_of(A.V, parts, j + 1));
-                pick_tokens(A, S, z, st, st.ref, T, [&](u64 key) {
+                pick_tokens(A, S, z, st, T, [&](u64 key) {
                     const uint32_t at = atomicAdd(&s_n, 1u);
                     if (at < kList) s_key[at] = key;
                 });
@@ -1121,22 +1208,20 @@ __global__ __launch_bounds__(kRowThreads, 8) void sample_row_kernel(SampleArgs A
 }
 
 template <int TYPE>
-__global__ __launch_bounds__(kThreads) void sample_pick_kernel(SampleArgs A, char* ws, int slices) {
+__global__ __launch_bounds__(kThreads) void sample_pick_kernel(SampleArgs A, char* ws, int slices, int parts) {
     __shared__ u64 s_key[kStage];
     __shared__ uint32_t s_n, s_at;
-    const int m = blockIdx.x / slices, j = blockIdx.x % slices, tid = threadIdx.x;
+    const int m = blockIdx.x / parts, j = blockIdx.x % parts, tid = threadIdx.x;
     const RowSpace R = row_space(ws, m, slices);
-    const Slice S = slice_of(A.V, slices, j);
+    const Slice S = slice_of(A.V, parts, j);
     float z[kGroups][4];
     load_slice<TYPE>(row_of<TYPE>(A, m), S, z);                  // (under way while the row's state is looked at)
     const RowState st = *R.row;
     if (st.state != kOpen) return;
     const float T = A.temperature ? A.temperature[m] : 1.f;
-    const SliceState mine = R.slice[j];
-    if (!has_any(mine, st, T)) return;                           // (uniform)
     if (tid == 0) s_n = 0;
     __syncthreads();
-    pick_tokens(A, S, z, st, mine.ref, T, [&](u64 key) {
+    pick_tokens(A, S, z, st, T, [&](u64 key) {
         const uint32_t at = atomicAdd(&s_n, 1u);
         if (at < kStage) {
             s_key[at] = key;
@@ -1204,15 +1289,19 @@ static hipError_t sample_as(const SampleArgs& a, char* ws, hipStream_t stream) {
     // slice, or there are enough of them; otherwise its slices side by side.  By itself against side by side: one row of 151,936 57 and
     // 41 us, 256 rows 153 and 147, 512 rows 232 and 242; 30 rows of 60,000 50 and 40, of 40,000 41 and 36.5; 60 rows of 20,000 41 and 46.
     const bool rest = a.top_k || whole_slices(a.V) == 1 || a.M >= kManyRows;
-    const int slices = a.top_k ? whole_slices(a.V) : many_slices(a.M, a.V);
-    const dim3 parts((unsigned)(a.M * slices));
-    if (TYPE == EVOSPEC_BF16 && a.V / slices >= kLeastByValue) sample_bins_kernel<TYPE, TYPE == EVOSPEC_BF16><<<parts, kThreads, 0, stream>>>(a, ws, slices);
-    else sample_bins_kernel<TYPE, false><<<parts, kThreads, 0, stream>>>(a, ws, slices);
+    const int parts = a.top_k ? whole_slices(a.V) : many_slices(a.M, a.V);
+    // (longer slices where two workgroups for each compute unit are left)
+    const int wide = TYPE != EVOSPEC_BF16 || a.top_k ? 1 : std::min((int)std::min((long long)a.M * parts / (2 * kUnits), 4ll), parts);
+    const int slices = wide > 1 ? (parts + wide - 1) / wide : parts;
+    const dim3 grid((unsigned)(a.M * slices));
+    if (wide > 1) sample_wide_bins_kernel<<<grid, kThreads, 0, stream>>>(a, ws, slices, wide);
+    else if (TYPE == EVOSPEC_BF16 && a.V / slices >= kLeastByValue) sample_bins_kernel<TYPE, TYPE == EVOSPEC_BF16><<<grid, kThreads, 0, stream>>>(a, ws, slices);
+    else sample_bins_kernel<TYPE, false><<<grid, kThreads, 0, stream>>>(a, ws, slices);
     if (rest) {
         sample_row_kernel<TYPE, true><<<dim3((unsigned)a.M), kRowThreads, 0, stream>>>(a, ws, slices);
     } else {
         sample_row_kernel<TYPE, false><<<dim3((unsigned)a.M), kRowThreads, 0, stream>>>(a, ws, slices);
-        sample_pick_kernel<TYPE><<<parts, kThreads, 0, stream>>>(a, ws, slices);
+        sample_pick_kernel<TYPE><<<dim3((unsigned)(a.M * parts)), kThreads, 0, stream>>>(a, ws, slices, parts);
         sample_finish_kernel<TYPE><<<dim3((unsigned)a.M), kThreads, 0, stream>>>(a, ws, slices);
     }
     return hipGetLastError();

@@ -285,3 +285,29 @@ def test_values_of_every_magnitude(ev):
     t = rng.choice([0.5, 1.0, 30.0], M)
     for f in ({}, dict(top_p=rng.random(M)), dict(min_p=rng.random(M) * 0.1), dict(top_k=rng.choice([300, 5000, 40000], M), top_p=rng.random(M))):
         run(ev, z, rng.random(M), "bf16", temperature=t, **f)
+
+
+@pytest.mark.parametrize("M,V", [(600, 20500), (300, 81930), (1100, 50001)])
+def test_many_rows_as_few(ev, M, V):
+    """Many rows of bf16, whose slices are the longer: the same tokens as 20 rows at a time, values of every magnitude among them."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(M)
+    z = torch.randn((M, V), generator=g, device="cuda").mul_(2.0)
+    scale = torch.exp2(torch.randint(-26, 8, (M, 1), generator=g, device="cuda").float())
+    scale[::2] = 1.0
+    z *= scale
+    z[5::7, V // 3:] = -float("inf")
+    z[6::7, :V // 2] = 0.0
+    z[7::11, ::3] = float("nan")
+    z[8::13] = z[8::13].round()
+    z = z.to(torch.bfloat16)
+    u = torch.rand(M, generator=g, device="cuda")
+    t = torch.where(torch.rand(M, generator=g, device="cuda") < 0.1, 0.0, 0.3 + torch.rand(M, generator=g, device="cuda"))
+    p, least = torch.rand(M, generator=g, device="cuda"), torch.rand(M, generator=g, device="cuda") * 0.1
+    for kw in (dict(), dict(temperature=t), dict(temperature=t, top_p=p), dict(min_p=least), dict(top_p=p, min_p=least)):
+        ids, lp = ev.sample(z, u, **kw)
+        for first in range(0, M, 20):
+            part = {k: v[first:first + 20] for k, v in kw.items()}
+            few, lq = ev.sample(z[first:first + 20], u[first:first + 20], **part)
+            assert torch.equal(ids[first:first + 20], few), (list(kw), first)
+            assert (lp[first:first + 20] - lq).abs().max() <= 1e-6
