@@ -300,8 +300,8 @@ __device__ __forceinline__ RowSpace row_space(char* ws, int m, int slices) {
 
 // Weights by table: with y = z log2(e) / T = k / kSteps + r, |r| <= 1 / (2 kSteps), and `ref` a whole power of two above the row's or
 // slice's largest, w = 2^(y - ref) = 2^(-m / kSteps) 2^r, m = kSteps ref - k >= 0.  2^r by its series to the fourth power is off by
-// 2^-39.  What bounds the bins is LDS, an addition to a bin for each logit; a table of 128 steps, whose reads meet in its banks,
-// made it 183 us for 146 million logits.
+// 2^-39.  What bounds the bins is LDS, an addition to a bin for each logit: 183 us for 146 million logits, and 191 with a table of 128
+// steps, whose reads meet in its banks.
 struct Steps {
     int m;
     double r;
