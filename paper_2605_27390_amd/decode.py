@@ -12,6 +12,7 @@ from .binding import _check, _expect, _get_device, _ptr, _raw_stream, lib
 _TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 _KINDS = {"e4m3": 0, "int8": 1}
 _i32, _f32 = torch.int32, torch.float32
+_new = torch.empty_strided      # (strides spelled out: 0.9 us a tensor, torch.empty 1.6)
 
 
 class _Cache(ctypes.Structure):
@@ -148,8 +149,10 @@ def kv_read(cache: KVCache, page_table, starts, row_off, max_rows: int, rows: in
             _expect(t, dtype, name, 3)
             if tuple(t.shape) != shape:
                 raise ValueError(f"{name} must be {shape}, got {tuple(t.shape)}")
-    out_k = torch.empty(shape, dtype=dtype, device=cache.data.device) if out_k is None else out_k
-    out_v = torch.empty(shape, dtype=dtype, device=cache.data.device) if out_v is None else out_v
+    if out_k is None:
+        out_k = _new(shape, (cache.heads * cache.dim, cache.dim, 1), dtype=dtype, device=cache.data.device)
+    if out_v is None:
+        out_v = _new(shape, (cache.heads * cache.dim, cache.dim, 1), dtype=dtype, device=cache.data.device)
     _check(lib.evospec_kv_read(cache._ref, page_table.data_ptr(), width, starts.data_ptr(), row_off.data_ptr(), S, max_rows, rows,
                                _TYPES[dtype], out_k.data_ptr(), out_v.data_ptr(), _raw_stream(_get_device())), "evospec_kv_read")
     return out_k, out_v
@@ -183,13 +186,13 @@ def kv_attention(q, cache: KVCache, page_table, lens, row_off, max_rows: int, ma
             raise ValueError("tree needs a word for every row of q")
     max_len = min(width * cache.page, 1 << 30) if max_len is None else int(max_len)
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        out = _new((T, heads, dim), (heads * dim, dim, 1), dtype=q.dtype, device=q.device)
     else:
         _expect(out, q.dtype, "out", 3)
         if out.shape != q.shape:
             raise ValueError("out must have q's shape")
     if out_lse is None:
-        out_lse = torch.empty((T, heads), dtype=torch.float32, device=q.device)
+        out_lse = _new((T, heads), (heads, 1), dtype=_f32, device=q.device)
     else:
         _expect(out_lse, torch.float32, "out_lse", 2)
         if tuple(out_lse.shape) != (T, heads):
@@ -198,7 +201,7 @@ def kv_attention(q, cache: KVCache, page_table, lens, row_off, max_rows: int, ma
         _expect(workspace, torch.uint8, "workspace")
     else:
         need = _attention_bytes(cache.pages, cache.page, cache.heads, cache.dim, cache._c.kind, group, S, T, max_rows, max_len)
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+        workspace = _new((need,), (1,), dtype=torch.uint8, device=q.device) if need else None
     _check(lib.evospec_kv_attention(cache._ref, q.data_ptr(), qs, type_, T, group, page_table.data_ptr(), width,
                                     lens.data_ptr(), row_off.data_ptr(), S, max_rows, max_len, _ptr(tree),
                                     dim ** -0.5 if scale is None else scale, out.data_ptr(), out_lse.data_ptr(), _ptr(workspace),
@@ -239,13 +242,13 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, ids=
             _expect(t, dtype, name, 1)
             if t.numel() != M:
                 raise ValueError(f"{name} needs a place for every row")
-    out_ids = torch.empty(M, dtype=_i32, device=logits.device) if out_ids is None else out_ids
-    out_logprob = torch.empty(M, dtype=_f32, device=logits.device) if out_logprob is None else out_logprob
+    out_ids = _new((M,), (1,), dtype=_i32, device=logits.device) if out_ids is None else out_ids
+    out_logprob = _new((M,), (1,), dtype=_f32, device=logits.device) if out_logprob is None else out_logprob
     if workspace is not None:
         _expect(workspace, torch.uint8, "workspace")
     else:
         need = _sample_bytes(M, V)
-        workspace = torch.empty(need, dtype=torch.uint8, device=logits.device) if need else None
+        workspace = _new((need,), (1,), dtype=torch.uint8, device=logits.device) if need else None
     _check(lib.evospec_sample(logits.data_ptr(), logits.stride(0) if M > 1 else V, _TYPES[logits.dtype], M, V, u.data_ptr(),
                               _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(ids), out_ids.data_ptr(),
                               out_logprob.data_ptr(), _ptr(workspace), 0 if workspace is None else workspace.numel(), _raw_stream(_get_device())),
