@@ -761,15 +761,16 @@ constexpr int kRowThreads = kThreads;
 constexpr int kRowList = 2048;
 
 // Of n keys in LDS, logits in [bound, top], those that can be among the k largest, k <= n: by their numbers in kRowThreads even steps
-// of the range.  Gives how many are left.
-__device__ int keep_front(u64* s_key, int n, int k, float bound, float top, uint32_t* s_n) {
-    __shared__ uint32_t s_num[kRowThreads + 1], s_wave[kRowThreads / 64];
+// of the range.  Gives how many are left, by a counter of its own: the caller's, from which n came, may still be read by wavefronts that
+// left the last barrier late.
+__device__ int keep_front(u64* s_key, int n, int k, float bound, float top) {
+    __shared__ uint32_t s_num[kRowThreads + 1], s_wave[kRowThreads / 64], s_left;
     __shared__ int s_cut;
     const int tid = threadIdx.x, lane = tid & 63;
     const float per = (float)kRowThreads / fmaxf(top - bound, 1e-30f);
     auto step_of = [&](u64 key) { return min(max((int)((top - key_value(key)) * per), 0), kRowThreads - 1); };
     s_num[tid] = 0;
-    if (tid == 0) *s_n = 0;
+    if (tid == 0) s_left = 0;
     __syncthreads();
     u64 mine[kRowList / kRowThreads];
 #pragma unroll
@@ -793,9 +794,9 @@ __device__ int keep_front(u64* s_key, int n, int k, float bound, float top, uint
     const int cut = s_cut;
 #pragma unroll
     for (int r = 0; r < kRowList / kRowThreads; ++r)
-        if (mine[r] && step_of(mine[r]) <= cut) s_key[atomicAdd(s_n, 1u)] = mine[r];
+        if (mine[r] && step_of(mine[r]) <= cut) s_key[atomicAdd(&s_left, 1u)] = mine[r];
     __syncthreads();
-    return (int)*s_n;
+    return (int)s_left;
 }
 
 // A row of a small top-k, from its slices' lists.  False if they do not hold what is needed.
@@ -826,7 +827,7 @@ __device__ bool finish_largest(const SampleArgs& A, int m, int k, const RowSpace
     __syncthreads();
     int n = (int)*s_n;
     if (n > kRowList) return false;
-    if (n > 2 * k) n = keep_front(s_key, n, k, bound, z_max, s_n);
+    if (n > 2 * k) n = keep_front(s_key, n, k, bound, z_max);
     sort_keys<kRowThreads>(s_key, n);
     n = min(n, k);
     sum_weights<kRowThreads, 1>(s_key, s_sum, n, A.temperature ? A.temperature[m] : 1.f, ref, s_table, s_part);     // (n <= k <= kMostK)

@@ -1,0 +1,104 @@
+"""The sampler's kernels (csrc/sample.hip) on the host, a workgroup's wavefronts in orders that are chosen here: an access that lacks a
+barrier gives a wrong token every time, and nothing of it has to run on a GPU to be seen."""
+import ctypes
+import os
+import re
+import shutil
+import subprocess
+
+import numpy as np
+import pytest
+
+import decode_reference as ref
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CSRC = os.path.join(ROOT, "paper_2605_27390_amd", "csrc")
+CLANG = "/opt/rocm/llvm/bin/clang++"                             # (bf16 and fp16 as the kernels spell them)
+
+
+def host_source(text):
+    """Launches as calls; inline assembly, which is there for the choice of registers, as what it computes."""
+    text, launches = re.subn(r"(\w+(?:<[\w, =]*>)?)<<<(.*?), (\w+), 0, stream>>>\((.*?)\);",
+                             r"wavefronts::launch(\2, \3, [&] { \1(\4); });", text)
+    assert launches >= 6 and "<<<" not in text
+    text = text.replace('asm("v_fma_f64 %0, %1, %2, %3" : "=v"(d) : "v"(x), "v"(y), "s"(c));', "d = fma(x, y, c);")
+    text = text.replace('asm("" : "+v"(first));', "")
+    assert "asm(" not in text
+    return text
+
+
+@pytest.fixture(scope="module")
+def host(tmp_path_factory):
+    cc = shutil.which(CLANG)
+    if cc is None:
+        pytest.skip(f"no {CLANG}")
+    tmp = tmp_path_factory.mktemp("sample")
+    with open(os.path.join(CSRC, "sample.hip")) as f:
+        (tmp / "sample.inc").write_text(host_source(f.read()))
+    lib = str(tmp / "sample.so")
+    res = subprocess.run([cc, "-std=c++17", "-O1", "-g", "-fPIC", "-shared", "-w", "-fsanitize=bounds", "-fsanitize-trap=bounds",
+                          f'-DSAMPLE_SOURCE="{tmp / "sample.inc"}"', "-I", os.path.join(ROOT, "tests", "stub_wavefronts"), "-I", CSRC,
+                          "-I", os.path.join(ROOT, "include"), os.path.join(ROOT, "tests", "host_sample.cpp"), "-o", lib],
+                         capture_output=True, text=True)
+    assert res.returncode == 0, res.stderr[-4000:]
+    lib = ctypes.CDLL(lib)
+    lib.host_sample_workspace.restype = ctypes.c_size_t
+    lib.host_sample.restype = ctypes.c_char_p
+    return lib
+
+
+TYPES = {"bf16": 0, "fp16": 1, "fp32": 2}
+ORDERS = (0, 1, 2, 3)                                            # the first wavefront first, the last one first, shuffled
+
+
+def run(host, z, u, type="fp32", ids=None, orders=ORDERS, **kw):
+    """Compares with the definition as the GPU's tests do, under every order; returns the tokens."""
+    import torch
+    t = torch.from_numpy(np.asarray(z, dtype=np.float64)).to({"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}[type])
+    M, V = t.shape
+    u = np.asarray(u, dtype=np.float32)
+    kw = {k: np.asarray(v, dtype=np.int32 if k == "top_k" else np.float32) for k, v in kw.items()}
+    want, want_lp, margin = ref.sample(t.double().numpy(), u, ids=ids, **kw)
+    sure = margin > 1e-11
+    cols = None if ids is None else np.asarray(ids, dtype=np.int32)
+    at = lambda x: None if x is None else ctypes.c_void_p(x.ctypes.data)   # noqa: E731
+    for order in orders:
+        got, lp = np.full(M, -7, np.int32), np.zeros(M, np.float32)
+        ws = np.full(host.host_sample_workspace(M, V) + 256, 0xA5, np.uint8)
+        error = host.host_sample(ctypes.c_uint(order), ctypes.c_void_p(t.data_ptr()), ctypes.c_longlong(V), TYPES[type], M, V, at(u),
+                         at(kw.get("temperature")), at(kw.get("top_k")), at(kw.get("top_p")), at(kw.get("min_p")), at(cols), at(got),
+                         at(lp), ctypes.c_void_p((ws.ctypes.data + 255) // 256 * 256))
+        assert error is None, (order, error)
+        lp = lp.astype(np.float64)
+        assert np.array_equal(got[sure], want[sure]), (order, got, want)
+        assert np.array_equal(np.isnan(lp[sure]), np.isnan(want_lp[sure])), order
+        ok = sure & ~np.isnan(want_lp)
+        assert (np.abs(lp - want_lp)[ok] <= 2.0 ** -23 * (1 + np.abs(want_lp[ok]))).all(), order
+    return got
+
+
+def test_lists_longer_than_twice_top_k(host):
+    """What the slices hand on is counted, and cut to what can be among the k largest: two numbers that must not be one."""
+    rng = np.random.default_rng(0)
+    M, V = 4, 30000
+    z = rng.standard_normal((M, V)) * 2
+    run(host, z, rng.random(M), top_k=[2, 20, 50, 100], top_p=[0.9] * M, min_p=[0.01] * M)
+
+
+@pytest.mark.parametrize("type", ["fp32", "bf16"])
+@pytest.mark.parametrize("M,V", [(1, 1), (3, 1000), (2, 21000)])
+def test_filters_in_every_order(host, type, M, V):
+    rng = np.random.default_rng(M + V)
+    z = rng.standard_normal((M, V)) * 2
+    z[:, :: 7] = -np.inf
+    for kw in ({}, dict(top_p=[0.8] * M), dict(top_k=[min(V, 300)] * M, top_p=[0.9] * M), dict(min_p=[0.02] * M),
+               dict(temperature=[0.0] * M), dict(top_k=[5] * M)):
+        run(host, z, rng.random(M), type, **kw)
+
+
+def test_flat_rows_in_every_order(host):
+    """More tokens at a border than lists hold: by digits of the keys."""
+    rng = np.random.default_rng(3)
+    z = np.zeros((2, 9000))
+    run(host, z, rng.random(2), top_p=[0.5, 1.0], orders=(0, 1))
+    run(host, z, rng.random(2), top_k=[200, 5000], orders=(0, 1))
