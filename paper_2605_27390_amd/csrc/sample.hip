@@ -913,8 +913,14 @@ __device__ void finish_row(const SampleArgs& A, int m, const RowState& st, u64* 
     int last = n;                                                // the place of the last token that is kept; n: all of the row are
     u64 kept = s_before[kAll];
     if (st.k_bin >= 0) {
-        last = min(place_of(st.k_bin) + st.k_left, n) - 1;
-        kept = upto(last);
+        const int first = place_of(st.k_bin), end = place_of(st.k_bin + 1);
+        if (first < end) {
+            last = min(first + st.k_left, n) - 1;
+            kept = upto(last);
+        } else {
+            // none of its tokens is on the list: a slice counted them in its last bin, and in the row they weigh nothing
+            kept = s_before[st.k_bin];
+        }
     }
     const float p = A.top_p ? A.top_p[m] : 1.f;
     if (p < 1.f) {

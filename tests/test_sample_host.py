@@ -102,3 +102,22 @@ def test_flat_rows_in_every_order(host):
     z = np.zeros((2, 9000))
     run(host, z, rng.random(2), top_p=[0.5, 1.0], orders=(0, 1))
     run(host, z, rng.random(2), top_k=[200, 5000], orders=(0, 1))
+
+
+def far_tokens(V):
+    """Tokens that no row counts any more, but their slice does: the row's first 500 in its first half, and in the other half one
+    at 2^-20 of them and the others at 2^-50 (or so: behind 2^-44 of the row's, not of the slice's)."""
+    z = np.full(V, -np.inf)
+    z[10:510] = -np.arange(500) * 1e-3
+    z[V - 700] = -20 * np.log(2)
+    z[V - 650:] = -50 * np.log(2) - np.arange(650) * 1e-3
+    return z
+
+
+def test_top_k_ends_behind_what_counts(host):
+    """The bin that top-k cuts holds tokens of a slice that weigh nothing in the row, and no others."""
+    M = 8
+    z = np.tile(far_tokens(30000), (M, 1))
+    u = (np.arange(M) + 0.5) / M
+    for kw in ({}, dict(top_p=[0.97] * M), dict(min_p=[0.8] * M)):
+        run(host, z, u, top_k=[600] * M, orders=(0,), **kw)
