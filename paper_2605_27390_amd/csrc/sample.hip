@@ -883,15 +883,11 @@ __device__ __forceinline__ void pick_tokens(const SampleArgs& A, Slice S, const 
             }
 }
 
-// Goes through the filters with a row's list (n tokens in LDS, in any order) and the sums of its bins.
-__device__ void finish_row(const SampleArgs& A, int m, const RowState& st, u64* s_key, int n, u64* s_sum, const u64* s_before,
-                           const double* s_table, u64* s_part) {
-    const int tid = threadIdx.x, lane = tid & 63;
-    const double c = log2e_over(A.temperature ? A.temperature[m] : 1.f);
-    sort_keys<kThreads>(s_key, n);
-    sum_weights<kThreads, kList / kThreads>(s_key, s_sum, n, A.temperature ? A.temperature[m] : 1.f, st.ref, s_table, s_part);
-    if (tid >= 64) return;
-    // One wavefront goes through the filters.  Every place is an index into the sorted list.
+// The part of one wavefront of finish_row below.
+__device__ __forceinline__ bool draw_from_list(const SampleArgs& A, int m, const RowState& st, const u64* s_key, int n, const u64* s_sum,
+                                               const u64* s_before, double c) {
+    const int lane = threadIdx.x & 63;
+    bool lost = false;
     auto bin_at = [&](int i) { return bin_of(locate(key_value(s_key[i]), c, (int)st.ref * kSteps).m); };
     // the first place of the list in bin b or behind
     auto place_of = [&](int b) { return search(0, n, lane, [&](int i) { return bin_at(i) >= b; }); };
@@ -906,9 +902,10 @@ __device__ void finish_row(const SampleArgs& A, int m, const RowState& st, u64* 
     auto place_at = [&](u64 target) {
         const int bin = min(search(0, kAll, lane, [&](int b) { return s_before[b + 1] >= target; }), kAll - 1);
         const int first = place_of(bin), end = place_of(bin + 1);
+        lost |= first == end;
         const u64 rest = target - s_before[bin] + sum_to(first);
         const int i = search(first, end, lane, [&](int i) { return s_sum[i] >= rest; });
-        return max(min(i, min(end, n) - 1), 0);                  // (the last of the bin if rounding leaves it short)
+        return max(min(i, end - 1), 0);                          // (the last of the bin if rounding leaves it short)
     };
     int last = n;                                                // the place of the last token that is kept; n: all of the row are
     u64 kept = s_before[kAll];
@@ -927,6 +924,7 @@ __device__ void finish_row(const SampleArgs& A, int m, const RowState& st, u64* 
         kept = share_up(p, kept);
         if (s_before[st.end_bin + 1] >= kept) {                  // (otherwise min-p cuts in front of that)
             last = min(last, place_at(kept));
+            if (lost) return false;
             kept = upto(last);
         }
     }
@@ -945,8 +943,28 @@ __device__ void finish_row(const SampleArgs& A, int m, const RowState& st, u64* 
         }
     }
     int at = place_at(share_past(A.u[m], kept));
+    if (lost) return false;
     if (last < n) at = min(at, last);
-    if (tid == 0) give(A, m, s_key[at], kept, c, st.ref);
+    if (lane == 0) give(A, m, s_key[at], kept, c, st.ref);
+    return true;
+}
+
+// Goes through the filters with a row's list (n tokens in LDS, in any order) and the sums of its bins.  False, and nothing given, where a
+// border falls into a bin that has weight but no token on the list (the last bin, by tokens of less than 2^-44 of the row's first).
+__device__ bool finish_row(const SampleArgs& A, int m, const RowState& st, u64* s_key, int n, u64* s_sum, const u64* s_before,
+                           const double* s_table, u64* s_part) {
+    const int tid = threadIdx.x;
+    const double c = log2e_over(A.temperature ? A.temperature[m] : 1.f);
+    sort_keys<kThreads>(s_key, n);
+    sum_weights<kThreads, kList / kThreads>(s_key, s_sum, n, A.temperature ? A.temperature[m] : 1.f, st.ref, s_table, s_part);
+    // One wavefront goes through the filters.  Every place is an index into the sorted list.
+    __shared__ int s_lost;
+    if (tid < 64) {
+        const bool lost = !draw_from_list(A, m, st, s_key, n, s_sum, s_before, c);
+        if (tid == 0) s_lost = lost;
+    }
+    __syncthreads();
+    return !s_lost;
 }
 
 // Joins the bins of a row's slices (s_before[b] = what lies in front of bin b) and says which bins have to be looked at.
@@ -1199,8 +1217,7 @@ __global__ __launch_bounds__(kRowThreads, 8) void sample_row_kernel(SampleArgs A
             }
             __syncthreads();
             if (s_n <= (uint32_t)kList) {                        // (uniform)
-                finish_row(A, m, st, s_key, (int)s_n, s_sum, s_before, s_table, s_part);
-                return;
+                if (finish_row(A, m, st, s_key, (int)s_n, s_sum, s_before, s_table, s_part)) return;
             }
         }
         __syncthreads();
@@ -1264,7 +1281,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_finish_kernel(SampleArgs A
     for (int b = tid; b <= kAll; b += kThreads) s_before[b] = R.before[b];
     for (int i = tid; i < n; i += kThreads) s_key[i] = R.list[i];
     __syncthreads();
-    finish_row(A, m, st, s_key, n, s_sum, s_before, s_table, s_part);
+    if (!finish_row(A, m, st, s_key, n, s_sum, s_before, s_table, s_part)) sample_by_digits<TYPE>(A, m, s_key, s_part, s_pick);
 }
 
 }  // namespace

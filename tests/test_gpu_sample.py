@@ -311,3 +311,29 @@ def test_many_rows_as_few(ev, M, V):
             few, lq = ev.sample(z[first:first + 20], u[first:first + 20], **part)
             assert torch.equal(ids[first:first + 20], few), (list(kw), first)
             assert (lp[first:first + 20] - lq).abs().max() <= 1e-6
+
+
+def test_last_bin_without_a_token(ev):
+    """u of 1 and above where the last bin has weight, of tokens below 2^-43.98 of the first, and no token on a list: a token of the row,
+    not -1.  By four launches, two, and for top-k past the lists."""
+    import torch
+    V = 30000
+    for M, k in ((1, None), (520, None), (2, 600)):
+        z = torch.full((M, V), -float("inf"), device="cuda")
+        z[:, 5], z[:, 29000] = 0.0, -43.99 * float(np.log(2))
+        for u in (1.0, float("inf"), float("nan")):
+            kw = {} if k is None else dict(top_k=torch.full((M,), k, dtype=torch.int32, device="cuda"))
+            ids, lp = ev.sample(z, torch.full((M,), u, device="cuda"), **kw)
+            assert ((ids == 5) | (ids == 29000)).all() and torch.isfinite(lp).all()
+
+
+def test_top_k_ends_behind_what_counts(ev):
+    """top-k past the lists that ends in a bin whose tokens count in their slice and weigh nothing in the row."""
+    V, M = 30000, 8
+    row = np.full(V, -np.inf)
+    row[10:510] = -np.arange(500) * 1e-3
+    row[V - 700] = -20 * np.log(2)
+    row[V - 650:] = -50 * np.log(2) - np.arange(650) * 1e-3
+    u = (np.arange(M) + 0.5) / M
+    for kw in ({}, dict(top_p=[0.97] * M), dict(min_p=[0.8] * M)):
+        run(ev, np.tile(row, (M, 1)), u, top_k=[600] * M, **kw)

@@ -121,3 +121,15 @@ def test_top_k_ends_behind_what_counts(host):
     u = (np.arange(M) + 0.5) / M
     for kw in ({}, dict(top_p=[0.97] * M), dict(min_p=[0.8] * M)):
         run(host, z, u, top_k=[600] * M, orders=(0,), **kw)
+
+
+@pytest.mark.parametrize("top_k", [None, 600])
+def test_last_bin_without_a_token(host, top_k):
+    """A slice whose best token weighs 2^-43.99 of the row's first: its weight is in the last bin, but too small for the list.  u = 1 ends
+    there; tokens below 2^-42 may be left out, so the row's first token is as right as that one."""
+    z = np.full((1, 30000), -np.inf)
+    z[0, 5], z[0, 29000] = 0.0, -43.99 * np.log(2)
+    kw = {} if top_k is None else dict(top_k=[top_k])
+    for u in (1.0, np.inf, np.nan):
+        got = run(host, z, [u], orders=(0,), **kw)
+        assert got[0] in (5, 29000)
