@@ -751,6 +751,11 @@ __device__ __forceinline__ int search(int lo, int hi, int lane, F f) {
     }
     return hi;
 }
+// Whether min-p leaves out the i-th of a sorted list, logit z.  Above 1 only the row's first token stays, which is on the list then, and
+// not those that tie with it.
+__device__ __forceinline__ bool too_light(int i, float z, float z_max, double c, float least) {
+    return least > 1.f ? i > 0 : z != z_max && weight(z, z_max, c) < (double)least;
+}
 __device__ __forceinline__ void give(const SampleArgs& A, int m, u64 key, u64 kept, double c, double ref) {
     A.out_ids[m] = key_id(key);
     if (A.out_logprob)
@@ -841,8 +846,7 @@ __device__ bool finish_largest(const SampleArgs& A, int m, int k, const RowSpace
     const float least = A.min_p ? A.min_p[m] : 0.f;
     if (least > 0.f) {
         const int first = search(0, n, lane, [&](int i) {
-            const float z = key_value(s_key[i]);
-            return z != z_max && weight(z, z_max, c) < (double)least;
+            return too_light(i, key_value(s_key[i]), z_max, c, least);
         });
         last = max(min(last, first - 1), 0);
     }
@@ -932,8 +936,7 @@ __device__ __forceinline__ bool draw_from_list(const SampleArgs& A, int m, const
     if (least > 0.f) {
         // the first place whose weight is too small; if that is not on the list, the last bin that may hold larger ones ends there
         const int first = search(0, n, lane, [&](int i) {
-            const float z = key_value(s_key[i]);
-            return z != st.z_max && weight(z, st.z_max, c) < (double)least;
+            return too_light(i, key_value(s_key[i]), st.z_max, c, least);
         });
         const bool on = first < n && bin_at(min(first, n - 1)) <= st.least_bin;
         const u64 mass = on ? before(first) : s_before[st.least_bin + 1];

@@ -337,3 +337,13 @@ def test_top_k_ends_behind_what_counts(ev):
     u = (np.arange(M) + 0.5) / M
     for kw in ({}, dict(top_p=[0.97] * M), dict(min_p=[0.8] * M)):
         run(ev, np.tile(row, (M, 1)), u, top_k=[600] * M, **kw)
+
+
+@pytest.mark.parametrize("V", [40, 30000])
+def test_min_p_above_one(ev, V):
+    """No token weighs more than 1: the first is kept, and those that tie with it are not."""
+    z = np.zeros((3, V))
+    z[:, 7:] = -np.arange(V - 7) - 1.0
+    for kw in ({}, dict(top_k=[20] * 3), dict(top_k=[300] * 3), dict(top_p=[0.999] * 3)):
+        assert run(ev, z, [0.1, 0.5, 0.9], min_p=[1.5, 1.0000001, np.inf], **kw).tolist() == [0, 0, 0]
+        run(ev, z, [0.1, 0.5, 0.9], min_p=[1.0, 1.0, 0.99], **kw)

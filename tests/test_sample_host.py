@@ -133,3 +133,13 @@ def test_last_bin_without_a_token(host, top_k):
     for u in (1.0, np.inf, np.nan):
         got = run(host, z, [u], orders=(0,), **kw)
         assert got[0] in (5, 29000)
+
+
+@pytest.mark.parametrize("V", [40, 30000])
+def test_min_p_above_one(host, V):
+    """No token weighs more than 1: the first is kept, and those that tie with it are not."""
+    z = np.zeros((3, V))
+    z[:, 7:] = -np.arange(V - 7) - 1.0
+    for kw in ({}, dict(top_k=[20] * 3), dict(top_k=[300] * 3), dict(top_p=[0.999] * 3)):
+        assert run(host, z, [0.1, 0.5, 0.9], min_p=[1.5, 1.0000001, np.inf], orders=(0,), **kw).tolist() == [0, 0, 0]
+        run(host, z, [0.1, 0.5, 0.9], min_p=[1.0, 1.0, 0.99], orders=(0,), **kw)
