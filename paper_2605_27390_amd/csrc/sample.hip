@@ -412,9 +412,12 @@ __device__ __forceinline__ void load_slice(const char* row, Slice S, float (&z)[
     raw.give(z);
 }
 
-__device__ __forceinline__ bool regular(float T, float z_max) {
-    return T < 0x1p60f && T > 0x1p-60f && fabsf(z_max) < T * 0x1p22f;
+// What bins can take: rows by their largest logit, the others go by digits.  Slices of such rows may lie a little past that (kRange factors of
+// 2 are 31 temperatures), and are taken to twice as far.
+__device__ __forceinline__ bool regular(float T, float z_max, float most = 0x1p22f) {
+    return T < 0x1p60f && T > 0x1p-60f && fabsf(z_max) < T * most;
 }
+__device__ __forceinline__ bool regular_slice(float T, float top) { return regular(T, top, 0x1p23f); }
 
 // Rows of a small top-k: tokens of the slice that can be among the row's k largest, as keys in the place of its bins, and a
 // bound that k of them reach.  Of every wavefront's 64 largest logits of a lane the q-th largest is taken, q times the wavefronts >= k, and
@@ -519,7 +522,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_bins_kernel(SampleArgs A, 
         return;
     }
     const double c = log2e_over(T);
-    const bool ok = top > -__builtin_inff() && regular(T, top);
+    const bool ok = top > -__builtin_inff() && regular_slice(T, top);
     const double ref = ok ? ceil((double)top * c) : 0.0;
     if (tid == 0) R.slice[j] = SliceState{ref, top > -__builtin_inff() ? make_key(top, 0) : 0, 0, 0};
     if (!ok) return;                                             // (uniform) nothing here, or a row for the digits
@@ -629,7 +632,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_wide_bins_kernel(SampleArg
         return;
     }
     const double c = log2e_over(T);
-    const bool ok = top > -__builtin_inff() && regular(T, top);
+    const bool ok = top > -__builtin_inff() && regular_slice(T, top);
     const double ref = ok ? ceil((double)top * c) : 0.0;
     if (tid == 0) R.slice[j] = SliceState{ref, top > -__builtin_inff() ? make_key(top, 0) : 0, 0, 0};
     if (!ok) return;                                             // (uniform) nothing here, or a row for the digits
@@ -980,7 +983,7 @@ __device__ __forceinline__ RowState plan_row(const SampleArgs& A, int m, const R
     __shared__ int s_shift[kMostSlices];
     if (tid < slices) {
         const SliceState s = s_slice[tid];
-        const double gap = s.top != 0 && regular(T, key_value(s.top)) ? ref - s.ref : kRange;      // (a whole number >= 0)
+        const double gap = s.top != 0 && regular_slice(T, key_value(s.top)) ? ref - s.ref : kRange;      // (a whole number >= 0)
         s_shift[tid] = gap < kRange ? (int)gap : -1;
     }
     if (tid <= kAll) {

@@ -347,3 +347,12 @@ def test_min_p_above_one(ev, V):
     for kw in ({}, dict(top_k=[20] * 3), dict(top_k=[300] * 3), dict(top_p=[0.999] * 3)):
         assert run(ev, z, [0.1, 0.5, 0.9], min_p=[1.5, 1.0000001, np.inf], **kw).tolist() == [0, 0, 0]
         run(ev, z, [0.1, 0.5, 0.9], min_p=[1.0, 1.0, 0.99], **kw)
+
+
+def test_slices_on_either_side_of_the_largest_quotient(ev):
+    """Logits of 2^22 temperatures: a row whose best lies just within what the bins take, and a slice whose best lies just past it."""
+    V = 24000
+    z = np.full((1, V), -np.inf)
+    z[0, 3], z[0, V - 5] = -4.0 + 2.0 ** -21, -4.0
+    for kw in ({}, dict(top_p=[0.9]), dict(top_k=[400]), dict(top_k=[4])):
+        run(ev, z, [0.8], temperature=[2.0 ** -20], **kw)
