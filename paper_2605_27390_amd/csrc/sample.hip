@@ -421,10 +421,12 @@ __device__ __forceinline__ bool regular_slice(float T, float top) { return regul
 
 // Rows of a small top-k: tokens of the slice that can be among the row's k largest, as keys in the place of its bins, and a
 // bound that k of them reach.  Of every wavefront's 64 largest logits of a lane the q-th largest is taken, q times the wavefronts >= k, and
-// the least of these: k logits reach it.  (k = 50 of 19,000: some 150 tokens pass.)
+// the least of these: k logits reach it.  (k = 50 of 19,000: some 150 tokens pass.)  Where that is no bound, because a mask leaves some
+// wavefronts nothing, or too many reach it, the slice's k-th largest logit is looked for bit by bit; what has no weight beside the slice's
+// largest is not listed then either (masked tokens that are all the same low value).
 template <int TYPE>
-__device__ __forceinline__ void list_largest(const SampleArgs& A, const float (&z)[kGroups][4], Slice S, int k, float top, const RowSpace& R,
-                                             int j, u64* s_key, float* s_bound) {
+__device__ __forceinline__ void list_largest(const SampleArgs& A, const float (&z)[kGroups][4], Slice S, int k, float top, float T,
+                                             const char* row, const RowSpace& R, int j, u64* s_key, float* s_bound) {
     __shared__ uint32_t s_n;
     const int tid = threadIdx.x;
     float mine = -__builtin_inff();
@@ -453,7 +455,42 @@ __device__ __forceinline__ void list_largest(const SampleArgs& A, const float (&
                 }
     }
     __syncthreads();
-    const uint32_t n = s_n;
+    uint32_t n = s_n;
+    // (uniform; lists without a bound may be too many for the row's, if each is short enough)
+    if (n > (uint32_t)(bound > -__builtin_inff() ? kAll : k)) {
+        __shared__ uint32_t s_reach[32];
+        if (tid < 32) s_reach[tid] = 0;
+        __syncthreads();
+        if (tid == 0) s_n = 0;
+        // f(logit, column) for all of the slice's, from memory again: kept in registers for this, they cost all lists 30 that spill
+        auto each = [&](auto f) {
+#pragma unroll 1
+            for (int first = S.first; first < S.last; first += kThreads) {
+                const int i = first + tid;
+                f(i < S.last ? logit<TYPE>(row, i) : -__builtin_inff(), i);
+            }
+        };
+        uint32_t kth = 0;                                        // the largest that k logits reach: n > k are numbers
+#pragma unroll 1
+        for (int bit = 31; bit >= 0; --bit) {
+            const uint32_t x = kth | 1u << bit;
+            uint32_t reach = 0;
+            each([&](float v, int) { reach += __popcll(__ballot(v == v && f32_to_ordered(v) >= x)); });
+            if ((tid & 63) == 0) atomicAdd(&s_reach[bit], reach);
+            __syncthreads();
+            if (s_reach[bit] >= (uint32_t)k) kth = x;
+        }
+        bound = ordered_to_f32(kth);
+        if (regular_slice(T, top)) bound = fmaxf(bound, cut_of(ceil((double)top * log2e_over(T)), T));
+        each([&](float v, int i) {
+            if (v >= bound && v > -__builtin_inff()) {
+                const uint32_t at = atomicAdd(&s_n, 1u);
+                if (at < kAll) s_key[at] = make_key(v, A.ids ? A.ids[i] : i);
+            }
+        });
+        __syncthreads();
+        n = s_n;
+    }
     for (int i = tid; i < (int)min(n, (uint32_t)kAll); i += kThreads) R.mass[(size_t)j * kAll + i] = s_key[i];
     if (tid == 0) {
         R.slice[j] = SliceState{(double)bound, top > -__builtin_inff() ? make_key(top, 0) : 0, n, 0};
@@ -518,7 +555,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_bins_kernel(SampleArgs A, 
         return;
     }
     if (counts && A.top_k[m] <= kMostK) {                        // (uniform)
-        list_largest<TYPE>(A, z, S, A.top_k[m], top, R, j, s_mass, s_max);
+        list_largest<TYPE>(A, z, S, A.top_k[m], top, T, row, R, j, s_mass, s_max);
         return;
     }
     const double c = log2e_over(T);
@@ -813,17 +850,17 @@ __device__ bool finish_largest(const SampleArgs& A, int m, int k, const RowSpace
     const int tid = threadIdx.x, lane = tid & 63;
     fill_table(s_table);
     if (tid == 0) *s_n = 0;
-    // k logits of one slice reach its bound: the largest bound is one for the row
-    float bound = -__builtin_inff();
+    // k logits of one slice reach its bound: the largest bound is one for the row, and so is what has weight
+    float bound = cut_of(ref, A.temperature ? A.temperature[m] : 1.f);
+    for (int j = 0; j < slices; ++j) bound = fmaxf(bound, (float)s_slice[j].ref);
+    // slices below that have nothing here, however many of them are equal
+    auto taken = [&](int j) { return s_slice[j].top != 0 && key_value(s_slice[j].top) >= bound; };
     bool full = false;
-    for (int j = 0; j < slices; ++j) {
-        bound = fmaxf(bound, (float)s_slice[j].ref);
-        full |= s_slice[j].n > (uint32_t)kAll;
-    }
+    for (int j = 0; j < slices; ++j) full |= taken(j) && s_slice[j].n > (uint32_t)kAll;
     if (full) return false;                                      // (uniform)
     __syncthreads();
     for (int j = tid >> 6; j < slices; j += kRowThreads / 64) {
-        const int n = (int)s_slice[j].n;
+        const int n = taken(j) ? (int)s_slice[j].n : 0;
         for (int i = lane; i < n; i += 64) {
             const u64 key = R.mass[(size_t)j * kAll + i];
             if (key_value(key) >= bound) {
@@ -1279,15 +1316,15 @@ __global__ __launch_bounds__(kThreads, 8) void sample_finish_kernel(SampleArgs A
     const RowState st = *R.row;
     if (st.state == kDone) return;
     const int n = (int)*R.ticket;
-    if (st.state == kDigits || n > kList) {
-        sample_by_digits<TYPE>(A, m, s_key, s_part, s_pick);
-        return;
+    bool ended = false;
+    if (st.state == kOpen && n <= kList) {                       // (uniform)
+        fill_table(s_table);
+        for (int b = tid; b <= kAll; b += kThreads) s_before[b] = R.before[b];
+        for (int i = tid; i < n; i += kThreads) s_key[i] = R.list[i];
+        __syncthreads();
+        ended = finish_row(A, m, st, s_key, n, s_sum, s_before, s_table, s_part);
     }
-    fill_table(s_table);
-    for (int b = tid; b <= kAll; b += kThreads) s_before[b] = R.before[b];
-    for (int i = tid; i < n; i += kThreads) s_key[i] = R.list[i];
-    __syncthreads();
-    if (!finish_row(A, m, st, s_key, n, s_sum, s_before, s_table, s_part)) sample_by_digits<TYPE>(A, m, s_key, s_part, s_pick);
+    if (!ended) sample_by_digits<TYPE>(A, m, s_key, s_part, s_pick);
 }
 
 }  // namespace

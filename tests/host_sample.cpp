@@ -8,6 +8,7 @@ extern "C" const char* host_sample(unsigned order, const void* logits, long long
                            const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, const int32_t* ids,
                            int32_t* out_ids, float* out_logprob, void* workspace) {
     wavefronts::order = order;
+    wavefronts::lines.clear();
     const evospec::SampleArgs a{logits, stride, M, V, u, temperature, top_k, top_p, min_p, ids, out_ids, out_logprob};
     static wavefronts::Error error;
     try {
@@ -17,4 +18,9 @@ extern "C" const char* host_sample(unsigned order, const void* logits, long long
         return error.text;
     }
     return nullptr;
+}
+// Barriers of the last call: lines of SAMPLE_SOURCE.
+extern "C" int host_barriers(const int** lines) {
+    *lines = wavefronts::lines.data();
+    return (int)wavefronts::lines.size();
 }

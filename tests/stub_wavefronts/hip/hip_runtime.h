@@ -69,6 +69,7 @@ inline Index block;
 // 0: the first wavefront first, and in a wavefront the last lane; 1: the other way round; others: wavefronts shuffled anew behind every
 // barrier, by this seed
 inline unsigned order = 0;
+inline std::vector<int> lines;                          // of the barriers that were passed, once for each time
 inline uint64_t random_state = 1;
 
 struct Error { char text[160]; };
@@ -151,6 +152,7 @@ inline void run_workgroup(int threads, std::function<void()> body) {
                 t.state = Thread::kReady;
             }
         if (!waiting) return;
+        lines.push_back(line);
     }
 }
 inline void launch(dim3 grid, int threads, std::function<void()> body) {

@@ -356,3 +356,33 @@ def test_slices_on_either_side_of_the_largest_quotient(ev):
     z[0, 3], z[0, V - 5] = -4.0 + 2.0 ** -21, -4.0
     for kw in ({}, dict(top_p=[0.9]), dict(top_k=[400]), dict(top_k=[4])):
         run(ev, z, [0.8], temperature=[2.0 ** -20], **kw)
+
+
+def test_top_k_of_a_range_of_columns(ev):
+    """Only columns of a range are allowed: the same tokens as the definition's, and no row that is gone through again and again (0.8 ms of a
+    workgroup against some 20 us; the borders here are far from both)."""
+    import torch
+    rng = np.random.default_rng(80)
+    M, V = 3, 151936
+
+    def us(z, u, kw):
+        for _ in range(3):
+            ev.sample(z, u, **kw)
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        for _ in range(20):
+            ev.sample(z, u, **kw)
+        b.record()
+        torch.cuda.synchronize()
+        return a.elapsed_time(b) * 50
+
+    u = rng.random(M).astype(np.float32)
+    kw = dict(top_k=torch.tensor([3, 50, 250], dtype=torch.int32, device="cuda"), top_p=torch.full((M,), 0.95, device="cuda"))
+    g = torch.from_numpy(u).cuda()
+    base = us(torch.from_numpy(rng.standard_normal((M, V)).astype(np.float32)).cuda(), g, kw)
+    for mask in (-np.inf, -3.0e38, -1.0e4):
+        for lo, hi in ((0, 3000), (70000, 70900), (0, 400), (100, 150000)):
+            z = np.full((M, V), mask)
+            z[:, lo:hi] = rng.standard_normal((M, hi - lo)) * 2
+            run(ev, z, u, top_k=[3, 50, 250], top_p=[0.95] * M)
+            assert us(torch.from_numpy(z.astype(np.float32)).cuda(), g, kw) < max(8 * base, 250), (mask, lo, hi)
