@@ -466,14 +466,13 @@ __global__ __launch_bounds__(256) void kv_attention_merge_kernel(AttnArgs A) {
     float o[kPer];
 #pragma unroll
     for (int k = 0; k < kPer; ++k) o[k] = 0.f;
-#pragma unroll 4
     for (int j = part; j < A.splits; j += WAVES) {
         const float wj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(j < 64 ? w[0] : w[1]), j & 63));
         const float* from = A.part_o + (j * all + row) * kDim + lane;
 #pragma unroll
         for (int k = 0; k < kPer; ++k) {
             const float v = kDim % 64 == 0 || 64 * k + lane < kDim ? from[64 * k] : 0.f;
-            o[k] += wj == 0.f ? 0.f : wj * v;                    // (a share of nothing was not written)
+            o[k] += wj * v;                                      // (also 0 * NaN: the row saw it, however little it weighs)
         }
     }
     if constexpr (WAVES > 1) {

@@ -93,3 +93,29 @@ def test_graph_of_a_split_call(ev):
         got = out.clone(), lse.clone()
         eager = ev.kv_attention(q, g, table, lens, off, 1, max_len=2560)
         assert torch.equal(got[0], eager[0]) and torch.equal(got[1], eager[1])
+
+
+@pytest.mark.parametrize("n", [1700, 5000])
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
+def test_nan_of_a_share_that_weighs_nothing(ev, n, kind):
+    """V has a NaN at a token whose probability is zero in 32 bits, alone in its share of the tokens or not: zero times NaN."""
+    import torch
+    dim = 64
+    k = torch.full((n, 1, dim), -10.0)
+    k[5] = 10.0
+    v = torch.randn(n, 1, dim, generator=torch.Generator().manual_seed(n))
+    v[n - 40, 0, 7] = float("nan")
+    q = torch.ones(1, 2, dim, dtype=torch.bfloat16, device="cuda")
+    pages = (n + 63) // 64
+    at = i32(np.arange(pages)[None])
+    c = ev.KVCache(pages, 64, 1, dim, kind)
+    ev.kv_write(c, k.to(torch.bfloat16).cuda(), v.to(torch.bfloat16).cuda(), at, i32([0]), i32([0, n]), n)
+    nan = {}
+    for max_len in (1, n):                                       # (one workgroup, and several)
+        assert (splits(ev, c, 2, 1, 1, 1, max_len) > 1) == (max_len == n)
+        out, lse = ev.kv_attention(q, c, at, i32([n]), i32([0, 1]), 1, max_len=max_len)
+        assert torch.isfinite(lse).all()
+        nan[max_len] = torch.isnan(out)
+    want = torch.zeros(1, 2, dim, dtype=torch.bool, device="cuda")
+    want[..., 7] = True
+    assert torch.equal(nan[1], want) and torch.equal(nan[n], want)
