@@ -27,7 +27,8 @@ typedef enum evospec_kv_kind { EVOSPEC_KV_E4M3 = 0, EVOSPEC_KV_INT8 = 1 } evospe
  *            V  [dim / 32][half g][dimension 32 s + d][16 bytes 4 a + i]: token 8 a + 4 g + i
  *          so that 64 lanes take 16 bytes each of 1 KB in a row, and hold operands of the matrix cores.
  *   scales dev fp32, 8-B aligned [pages][heads][page / 32][2]: of K and of V of a block and head.  A value is
- *          code * |scale|; a negative scale says that there may be a NaN among the block's values.
+ *          code * |scale|; a negative scale says that there may be a NaN among the block's values.  A caller's own scales
+ *          are finite; V of a scale below 2^-100, zero among them, counts as zero in the attention.
  * Codes: EVOSPEC_KV_E4M3 (4 exponent and 3 mantissa bits, largest 448, 0x7f is NaN) with scales that are powers of
  * two (the least 2^e, -100 <= e <= 120, with amax <= 448 * 2^e); EVOSPEC_KV_INT8 (-127 .. 127, -128 is NaN) with
  * scale max(amax / 127, 2^-100).

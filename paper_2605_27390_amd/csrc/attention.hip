@@ -228,7 +228,9 @@ __global__ __launch_bounds__(64 * kWaves, NQ >= 6 ? 1 : 2) void kv_attention_ker
         page_next = page_of(b + 2 * kWaves);
         const float sc_x = there ? sc.x : 1.f, sc_y = there ? sc.y : 1.f;
         const float ck = fmaxf(fabsf(sc_x) * (A.scale * kLog2e), 0x1p-126f);       // (not zero: -inf stays what it is)
-        const float sv = fabsf(sc_y), lv = __log2f(sv), iv = __builtin_amdgcn_rcpf(sv);
+        // (V of a scale of zero, which a caller's own may have, is zero: 2^-100 is the least that kv_write gives)
+        const bool v_zero = fabsf(sc_y) < 0x1p-100f;
+        const float sv = v_zero ? 0x1p-100f : fabsf(sc_y), lv = __log2f(sv), iv = __builtin_amdgcn_rcpf(sv);
 
         uint32_t nan_tokens = 0;                                 // of K (e4m3's NaN code is one for the matrix cores)
         if (KIND == EVOSPEC_KV_INT8 && __float_as_uint(sc_x) >> 31) {
@@ -305,7 +307,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ >= 6 ? 1 : 2) void kv_attention_ker
             pf[rt][1] = __builtin_bit_cast(u32x4, p[1]);
         }
         __builtin_amdgcn_sched_barrier(0);
-        const int end = there ? len : t0;
+        const int end = there && !v_zero ? len : t0;
         if (t0 + kBlock > end) {                                 // bytes behind the last token may be anything
 #pragma unroll
             for (int k = 0; k < NQ; ++k)

@@ -119,3 +119,26 @@ def test_nan_of_a_share_that_weighs_nothing(ev, n, kind):
     want = torch.zeros(1, 2, dim, dtype=torch.bool, device="cuda")
     want[..., 7] = True
     assert torch.equal(nan[1], want) and torch.equal(nan[n], want)
+
+
+@pytest.mark.parametrize("kind,type", [("e4m3", "bf16"), ("int8", "fp16")])
+@pytest.mark.parametrize("zero", [0.0, -0.0, 2.0 ** -140])
+def test_scales_of_zero(ev, kind, type, zero):
+    """A caller's own scales: those of V and of K that are zero, or next to it, make values of zero, whatever the codes are."""
+    import torch
+    rng = np.random.default_rng(50)
+    dim, page, lens, rows = 64, 64, [300, 40], [3, 1]
+    for part in (0, 1, 2):                                       # K, V, both
+        for share in (0.3, 1.0):
+            c = ref.Cache(12, page, 2, dim, kind, rng)
+            table = rng.permutation(12)[:10].reshape(2, 5)
+            w = [part] if part < 2 else [0, 1]
+            for i in w:
+                c.scales[..., i][rng.random(c.scales[..., i].shape) < share] = zero
+            q = torch.from_numpy(rng.standard_normal((4, 4, dim))).to(torch_type(type))
+            off = [0, 3, 4]
+            out, lse = attend(ev, to_gpu(ev, c), c, q, table, lens, off, type)
+            want = bounds.attention(c, q.double().numpy(), table, lens, off, 2, type)
+            assert bounds.differs(out, lse, want) is None, (part, share)
+            if part and share == 1.0:
+                assert (out == 0).all()
