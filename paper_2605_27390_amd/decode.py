@@ -15,6 +15,14 @@ _i32, _f32 = torch.int32, torch.float32
 _new = torch.empty_strided      # (strides spelled out: 0.9 us a tensor, torch.empty 1.6)
 
 
+def _stream_of(device):
+    """The current stream, for tensors of GPU `device`: work goes to the current GPU, which may not reach another one's memory."""
+    current = _get_device()
+    if device != current:
+        raise ValueError(f"tensors are on GPU {device}, and the current one is {current}")
+    return _raw_stream(current)
+
+
 class _Cache(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("scales", ctypes.c_void_p)] + [
         (n, ctypes.c_int) for n in ("pages", "page", "heads", "dim", "kind")]
@@ -79,40 +87,50 @@ class KVCache:
             data = torch.empty(n_data, dtype=torch.uint8, device=device)
         if scales is None:
             scales = torch.empty(n_scales // 4, dtype=torch.float32, device=device)
-        if not (data.dtype is torch.uint8 and scales.dtype is _f32 and data.is_cuda and scales.is_cuda and data.is_contiguous()
+        dev = data.get_device()
+        if not (data.dtype is torch.uint8 and scales.dtype is _f32 and dev >= 0 and scales.get_device() == dev and data.is_contiguous()
                 and scales.is_contiguous()):
             _expect(data, torch.uint8, "data")
             _expect(scales, _f32, "scales")
+            raise ValueError("data and scales are on different GPUs")
         if data.numel() < n_data or scales.numel() * 4 < n_scales:
             raise ValueError("data or scales is smaller than evospec_kv_cache_bytes reports")
-        self.data, self.scales = data, scales
+        self.data, self.scales, self._device = data, scales, dev
         self._c = _Cache(data.data_ptr(), scales.data_ptr(), pages, page, heads, dim, _KINDS[kind])
         self._ref = ctypes.byref(self._c)
 
 
-def _rows(page_table, at, name, row_off):
-    """(width, S) of the index tensors of a call.  (Checks here and below are written out: a call is about 4 us of launch, and
-    a function for each check cost another 3.)"""
+def _elsewhere(t, dev, name):
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on GPU {t.get_device()}, others are on {dev}")
+
+
+def _rows(page_table, at, name, row_off, dev):
+    """(width, S) of the index tensors of a call, which are on GPU `dev`.  (Checks here and below are written out: a call is about
+    4 us of launch, and a function for each check cost another 3.)"""
     try:
-        ok = (page_table.dtype is at.dtype is row_off.dtype is _i32 and page_table.is_cuda and at.is_cuda and row_off.is_cuda
+        ok = (page_table.dtype is at.dtype is row_off.dtype is _i32
+              and page_table.get_device() == at.get_device() == row_off.get_device() == dev
               and page_table.dim() == 2 and at.dim() == row_off.dim() == 1
               and page_table.is_contiguous() and at.is_contiguous() and row_off.is_contiguous())
     except AttributeError:
         ok = False
     if not ok:
-        _expect(page_table, _i32, "page_table", 2)
-        _expect(at, _i32, name, 1)
-        _expect(row_off, _i32, "row_off", 1)
+        for t, n, ndim in ((page_table, "page_table", 2), (at, name, 1), (row_off, "row_off", 1)):
+            _expect(t, _i32, n, ndim)
+            _elsewhere(t, dev, n)
     S, width = page_table.shape
     if at.numel() != S or row_off.numel() != S + 1:
         raise ValueError(f"page_table, {name} and row_off disagree about the number of sequences")
     return width, S
 
 
-def _strided(x, heads, dim, name):
-    """Row stride in elements of a GPU tensor [T, heads, dim] whose rows are contiguous in themselves."""
-    if not isinstance(x, torch.Tensor) or not x.is_cuda:
-        raise TypeError(f"{name} must be a GPU torch tensor")
+def _strided(x, heads, dim, name, dev):
+    """Row stride in elements of a tensor [T, heads, dim] on GPU `dev` whose rows are contiguous in themselves."""
+    if not isinstance(x, torch.Tensor) or x.get_device() != dev:
+        if not isinstance(x, torch.Tensor) or not x.is_cuda:
+            raise TypeError(f"{name} must be a GPU torch tensor")
+        _elsewhere(x, dev, name)
     if x.dim() != 3 or x.size(1) != heads or x.size(2) != dim:
         raise ValueError(f"{name} must be [rows, {heads}, {dim}], got {tuple(x.shape)}")
     s = x.stride()
@@ -124,8 +142,8 @@ def _strided(x, heads, dim, name):
 def kv_write(cache: KVCache, k, v, page_table, starts, row_off, max_rows: int) -> None:
     """Quantise rows row_off[s] .. row_off[s + 1] of k and v [T, heads, dim] into the cache as the tokens starts[s],
     starts[s] + 1, ... of sequence s.  No sequence may have more than max_rows of them."""
-    width, S = _rows(page_table, starts, "starts", row_off)
-    ks, vs = _strided(k, cache.heads, cache.dim, "k"), _strided(v, cache.heads, cache.dim, "v")
+    width, S = _rows(page_table, starts, "starts", row_off, cache._device)
+    ks, vs = _strided(k, cache.heads, cache.dim, "k", cache._device), _strided(v, cache.heads, cache.dim, "v", cache._device)
     type_ = _TYPES.get(k.dtype)
     if type_ is None or v.dtype != k.dtype:
         raise TypeError(f"k and v must share one of {list(_TYPES)}")
@@ -133,13 +151,13 @@ def kv_write(cache: KVCache, k, v, page_table, starts, row_off, max_rows: int) -
     if v.size(0) != T:
         raise ValueError("k and v differ in length")
     _check(lib.evospec_kv_write(cache._ref, k.data_ptr(), ks, v.data_ptr(), vs, type_, T, page_table.data_ptr(),
-                                width, starts.data_ptr(), row_off.data_ptr(), S, max_rows, _raw_stream(_get_device())), "evospec_kv_write")
+                                width, starts.data_ptr(), row_off.data_ptr(), S, max_rows, _stream_of(cache._device)), "evospec_kv_write")
 
 
 def kv_read(cache: KVCache, page_table, starts, row_off, max_rows: int, rows: int, dtype=torch.bfloat16, out_k=None, out_v=None):
     """The values of the tokens starts[s], starts[s] + 1, ... of every sequence as rows row_off[s] .. row_off[s + 1]:
     (k, v), `dtype` [rows, heads, dim].  Rows that belong to no sequence are left as they are."""
-    width, S = _rows(page_table, starts, "starts", row_off)
+    width, S = _rows(page_table, starts, "starts", row_off, cache._device)
     if dtype not in _TYPES:
         raise TypeError(f"dtype must be one of {list(_TYPES)}")
     rows = int(rows)
@@ -147,6 +165,7 @@ def kv_read(cache: KVCache, page_table, starts, row_off, max_rows: int, rows: in
     for t, name in ((out_k, "out_k"), (out_v, "out_v")):
         if t is not None:
             _expect(t, dtype, name, 3)
+            _elsewhere(t, cache._device, name)
             if tuple(t.shape) != shape:
                 raise ValueError(f"{name} must be {shape}, got {tuple(t.shape)}")
     if out_k is None:
@@ -154,7 +173,7 @@ def kv_read(cache: KVCache, page_table, starts, row_off, max_rows: int, rows: in
     if out_v is None:
         out_v = _new(shape, (cache.heads * cache.dim, cache.dim, 1), dtype=dtype, device=cache.data.device)
     _check(lib.evospec_kv_read(cache._ref, page_table.data_ptr(), width, starts.data_ptr(), row_off.data_ptr(), S, max_rows, rows,
-                               _TYPES[dtype], out_k.data_ptr(), out_v.data_ptr(), _raw_stream(_get_device())), "evospec_kv_read")
+                               _TYPES[dtype], out_k.data_ptr(), out_v.data_ptr(), _stream_of(cache._device)), "evospec_kv_read")
     return out_k, out_v
 
 
@@ -169,19 +188,20 @@ def kv_attention(q, cache: KVCache, page_table, lens, row_off, max_rows: int, ma
     the tokens up to its own; with `tree` (int64 [T], bit j: the row sees the j-th of the sequence's rows) it sees all that
     come before the sequence's rows, and those of its bits.  `scale` is 1 / sqrt(dim) if not given; max_len (a bound of lens)
     only decides how the work is split."""
-    width, S = _rows(page_table, lens, "lens", row_off)
+    width, S = _rows(page_table, lens, "lens", row_off, cache._device)
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a tensor [rows, query heads, dim]")
     T, heads, dim = q.shape
     group = heads // cache.heads
     if group * cache.heads != heads:
         raise ValueError("q must have a multiple of the cache's heads")
-    qs = _strided(q, heads, cache.dim, "q")
+    qs = _strided(q, heads, cache.dim, "q", cache._device)
     type_ = _TYPES.get(q.dtype, 2)
     if type_ == 2:
         raise TypeError(f"q must be bfloat16 or float16, got {q.dtype}")
     if tree is not None:
         _expect(tree, torch.int64, "tree", 1)
+        _elsewhere(tree, cache._device, "tree")
         if tree.shape[0] != T:
             raise ValueError("tree needs a word for every row of q")
     max_len = min(width * cache.page, 1 << 30) if max_len is None else int(max_len)
@@ -189,23 +209,26 @@ def kv_attention(q, cache: KVCache, page_table, lens, row_off, max_rows: int, ma
         out = _new((T, heads, dim), (heads * dim, dim, 1), dtype=q.dtype, device=q.device)
     else:
         _expect(out, q.dtype, "out", 3)
+        _elsewhere(out, cache._device, "out")
         if out.shape != q.shape:
             raise ValueError("out must have q's shape")
     if out_lse is None:
         out_lse = _new((T, heads), (heads, 1), dtype=_f32, device=q.device)
     else:
         _expect(out_lse, torch.float32, "out_lse", 2)
+        _elsewhere(out_lse, cache._device, "out_lse")
         if tuple(out_lse.shape) != (T, heads):
             raise ValueError("out_lse must be [rows, query heads]")
     if workspace is not None:
         _expect(workspace, torch.uint8, "workspace")
+        _elsewhere(workspace, cache._device, "workspace")
     else:
         need = _attention_bytes(cache.pages, cache.page, cache.heads, cache.dim, cache._c.kind, group, S, T, max_rows, max_len)
         workspace = _new((need,), (1,), dtype=torch.uint8, device=q.device) if need else None
     _check(lib.evospec_kv_attention(cache._ref, q.data_ptr(), qs, type_, T, group, page_table.data_ptr(), width,
                                     lens.data_ptr(), row_off.data_ptr(), S, max_rows, max_len, _ptr(tree),
                                     dim ** -0.5 if scale is None else scale, out.data_ptr(), out_lse.data_ptr(), _ptr(workspace),
-                                    0 if workspace is None else workspace.numel(), _raw_stream(_get_device())), "evospec_kv_attention")
+                                    0 if workspace is None else workspace.numel(), _stream_of(cache._device)), "evospec_kv_attention")
     return out, out_lse
 
 
@@ -219,8 +242,9 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, ids=
     temperature, top_p, min_p are fp32 [M], top_k int32 [M], each may be None (1, all, all, all).  ids (int32 [V]) are the
     columns' token ids, as of an active vocabulary.  What is kept, and in which order u runs through it, is in
     include/evospec_decode.h; temperature 0 takes the largest logit."""
-    if not isinstance(logits, torch.Tensor) or not logits.is_cuda:
+    if not isinstance(logits, torch.Tensor) or logits.get_device() < 0:
         raise TypeError("logits must be a GPU torch tensor")
+    dev = logits.get_device()
     if logits.dtype not in _TYPES:
         raise TypeError(f"logits must be one of {list(_TYPES)}")
     if logits.dim() != 2 or (logits.stride(1) != 1 and logits.shape[1] > 1):
@@ -229,28 +253,32 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, ids=
     for t, dtype, name in ((u, torch.float32, "u"), (temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
                            (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p")):
         if t is not None or name == "u":
-            if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.dim() == 1 and t.is_contiguous()):
+            if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == dev and t.dim() == 1 and t.is_contiguous()):
                 _expect(t, dtype, name, 1)
+                _elsewhere(t, dev, name)
             if t.numel() != M:
                 raise ValueError(f"{name} needs a value for every row")
     if ids is not None:
         _expect(ids, torch.int32, "ids", 1)
+        _elsewhere(ids, dev, "ids")
         if ids.shape[0] != V:
             raise ValueError("ids needs an id for every column")
     for t, dtype, name in ((out_ids, _i32, "out_ids"), (out_logprob, _f32, "out_logprob")):
         if t is not None:
             _expect(t, dtype, name, 1)
+            _elsewhere(t, dev, name)
             if t.numel() != M:
                 raise ValueError(f"{name} needs a place for every row")
     out_ids = _new((M,), (1,), dtype=_i32, device=logits.device) if out_ids is None else out_ids
     out_logprob = _new((M,), (1,), dtype=_f32, device=logits.device) if out_logprob is None else out_logprob
     if workspace is not None:
         _expect(workspace, torch.uint8, "workspace")
+        _elsewhere(workspace, dev, "workspace")
     else:
         need = _sample_bytes(M, V)
         workspace = _new((need,), (1,), dtype=torch.uint8, device=logits.device) if need else None
     _check(lib.evospec_sample(logits.data_ptr(), logits.stride(0) if M > 1 else V, _TYPES[logits.dtype], M, V, u.data_ptr(),
                               _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(ids), out_ids.data_ptr(),
-                              out_logprob.data_ptr(), _ptr(workspace), 0 if workspace is None else workspace.numel(), _raw_stream(_get_device())),
+                              out_logprob.data_ptr(), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_of(dev)),
            "evospec_sample")
     return out_ids, out_logprob
