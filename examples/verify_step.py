@@ -42,6 +42,7 @@ class Loop:
         ev.active_gather(self.W_lm, ids, None, self.W_act, self.act_ids)
         # the cache: every sequence has its pages
         width = capacity // page
+        self.capacity = width * page                          # tokens of a sequence, the nodes of a tree among them
         self.cache = ev.KVCache(S * width, page, heads, dim, kind)
         self.table = torch.randperm(S * width, generator=g, device="cuda").to(torch.int32).view(S, width)
         self.lens = [0] * S                                   # tokens in the cache
@@ -75,6 +76,9 @@ class Loop:
         """One round of drafting and verification; returns what the target saw (for a look from outside)."""
         nodes = self.trees()
         rows = [len(n) for n in nodes]
+        for s, (n, r) in enumerate(zip(self.lens, rows)):
+            if n + r > self.capacity:                         # (tokens past the page table are dropped, and rows would lose their places)
+                raise ValueError(f"sequence {s} has {n} tokens, and {r} nodes more do not fit its {self.capacity}")
         off = [0]
         for n in rows:
             off.append(off[-1] + n)
@@ -130,6 +134,9 @@ def main():
     a = p.parse_args()
     loop = Loop()
     for i in range(a.steps):
+        if max(loop.lens) + 1 + WIDTH * DEPTH > loop.capacity:
+            print(f"after {i} steps: no room for another tree")
+            break
         r = loop.step(temperature=a.temperature)
         print(f"step {i}: tokens per sequence {[len(x) for x in r['grown']]}, lengths {loop.lens}")
     for s, t in enumerate(loop.tokens):

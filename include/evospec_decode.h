@@ -79,7 +79,9 @@ int evospec_kv_read(const evospec_kv_cache *cache, const int32_t *page_table, in
  * Values of tokens that a row does not see, NaN among them, do not reach it.
  *   q         dev `type` (EVOSPEC_BF16 or EVOSPEC_FP16) [T, heads * group, dim], rows q_stride elements apart and 16-B aligned
  *   lens      dev int32 [S]            row_off, max_rows as above (rows past max_rows of a sequence are not written)
- *   max_len   host: no lens[s] is larger (only the split of the work depends on it; lens are clamped to width * page and 2^30)
+ *   max_len   host: no lens[s] is larger (only the split of the work depends on it)
+ *             A lens[s] above width * page or 2^30 is taken as that, which moves the positions of its rows as well: they then
+ *             stand for the last n tokens that the table has.  Callers keep lengths, new rows among them, within the table.
  *   tree      dev uint64 [T] or NULL   scale host, > 0 and finite
  *   out       dev `type` [T, heads * group, dim] contiguous, 16-B aligned       lse dev fp32 [T, heads * group] or NULL
  *   workspace dev, 16-B aligned, at least evospec_kv_attention_workspace_bytes(...) bytes, scratch

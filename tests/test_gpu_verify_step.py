@@ -71,3 +71,22 @@ def test_command_line(example, capsys, monkeypatch):
     monkeypatch.setattr("sys.argv", ["verify_step.py", "--steps", "2"])
     example.main()
     assert "step 1" in capsys.readouterr().out
+
+
+def test_a_full_cache(example, capsys, monkeypatch):
+    """The last tree that fits is taken, the next one is refused, and the command ends in front of it."""
+    loop = example.Loop(S=2, capacity=64, seed=3)
+    nodes = 1 + example.WIDTH * example.DEPTH
+    while max(loop.lens) + nodes <= 64:
+        before = list(loop.lens)
+        loop.step()
+        assert all(a < b for a, b in zip(before, loop.lens))
+    before, tokens = list(loop.lens), [list(t) for t in loop.tokens]
+    with pytest.raises(ValueError, match="do not fit"):
+        loop.step()
+    assert loop.lens == before and loop.tokens == tokens
+    whole = example.Loop
+    monkeypatch.setattr(example, "Loop", lambda: whole(S=2, capacity=64, seed=3))
+    monkeypatch.setattr("sys.argv", ["verify_step.py", "--steps", "100"])
+    example.main()
+    assert "no room" in capsys.readouterr().out
