@@ -386,3 +386,36 @@ def test_top_k_of_a_range_of_columns(ev):
             z[:, lo:hi] = rng.standard_normal((M, hi - lo)) * 2
             run(ev, z, u, top_k=[3, 50, 250], top_p=[0.95] * M)
             assert us(torch.from_numpy(z.astype(np.float32)).cuda(), g, kw) < max(8 * base, 250), (mask, lo, hi)
+
+
+@pytest.mark.parametrize("type", ["fp32", "bf16"])
+def test_long_tails_of_equal_weights(ev, type):
+    """Weights are whole multiples of 2^-43, and equal ones are rounded the same way, so that errors add up: over V tokens to V 2^-44, and once
+    more where slices' sums are joined; each weight is off by 2^-39 of itself besides.  u's place among the drawn token's borders is
+    right to V 2^-43 + 2^-38 of the sum, and the token is the definition's wherever no border is as near."""
+    import torch
+    V = int(0.9 * 2 ** 20)
+    near = V * 2.0 ** -43 + 2.0 ** -38
+    u = np.array([1 - 5 * 2.0 ** -24, 1 - 2.0 ** -24, 1 - 2.0 ** -20, 0.999], dtype=np.float32)
+    for tail in (2.55, 2.45, 4.5, 100.5):
+        z = np.full((len(u), V), np.log(tail * 2.0 ** -43))
+        z[:, 777] = 0.0
+        t = torch.from_numpy(z).to(torch.float32 if type == "fp32" else torch.bfloat16)
+        d = t.double().numpy()
+        for kw in ({}, dict(top_p=[0.99999994] * len(u)), dict(top_k=[V - 1] * len(u))):
+            dev = {k: torch.tensor(v, dtype=torch.int32 if k == "top_k" else torch.float32, device="cuda") for k, v in kw.items()}
+            got, lp = ev.sample(t.cuda(), torch.from_numpy(u).cuda(), **dev)
+            for m, j in enumerate(got.tolist()):
+                w = float(np.exp(d[m, 0]))                       # of every token of the tail, which go by id behind the first
+                n = V - 1
+                if "top_k" in kw:
+                    n -= 1
+                if "top_p" in kw:                                # the cut itself may be as far off
+                    n = int(min(n, max(0, np.ceil((np.float32(0.99999994) * (1 + n * w) - 1) / w))))
+                total = 1 + n * w
+                place = 0 if j == 777 else 1 + (j if j < 777 else j - 1) * w
+                size = 1 if j == 777 else w
+                assert place / total - 2 * near <= float(u[m]) <= (place + size) / total + 2 * near, (tail, kw, m, j)
+                want = np.log(size / total)
+                # (the tail's own weight in 43 bits is not in the logprob: its logit is)
+                assert abs(float(lp[m]) - want) <= 2.0 ** -23 * (1 + abs(want)) + 2 * near
