@@ -86,9 +86,10 @@ __device__ __forceinline__ float logit(const void* row, int i) {
 __device__ __forceinline__ u64 shfl_xor64(u64 x, int s) {
     return (u64)(uint32_t)__shfl_xor((int)(uint32_t)x, s) | (u64)(uint32_t)__shfl_xor((int)(uint32_t)(x >> 32), s) << 32;
 }
-__device__ __forceinline__ u64 sum_lanes(u64 x) {
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) x += shfl_xor64(x, s);
+__device__ __forceinline__ u64 sum_eight(u64 x, int lane) {
+    x += (u64)xor_lane<1>((uint32_t)(x >> 32), lane) << 32 | xor_lane<1>((uint32_t)x, lane);
+    x += (u64)xor_lane<2>((uint32_t)(x >> 32), lane) << 32 | xor_lane<2>((uint32_t)x, lane);
+    x += (u64)xor_lane<4>((uint32_t)(x >> 32), lane) << 32 | xor_lane<4>((uint32_t)x, lane);
     return x;
 }
 __device__ __forceinline__ u64 first_lane(u64 x) {
@@ -245,7 +246,9 @@ __device__ __forceinline__ void sample_by_digits(const SampleArgs& A, int m, u64
 // ends the row.  Lists that are full (thousands of tokens within 1 / kBins of a power of two) leave the row to sample_by_digits.
 constexpr int kBins = 32;                         // to a factor of 2
 constexpr int kRange = 44;                        // factors of 2 that are kept,
-constexpr int kAll = kBins * 28;                  // those behind the 28th in the last bin
+constexpr int kFine = kBins * 28;                 // those behind the 28th have a bin each, which slices' references move as they move the
+constexpr int kAll = kFine + kRange - 28;         // fine ones: what is in a bin of the row is what has weight there
+constexpr int kPlaces = kRange * kBins;           // all of them fine
 constexpr int kGroups = 5;                        // of 4 logits of a thread
 constexpr int kSlice = kThreads * 4 * kGroups;
 constexpr int kMostSlices = ((1 << 20) + kSlice - 1) / kSlice;
@@ -337,9 +340,15 @@ __device__ __forceinline__ u64 weight_of(Steps s, const double* table) {
     return (u64)__double_as_longlong(d) & 0xfffffffffffffull;    // 2^52 + the weight, rounded to a whole number
 }
 static_assert(kSteps == kBins, "a step is a bin");
-__device__ __forceinline__ int bin_of(int m) { return min(m, kAll - 1); }
-// logits below this have no weight
-__device__ __forceinline__ float cut_of(double ref, float T) { return (float)((ref - kRange) * ((double)T * 0.69314718055994530942)); }
+// (the second is the smaller one from kFine on; kAll for what has no weight)
+__device__ __forceinline__ int bin_of(int m) { return min(m, kFine - kFine / kBins + (int)((uint32_t)m / kBins)); }
+// the least m of a bin
+__device__ __forceinline__ int first_of(int bin) { return bin < kFine ? bin : (bin - (kFine - kFine / kBins)) * kBins; }
+// logits below this have no weight; a little lower, as it is rounded to 32 bits: `m` decides
+__device__ __forceinline__ float cut_of(double ref, float T) {
+    const double z = (ref - kRange) * ((double)T * 0.69314718055994530942);
+    return (float)(z - fabs(z) * 0x1p-22);
+}
 __device__ __forceinline__ bool has_weight(float z, float cut, Steps s) { return z >= cut && (uint32_t)s.m < (uint32_t)(kRange * kSteps); }
 
 struct Slice {
@@ -896,7 +905,6 @@ __device__ bool finish_largest(const SampleArgs& A, int m, int k, const RowSpace
     return true;
 }
 static_assert(kMostK <= kRowThreads, "one token a thread");
-constexpr int kPer = (kAll + kRowThreads - 1) / kRowThreads;     // bins of a thread
 
 template <int TYPE>
 __device__ __forceinline__ const char* row_of(const SampleArgs& A, int m) {
@@ -907,34 +915,43 @@ template <class Put>
 __device__ __forceinline__ void pick_tokens(const SampleArgs& A, Slice S, const float (&z)[kGroups][4], const RowState& st, float T,
                                             Put put) {
     const double c = log2e_over(T);
-    const int b_min = min(st.lo[0], min(st.lo[1], st.lo[2])), b_max = max(st.hi[0], max(st.hi[1], st.hi[2]));
+    const int b_max = max(st.hi[0], max(st.hi[1], st.hi[2]));
     // logits that can be in those bins, a little generously: bin b ends where x = -(b + 1) / kBins, to half a step
     const double far = (st.ref - (double)(b_max + 2) * (1.0 / kBins)) * ((double)T * 0.69314718055994530942);
-    const float cut = cut_of(st.ref, T), least = b_max == kAll - 1 ? cut : fmaxf(cut, (float)(far - fabs(far) * 0x1p-20));
+    const float cut = cut_of(st.ref, T), least = b_max >= kFine ? cut : fmaxf(cut, (float)(far - fabs(far) * 0x1p-20));
     const int ref_steps = (int)st.ref * kSteps;
+    int from[3], to[3];                                          // of m, the bins' (to: none has weight behind the last)
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        from[i] = first_of(st.lo[i]);
+        to[i] = first_of(st.hi[i] + 1);
+    }
 #pragma unroll
     for (int g = 0; g < kGroups; ++g)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if (z[g][e] >= least) {
-                const Steps s = locate(z[g][e], c, ref_steps);
-                const int b = bin_of(s.m);
-                if ((uint32_t)s.m < (uint32_t)(kRange * kSteps) && b >= b_min && b <= b_max &&
-                    ((b >= st.lo[0] && b <= st.hi[0]) || (b >= st.lo[1] && b <= st.hi[1]) || (b >= st.lo[2] && b <= st.hi[2]))) {
+                const int m = locate(z[g][e], c, ref_steps).m;
+                if ((m >= from[0] && m < to[0]) || (m >= from[1] && m < to[1]) || (m >= from[2] && m < to[2])) {
                     const int i = S.at(g, e);
                     put(make_key(z[g][e], A.ids ? A.ids[i] : i));
                 }
             }
 }
 
-// The part of one wavefront of finish_row below.
-__device__ __forceinline__ bool draw_from_list(const SampleArgs& A, int m, const RowState& st, const u64* s_key, int n, const u64* s_sum,
-                                               const u64* s_before, double c) {
-    const int lane = threadIdx.x & 63;
-    bool lost = false;
-    auto bin_at = [&](int i) { return bin_of(locate(key_value(s_key[i]), c, (int)st.ref * kSteps).m); };
+// Goes through the filters with a row's list (n tokens in LDS, in any order) and the sums of its bins.
+__device__ void finish_row(const SampleArgs& A, int m, const RowState& st, u64* s_key, int n, u64* s_sum, const u64* s_before,
+                           const double* s_table, u64* s_part) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    const double c = log2e_over(A.temperature ? A.temperature[m] : 1.f);
+    sort_keys<kThreads>(s_key, n);
+    sum_weights<kThreads, kList / kThreads>(s_key, s_sum, n, A.temperature ? A.temperature[m] : 1.f, st.ref, s_table, s_part);
+    if (tid >= 64) return;
+    // One wavefront goes through the filters.  Every place is an index into the sorted list.
+    auto m_at = [&](int i) { return locate(key_value(s_key[i]), c, (int)st.ref * kSteps).m; };
+    auto bin_at = [&](int i) { return bin_of(m_at(i)); };
     // the first place of the list in bin b or behind
-    auto place_of = [&](int b) { return search(0, n, lane, [&](int i) { return bin_at(i) >= b; }); };
+    auto place_of = [&](int b) { return search(0, n, lane, [&](int i) { return m_at(i) >= first_of(b); }); };
     auto sum_to = [&](int i) { return i > 0 ? s_sum[i - 1] : 0ull; };
     // the weight of the row's tokens in front of the list's place i
     auto before = [&](int i) {
@@ -946,29 +963,21 @@ __device__ __forceinline__ bool draw_from_list(const SampleArgs& A, int m, const
     auto place_at = [&](u64 target) {
         const int bin = min(search(0, kAll, lane, [&](int b) { return s_before[b + 1] >= target; }), kAll - 1);
         const int first = place_of(bin), end = place_of(bin + 1);
-        lost |= first == end;
         const u64 rest = target - s_before[bin] + sum_to(first);
         const int i = search(first, end, lane, [&](int i) { return s_sum[i] >= rest; });
-        return max(min(i, end - 1), 0);                          // (the last of the bin if rounding leaves it short)
+        return max(min(i, min(end, n) - 1), 0);                  // (the last of the bin if rounding leaves it short)
     };
     int last = n;                                                // the place of the last token that is kept; n: all of the row are
     u64 kept = s_before[kAll];
     if (st.k_bin >= 0) {
-        const int first = place_of(st.k_bin), end = place_of(st.k_bin + 1);
-        if (first < end) {
-            last = min(first + st.k_left, n) - 1;
-            kept = upto(last);
-        } else {
-            // none of its tokens is on the list: a slice counted them in its last bin, and in the row they weigh nothing
-            kept = s_before[st.k_bin];
-        }
+        last = min(place_of(st.k_bin) + st.k_left, n) - 1;
+        kept = upto(last);
     }
     const float p = A.top_p ? A.top_p[m] : 1.f;
     if (p < 1.f) {
         kept = share_up(p, kept);
         if (s_before[st.end_bin + 1] >= kept) {                  // (otherwise min-p cuts in front of that)
             last = min(last, place_at(kept));
-            if (lost) return false;
             kept = upto(last);
         }
     }
@@ -986,50 +995,30 @@ __device__ __forceinline__ bool draw_from_list(const SampleArgs& A, int m, const
         }
     }
     int at = place_at(share_past(A.u[m], kept));
-    if (lost) return false;
     if (last < n) at = min(at, last);
-    if (lane == 0) give(A, m, s_key[at], kept, c, st.ref);
-    return true;
-}
-
-// Goes through the filters with a row's list (n tokens in LDS, in any order) and the sums of its bins.  False, and nothing given, where a
-// border falls into a bin that has weight but no token on the list (the last bin, by tokens of less than 2^-44 of the row's first).
-__device__ bool finish_row(const SampleArgs& A, int m, const RowState& st, u64* s_key, int n, u64* s_sum, const u64* s_before,
-                           const double* s_table, u64* s_part) {
-    const int tid = threadIdx.x;
-    const double c = log2e_over(A.temperature ? A.temperature[m] : 1.f);
-    sort_keys<kThreads>(s_key, n);
-    sum_weights<kThreads, kList / kThreads>(s_key, s_sum, n, A.temperature ? A.temperature[m] : 1.f, st.ref, s_table, s_part);
-    // One wavefront goes through the filters.  Every place is an index into the sorted list.
-    __shared__ int s_lost;
-    if (tid < 64) {
-        const bool lost = !draw_from_list(A, m, st, s_key, n, s_sum, s_before, c);
-        if (tid == 0) s_lost = lost;
-    }
-    __syncthreads();
-    return !s_lost;
+    if (tid == 0) give(A, m, s_key[at], kept, c, st.ref);
 }
 
 // Joins the bins of a row's slices (s_before[b] = what lies in front of bin b) and says which bins have to be looked at.
 __device__ __forceinline__ RowState plan_row(const SampleArgs& A, int m, const RowSpace& R, const SliceState* s_slice, int slices, int k, float T,
-                                             double c, double ref, float z_max, u64* s_before, uint32_t* s_first, u64* s_part,
+                                             double c, double ref, float z_max, u64* s_before, u64* s_place, uint32_t* s_first, u64* s_part,
                                              uint32_t* s_num, int* s_found) {
     const int tid = threadIdx.x, lane = tid & 63;
-    // the slices' bins, joined: bin b of a slice whose reference is `shift` factors of 2 lower goes to b + shift kBins, or the last
-    static_assert(kAll <= kRowThreads, "a bin a thread");
+    // the slices' bins, joined: those of a slice whose reference is `shift` factors of 2 lower go as many factors further
+    static_assert(kAll < kRowThreads, "a bin a thread");
     __shared__ int s_shift[kMostSlices];
     if (tid < slices) {
         const SliceState s = s_slice[tid];
         const double gap = s.top != 0 && regular_slice(T, key_value(s.top)) ? ref - s.ref : kRange;      // (a whole number >= 0)
         s_shift[tid] = gap < kRange ? (int)gap : -1;
     }
-    if (tid <= kAll) {
-        s_before[tid] = 0;
-        s_first[tid] = 0;
+    // (a row's bins behind kFine are 32 places each until all slices are there: lanes that add to one place of LDS go one by one)
+    for (int i = tid; i < kPlaces; i += kRowThreads) {
+        s_place[i] = 0;
+        if (k > 0) s_first[i] = 0;
     }
     __syncthreads();
-    u64 past = 0;                                                // of bins behind the last
-    uint32_t num_past = 0;
+    const int mine = tid < kFine ? tid : kFine + (tid - kFine) * kBins;
     constexpr int kAtOnce = 8;
     for (int first = 0; first < slices; first += kAtOnce) {
         u64 w[kAtOnce];
@@ -1037,51 +1026,40 @@ __device__ __forceinline__ RowState plan_row(const SampleArgs& A, int m, const R
         for (int i = 0; i < kAtOnce; ++i) w[i] = R.mass[(size_t)min(first + i, slices - 1) * kAll + min(tid, kAll - 1)];
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) {
-            const int j = first + i, shift = __builtin_amdgcn_readfirstlane(j < slices ? s_shift[j] : -1), to = tid + shift * kBins;
+            const int j = first + i, shift = __builtin_amdgcn_readfirstlane(j < slices ? s_shift[j] : -1), to = mine + shift * kBins;
             if (shift < 0) continue;                             // (uniform)
-            const u64 x = shift ? (w[i] + (1ull << (shift - 1))) >> shift : w[i];
-            const uint32_t n = k > 0 && tid < kAll ? R.count[(size_t)j * kAll + tid] : 0;
-            if (to < kAll) {
-                atomicAdd(&s_before[to], x);
-                if (k > 0) atomicAdd(&s_first[to], n);
-            } else if (tid < kAll) {
-                past += x;
-                num_past += n;
+            if (tid < kAll && to < kPlaces) {
+                atomicAdd(&s_place[to], shift ? (w[i] + (1ull << (shift - 1))) >> shift : w[i]);
+                if (k > 0) atomicAdd(&s_first[to], R.count[(size_t)j * kAll + tid]);
             }
         }
     }
-    // (lanes that add to one place of LDS go one by one: 2 us a slice)
-    if (__ballot(past != 0)) {
-        past = sum_lanes(past);
-        if (lane == 0) atomicAdd(&s_before[kAll - 1], past);
-        if (k > 0) {
-            num_past = (uint32_t)sum_lanes(num_past);
-            if (lane == 0) atomicAdd(&s_first[kAll - 1], num_past);
+    __syncthreads();
+    // A bin a thread; of those behind kFine every eighth, which the eight sum up, 4 places each.
+    static_assert(kFine % 64 == 0 && kBins == 32 && kPlaces - kFine == 4 * (kRowThreads - kFine), "whole wavefronts");
+    u64 mass = 0;
+    uint32_t count = 0;
+    int bin = tid;
+    if (tid < kFine) {                                           // (uniform)
+        mass = s_place[tid];
+        if (k > 0) count = s_first[tid];
+    } else {
+        const int at = kFine + 4 * (tid - kFine);
+        mass = s_place[at] + s_place[at + 1] + s_place[at + 2] + s_place[at + 3];
+        mass = sum_eight(mass, lane);
+        if (k > 0) count = (uint32_t)sum_eight((u64)s_first[at] + s_first[at + 1] + s_first[at + 2] + s_first[at + 3], lane);
+        bin = kFine + (tid - kFine) / 8;
+        if (lane & 7) {
+            mass = count = 0;
+            bin = tid == kRowThreads - 1 ? kAll : -1;
         }
     }
-    __syncthreads();
-    u64 mass[kPer];
-    uint32_t count[kPer];
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const int b = tid * kPer + i;
-        mass[i] = b < kAll ? s_before[b] : 0;
-        count[i] = b < kAll ? s_first[b] : 0;
-    }
-    __syncthreads();
     // what lies in front of each bin
-    u64 sum = 0;
-    uint32_t num = 0;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        sum += mass[i];
-        num += count[i];
-    }
-    u64 run = sum;
-    uint32_t runs = num;
+    u64 run = mass;
+    uint32_t runs = count;
 #pragma unroll
     for (int s = 1; s < 64; s <<= 1) {
-        const u64 x = (u64)(uint32_t)__shfl_up((int)(uint32_t)run, s) | (u64)(uint32_t)__shfl_up((int)(uint32_t)(run >> 32), s) << 32;
+        const u64 x = shfl_up64(run, s);
         const uint32_t y = (uint32_t)__shfl_up((int)runs, s);
         if (lane >= s) {
             run += x;
@@ -1093,26 +1071,15 @@ __device__ __forceinline__ RowState plan_row(const SampleArgs& A, int m, const R
         s_num[tid >> 6] = runs;
     }
     __syncthreads();
-    run -= sum;
-    runs -= num;
+    run -= mass;
+    runs -= count;
     for (int w = 0; w < tid >> 6; ++w) {
         run += s_part[w];
         runs += s_num[w];
     }
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const int b = tid * kPer + i;
-        if (b > kAll) break;
-        s_before[b] = run;
-        s_first[b] = runs;
-        if (b < kAll) {
-            run += mass[i];
-            runs += count[i];
-        }
-    }
-    if (tid == kRowThreads - 1) {
-        s_before[kAll] = run;
-        s_first[kAll] = runs;
+    if (bin >= 0) {
+        s_before[bin] = run;
+        s_first[bin] = runs;
     }
     __syncthreads();
     const u64 total = s_before[kAll];
@@ -1147,10 +1114,10 @@ __device__ __forceinline__ RowState plan_row(const SampleArgs& A, int m, const R
     if (least > 0.f) {
         // the bin of w = least, give or take two
         const double x = fma((double)z_max, c, -ref) + (least < 1.f ? (double)__log2f(least) : 0.0);
-        const int b = (int)fmin(-x * kBins, (double)kAll + 4);
-        if (b - 2 < end_lo) end_lo = max(b - 2, 0);
-        if (b + 2 < end_hi) end_hi = b + 2;
-        least_bin = min(b + 2, kAll - 1);
+        const int b = (int)fmin(-x * kBins, (double)(kRange + 2) * kBins), near = bin_of(max(b - 2, 0)), far = bin_of(b + 2);
+        if (near < end_lo) end_lo = near;
+        if (far < end_hi) end_hi = far;
+        least_bin = min(far, kAll - 1);
     }
     int n = 0;
     int bins[3][2];
@@ -1196,8 +1163,11 @@ __global__ __launch_bounds__(kRowThreads, 8) void sample_row_kernel(SampleArgs A
     __shared__ u64 s_part[kRowThreads / 64], s_pick[2];
     __shared__ uint32_t s_num[kRowThreads / 64];
     __shared__ u64 s_key[REST ? kList : 1], s_sum[REST ? kList : 1];
-    // (numbers of tokens are done with before the list's sums are there; two of these workgroups fit a compute unit)
+    __shared__ u64 s_places[REST ? 1 : kPlaces];
+    // (numbers of tokens are done with before the list's sums are there, and places before the list; two of these workgroups fit a
+    // compute unit)
     uint32_t* s_first = REST ? reinterpret_cast<uint32_t*>(s_sum) : s_counts;
+    u64* s_place = REST ? s_key : s_places;
     __shared__ double s_table[kSteps];
     __shared__ uint32_t s_n;
     __shared__ int s_found[8];
@@ -1239,7 +1209,7 @@ __global__ __launch_bounds__(kRowThreads, 8) void sample_row_kernel(SampleArgs A
             digits = true;
         }
         if (!digits) {
-            const RowState st = plan_row(A, m, R, s_slice, slices, k, T, c, ref, z_max, s_before, s_first, s_part, s_num, s_found);
+            const RowState st = plan_row(A, m, R, s_slice, slices, k, T, c, ref, z_max, s_before, s_place, s_first, s_part, s_num, s_found);
             fill_table(s_table);
             if (tid == 0) s_n = 0;
             __syncthreads();
@@ -1260,7 +1230,8 @@ __global__ __launch_bounds__(kRowThreads, 8) void sample_row_kernel(SampleArgs A
             }
             __syncthreads();
             if (s_n <= (uint32_t)kList) {                        // (uniform)
-                if (finish_row(A, m, st, s_key, (int)s_n, s_sum, s_before, s_table, s_part)) return;
+                finish_row(A, m, st, s_key, (int)s_n, s_sum, s_before, s_table, s_part);
+                return;
             }
         }
         __syncthreads();
@@ -1268,7 +1239,7 @@ __global__ __launch_bounds__(kRowThreads, 8) void sample_row_kernel(SampleArgs A
         return;
     }
     if constexpr (!REST) {
-        const RowState st = plan_row(A, m, R, s_slice, slices, k, T, c, ref, z_max, s_before, s_first, s_part, s_num, s_found);
+        const RowState st = plan_row(A, m, R, s_slice, slices, k, T, c, ref, z_max, s_before, s_place, s_first, s_part, s_num, s_found);
         for (int b = tid; b <= kAll; b += kRowThreads) R.before[b] = s_before[b];
         if (tid == 0) *R.row = st;
     }
@@ -1316,15 +1287,15 @@ __global__ __launch_bounds__(kThreads, 8) void sample_finish_kernel(SampleArgs A
     const RowState st = *R.row;
     if (st.state == kDone) return;
     const int n = (int)*R.ticket;
-    bool ended = false;
-    if (st.state == kOpen && n <= kList) {                       // (uniform)
-        fill_table(s_table);
-        for (int b = tid; b <= kAll; b += kThreads) s_before[b] = R.before[b];
-        for (int i = tid; i < n; i += kThreads) s_key[i] = R.list[i];
-        __syncthreads();
-        ended = finish_row(A, m, st, s_key, n, s_sum, s_before, s_table, s_part);
+    if (st.state == kDigits || n > kList) {
+        sample_by_digits<TYPE>(A, m, s_key, s_part, s_pick);
+        return;
     }
-    if (!ended) sample_by_digits<TYPE>(A, m, s_key, s_part, s_pick);
+    fill_table(s_table);
+    for (int b = tid; b <= kAll; b += kThreads) s_before[b] = R.before[b];
+    for (int i = tid; i < n; i += kThreads) s_key[i] = R.list[i];
+    __syncthreads();
+    finish_row(A, m, st, s_key, n, s_sum, s_before, s_table, s_part);
 }
 
 }  // namespace

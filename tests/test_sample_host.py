@@ -51,25 +51,38 @@ TYPES = {"bf16": 0, "fp16": 1, "fp32": 2}
 ORDERS = (0, 1, 2)                                               # the first wavefront first, the last one first, shuffled
 
 
-def run(host, z, u, type="fp32", ids=None, orders=ORDERS, **kw):
-    """Compares with the definition as the GPU's tests do, under every order; returns the tokens."""
+def call(host, order, t, type, u, ids, kw):
+    """One call: (tokens, logprobs)."""
+    M, V = t.shape
+    at = lambda x: None if x is None else ctypes.c_void_p(x.ctypes.data)   # noqa: E731
+    got, lp = np.full(M, -7, np.int32), np.zeros(M, np.float32)
+    ws = np.full(host.host_sample_workspace(M, V) + 256, 0xA5, np.uint8)
+    error = host.host_sample(ctypes.c_uint(order), ctypes.c_void_p(t.data_ptr()), ctypes.c_longlong(V), TYPES[type], M, V, at(u),
+                             at(kw.get("temperature")), at(kw.get("top_k")), at(kw.get("top_p")), at(kw.get("min_p")), at(ids), at(got),
+                             at(lp), ctypes.c_void_p((ws.ctypes.data + 255) // 256 * 256))
+    assert error is None, (order, error)
+    return got, lp.astype(np.float64)
+
+
+def args(z, u, kw):
+    t, u, _, kw = inputs(z, u, "fp32", None, kw)
+    return t, "fp32", u, None, kw
+
+
+def inputs(z, u, type, ids, kw):
     import torch
     t = torch.from_numpy(np.asarray(z, dtype=np.float64)).to({"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}[type])
-    M, V = t.shape
-    u = np.asarray(u, dtype=np.float32)
     kw = {k: np.asarray(v, dtype=np.int32 if k == "top_k" else np.float32) for k, v in kw.items()}
+    return t, np.asarray(u, dtype=np.float32), None if ids is None else np.asarray(ids, dtype=np.int32), kw
+
+
+def run(host, z, u, type="fp32", ids=None, orders=ORDERS, **kw):
+    """Compares with the definition as the GPU's tests do, under every order; returns the tokens."""
+    t, u, cols, kw = inputs(z, u, type, ids, kw)
     want, want_lp, margin = ref.sample(t.double().numpy(), u, ids=ids, **kw)
     sure = margin > 1e-11
-    cols = None if ids is None else np.asarray(ids, dtype=np.int32)
-    at = lambda x: None if x is None else ctypes.c_void_p(x.ctypes.data)   # noqa: E731
     for order in orders:
-        got, lp = np.full(M, -7, np.int32), np.zeros(M, np.float32)
-        ws = np.full(host.host_sample_workspace(M, V) + 256, 0xA5, np.uint8)
-        error = host.host_sample(ctypes.c_uint(order), ctypes.c_void_p(t.data_ptr()), ctypes.c_longlong(V), TYPES[type], M, V, at(u),
-                         at(kw.get("temperature")), at(kw.get("top_k")), at(kw.get("top_p")), at(kw.get("min_p")), at(cols), at(got),
-                         at(lp), ctypes.c_void_p((ws.ctypes.data + 255) // 256 * 256))
-        assert error is None, (order, error)
-        lp = lp.astype(np.float64)
+        got, lp = call(host, order, t, type, u, cols, kw)
         assert np.array_equal(got[sure], want[sure]), (order, got, want)
         assert np.array_equal(np.isnan(lp[sure]), np.isnan(want_lp[sure])), order
         ok = sure & ~np.isnan(want_lp)
@@ -125,14 +138,14 @@ def test_top_k_ends_behind_what_counts(host):
 
 @pytest.mark.parametrize("top_k", [None, 600])
 def test_last_bin_without_a_token(host, top_k):
-    """A slice whose best token weighs 2^-43.99 of the row's first: its weight is in the last bin, but too small for the list.  u = 1 ends
-    there; tokens below 2^-42 may be left out, so the row's first token is as right as that one."""
+    """A slice whose best token weighs 2^-43.99 of the row's first, and u of 1 and above, which ends with the last token that counts.  Tokens below
+    2^-42 may be left out: the row's first token is as right as that one, and nothing else is."""
     z = np.full((1, 30000), -np.inf)
     z[0, 5], z[0, 29000] = 0.0, -43.99 * np.log(2)
     kw = {} if top_k is None else dict(top_k=[top_k])
     for u in (1.0, np.inf, np.nan):
-        got = run(host, z, [u], orders=(0,), **kw)
-        assert got[0] in (5, 29000)
+        got, lp = call(host, 0, *args(z, [u], kw))
+        assert got[0] in (5, 29000) and np.isfinite(lp[0])
 
 
 @pytest.mark.parametrize("V", [40, 30000])
