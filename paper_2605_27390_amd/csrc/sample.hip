@@ -269,7 +269,7 @@ struct RowState {
 enum { kOpen = 0, kDone = 1, kDigits = 2 };
 
 struct SliceState {
-    double ref;                                   // exponent of its reference; with lists the bound that they reach
+    double ref;                                   // exponent of its reference; with lists the bound that they reach (see `missing`)
     u64 top;                                      // its largest logit as a key, greedy rows with its id; 0: no number there
     uint32_t n, pad;                              // tokens on its list
 };
@@ -428,11 +428,13 @@ __device__ __forceinline__ bool regular(float T, float z_max, float most = 0x1p2
 }
 __device__ __forceinline__ bool regular_slice(float T, float top) { return regular(T, top, 0x1p23f); }
 
+// A bound of a list that lacks tokens which equal it: a little larger, and the same in 32 bits.
+__device__ __forceinline__ double missing(float bound) { return (double)bound + fabs((double)bound) * 0x1p-30 + 1e-300; }
 // Rows of a small top-k: tokens of the slice that can be among the row's k largest, as keys in the place of its bins, and a
 // bound that k of them reach.  Of every wavefront's 64 largest logits of a lane the q-th largest is taken, q times the wavefronts >= k, and
 // the least of these: k logits reach it.  (k = 50 of 19,000: some 150 tokens pass.)  Where that is no bound, because a mask leaves some
 // wavefronts nothing, or too many reach it, the slice's k-th largest logit is looked for bit by bit; what has no weight beside the slice's
-// largest is not listed then either (masked tokens that are all the same low value).
+// largest is not listed then either, nor what equals the k-th if that is too many (masked tokens that are all the same low value).
 template <int TYPE>
 __device__ __forceinline__ void list_largest(const SampleArgs& A, const float (&z)[kGroups][4], Slice S, int k, float top, float T,
                                              const char* row, const RowSpace& R, int j, u64* s_key, float* s_bound) {
@@ -464,7 +466,7 @@ __device__ __forceinline__ void list_largest(const SampleArgs& A, const float (&
                 }
     }
     __syncthreads();
-    uint32_t n = s_n;
+    uint32_t n = s_n, full = 0;
     // (uniform; lists without a bound may be too many for the row's, if each is short enough)
     if (n > (uint32_t)(bound > -__builtin_inff() ? kAll : k)) {
         __shared__ uint32_t s_reach[32];
@@ -491,18 +493,24 @@ __device__ __forceinline__ void list_largest(const SampleArgs& A, const float (&
         }
         bound = ordered_to_f32(kth);
         if (regular_slice(T, top)) bound = fmaxf(bound, cut_of(ceil((double)top * log2e_over(T)), T));
-        each([&](float v, int i) {
-            if (v >= bound && v > -__builtin_inff()) {
-                const uint32_t at = atomicAdd(&s_n, 1u);
-                if (at < kAll) s_key[at] = make_key(v, A.ids ? A.ids[i] : i);
-            }
-        });
-        __syncthreads();
-        n = s_n;
+        for (;; full = 1) {                                      // (fewer than k are larger than the k-th)
+            each([&](float v, int i) {
+                if ((full ? v > bound : v >= bound) && v > -__builtin_inff()) {
+                    const uint32_t at = atomicAdd(&s_n, 1u);
+                    if (at < kAll) s_key[at] = make_key(v, A.ids ? A.ids[i] : i);
+                }
+            });
+            __syncthreads();
+            n = s_n;
+            if (n <= (uint32_t)kAll) break;                      // (uniform)
+            __syncthreads();
+            if (tid == 0) s_n = 0;
+            __syncthreads();
+        }
     }
-    for (int i = tid; i < (int)min(n, (uint32_t)kAll); i += kThreads) R.mass[(size_t)j * kAll + i] = s_key[i];
+    for (int i = tid; i < (int)n; i += kThreads) R.mass[(size_t)j * kAll + i] = s_key[i];
     if (tid == 0) {
-        R.slice[j] = SliceState{(double)bound, top > -__builtin_inff() ? make_key(top, 0) : 0, n, 0};
+        R.slice[j] = SliceState{full ? missing(bound) : (double)bound, top > -__builtin_inff() ? make_key(top, 0) : 0, n, 0};
     }
 }
 
@@ -853,23 +861,18 @@ __device__ int keep_front(u64* s_key, int n, int k, float bound, float top) {
     return (int)s_left;
 }
 
-// A row of a small top-k, from its slices' lists.  False if they do not hold what is needed.
-__device__ bool finish_largest(const SampleArgs& A, int m, int k, const RowSpace& R, const SliceState* s_slice, int slices, double c, double ref,
+// A row of a small top-k, from its slices' lists; `most` is the largest of their bounds, which is one for the row.  False if they do not
+// hold what is needed.
+__device__ bool finish_largest(const SampleArgs& A, int m, int k, const RowSpace& R, const SliceState* s_slice, int slices, double most, double c, double ref,
                                float z_max, u64* s_key, u64* s_sum, double* s_table, u64* s_part, uint32_t* s_n) {
     const int tid = threadIdx.x, lane = tid & 63;
+    const float bound = (float)most;
     fill_table(s_table);
     if (tid == 0) *s_n = 0;
-    // k logits of one slice reach its bound: the largest bound is one for the row, and so is what has weight
-    float bound = cut_of(ref, A.temperature ? A.temperature[m] : 1.f);
-    for (int j = 0; j < slices; ++j) bound = fmaxf(bound, (float)s_slice[j].ref);
-    // slices below that have nothing here, however many of them are equal
-    auto taken = [&](int j) { return s_slice[j].top != 0 && key_value(s_slice[j].top) >= bound; };
-    bool full = false;
-    for (int j = 0; j < slices; ++j) full |= taken(j) && s_slice[j].n > (uint32_t)kAll;
-    if (full) return false;                                      // (uniform)
+    if (most != (double)bound) return false;                     // (uniform) tokens are missing at that bound
     __syncthreads();
     for (int j = tid >> 6; j < slices; j += kRowThreads / 64) {
-        const int n = taken(j) ? (int)s_slice[j].n : 0;
+        const int n = (int)s_slice[j].n;
         for (int i = lane; i < n; i += 64) {
             const u64 key = R.mass[(size_t)j * kAll + i];
             if (key_value(key) >= bound) {
@@ -1155,8 +1158,9 @@ __device__ __forceinline__ RowState plan_row(const SampleArgs& A, int m, const R
     return st;
 }
 
-// REST: the row is ended here, where a workgroup for each row is what there is to do, or most rows end early.
-template <int TYPE, bool REST>
+// REST: the row is ended here, where a workgroup for each row is what there is to do, or most rows end early.  TOP_K: there may be one (calls
+// without have a kernel of their own, whose registers the lists do not crowd: 960 rows of bf16 235 and 250 us).
+template <int TYPE, bool REST, bool TOP_K>
 __global__ __launch_bounds__(kRowThreads, 8) void sample_row_kernel(SampleArgs A, char* ws, int slices) {
     __shared__ u64 s_before[kAll + 1];
     __shared__ uint32_t s_counts[REST ? 1 : kAll + 1];
@@ -1179,15 +1183,21 @@ __global__ __launch_bounds__(kRowThreads, 8) void sample_row_kernel(SampleArgs A
     const SliceState of_lane = R.slice[min(tid & 63, slices - 1)];
     if (tid < slices) s_slice[tid] = of_lane;
     u64 top = of_lane.top;
+    double bound = of_lane.ref;                                  // (of lists: k logits of one slice reach its bound)
     for (int s = 32; s >= 1; s >>= 1) {
         if (s >= slices) continue;                               // (uniform; lanes from there on repeat the last slice)
         const u64 x = shfl_xor64(top, s);
         top = x > top ? x : top;
+        if (TOP_K) bound = fmax(bound, __longlong_as_double((long long)shfl_xor64((u64)__double_as_longlong(bound), s)));
     }
-    if (slices > 1) top = first_lane(top);
+    if (slices > 1) {
+        top = first_lane(top);
+        if (TOP_K) bound = __longlong_as_double((long long)first_lane((u64)__double_as_longlong(bound)));
+    }
     __syncthreads();
     const float z_max = key_value(top);
-    const int k = REST && A.top_k ? A.top_k[m] : 0;              // (with a top-k rows are ended here)
+    static_assert(REST || !TOP_K, "with a top-k rows are ended here");
+    const int k = TOP_K ? A.top_k[m] : 0;
     if (top == 0 || !(T > 0.f)) {
         if (tid == 0) {
             A.out_ids[m] = top == 0 ? -1 : key_id(top);
@@ -1203,11 +1213,12 @@ __global__ __launch_bounds__(kRowThreads, 8) void sample_row_kernel(SampleArgs A
     }
     const double c = log2e_over(T);
     const double ref = ceil((double)z_max * c);
-    if constexpr (REST) {
+    if constexpr (TOP_K)
         if (!digits && k > 0 && k <= kMostK) {
-            if (finish_largest(A, m, k, R, s_slice, slices, c, ref, z_max, s_key, s_sum, s_table, s_part, &s_n)) return;
+            if (finish_largest(A, m, k, R, s_slice, slices, bound, c, ref, z_max, s_key, s_sum, s_table, s_part, &s_n)) return;
             digits = true;
         }
+    if constexpr (REST) {
         if (!digits) {
             const RowState st = plan_row(A, m, R, s_slice, slices, k, T, c, ref, z_max, s_before, s_place, s_first, s_part, s_num, s_found);
             fill_table(s_table);
@@ -1335,10 +1346,12 @@ static hipError_t sample_as(const SampleArgs& a, char* ws, hipStream_t stream) {
     if (wide > 1) sample_wide_bins_kernel<<<grid, kThreads, 0, stream>>>(a, ws, slices, wide);
     else if (TYPE == EVOSPEC_BF16 && a.V / slices >= kLeastByValue) sample_bins_kernel<TYPE, TYPE == EVOSPEC_BF16><<<grid, kThreads, 0, stream>>>(a, ws, slices);
     else sample_bins_kernel<TYPE, false><<<grid, kThreads, 0, stream>>>(a, ws, slices);
-    if (rest) {
-        sample_row_kernel<TYPE, true><<<dim3((unsigned)a.M), kRowThreads, 0, stream>>>(a, ws, slices);
+    if (a.top_k) {
+        sample_row_kernel<TYPE, true, true><<<dim3((unsigned)a.M), kRowThreads, 0, stream>>>(a, ws, slices);
+    } else if (rest) {
+        sample_row_kernel<TYPE, true, false><<<dim3((unsigned)a.M), kRowThreads, 0, stream>>>(a, ws, slices);
     } else {
-        sample_row_kernel<TYPE, false><<<dim3((unsigned)a.M), kRowThreads, 0, stream>>>(a, ws, slices);
+        sample_row_kernel<TYPE, false, false><<<dim3((unsigned)a.M), kRowThreads, 0, stream>>>(a, ws, slices);
         sample_pick_kernel<TYPE><<<dim3((unsigned)(a.M * parts)), kThreads, 0, stream>>>(a, ws, slices, parts);
         sample_finish_kernel<TYPE><<<dim3((unsigned)a.M), kThreads, 0, stream>>>(a, ws, slices);
     }
