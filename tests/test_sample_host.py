@@ -208,3 +208,19 @@ def test_top_k_of_ranges_in_every_slice(host):
         z[0, j * 20480 + 1000:j * 20480 + 1700] = rng.standard_normal(700)
     run(host, z, [0.7], top_k=[50], orders=(0,))
     assert not by_digits(host)
+
+
+def test_top_k_over_slices_that_list_what_is_above_their_bound(host):
+    """Each slice has fewer tokens above a common value than k, together they have more, or just as many, or fewer."""
+    rng = np.random.default_rng(8)
+    V = 30000
+    for low in (-5.0, -1.0e4, -3.0e38):
+        z = np.full((3, V), low)
+        for m, each in enumerate((30, 25, 12)):
+            for first in (0, 15000):
+                at = first + rng.choice(15000, each, replace=False)
+                z[m, at] = rng.standard_normal(each)
+        run(host, z, rng.random(3), top_k=[50] * 3, orders=(0,))
+        z[:, 100:200] = 3.0 + rng.standard_normal((3, 100))     # one slice has enough by itself
+        run(host, z, rng.random(3), top_k=[50] * 3, orders=(0, 1))
+        assert not by_digits(host)
