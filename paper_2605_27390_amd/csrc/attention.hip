@@ -33,6 +33,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kNone = -3.0e38f;                 // the reference of a row that has seen nothing
+constexpr float kLeastScale = 0x1p-100f;          // of what kv_write gives
 constexpr int kMostSplits = 128;
 constexpr int kWaves = 4;                         // of a workgroup
 constexpr float kSlack = 6.f;                     // a row's reference moves when a score passes it by more than that
@@ -228,9 +229,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ >= 6 ? 1 : 2) void kv_attention_ker
         page_next = page_of(b + 2 * kWaves);
         const float sc_x = there ? sc.x : 1.f, sc_y = there ? sc.y : 1.f;
         const float ck = fmaxf(fabsf(sc_x) * (A.scale * kLog2e), 0x1p-126f);       // (not zero: -inf stays what it is)
-        // (V of a scale of zero, which a caller's own may have, is zero: 2^-100 is the least that kv_write gives)
-        const bool v_zero = fabsf(sc_y) < 0x1p-100f;
-        const float sv = v_zero ? 0x1p-100f : fabsf(sc_y), lv = __log2f(sv), iv = __builtin_amdgcn_rcpf(sv);
+        const float sv = fmaxf(fabsf(sc_y), kLeastScale), lv = __log2f(sv), iv = __builtin_amdgcn_rcpf(sv);
 
         uint32_t nan_tokens = 0;                                 // of K (e4m3's NaN code is one for the matrix cores)
         if (KIND == EVOSPEC_KV_INT8 && __float_as_uint(sc_x) >> 31) {
@@ -307,7 +306,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ >= 6 ? 1 : 2) void kv_attention_ker
             pf[rt][1] = __builtin_bit_cast(u32x4, p[1]);
         }
         __builtin_amdgcn_sched_barrier(0);
-        const int end = there && !v_zero ? len : t0;
+        const int end = there ? len : t0;
         if (t0 + kBlock > end) {                                 // bytes behind the last token may be anything
 #pragma unroll
             for (int k = 0; k < NQ; ++k)
@@ -317,12 +316,14 @@ __global__ __launch_bounds__(64 * kWaves, NQ >= 6 ? 1 : 2) void kv_attention_ker
                     vr[k][a] &= left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
                 }
         }
-        if (__float_as_uint(sc_y) >> 31) {                       // (uniform) NaN is left out, and looked at behind the loop
-            nan_blocks = true;
+        if ((int)__float_as_uint(sc_y) < (int)__builtin_bit_cast(uint32_t, kLeastScale)) {        // (uniform) negative, or next to zero
+            // NaN is left out, and looked at behind the loop; V of a scale of zero, which a caller's own may have, is zero
+            if (__float_as_uint(sc_y) >> 31) nan_blocks = true;
+            const uint32_t all = fabsf(sc_y) < kLeastScale ? ~0u : 0u;
 #pragma unroll
             for (int k = 0; k < NQ; ++k)
 #pragma unroll
-                for (int a = 0; a < 4; ++a) vr[k][a] &= ~nan_bytes<KIND>(vr[k][a]);
+                for (int a = 0; a < 4; ++a) vr[k][a] &= ~(nan_bytes<KIND>(vr[k][a]) | all);
         }
 #pragma unroll
         for (int k = 0; k < NQ; ++k)
