@@ -112,9 +112,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ >= 6 ? 1 : 2) void kv_attention_ker
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
-    // workgroups go round the 8 dies in turn: each die gets neighbours, which read the same tokens, for its cache
-    const int die = blockIdx.x & 7, most = gridDim.x >> 3, rest = gridDim.x & 7;
-    int id = die * most + min(die, rest) + (blockIdx.x >> 3);
+    int id = dealt_out(blockIdx.x, gridDim.x, A.run);
     const int tile = id % A.tiles;
     id /= A.tiles;
     const int split = id % A.splits;
@@ -529,6 +527,10 @@ hipError_t launch_as(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
 // heads over 16, 32 and 64 workgroups a head 62 + 4.5, 44 + 5.1 and 46 + 7.5 us (attention + joining the shares), 16 x 4,096 tokens
 // over 1, 2 and 4 30, 22 + 4 and 22 + 4; 4,096 tokens over 1, 4, 8 and 16 23, 11 + 3.6, 8.6 + 3.6 and 7.3 + 4.2, but 1,000 of 64
 // elements over 1 and 4 9.0 and 6.3 + 3.4, and another launch.
+// Runs for a die (dealt_out): a sequence of several tiles is dealt out to all 8 dies, an eighth each, so that one of many rows has all of
+// them whatever stands beside it: 2,048 rows on 8,192 tokens before 32 single ones on 4,096 2,003 us with an eighth of the call for each die,
+// 439 so; 8 trees of 60 rows 32.5 and 28.2.  Sequences of a single tile go to the dies by twos: 64 on 8,192 down to 128 tokens 122 us by
+// eighths of the call, 93 one by one and 91 by twos, in any order 103, 104 and 98; 64 on 2,048 to 4,096 67.6, 69.4 and 68.1.
 // K and V are loaded past the caches where one workgroup reads them once (64 x 4,096 tokens 75 and 66.6 us, 16 x 4,096 24 and 22).
 AttnPlan attention_plan(int dim, int heads, int group, int S, int max_rows, int max_len) {
     constexpr long long kUnits = 256, kLeast = 48, kShare = 4;   // compute units; blocks that are worth a split, and of a wavefront then
@@ -543,6 +545,7 @@ AttnPlan attention_plan(int dim, int heads, int group, int S, int max_rows, int 
     splits = splits > most ? most : splits;
     p.splits = (int)(splits > kMostSplits ? kMostSplits : splits);
     p.once = p.tiles == 1;
+    p.run = p.tiles == 1 ? 2 * heads : (int)(((long long)p.tiles * p.splits * heads + 7) / 8);
     return p;
 }
 

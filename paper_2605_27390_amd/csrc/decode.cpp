@@ -139,7 +139,7 @@ int evospec_kv_attention(const evospec_kv_cache* cache, const void* q, long long
     a.c = cache_of(cache);
     a.r = Rows{page_table, width, lens, row_off, S, T, max_rows};
     a.q = q; a.q_stride = q_stride; a.group = group; a.tree = tree; a.scale = scale; a.out = out; a.lse = lse;
-    a.splits = p.splits; a.tiles = p.tiles;
+    a.splits = p.splits; a.tiles = p.tiles; a.run = p.run;
     a.part_o = static_cast<float*>(workspace);
     a.part_ml = need ? reinterpret_cast<float2*>(static_cast<char*>(workspace) + (size_t)p.splits * T * cache->heads * group * cache->dim * 4) : nullptr;
     return failed(launch_kv_attention(a, p, cache->dim, cache->kind, type, static_cast<hipStream_t>(stream)));

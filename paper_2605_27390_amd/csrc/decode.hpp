@@ -33,12 +33,26 @@ hipError_t launch_kv_write(const Cache& c, int dim, int kind, const void* k, lon
                            int type, const Rows& r, hipStream_t stream);
 hipError_t launch_kv_read(const Cache& c, int dim, int kind, const Rows& r, int type, void* out_k, void* out_v, hipStream_t stream);
 
+// Workgroups go round the 8 dies in turn.  Runs of `run` neighbours, which read the same tokens, go to one die, for its cache: a run for each die
+// in a round, and the next round three dies on, so that what repeats every 8 runs does not meet one die.  What is left over is dealt out in
+// eighths.  The task of workgroup b of n.
+__host__ __device__ inline int dealt_out(int b, int n, int run) {
+    const int whole = n / (8 * run) * (8 * run);
+    if (b < whole) {
+        const int place = b / 8, round = place / run;
+        return (round * 8 + ((b + 3 * round) & 7)) * run + place % run;
+    }
+    const int left = n - whole, die = (b - whole) & 7, most = left / 8, rest = left & 7;
+    return whole + die * most + (die < rest ? die : rest) + (b - whole) / 8;
+}
+
 // How an attention call is laid out.
 struct AttnPlan {
     int row_tiles;                            // tiles of 32 rows of a workgroup
     int tiles;                                // workgroups over the rows of a sequence and head
     int splits;                               // workgroups over its tokens
     bool once;                                // K and V past the caches
+    int run;                                  // workgroups in a row for one die
 };
 AttnPlan attention_plan(int dim, int heads, int group, int S, int max_rows, int max_len);
 size_t attention_workspace(const AttnPlan& p, int dim, int heads, int group, int T);
@@ -55,7 +69,7 @@ struct AttnArgs {
     float* lse;
     float* part_o;                            // [splits][T * heads * group][dim], of splits > 1
     float2* part_ml;                          // [splits][T * heads * group]: reference and sum
-    int splits, tiles;
+    int splits, tiles, run;
 };
 hipError_t launch_kv_attention(const AttnArgs& a, const AttnPlan& p, int dim, int kind, int type, hipStream_t stream);
 
