@@ -56,7 +56,10 @@ int evospec_kv_cache_bytes(const evospec_kv_cache *cache, size_t *out_data_bytes
  * block the scale only grows, and where it does the codes of the tokens before starts[s] become
  * round(code * old / new).  The scale is that of the largest finite magnitude; infinities saturate, NaN stays NaN.
  * Codes of a block behind the last token written are unspecified.  Two sequences of one call must not write to the
- * same block.
+ * same block.  int8 codes are rounded again whenever their block's scale grows: a block that is written token by token, up to
+ * 31 times.
+ * There is a workgroup for each head and each block that max_rows rows of a sequence can touch, S * heads * ((max_rows + 30) / 32 + 1)
+ * in all, which have to be fewer than 2^24 - 1023 (as in evospec_kv_read): where lengths lie far apart, call by groups of them.
  */
 int evospec_kv_write(const evospec_kv_cache *cache, const void *k, long long k_stride, const void *v, long long v_stride,
                      int type, int T, const int32_t *page_table, int width, const int32_t *starts, const int32_t *row_off,
@@ -75,7 +78,10 @@ int evospec_kv_read(const evospec_kv_cache *cache, const int32_t *page_table, in
  * a reads head a / group.
  *   row i sees token t when   tree == NULL:  t <= lens[s] - n + i
  *                             otherwise:     t < lens[s] - n, or bit t - (lens[s] - n) of tree[row] is set (n <= 64)
- *   x = scale * q . k;  out = sum softmax(x) v;  lse = log sum exp x   (sums in fp32; a row that sees nothing: 0, -inf)
+ *   x = scale * q . k;  out = sum softmax(x) v;  lse = log sum exp x   (a row that sees nothing: 0, -inf)
+ * Products with q and with V's codes are summed in fp32, and so is the softmax; its weights are rounded to fp16 for the product with V
+ * (to 2^-11 of each, or 2^-25 of the row's largest weight times scale where they are below 2^-14 of that), whatever q's type.
+ * Scales of V of the blocks that a row sees may differ by a factor of 2^100.
  * Values of tokens that a row does not see, NaN among them, do not reach it.
  *   q         dev `type` (EVOSPEC_BF16 or EVOSPEC_FP16) [T, heads * group, dim], rows q_stride elements apart and 16-B aligned
  *   lens      dev int32 [S]            row_off, max_rows as above (rows past max_rows of a sequence are not written)
@@ -103,6 +109,8 @@ int evospec_kv_attention(const evospec_kv_cache *cache, const void *q, long long
  *      kept one if none does).
  * out_logprob = log of the drawn token's share in the kept ones.  temperature that is not > 0 draws the first token.
  * Tokens with w below 2^-42 may be left out of 4.  A row without a number above -inf gives id -1, logprob NaN.
+ * Sums are of weights that are rounded to multiples of 2^-43: a cut of 2 and the draw of 4 are the definition's wherever their place is
+ * further than V 2^-43 + 2^-38 from a border between two tokens, as a share of the kept sum, and out_logprob is as exact, in fp32.
  *   logits dev `type` [M, V], rows `stride` elements apart; V <= 2^20, M * ceil(V / 20480) < 2^22
  *   u, temperature, top_p, min_p dev fp32 [M]; top_k dev int32 [M]; each of the last four may be NULL (1, all, all, all)
  *   ids dev int32 [V] or NULL: the id of column i (distinct, not negative); NULL: i

@@ -11,8 +11,10 @@
 // One pass over the tokens (running maximum and sum).  With s_k, s_v the scales of a block, t = x log2(e) + log2(s_v)
 // has the running reference M (of the lane's row), p = 2^(t - M) is at most 2^kSlack whatever the scales are, and
 //   l += sum p / s_v,   O += sum p code_v,   so out = O / l,   lse = (M + log2 l) ln 2.
-// Measured: 64 tokens of 32 heads on 2,048 to 4,096 tokens 66.6 us (6.1 TB/s, HBM bound), a chunk of 2,048 rows on 8,192 308 us (1.0
-// PFLOP/s, bound by the matrix instructions), the trees of 8 x 60 rows on 1,500 to 3,000 31 us.
+// Measured: 64 tokens of 32 heads on 2,048 to 4,096 tokens 68 us (6.0 TB/s, HBM bound), a chunk of 2,048 rows on 8,192 308 us (1.0
+// PFLOP/s, bound by the matrix instructions), the trees of 8 x 60 rows on 1,500 to 3,000 28 us.  Heads of 192 and 256 elements, whose queries,
+// sums and operands do not fit the vector registers beside each other (112 and 193 of them lie in accumulation registers, one wavefront
+// to a SIMD): the 64 tokens 100 and 132 us (6.1 TB/s), the chunk 610 and 775 (0.76 and 0.80 PFLOP/s).
 // p is rounded to fp16 (2^-11 of itself): the smallest normal fp16 is 2^-14 of the reference, and what is below keeps an
 // absolute error of 2^-25 of it.
 #include <hip/hip_runtime.h>
@@ -521,8 +523,8 @@ hipError_t launch_as(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
 }  // namespace
 
 // Two tiles of rows a wavefront halve what is loaded and converted for a row, and leave half as many workgroups: taken where these still
-// fill 256 compute units twice (2,048 rows of 8 x 4 heads on 10,240 tokens 324 us with one tile, 298 with two; 60 rows of 8
-// sequences, 256 workgroups of two tiles, 31 and 40).  From 160 elements on there are no registers for them.
+// fill 256 compute units twice (2,048 rows of 8 x 4 heads on 10,240 tokens 347 us with one tile, 315 with two; 60 rows of 8
+// sequences, 256 workgroups of two tiles, 28 and 37).  From 160 elements on there are no registers for them.
 // The tokens are split over workgroups where there are fewer of these than compute units, and enough to split: 131,072 tokens of 8
 // heads over 16, 32 and 64 workgroups a head 62 + 4.5, 44 + 5.1 and 46 + 7.5 us (attention + joining the shares), 16 x 4,096 tokens
 // over 1, 2 and 4 30, 22 + 4 and 22 + 4; 4,096 tokens over 1, 4, 8 and 16 23, 11 + 3.6, 8.6 + 3.6 and 7.3 + 4.2, but 1,000 of 64
@@ -531,7 +533,9 @@ hipError_t launch_as(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
 // them whatever stands beside it: 2,048 rows on 8,192 tokens before 32 single ones on 4,096 2,003 us with an eighth of the call for each die,
 // 439 so; 8 trees of 60 rows 32.5 and 28.2.  Sequences of a single tile go to the dies by twos: 64 on 8,192 down to 128 tokens 122 us by
 // eighths of the call, 93 one by one and 91 by twos, in any order 103, 104 and 98; 64 on 2,048 to 4,096 67.6, 69.4 and 68.1.
-// K and V are loaded past the caches where one workgroup reads them once (64 x 4,096 tokens 75 and 66.6 us, 16 x 4,096 24 and 22).
+// K and V are loaded past the caches where a sequence's workgroup reads them once: 64 tokens on 2,048 to 4,096 76 and 68 us, one on 131,072
+// 56 and 50, 16 x 4,096 29.5 and 28.5.  (Pages that sequences share are read by each of them, which the page table alone knows: 64 x 4,096
+// shared tokens 42 us through the caches and 47 past them, still below the 84 of 64 x 4,096 of their own.)
 AttnPlan attention_plan(int dim, int heads, int group, int S, int max_rows, int max_len) {
     constexpr long long kUnits = 256, kLeast = 48, kShare = 4;   // compute units; blocks that are worth a split, and of a wavefront then
     AttnPlan p;

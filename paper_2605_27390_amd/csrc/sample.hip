@@ -5,7 +5,8 @@
 // cumulative weight of the kept ones passes u times their sum.  Such keys are found digit by digit from a histogram of the
 // keys that agree so far, of numbers (top-k) or of weights (top-p, the draw).  Weights w = exp((z - z_max) / T) are computed
 // in 64 bits and kept as whole multiples of 2^-43: their sums do not depend on an order, so that a histogram may be filled by
-// atomics, and 2^20 of them fit 64 bits.  Measured on rows of 151,936: one in 17 us, 60 with top-k in 26, 960 of bf16 with top-p in 262.
+// atomics, and 2^20 of them fit 64 bits.  (They are off by 2^-44 each, and by a table to 2^-39 of themselves: sums to V 2^-44, and to as much
+// again where slices' bins are joined.)  Measured on rows of 151,936: one in 19 us, 60 with top-k in 27, 960 of bf16 with top-p in 222.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -304,8 +305,8 @@ __device__ __forceinline__ RowSpace row_space(char* ws, int m, int slices) {
 
 // Weights by table: with y = z log2(e) / T = k / kSteps + r, |r| <= 1 / (2 kSteps), and `ref` a whole power of two above the row's or
 // slice's largest, w = 2^(y - ref) = 2^(-m / kSteps) 2^r, m = kSteps ref - k >= 0.  2^r by its series to the fourth power is off by
-// 2^-39.  What bounds the bins is LDS, an addition to a bin for each logit: 183 us for 146 million logits, and 191 with a table of 128
-// steps, whose reads meet in its banks.
+// 2^-39.  What bounds the bins is LDS, an addition to a bin for each logit: 151 us for 146 million logits of bf16 (183 when the tail had one
+// bin for all, and 191 then with a table of 128 steps, whose reads meet in its banks).
 struct Steps {
     int m;
     double r;
@@ -523,8 +524,9 @@ __device__ __forceinline__ void list_largest(const SampleArgs& A, const float (&
 }
 
 // bf16 has 128 values to a factor of 2: a slice's logits between 2^-12 and 2^6, of either sign, are counted by value, and each value is
-// weighed once, times its number (whole numbers: the sums are the same).  960 rows of 151,936 183 us one by one, 132 so, 64 rows 29 and 13.
-constexpr int kLeastByValue = 8192;               // logits of a slice (8 rows of 50,000 in slices of 4,168 8.9 us by value, 7.4 one by one)
+// weighed once, times its number (whole numbers: the sums are the same).  960 rows of 151,936 151 us one by one, 134 so, 64 rows 13.9 and
+// 12.7.
+constexpr int kLeastByValue = 8192;               // logits of a slice (8 rows of 50,000 in slices of 6,252 8.6 us by value, 6.8 one by one)
 constexpr int kLowCode = 0x3980, kCodes = 0x4280 - kLowCode;    // upper halves of 2^-12 and 2^6
 
 template <int TYPE, bool BY_VALUE>
@@ -628,7 +630,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_bins_kernel(SampleArgs A, 
 
 // The same by value for many rows of bf16 without a top-k: a slice is `parts` times as long, taken in parts with the next one under way,
 // and its values are weighed once.  The window goes down to 2^-22, and what lies outside of it is read again at the end, when the
-// slice's largest logit is known.  960 rows of 151,936 in slices of 75,968: 132 and 91 us; 128 rows 38 and 19.
+// slice's largest logit is known.  960 rows of 151,936 in slices of 75,968: 134 and 92 us; 128 rows 22 and 19.
 constexpr int kWideLow = 0x3480, kWideCodes = 0x4280 - kWideLow;
 __global__ __launch_bounds__(kThreads, 8) void sample_wide_bins_kernel(SampleArgs A, char* ws, int slices, int parts) {
     __shared__ u64 s_mass[kAll];
@@ -1166,7 +1168,7 @@ __device__ __forceinline__ RowState plan_row(const SampleArgs& A, int m, const R
 }
 
 // REST: the row is ended here, where a workgroup for each row is what there is to do, or most rows end early.  TOP_K: there may be one (calls
-// without have a kernel of their own, whose registers the lists do not crowd: 960 rows of bf16 235 and 250 us).
+// without have a kernel of their own, whose registers the lists do not crowd: 960 rows of bf16 222 us, and 235 to 250 together).
 template <int TYPE, bool REST, bool TOP_K>
 __global__ __launch_bounds__(kRowThreads, 8) void sample_row_kernel(SampleArgs A, char* ws, int slices) {
     __shared__ u64 s_before[kAll + 1];
@@ -1342,8 +1344,9 @@ size_t sample_workspace(int M, int V) {
 template <int TYPE>
 static hipError_t sample_as(const SampleArgs& a, char* ws, hipStream_t stream) {
     // Who ends the rows: a workgroup for each, with less to launch and to pass on, where top-k leaves little, rows would fit one
-    // slice, or there are enough of them; otherwise its slices side by side.  By itself against side by side: one row of 151,936 57 and
-    // 41 us, 256 rows 153 and 147, 512 rows 232 and 242; 30 rows of 60,000 50 and 40, of 40,000 41 and 36.5; 60 rows of 20,000 41 and 46.
+    // slice, or there are enough of them; otherwise its slices side by side.  By itself against side by side (top-p, fp32): one row of 151,936
+    // 42 and 32 us, 256 rows 122 and 116, 384 155 and 155, 512 175 and 191; 30 rows of 60,000 38 and 33; 60 rows of 20,000 28 and 29.  A call
+    // with a top-k has its rows ended by a workgroup each whatever their own says: one row without 55 us there, 60 rows 64 and 48.
     const bool rest = a.top_k || whole_slices(a.V) == 1 || a.M >= kManyRows;
     const int parts = a.top_k ? whole_slices(a.V) : many_slices(a.M, a.V);
     // (longer slices where two workgroups for each compute unit are left)

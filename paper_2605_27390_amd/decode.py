@@ -187,7 +187,7 @@ def kv_attention(q, cache: KVCache, page_table, lens, row_off, max_rows: int, ma
     row_off[s] .. row_off[s + 1] are the last tokens of sequence s, which has lens[s] tokens in the cache.  A row sees
     the tokens up to its own; with `tree` (int64 [T], bit j: the row sees the j-th of the sequence's rows) it sees all that
     come before the sequence's rows, and those of its bits.  `scale` is 1 / sqrt(dim) if not given; max_len (a bound of lens)
-    only decides how the work is split."""
+    only decides how the work is split.  Lengths have to lie within the page table.  No gradients: outputs do not require any."""
     width, S = _rows(page_table, lens, "lens", row_off, cache._device)
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a tensor [rows, query heads, dim]")
