@@ -90,3 +90,51 @@ def test_a_full_cache(example, capsys, monkeypatch):
     monkeypatch.setattr("sys.argv", ["verify_step.py", "--steps", "100"])
     example.main()
     assert "no room" in capsys.readouterr().out
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
+def test_every_call_of_a_step(example, kind, monkeypatch):
+    """What each call finds and leaves, against the definition: writes value by value, attention of every node of every tree within its bounds, and
+    tokens equal."""
+    import attention_bounds as bounds
+    ev, seen = example.ev, []
+    write, attend, sample = ev.kv_write, ev.kv_attention, ev.sample
+
+    def checked_write(c, k, v, table, starts, row_off, max_rows):
+        h = host_cache(c)
+        h.data, h.scales = h.data.copy(), h.scales.copy()
+        write(c, k, v, table, starts, row_off, max_rows)
+        h.write(k.float().cpu().numpy(), v.float().cpu().numpy(), table.cpu().numpy(), starts.tolist(), row_off.tolist())
+        after = host_cache(c)
+        assert (after.scales == h.scales).all()
+        rows = np.diff(row_off.tolist())
+        for s, (a, n) in enumerate(zip(starts.tolist(), rows)):  # (what lies behind the last token is nobody's)
+            for got, want in zip(after.values(table.cpu().numpy(), s, a + n), h.values(table.cpu().numpy(), s, a + n)):
+                assert (got == want).all()
+        seen.append("write")
+
+    def checked_attention(q, c, table, lens, row_off, max_rows, tree=None):
+        out, lse = attend(q, c, table, lens, row_off, max_rows, tree=tree)
+        want = bounds.attention(host_cache(c), q.double().cpu().numpy(), table.cpu().numpy(), lens.tolist(), row_off.tolist(),
+                                q.shape[1] // c.heads, "bf16", tree.tolist())
+        assert bounds.differs(out.double().cpu().numpy(), lse.double().cpu().numpy(), want) is None
+        seen.append("attention")
+        return out, lse
+
+    def checked_sample(logits, u, **kw):
+        got, lp = sample(logits, u, **kw)
+        host = {k: x.cpu().numpy() for k, x in kw.items()}
+        want, want_lp, margin = ref.sample(logits.double().cpu().numpy(), u.cpu().numpy(), **host)
+        sure = margin > logits.shape[1] * 2.0 ** -43 + 2.0 ** -38
+        assert sure.any() and np.array_equal(got.cpu().numpy()[sure], want[sure])
+        seen.append("sample")
+        return got, lp
+
+    loop = example.Loop(S=2, kind=kind, seed=5, V=4096, active=1024)
+    loop.cache.data.zero_()
+    loop.cache.scales.fill_(1.0)
+    for name, f in (("kv_write", checked_write), ("kv_attention", checked_attention), ("sample", checked_sample)):
+        monkeypatch.setattr(ev, name, f)
+    for _ in range(4):
+        loop.step()
+    assert seen == ["write", "attention", "sample", "write"] * 4
