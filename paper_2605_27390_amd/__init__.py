@@ -41,3 +41,14 @@ from .decode import (  # noqa: F401,E402
     sample,
     sample_workspace_bytes,
 )
+from .adapt import (  # noqa: F401,E402
+    AdamW,
+    LoraBank,
+    adamw_moments,
+    adamw_step,
+    kd_loss,
+    kd_loss_workspace_bytes,
+    lora_backward,
+    lora_forward,
+    lora_workspace_bytes,
+)

@@ -11,10 +11,11 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libevospec.so")
 SOURCES = ["kernels.hip", "gemm.hip", "tile.hip", "narrow.hip", "klgate.hip", "noalloc.hip", "kvcache.hip", "attention.hip", "sample.hip",
-           "api.cpp", "decode.cpp", "arc.cpp", "path_a.cpp"]
+           "lora.hip", "kdloss.hip", "adamw.hip", "api.cpp", "decode.cpp", "adapt.cpp", "arc.cpp", "path_a.cpp"]
 OBJECTS = os.path.join(HERE, "_build")
-HEADERS = ["plan.hpp", "launch.hpp", "common.hpp", "slab.hpp", "slab_epilogue.hpp", "decode.hpp", os.path.join(ROOT, "include", "evospec.h"),
-           os.path.join(ROOT, "include", "evospec_arc.h"), os.path.join(ROOT, "include", "evospec_decode.h")]
+HEADERS = ["plan.hpp", "launch.hpp", "common.hpp", "slab.hpp", "slab_epilogue.hpp", "decode.hpp", "adapt.hpp", os.path.join(ROOT, "include", "evospec.h"),
+           os.path.join(ROOT, "include", "evospec_arc.h"), os.path.join(ROOT, "include", "evospec_decode.h"),
+           os.path.join(ROOT, "include", "evospec_adapt.h")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -1,0 +1,257 @@
+// AdamW over many tensors at once, with moments in 32 or in 8 bits (evospec_adapt.h has the formulas and the codes).
+//
+// Every element is read and written once: 22 bytes with moments in 32 bits beside bf16 parameters, 10 with 8 bits.  A wavefront has
+// blocks of 256 elements, 4 in a row to a lane, so that the largest magnitude of a block is a reduction within it.  Addresses
+// of up to kTensors tensors go along with the launch itself; a wavefront finds its block's tensor by one comparison in every lane.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "adapt.hpp"
+#include "common.hpp"
+
+namespace evospec {
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kBlock = EVOSPEC_ADAMW_BLOCK;
+constexpr int kTensors = 112;                 // of a launch: 28 bytes each, of 4 KB of arguments
+
+struct Table {
+    uint64_t param[kTensors], grad[kTensors];
+    uint64_t n[kTensors];
+    uint32_t first[kTensors];                 // block, counted from the launch's first
+    int count;
+    uint32_t blocks;
+    long long base;                           // the launch's first block
+};
+static_assert(sizeof(Table) <= 3500, "arguments of a launch");
+
+template <int TYPE>
+struct Element;
+template <>
+struct Element<EVOSPEC_BF16> {
+    using type = __bf16;
+};
+template <>
+struct Element<EVOSPEC_FP16> {
+    using type = _Float16;
+};
+template <>
+struct Element<EVOSPEC_FP32> {
+    using type = float;
+};
+
+// 4 elements from `at` on; of a tensor's end those that there are, and zeros.
+template <int TYPE>
+__device__ __forceinline__ void load4(const void* base, long long at, int there, float (&x)[4]) {
+    using T = typename Element<TYPE>::type;
+    typedef T vec __attribute__((ext_vector_type(4)));
+    const T* p = (const T*)base + at;
+    if (there >= 4) {
+        const vec v = *reinterpret_cast<const vec*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = (float)v[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = i < there ? (float)p[i] : 0.f;
+    }
+}
+template <int TYPE>
+__device__ __forceinline__ void store4(void* base, long long at, int there, const float (&x)[4]) {
+    using T = typename Element<TYPE>::type;
+    typedef T vec __attribute__((ext_vector_type(4)));
+    T* p = (T*)base + at;
+    if (there >= 4) {
+        *reinterpret_cast<vec*>(p) = vec{(T)x[0], (T)x[1], (T)x[2], (T)x[3]};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < there) p[i] = (T)x[i];
+    }
+}
+
+// 2^e, the least from 2^-100 to 2^100 with amax <= most 2^e, most = (1 + FRACTION / 2^23) 2^LEAST
+template <int LEAST, uint32_t FRACTION>
+__device__ __forceinline__ float power_for(float amax) {
+    const uint32_t u = __float_as_uint(amax);
+    const int e = (int)(u >> 23) - 127 - LEAST + ((u & 0x7fffffu) > FRACTION);
+    return __uint_as_float((uint32_t)(min(max(e, -100), 100) + 127) << 23);
+}
+__device__ __forceinline__ float reciprocal(float power) { return __uint_as_float((254u << 23) - __float_as_uint(power)); }
+
+// The code of a magnitude that is divided by its scale; bits: 16 random ones.
+template <int BIAS>
+__device__ __forceinline__ uint32_t code_of(float y, uint32_t bits) {
+    const float least = __uint_as_float((uint32_t)(128 - BIAS) << 23);
+    const bool tiny = y < least;
+    const uint32_t b = __float_as_uint(tiny ? y + least : y) + (bits << 4);
+    return (b >> 20) - (tiny ? (128 - BIAS) * 8 : (127 - BIAS) * 8);
+}
+__device__ __forceinline__ float v_value(uint32_t code) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(code << 7)); }
+
+__device__ __forceinline__ uint32_t random_bits(uint32_t place, uint32_t key) {
+    uint32_t x = place * 0x9e3779b1u + key;
+    x = (x ^ (x >> 16)) * 0x21f0aaadu;
+    x = (x ^ (x >> 15)) * 0x735a2d97u;
+    return x ^ (x >> 15);
+}
+
+template <int PT, int GT, int KIND, bool MASTER>
+__global__ __launch_bounds__(kThreads) void adamw_kernel(Table table, AdamwArgs a) {
+    const int lane = threadIdx.x & 63;
+    const uint32_t block = blockIdx.x * kWaves + (threadIdx.x >> 6);
+    if (block >= table.blocks) return;
+    // the last tensor that begins at or before the block
+    int at = 0;
+#pragma unroll
+    for (int i = 0; i < kTensors; i += 64) {
+        const int t = i + lane;
+        at += __popcll(__ballot(t < table.count && table.first[min(t, kTensors - 1)] <= block));
+    }
+    at = __builtin_amdgcn_readfirstlane(at - 1);
+    const float scale = a.grad_scale ? *a.grad_scale : 1.f;
+    if (!(fabsf(scale) < __builtin_inff())) return;
+    float decay = a.decay, rate = a.rate, root = a.root;
+    uint32_t key = a.seed_key + a.t_key;
+    if (a.schedule) {
+        const float lr = a.schedule[0], t = a.schedule[1];
+        decay = 1.f - lr * a.weight_decay;
+        rate = lr / -expm1f(t * a.log_beta1);
+        root = 1.f / sqrtf(-expm1f(t * a.log_beta2));
+        key = a.seed_key + (uint32_t)t * 0xc2b2ae35u;
+    }
+    const long long within = (long long)(block - table.first[at]) * kBlock + 4 * lane;
+    const long long flat = (table.base + block) * kBlock + 4 * lane;
+    const long long rest = (long long)table.n[at] - within;
+    const int there = rest >= 4 ? 4 : rest > 0 ? (int)rest : 0;
+    float g[4], p[4], m[4], v[4];
+    load4<GT>((const void*)table.grad[at], within, there, g);
+    if constexpr (MASTER) load4<EVOSPEC_FP32>(a.master, flat, 4, p);
+    else load4<PT>((const void*)table.param[at], within, there, p);
+    float sm, sv;
+    if constexpr (KIND == EVOSPEC_MOMENTS_8BIT) {
+        const uint32_t cm = *(const uint32_t*)((const uint8_t*)a.m + flat), cv = *(const uint32_t*)((const uint8_t*)a.v + flat);
+        const float2 s = reinterpret_cast<const float2*>(a.scales)[table.base + block];
+        m[0] = __builtin_amdgcn_cvt_f32_fp8((int)cm, 0) * s.x;
+        m[1] = __builtin_amdgcn_cvt_f32_fp8((int)cm, 1) * s.x;
+        m[2] = __builtin_amdgcn_cvt_f32_fp8((int)cm, 2) * s.x;
+        m[3] = __builtin_amdgcn_cvt_f32_fp8((int)cm, 3) * s.x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = v_value((cv >> (8 * i)) & 255u) * s.y;
+    } else {
+        load4<EVOSPEC_FP32>(a.m, flat, 4, m);
+        load4<EVOSPEC_FP32>(a.v, flat, 4, v);
+    }
+    float top_m = 0.f, top_v = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (i >= there) p[i] = m[i] = v[i] = 0.f;                // (g is)
+        const float x = g[i] * scale;
+        m[i] = fmaf(a.beta1, m[i], a.beta1c * x);
+        v[i] = fmaf(a.beta2, v[i], a.beta2c * (x * x));
+        // (reciprocal and root to the last bit or so: 2^-23 of an update, which is itself small beside p)
+        p[i] = fmaf(p[i], decay, -(rate * m[i]) * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(v[i]), root, a.eps)));
+        if constexpr (KIND == EVOSPEC_MOMENTS_8BIT) {
+            const bool fine = fabsf(m[i]) < __builtin_inff() && v[i] < __builtin_inff();
+            top_m = fmaxf(top_m, fine ? fabsf(m[i]) : 0.f);
+            top_v = fmaxf(top_v, fine ? v[i] : 0.f);
+        }
+    }
+    store4<PT>((void*)table.param[at], within, there, p);
+    if constexpr (MASTER) store4<EVOSPEC_FP32>(a.master, flat, 4, p);
+    if constexpr (KIND == EVOSPEC_MOMENTS_8BIT) {
+        sm = power_for<8, 0x600000u>(wave_max(top_m, lane));
+        sv = power_for<15, 0x700000u>(wave_max(top_v, lane));
+        const float im = reciprocal(sm), iv = reciprocal(sv);
+        uint32_t cm = 0, cv = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t bits = random_bits((uint32_t)(flat + i), key);
+            const bool fine = fabsf(m[i]) < __builtin_inff() && v[i] < __builtin_inff();
+            uint32_t x = code_of<7>(fminf(fabsf(m[i]) * im, 448.f), bits & 0xffffu) | (__float_as_uint(m[i]) >> 31) << 7;
+            uint32_t y = code_of<15>(fminf(v[i] * iv, 61440.f), bits >> 16);
+            if (y == 0 && v[i] > 0.f) y = 1;
+            if (!fine) { x = 0x7f; y = 0xf7; }
+            cm |= x << (8 * i);
+            cv |= y << (8 * i);
+        }
+        *(uint32_t*)((uint8_t*)a.m + flat) = cm;
+        *(uint32_t*)((uint8_t*)a.v + flat) = cv;
+        if (lane == 0) reinterpret_cast<float2*>(a.scales)[table.base + block] = make_float2(sm, sv);
+    } else {
+        store4<EVOSPEC_FP32>(a.m, flat, 4, m);
+        store4<EVOSPEC_FP32>(a.v, flat, 4, v);
+    }
+}
+
+template <int TYPE>
+__global__ __launch_bounds__(kThreads) void adamw_moments_kernel(const uint8_t* m, const uint8_t* v, const float2* scales, long long blocks,
+                                                                 void* out_m, void* out_v) {
+    const long long block = (long long)blockIdx.x * kWaves + (threadIdx.x >> 6);
+    if (block >= blocks) return;
+    const long long flat = block * kBlock + 4 * (threadIdx.x & 63);
+    const float2 s = scales[block];
+    const uint32_t cm = *(const uint32_t*)(m + flat), cv = *(const uint32_t*)(v + flat);
+    const float x[4] = {__builtin_amdgcn_cvt_f32_fp8((int)cm, 0) * s.x, __builtin_amdgcn_cvt_f32_fp8((int)cm, 1) * s.x,
+                        __builtin_amdgcn_cvt_f32_fp8((int)cm, 2) * s.x, __builtin_amdgcn_cvt_f32_fp8((int)cm, 3) * s.x};
+    const float y[4] = {v_value(cv & 255u) * s.y, v_value((cv >> 8) & 255u) * s.y, v_value((cv >> 16) & 255u) * s.y, v_value(cv >> 24) * s.y};
+    store4<TYPE>(out_m, flat, 4, x);
+    store4<TYPE>(out_v, flat, 4, y);
+}
+
+template <int I>
+using Const = std::integral_constant<int, I>;
+
+}  // namespace
+
+hipError_t launch_adamw(const evospec_adamw_tensor* tensors, int count, int param_type, int grad_type, int kind, const AdamwArgs& a,
+                        hipStream_t stream) {
+    long long base = 0;
+    for (int at = 0; at < count;) {
+        Table t{};
+        t.base = base;
+        long long blocks = 0;
+        for (; at < count && t.count < kTensors; ++at) {
+            const long long more = (tensors[at].n + kBlock - 1) / kBlock;
+            if (more == 0) continue;
+            if (blocks + more > (1ll << 25)) break;              // (the C entry takes tensors of up to that many blocks)
+            t.param[t.count] = (uint64_t)tensors[at].param;
+            t.grad[t.count] = (uint64_t)tensors[at].grad;
+            t.n[t.count] = (uint64_t)tensors[at].n;
+            t.first[t.count++] = (uint32_t)blocks;
+            blocks += more;
+        }
+        if (blocks == 0) break;
+        t.blocks = (uint32_t)blocks;
+        const dim3 grid((unsigned)((blocks + kWaves - 1) / kWaves));
+        auto go = [&](auto pt, auto gt, auto kd, auto ms) {
+            adamw_kernel<pt.value, gt.value, kd.value, (bool)ms.value><<<grid, kThreads, 0, stream>>>(t, a);
+        };
+        auto with_kind = [&](auto pt, auto gt) {
+            if (kind == EVOSPEC_MOMENTS_8BIT) a.master ? go(pt, gt, Const<1>{}, Const<1>{}) : go(pt, gt, Const<1>{}, Const<0>{});
+            else a.master ? go(pt, gt, Const<0>{}, Const<1>{}) : go(pt, gt, Const<0>{}, Const<0>{});
+        };
+        if (param_type == EVOSPEC_FP32) with_kind(Const<EVOSPEC_FP32>{}, Const<EVOSPEC_FP32>{});
+        else if (param_type == EVOSPEC_BF16)
+            grad_type == EVOSPEC_FP32 ? with_kind(Const<EVOSPEC_BF16>{}, Const<EVOSPEC_FP32>{}) : with_kind(Const<EVOSPEC_BF16>{}, Const<EVOSPEC_BF16>{});
+        else
+            grad_type == EVOSPEC_FP32 ? with_kind(Const<EVOSPEC_FP16>{}, Const<EVOSPEC_FP32>{}) : with_kind(Const<EVOSPEC_FP16>{}, Const<EVOSPEC_FP16>{});
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        base += blocks;
+    }
+    return hipSuccess;
+}
+
+hipError_t launch_adamw_moments(const void* m, const void* v, const float* scales, long long blocks, int type, void* out_m, void* out_v,
+                                hipStream_t stream) {
+    const dim3 grid((unsigned)((blocks + kWaves - 1) / kWaves));
+    const float2* s = reinterpret_cast<const float2*>(scales);
+    if (type == EVOSPEC_FP32) adamw_moments_kernel<EVOSPEC_FP32><<<grid, kThreads, 0, stream>>>((const uint8_t*)m, (const uint8_t*)v, s, blocks, out_m, out_v);
+    else adamw_moments_kernel<EVOSPEC_BF16><<<grid, kThreads, 0, stream>>>((const uint8_t*)m, (const uint8_t*)v, s, blocks, out_m, out_v);
+    return hipGetLastError();
+}
+
+}  // namespace evospec

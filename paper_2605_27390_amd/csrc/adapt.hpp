@@ -1,0 +1,102 @@
+// Adapters, the distillation loss and AdamW: host-side plans, arguments and launchers.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "evospec_adapt.h"
+
+namespace evospec {
+
+// The rows of a call and whose adapter they have.
+struct Requests {
+    const int32_t* row_off;
+    const int32_t* adapter;
+    int S, T, n;                              // n adapters
+};
+
+// How a product of rows with adapters is laid out: tiles of 16 << shift rows, their long axis in `splits` parts.
+struct LoraPlan {
+    int shift;                                // of the rows' tiles
+    int tiles;                                // workgroups for them: every request may begin one of its own
+    int down_splits;                          // parts of d in x A^T
+    int up_slices;                            // parts of d in h B^T
+};
+LoraPlan lora_plan(int S, int T, int d_down, int d_up);
+
+struct DownArgs {                             // out[split][rank][row] = factor * sum_k x[row][k] w[rank][k] over a part of k
+    Requests q;
+    const void* x;
+    long long x_stride;
+    const void* w;                            // [n][r][d], or [n][d][r]
+    const float* factor;                      // [n] or NULL
+    float* out;
+    int r, d, shift;
+};
+hipError_t launch_lora_down(const DownArgs& a, const LoraPlan& p, bool rank_last, hipStream_t stream);
+
+struct UpArgs {                               // y[row][c] += factor * sum_k h[k][row] w[c][k]
+    Requests q;
+    const float* h;                           // [splits][r][T]
+    int splits;
+    const float* factor;
+    const void* w;                            // [n][d][r], or [n][r][d]
+    void* y;
+    long long y_stride;
+    float* out_h;                             // [r][T]: the splits' sum, or NULL
+    int r, d, shift;
+};
+hipError_t launch_lora_up(const UpArgs& a, const LoraPlan& p, bool rank_last, hipStream_t stream);
+
+struct GradJob {                              // out[rank][c] (or [c][rank]) = sum_rows factor * h[rank][row] x[row][c]
+    const float* h;
+    int splits;
+    const float* factor;
+    const void* x;
+    long long x_stride;
+    int d;
+    bool rank_last;                           // of the output
+    float* out;                               // [n][...]
+};
+struct GradArgs {
+    Requests q;
+    GradJob job[2];
+    int r, parts;                             // parts of an adapter's rows
+    float* partial;                           // [parts][n r d0 + n r d1] of parts > 1
+};
+int lora_grad_parts(int n, int T, int d0, int d1);
+hipError_t launch_lora_grads(const GradArgs& a, hipStream_t stream);
+
+struct KdArgs {
+    const void* h;
+    const void* W;
+    const int32_t* support;
+    const float* target;
+    const float* weight;
+    int E, d, V, K, splits;
+    float T;
+    int type;
+    float* loss;
+    void* dh;
+    float* draft;
+    float* part;                              // [E][splits][2][d] of splits > 1
+    float2* part_ml;                          // [E][splits]: reference and sum
+};
+int kd_splits(int E, int K);
+hipError_t launch_kd(const KdArgs& a, hipStream_t stream);
+
+struct AdamwArgs {
+    void *m, *v;
+    float* scales;
+    float* master;
+    float decay, rate, beta1, beta1c, beta2, beta2c, root, eps;       // 1 - lr wd, lr / (1 - beta1^t), ..., 1 / sqrt(1 - beta2^t)
+    float log_beta1, log_beta2, weight_decay;                        // with a schedule
+    uint32_t seed_key, t_key;
+    const float* schedule;
+    const float* grad_scale;
+};
+hipError_t launch_adamw(const evospec_adamw_tensor* tensors, int count, int param_type, int grad_type, int kind, const AdamwArgs& a,
+                        hipStream_t stream);
+hipError_t launch_adamw_moments(const void* m, const void* v, const float* scales, long long blocks, int type, void* out_m, void* out_v,
+                                hipStream_t stream);
+
+}  // namespace evospec
