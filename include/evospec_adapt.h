@@ -33,14 +33,11 @@ typedef struct evospec_lora {
  *   y         dev bf16 [T, d_out], rows y_stride elements apart, 16-B aligned; no overlap with x.  Rounded once.
  *   out_h     dev fp32 [r, T] or NULL: h = x A^T, transposed, for evospec_lora_backward; columns of rows without an adapter
  *             are left as they are
- *   workspace dev, 16-B aligned, at least evospec_lora_workspace_bytes(...) bytes, scratch
  * Sums are fp32.  h goes into the second product as two bf16 numbers, which keep 2^-16 of it.
  * T at most 2^24, S at most 2^16.
  */
-int evospec_lora_workspace_bytes(const evospec_lora *lora, int S, int T, size_t *out_bytes /*host*/);
 int evospec_lora_forward(const evospec_lora *lora, const void *x, long long x_stride, const int32_t *row_off,
-                         const int32_t *adapter, int S, int T, void *y, long long y_stride, float *out_h, void *workspace,
-                         size_t workspace_bytes, void *stream);
+                         const int32_t *adapter, int S, int T, void *y, long long y_stride, float *out_h, void *stream);
 
 /*
  * Its backward pass from dy, the gradient of y:  g = scale * dy B,  dx += g A,  dA = sum_t g[t]^T x[t],
@@ -50,6 +47,7 @@ int evospec_lora_forward(const evospec_lora *lora, const void *x, long long x_st
  *   dx        dev bf16 [T, d_in], rows dx_stride elements apart, 16-B aligned, or NULL; rounded once; no overlap with x or dy
  *   out_da    dev fp32 [n][r][d_in], 16-B aligned      out_db dev fp32 [n][d_out][r], 16-B aligned: written whole (zeros where an
  *             adapter has no rows)
+ *   workspace dev, 16-B aligned, at least evospec_lora_backward_workspace_bytes(...) bytes, scratch
  * Sums are fp32 in an order that depends on the sizes only: the same inputs give the same bits.
  */
 int evospec_lora_backward_workspace_bytes(const evospec_lora *lora, int S, int T, size_t *out_bytes /*host*/);

@@ -49,6 +49,6 @@ from .adapt import (  # noqa: F401,E402
     kd_loss,
     kd_loss_workspace_bytes,
     lora_backward,
+    lora_backward_workspace_bytes,
     lora_forward,
-    lora_workspace_bytes,
 )

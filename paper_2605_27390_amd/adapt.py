@@ -27,8 +27,7 @@ class _Tensor(ctypes.Structure):
 _vp, _ci, _ll, _sz, _d = ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes.c_size_t, ctypes.c_double
 _szp, _lorap, _tensorp = ctypes.POINTER(_sz), ctypes.POINTER(_Lora), ctypes.POINTER(_Tensor)
 for _name, _args in {
-        "evospec_lora_workspace_bytes": [_lorap, _ci, _ci, _szp],
-        "evospec_lora_forward": [_lorap, _vp, _ll, _vp, _vp, _ci, _ci, _vp, _ll, _vp, _vp, _sz, _vp],
+        "evospec_lora_forward": [_lorap, _vp, _ll, _vp, _vp, _ci, _ci, _vp, _ll, _vp, _vp],
         "evospec_lora_backward_workspace_bytes": [_lorap, _ci, _ci, _szp],
         "evospec_lora_backward": [_lorap, _vp, _ll, _vp, _vp, _ll, _vp, _vp, _ci, _ci, _vp, _ll, _vp, _vp, _vp, _sz, _vp],
         "evospec_kd_loss_workspace_bytes": [_ci, _ci, _ci, _szp],
@@ -42,10 +41,10 @@ for _name, _args in {
 
 # The sizes that the library reports depend on few numbers, which are the same from call to call.
 @functools.lru_cache(maxsize=256)
-def _lora_bytes(n, r, d_in, d_out, S, T, backward):
+def _lora_bytes(n, r, d_in, d_out, S, T):
     out = _sz(0)
-    name = "evospec_lora_backward_workspace_bytes" if backward else "evospec_lora_workspace_bytes"
-    _check(getattr(lib, name)(ctypes.byref(_Lora(None, None, None, n, r, d_in, d_out)), S, T, ctypes.byref(out)), name)
+    _check(lib.evospec_lora_backward_workspace_bytes(ctypes.byref(_Lora(None, None, None, n, r, d_in, d_out)), S, T, ctypes.byref(out)),
+           "evospec_lora_backward_workspace_bytes")
     return out.value
 
 
@@ -83,7 +82,7 @@ class LoraBank:
             _elsewhere(scale, self._device, "scale")
             if scale.numel() != self.n:
                 raise ValueError("scale needs a value for every adapter")
-        _lora_bytes(self.n, self.r, self.d_in, self.d_out, 0, 0, False)      # (refuses the sizes that no call takes)
+        _lora_bytes(self.n, self.r, self.d_in, self.d_out, 0, 0)      # (refuses the sizes that no call takes)
         self.a, self.b, self.scale = a, b, scale
         self._c = _Lora(a.data_ptr(), b.data_ptr(), _ptr(scale), self.n, self.r, self.d_in, self.d_out)
         self._ref = ctypes.byref(self._c)
@@ -142,11 +141,7 @@ def _apart(out, name, *others):
             raise ValueError(f"{name} overlaps {other}")
 
 
-def lora_workspace_bytes(bank: LoraBank, S: int, T: int, backward: bool = False) -> int:
-    return _lora_bytes(bank.n, bank.r, bank.d_in, bank.d_out, S, T, bool(backward))
-
-
-def lora_forward(x, bank: LoraBank, row_off, adapter, y, keep: bool = False, out_h=None, workspace=None):
+def lora_forward(x, bank: LoraBank, row_off, adapter, y, keep: bool = False, out_h=None):
     """y[t] += scale (x[t] A^T) B^T in place, with the adapter of the request that row t belongs to: rows row_off[s] .. row_off[s + 1] have
     adapter[s] (int32, both on the GPU); rows of a request whose adapter is not in 0 .. n - 1, and rows of none, stay as they are.
     x [T, d_in], y [T, d_out] in bf16.  Returns h = x A^T, transposed, fp32 [r, T] (with keep, or as out_h), for lora_backward, else y."""
@@ -163,11 +158,13 @@ def lora_forward(x, bank: LoraBank, row_off, adapter, y, keep: bool = False, out
             raise ValueError(f"out_h must be [{bank.r}, {T}], got {tuple(out_h.shape)}")
     elif keep:
         out_h = _new((bank.r, T), (T, 1), dtype=_f32, device=x.device)
-    workspace = _workspace_of(workspace, _lora_bytes(bank.n, bank.r, bank.d_in, bank.d_out, S, T, False), dev, x.device)
     _check(lib.evospec_lora_forward(bank._ref, x.data_ptr(), xs, row_off.data_ptr(), adapter.data_ptr(), S, T, y.data_ptr(), ys,
-                                    _ptr(out_h), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_of(dev)),
-           "evospec_lora_forward")
+                                    _ptr(out_h), _stream_of(dev)), "evospec_lora_forward")
     return y if out_h is None else out_h
+
+
+def lora_backward_workspace_bytes(bank: LoraBank, S: int, T: int) -> int:
+    return _lora_bytes(bank.n, bank.r, bank.d_in, bank.d_out, S, T)
 
 
 def lora_backward(x, dy, bank: LoraBank, row_off, adapter, h=None, dx=None, out_da=None, out_db=None, workspace=None):
@@ -198,7 +195,7 @@ def lora_backward(x, dy, bank: LoraBank, row_off, adapter, h=None, dx=None, out_
         out_da = _new((bank.n, bank.r, bank.d_in), (bank.r * bank.d_in, bank.d_in, 1), dtype=_f32, device=x.device)
     if out_db is None:
         out_db = _new((bank.n, bank.d_out, bank.r), (bank.r * bank.d_out, bank.r, 1), dtype=_f32, device=x.device)
-    workspace = _workspace_of(workspace, _lora_bytes(bank.n, bank.r, bank.d_in, bank.d_out, S, T, True), dev, x.device)
+    workspace = _workspace_of(workspace, _lora_bytes(bank.n, bank.r, bank.d_in, bank.d_out, S, T), dev, x.device)
     _check(lib.evospec_lora_backward(bank._ref, x.data_ptr(), xs, _ptr(h), dy.data_ptr(), gs, row_off.data_ptr(), adapter.data_ptr(), S, T,
                                      _ptr(dx), ds, out_da.data_ptr(), out_db.data_ptr(), _ptr(workspace),
                                      0 if workspace is None else workspace.numel(), _stream_of(dev)), "evospec_lora_backward")

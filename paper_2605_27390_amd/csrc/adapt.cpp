@@ -31,7 +31,7 @@ int check_matrix(const void* p, long long stride, int d) {
     if (stride < d || stride > (1ll << 32)) return EVOSPEC_BAD_SHAPE;
     return stride % 8 == 0 && aligned(p, 16) ? EVOSPEC_OK : EVOSPEC_MISALIGNED;
 }
-size_t h_bytes(const evospec_lora* l, int T, int splits) { return up_to((size_t)splits * l->r * T * sizeof(float)); }
+size_t h_bytes(const evospec_lora* l, int T) { return up_to((size_t)l->r * T * sizeof(float)); }
 
 int check_kd(int E, int K, int d) {
     return E < 0 || E >= (1 << 20) || K < 1 || K > EVOSPEC_KD_K_MAX || d < 8 || d % 8 || d > EVOSPEC_KD_D_MAX ? EVOSPEC_BAD_SHAPE : EVOSPEC_OK;
@@ -58,32 +58,17 @@ int check_tensors(const evospec_adamw_tensor* tensors, int count, long long* blo
 
 extern "C" {
 
-int evospec_lora_workspace_bytes(const evospec_lora* lora, int S, int T, size_t* out_bytes) {
-    if (!out_bytes) return EVOSPEC_NULL_POINTER;
-    const int rc = check_lora(lora, S, T);
-    if (rc) return rc;
-    *out_bytes = S && T ? h_bytes(lora, T, lora_plan(S, T, lora->d_in, lora->d_out).down_splits) : 0;
-    return EVOSPEC_OK;
-}
-
 int evospec_lora_forward(const evospec_lora* lora, const void* x, long long x_stride, const int32_t* row_off, const int32_t* adapter,
-                         int S, int T, void* y, long long y_stride, float* out_h, void* workspace, size_t workspace_bytes, void* stream) {
+                         int S, int T, void* y, long long y_stride, float* out_h, void* stream) {
     int rc = check_lora(lora, S, T);
     if (rc) return rc;
     if (S == 0 || T == 0) return EVOSPEC_OK;
     if ((rc = check_weights(lora))) return rc;
     if ((rc = check_matrix(x, x_stride, lora->d_in)) || (rc = check_matrix(y, y_stride, lora->d_out))) return rc;
-    if (!row_off || !adapter || !workspace) return EVOSPEC_NULL_POINTER;
-    if (!aligned(workspace, 16) || !aligned(out_h, 4)) return EVOSPEC_MISALIGNED;
-    const LoraPlan p = lora_plan(S, T, lora->d_in, lora->d_out);
-    if (workspace_bytes < h_bytes(lora, T, p.down_splits)) return EVOSPEC_WORKSPACE_TOO_SMALL;
-    const Requests q{row_off, adapter, S, T, lora->n};
-    const bool at_once = out_h && p.down_splits == 1;            // nothing is left to add up
-    float* h = at_once ? out_h : static_cast<float*>(workspace);
-    const DownArgs down{q, x, x_stride, lora->a, nullptr, h, lora->r, lora->d_in, p.shift};
-    if ((rc = failed(launch_lora_down(down, p, false, static_cast<hipStream_t>(stream))))) return rc;
-    const UpArgs up{q, h, p.down_splits, lora->scale, lora->b, y, y_stride, at_once ? nullptr : out_h, lora->r, lora->d_out, p.shift};
-    return failed(launch_lora_up(up, p, true, static_cast<hipStream_t>(stream)));
+    if (!row_off || !adapter) return EVOSPEC_NULL_POINTER;
+    if (!aligned(out_h, 4)) return EVOSPEC_MISALIGNED;
+    const LoraArgs rows{{row_off, adapter, S, T, lora->n}, x, x_stride, lora->a, lora->d_in, lora->scale, lora->b, lora->d_out, y, y_stride, out_h, lora->r};
+    return failed(launch_lora_rows(rows, lora_plan(S, T, lora->d_out), false, static_cast<hipStream_t>(stream)));
 }
 
 int evospec_lora_backward_workspace_bytes(const evospec_lora* lora, int S, int T, size_t* out_bytes) {
@@ -93,9 +78,7 @@ int evospec_lora_backward_workspace_bytes(const evospec_lora* lora, int S, int T
     *out_bytes = 0;
     if (S == 0 || T == 0) return EVOSPEC_OK;
     const int parts = lora_grad_parts(lora->n, T, lora->d_in, lora->d_out);
-    *out_bytes = h_bytes(lora, T, lora_plan(S, T, lora->d_in, lora->d_out).down_splits) +
-                 h_bytes(lora, T, lora_plan(S, T, lora->d_out, lora->d_in).down_splits) +
-                 (parts > 1 ? (size_t)parts * lora->n * lora->r * ((size_t)lora->d_in + lora->d_out) * sizeof(float) : 0);
+    *out_bytes = 2 * h_bytes(lora, T) + (parts > 1 ? (size_t)parts * lora->n * lora->r * ((size_t)lora->d_in + lora->d_out) * sizeof(float) : 0);
     return EVOSPEC_OK;
 }
 
@@ -117,30 +100,25 @@ int evospec_lora_backward(const evospec_lora* lora, const void* x, long long x_s
     hipStream_t st = static_cast<hipStream_t>(stream);
     Requests q{row_off, adapter, S, T, lora->n};
     if (!rows) q.S = 0;
-    const LoraPlan px = lora_plan(rows ? S : 1, rows ? T : 1, lora->d_in, lora->d_out), py = lora_plan(rows ? S : 1, rows ? T : 1, lora->d_out, lora->d_in);
     char* ws = static_cast<char*>(workspace);
-    float* h_parts = reinterpret_cast<float*>(ws);
-    float* g = reinterpret_cast<float*>(ws + (rows ? h_bytes(lora, T, px.down_splits) : 0));
-    float* partial = reinterpret_cast<float*>(ws + (rows ? h_bytes(lora, T, px.down_splits) + h_bytes(lora, T, py.down_splits) : 0));
+    float* g = reinterpret_cast<float*>(ws);
+    float* again = reinterpret_cast<float*>(ws + (rows ? h_bytes(lora, T) : 0));
     if (rows) {
+        const LoraPlan p = lora_plan(S, T, lora->d_in);
         if (!h) {
-            const DownArgs down{q, x, x_stride, lora->a, nullptr, h_parts, lora->r, lora->d_in, px.shift};
-            if ((rc = failed(launch_lora_down(down, px, false, st)))) return rc;
+            const LoraArgs down{q, x, x_stride, lora->a, lora->d_in, nullptr, nullptr, 0, nullptr, 0, again, lora->r};
+            if ((rc = failed(launch_lora_rows(down, p, false, st)))) return rc;
         }
-        const DownArgs down{q, dy, dy_stride, lora->b, lora->scale, g, lora->r, lora->d_out, py.shift};
-        if ((rc = failed(launch_lora_down(down, py, true, st)))) return rc;
-        if (dx) {
-            const UpArgs up{q, g, py.down_splits, nullptr, lora->a, dx, dx_stride, nullptr, lora->r, lora->d_in, py.shift};
-            if ((rc = failed(launch_lora_up(up, py, false, st)))) return rc;
-        }
+        const LoraArgs back{q, dy, dy_stride, lora->b, lora->d_out, lora->scale, lora->a, lora->d_in, dx, dx_stride, g, lora->r};
+        if ((rc = failed(launch_lora_rows(back, p, true, st)))) return rc;
     }
     GradArgs a{};
     a.q = q;
-    a.job[0] = GradJob{g, py.down_splits, nullptr, x, x_stride, lora->d_in, false, out_da};
-    a.job[1] = GradJob{h ? h : h_parts, h ? 1 : px.down_splits, lora->scale, dy, dy_stride, lora->d_out, true, out_db};
+    a.job[0] = GradJob{g, nullptr, x, x_stride, lora->d_in, false, out_da};
+    a.job[1] = GradJob{h ? h : again, lora->scale, dy, dy_stride, lora->d_out, true, out_db};
     a.r = lora->r;
     a.parts = rows ? lora_grad_parts(lora->n, T, lora->d_in, lora->d_out) : 1;
-    a.partial = partial;
+    a.partial = reinterpret_cast<float*>(ws + (rows ? 2 * h_bytes(lora, T) : 0));
     return failed(launch_lora_grads(a, st));
 }
 

@@ -14,42 +14,33 @@ struct Requests {
     int S, T, n;                              // n adapters
 };
 
-// How a product of rows with adapters is laid out: tiles of 16 << shift rows, their long axis in `splits` parts.
+// How the products of rows with adapters are laid out: tiles of 16 << shift rows, the columns of the second product in `slices`.
 struct LoraPlan {
-    int shift;                                // of the rows' tiles
-    int tiles;                                // workgroups for them: every request may begin one of its own
-    int down_splits;                          // parts of d in x A^T
-    int up_slices;                            // parts of d in h B^T
+    int shift;
+    int tiles;                                // workgroups for the rows: every request may begin a tile of its own
+    int slices;
 };
-LoraPlan lora_plan(int S, int T, int d_down, int d_up);
+LoraPlan lora_plan(int S, int T, int d_up);
 
-struct DownArgs {                             // out[split][rank][row] = factor * sum_k x[row][k] w[rank][k] over a part of k
+struct LoraArgs {                             // h = x w_down^T (times factor, backward), y += factor h w_up
     Requests q;
     const void* x;
     long long x_stride;
-    const void* w;                            // [n][r][d], or [n][d][r]
+    const void* w_down;
+    int d_down;
     const float* factor;                      // [n] or NULL
-    float* out;
-    int r, d, shift;
-};
-hipError_t launch_lora_down(const DownArgs& a, const LoraPlan& p, bool rank_last, hipStream_t stream);
-
-struct UpArgs {                               // y[row][c] += factor * sum_k h[k][row] w[c][k]
-    Requests q;
-    const float* h;                           // [splits][r][T]
-    int splits;
-    const float* factor;
-    const void* w;                            // [n][d][r], or [n][r][d]
-    void* y;
+    const void* w_up;
+    int d_up;
+    void* y;                                  // NULL: h alone
     long long y_stride;
-    float* out_h;                             // [r][T]: the splits' sum, or NULL
-    int r, d, shift;
+    float* h;                                 // [r][T] or NULL
+    int r;
 };
-hipError_t launch_lora_up(const UpArgs& a, const LoraPlan& p, bool rank_last, hipStream_t stream);
+// back: w_down is [n][d][r] and w_up [n][r][d], else the other way round
+hipError_t launch_lora_rows(const LoraArgs& a, const LoraPlan& p, bool back, hipStream_t stream);
 
-struct GradJob {                              // out[rank][c] (or [c][rank]) = sum_rows factor * h[rank][row] x[row][c]
+struct GradJob {                              // out[rank][c] (or [c][rank]) = factor * sum_rows h[rank][row] x[row][c]
     const float* h;
-    int splits;
     const float* factor;
     const void* x;
     long long x_stride;

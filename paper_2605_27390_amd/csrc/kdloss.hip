@@ -17,65 +17,79 @@ namespace {
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kMost = EVOSPEC_KD_K_MAX;
 
-// Sum over the workgroup in a fixed order; every thread has it.
-template <typename T>
-__device__ __forceinline__ T block_sum(T x, T* buf /*LDS [kWaves]*/) {
+// Sums over the workgroup in a fixed order; every thread has them.
+template <int N, typename T>
+__device__ __forceinline__ void block_sums(T (&x)[N], T (*buf)[N] /*LDS [kWaves][N]*/) {
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = x;
-    __syncthreads();
-    T s = buf[0];
+    for (int o = 32; o > 0; o >>= 1)
 #pragma unroll
-    for (int i = 1; i < kWaves; ++i) s += buf[i];
-    return s;
+        for (int i = 0; i < N; ++i) x[i] += __shfl_xor(x[i], o);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i) buf[threadIdx.x >> 6][i] = x[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        x[i] = buf[0][i];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) x[i] += buf[w][i];
+    }
 }
-// The largest, leaving NaN out.
-__device__ __forceinline__ float block_max(float x, float* buf) {
-    x = wave_max(x, threadIdx.x & 63);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = x;
-    __syncthreads();
-    float s = buf[0];
+// The largest of each, leaving NaN out.
+template <int N>
+__device__ __forceinline__ void block_max(float (&x)[N], float (*buf)[N]) {
 #pragma unroll
-    for (int i = 1; i < kWaves; ++i) s = fmaxf(s, buf[i]);
-    return s;
+    for (int i = 0; i < N; ++i) x[i] = wave_max(x[i], threadIdx.x & 63);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i) buf[threadIdx.x >> 6][i] = x[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        x[i] = buf[0][i];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) x[i] = fmaxf(x[i], buf[w][i]);
+    }
 }
 
-// weight T^2 KL(p || q) of an event in 64 bits, by all threads; draft: its logits.
-__device__ __forceinline__ void event_loss(const KdArgs& a, int e, const float* draft, double* buf, float* fbuf) {
-    const int32_t* ids = a.support + (long long)e * a.K;
-    const float* target = a.target + (long long)e * a.K;
-    float mt = -__builtin_inff(), mz = mt;
-    for (int j = threadIdx.x; j < a.K; j += kThreads)
-        if ((unsigned)ids[j] < (unsigned)a.V) {
-            mt = fmaxf(mt, target[j]);
-            mz = fmaxf(mz, draft[j]);
-        }
-    mt = block_max(mt, fbuf);
-    mz = block_max(mz, fbuf);
+struct LossShared {
+    float top[kWaves][2];
+    double sum[kWaves][4];
+};
+// weight T^2 KL(p || q) of an event in 64 bits, by all threads; draft: its logits.  With t and z relative to their largest, over T:
+// KL = sum e^t (t - z) / sum e^t - log sum e^t + log sum e^z.
+__device__ __forceinline__ void event_loss(const KdArgs& a, int e, const float* draft, LossShared& sh) {
+    constexpr int kPer = kMost / kThreads;
+    const float inf = __builtin_inff();
+    float t[kPer], z[kPer], top[2] = {-inf, -inf};
+    bool mine[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int j = i * kThreads + threadIdx.x;
+        mine[i] = j < a.K && (unsigned)a.support[(long long)e * a.K + j] < (unsigned)a.V;
+        t[i] = mine[i] ? a.target[(long long)e * a.K + j] : -inf;
+        z[i] = mine[i] ? draft[j] : -inf;
+        top[0] = fmaxf(top[0], t[i]);
+        top[1] = fmaxf(top[1], z[i]);
+    }
+    block_max(top, sh.top);
     const double inv = 1.0 / (double)a.T;
-    double st = 0.0, sz = 0.0;
-    bool any_nan = false;
-    for (int j = threadIdx.x; j < a.K; j += kThreads)
-        if ((unsigned)ids[j] < (unsigned)a.V) {
-            any_nan |= target[j] != target[j];
-            st += exp(((double)target[j] - mt) * inv);
-            sz += exp(((double)draft[j] - mz) * inv);
+    double s[4] = {};                                            // (the last counts NaN)
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+        if (mine[i]) {
+            const double dt = ((double)t[i] - top[0]) * inv, dz = ((double)z[i] - top[1]) * inv, p = exp(dt);
+            s[0] += p;
+            s[1] += exp(dz);
+            if (!(p == 0.0)) s[2] += p * (dt - dz);
+            s[3] += t[i] != t[i] ? 1.0 : 0.0;
         }
-    any_nan = __syncthreads_or(any_nan);
-    st = block_sum(st, buf);
-    sz = block_sum(sz, buf);
-    const double lt = log(st), lz = log(sz);
-    double kl = 0.0;
-    for (int j = threadIdx.x; j < a.K; j += kThreads)
-        if ((unsigned)ids[j] < (unsigned)a.V) {
-            const double lp = ((double)target[j] - mt) * inv - lt, lq = ((double)draft[j] - mz) * inv - lz, p = exp(lp);
-            if (!(p == 0.0)) kl += p * (lp - lq);
-        }
-    kl = block_sum(kl, buf);
+    block_sums(s, sh.sum);
     if (threadIdx.x == 0) {
-        const bool none = mt == -__builtin_inff() && !any_nan;   // no entry, or no target mass
+        const bool none = top[0] == -inf && s[3] == 0.0;         // no entry, or no target mass
+        const double kl = s[2] / s[0] - log(s[0]) + log(s[1]);
         a.loss[e] = none ? 0.f : (float)((double)(a.weight ? a.weight[e] : 1.f) * a.T * a.T * kl);
     }
 }
@@ -93,18 +107,26 @@ __device__ __forceinline__ void store8(void* out, long long at, const float* x) 
     }
 }
 
-// NC pieces of 8 elements to a thread, RB rows at a time.
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+// lanes with bit STRIDE keep b's sum with their partner, the others a's
+template <int STRIDE>
+__device__ __forceinline__ float fold(float a, float b, int lane) {
+    const bool high = lane & STRIDE;
+    const float keep = high ? b : a, give = high ? a : b;
+    return keep + __uint_as_float(xor_lane<STRIDE>(__float_as_uint(give), lane));
+}
+
+// NC pieces of 8 elements to a thread, RB rows at a time, the next ones under way meanwhile.
 template <int NC, int RB, int TYPE>
 __global__ __launch_bounds__(kThreads) void kd_rows_kernel(KdArgs a) {
-    __shared__ float dots[2][kWaves][RB];
-    __shared__ float p[kMost];                                   // of this workgroup's entries
-    __shared__ float z[kMost];
-    __shared__ int32_t ids[kMost];
-    __shared__ double dbuf[kWaves];
-    __shared__ float fbuf[kWaves];
+    __shared__ __align__(16) float dots[2][RB][kWaves];
+    __shared__ float p[kMost + 16];                                   // of this workgroup's entries
+    __shared__ float z[kMost + 16];
+    __shared__ int32_t ids[kMost + 16];
+    __shared__ LossShared loss;
     const int e = blockIdx.x, part = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int j0 = (int)((long long)a.K * part / a.splits), j1 = (int)((long long)a.K * (part + 1) / a.splits);
-    const float inv = 1.f / a.T;
+    const int j0 = (int)((long long)a.K * part / a.splits), j1 = (int)((long long)a.K * (part + 1) / a.splits), n = j1 - j0;
+    const float inv = 1.f / a.T, inf = __builtin_inff();
     bool in[NC];
     u32x4 h[NC];
 #pragma unroll
@@ -112,96 +134,128 @@ __global__ __launch_bounds__(kThreads) void kd_rows_kernel(KdArgs a) {
         in[c] = 8 * (c * kThreads + tid) < a.d;
         h[c] = in[c] ? *(gvec_ptr)((const uint16_t*)a.h + (long long)e * a.d + 8 * (c * kThreads + tid)) : u32x4{0, 0, 0, 0};
     }
-    // p, from all entries of the event
-    float mt = -__builtin_inff();
-    for (int j = tid; j < a.K; j += kThreads)
-        if ((unsigned)a.support[(long long)e * a.K + j] < (unsigned)a.V) mt = fmaxf(mt, a.target[(long long)e * a.K + j]);
-    mt = block_max(mt, fbuf);
-    float sum = 0.f;
+    // all entries of the event: p needs their sum
+    constexpr int kPer = kMost / kThreads;
+    float t[kPer], top_t[1] = {-inf};
     bool nan = false;
-    for (int j = tid; j < a.K; j += kThreads) {
-        const int32_t id = a.support[(long long)e * a.K + j];
-        const float t = a.target[(long long)e * a.K + j];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int j = i * kThreads + tid;
+        const int32_t id = j < a.K ? a.support[(long long)e * a.K + j] : -1;
         const bool mine = (unsigned)id < (unsigned)a.V;
-        const float x = mine ? expf((t - mt) * inv) : 0.f;
-        sum += x;
-        nan |= mine && t != t;
-        if (j >= j0 && j < j1) {
-            p[j - j0] = x;
-            ids[j - j0] = mine ? id : -1;
-        }
+        t[i] = mine ? a.target[(long long)e * a.K + j] : -inf;
+        top_t[0] = fmaxf(top_t[0], t[i]);
+        nan |= t[i] != t[i];
+        if (j >= j0 && j < j1) ids[j - j0] = mine ? id : -1;
     }
+    __syncthreads();
+
+    u32x4 even[RB][NC], odd[RB][NC];
+    auto load = [&](u32x4 (&row)[RB][NC], int at) {
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            const int id = at + r < n ? __builtin_amdgcn_readfirstlane(ids[at + r]) : -1;
+            if (id >= 0) {
+                const uint16_t* w = (const uint16_t*)a.W + (long long)id * a.d;
+#pragma unroll
+                for (int c = 0; c < NC; ++c) row[r][c] = in[c] ? *(gvec_ptr)(w + 8 * (c * kThreads + tid)) : u32x4{0, 0, 0, 0};
+            } else {
+#pragma unroll
+                for (int c = 0; c < NC; ++c) row[r][c] = u32x4{0, 0, 0, 0};
+            }
+        }
+    };
+    load(even, 0);                                               // (on their way during the sum)
+    block_max(top_t, reinterpret_cast<float (*)[1]>(loss.top));
     nan = __syncthreads_or(nan);
-    const float total = block_sum(sum, fbuf);
-    const bool none = mt == -__builtin_inff() && !nan;
-    const float per = none ? 0.f : 1.f / total;
+    const bool none = top_t[0] == -inf && !nan;
+    float x[kPer], total[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        x[i] = t[i] == -inf ? 0.f : expf((t[i] - top_t[0]) * inv);
+        total[0] += x[i];
+    }
+    block_sums(total, reinterpret_cast<float (*)[1]>(loss.top));
+    const float per = none ? 0.f : 1.f / total[0];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int j = i * kThreads + tid;
+        if (j >= j0 && j < j1) p[j - j0] = x[i] * per;
+    }
     __syncthreads();
 
     float o1[NC][8] = {}, o2[NC][8] = {};
-    float m = -__builtin_inff(), l = 0.f;
-    u32x4 row[RB][NC];
-    const int n = j1 - j0;
-    auto load = [&](int at) {
+    float m = -inf, l = 0.f;
+    const int mod = lane & (RB - 1);                             // the row of a turn whose logit and weights this lane looks after
+    auto add = [&](const u32x4 (&row)[RB][NC], int at, int turn) {
+        float dot[RB];
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
-            const int id = at + r < n ? ids[at + r] : -1;        // (uniform)
-            const uint16_t* w = (const uint16_t*)a.W + (long long)(id < 0 ? 0 : id) * a.d;
-#pragma unroll
-            for (int c = 0; c < NC; ++c)
-                row[r][c] = in[c] && id >= 0 ? *(gvec_ptr)(w + 8 * (c * kThreads + tid)) : u32x4{0, 0, 0, 0};
-        }
-    };
-    for (int at = 0, turn = 0; at < n; at += RB, turn ^= 1) {
-        load(at);
-#pragma unroll
-        for (int r = 0; r < RB; ++r) {
-            float dot = 0.f;
+            dot[r] = 0.f;
 #pragma unroll
             for (int c = 0; c < NC; ++c)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    dot = fmaf(__uint_as_float(row[r][c][q] << 16), __uint_as_float(h[c][q] << 16), dot);
-                    dot = fmaf(__uint_as_float(row[r][c][q] & 0xffff0000u), __uint_as_float(h[c][q] & 0xffff0000u), dot);
+                    const uint32_t w = row[r][c][q], x = h[c][q];        // (a bit_cast of a vector's element takes its first one)
+                    dot[r] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), __builtin_bit_cast(bf16x2, x), dot[r], false);
                 }
-            dot = wave_sum(dot, lane);
-            if (lane == 0) dots[turn][wave][r] = dot;
         }
-        __syncthreads();
-        float x[RB], top = m;
-#pragma unroll
-        for (int r = 0; r < RB; ++r) {
-            x[r] = dots[turn][0][r];
-#pragma unroll
-            for (int w = 1; w < kWaves; ++w) x[r] += dots[turn][w][r];
-            const bool mine = at + r < n && ids[at + r] >= 0;
-            if (tid == 0 && at + r < n) z[at + r] = mine ? x[r] : __builtin_nanf("");
-            if (!mine) x[r] = -__builtin_inff();
-            else x[r] *= inv;
-            top = fmaxf(top, x[r]);
+        // sums of RB rows at once: lanes whose low bits are r end up with row r
+        if constexpr (RB == 4) {
+            const float a0 = fold<1>(dot[0], dot[1], lane), a1 = fold<1>(dot[2], dot[3], lane);
+            dot[0] = fold<2>(a0, a1, lane);
+        } else if constexpr (RB == 2) {
+            dot[0] = fold<1>(dot[0], dot[1], lane);
+            dot[0] += __uint_as_float(xor_lane<2>(__float_as_uint(dot[0]), lane));
+        } else {
+            dot[0] += __uint_as_float(xor_lane<1>(__float_as_uint(dot[0]), lane));
+            dot[0] += __uint_as_float(xor_lane<2>(__float_as_uint(dot[0]), lane));
         }
-        const float back = top == m ? 1.f : expf(m - top);       // (uniform)
-        if (back != 1.f) {
+        dot[0] += __uint_as_float(xor_lane<4>(__float_as_uint(dot[0]), lane));
+        dot[0] += __uint_as_float(xor_lane<8>(__float_as_uint(dot[0]), lane));
+        dot[0] += __uint_as_float(xor_lane<16>(__float_as_uint(dot[0]), lane));
+        dot[0] += __uint_as_float(xor_lane<32>(__float_as_uint(dot[0]), lane));
+        if (lane < RB) dots[turn][lane][wave] = dot[0];
+        lds_barrier();                                           // (the rows under way stay so; the two halves of dots take turns)
+        const float4 d = *reinterpret_cast<const float4*>(dots[turn][mod]);
+        float x = (d.x + d.y) + (d.z + d.w);
+        const bool mine = at + mod < n && ids[at + mod] >= 0;
+        if (tid < RB && at + mod < n) z[at + mod] = mine ? x : __builtin_nanf("");
+        x = mine ? x * inv : -inf;
+        float top = x;
+        if constexpr (RB >= 2) top = fmaxf(top, __uint_as_float(xor_lane<1>(__float_as_uint(top), lane)));
+        if constexpr (RB >= 4) top = fmaxf(top, __uint_as_float(xor_lane<2>(__float_as_uint(top), lane)));
+        top = fmaxf(top, m);
+        if (__builtin_amdgcn_readfirstlane(top != m)) {          // (the same in all lanes)
+            const float back = expf(m - top);
             l *= back;
 #pragma unroll
             for (int c = 0; c < NC; ++c)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) o1[c][i] *= back;
+            m = top;
         }
-        m = top;
+        const float q = mine ? expf(x - m) : 0.f, w = mine ? p[at + mod] : 0.f;
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
-            if (at + r >= n || ids[at + r] < 0) continue;
-            const float q = expf(x[r] - m), w = p[at + r] * per;
-            l += q;
+            const float qr = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(q), r));
+            const float wr = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), r));
+            l += qr;
 #pragma unroll
             for (int c = 0; c < NC; ++c)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float v = i & 1 ? __uint_as_float(row[r][c][i / 2] & 0xffff0000u) : __uint_as_float(row[r][c][i / 2] << 16);
-                    o1[c][i] = fmaf(q, v, o1[c][i]);
-                    o2[c][i] = fmaf(w, v, o2[c][i]);
+                    o1[c][i] = fmaf(qr, v, o1[c][i]);
+                    o2[c][i] = fmaf(wr, v, o2[c][i]);
                 }
         }
+    };
+    for (int at = 0; at < n; at += 2 * RB) {
+        load(odd, at + RB);
+        add(even, at, 0);
+        load(even, at + 2 * RB);
+        add(odd, at + RB, 1);
     }
     __syncthreads();
     for (int j = tid; j < n; j += kThreads) a.draft[(long long)e * a.K + j0 + j] = z[j];
@@ -215,7 +269,7 @@ __global__ __launch_bounds__(kThreads) void kd_rows_kernel(KdArgs a) {
                 for (int i = 0; i < 8; ++i) g[i] = none ? 0.f : factor * (o1[c][i] * li - o2[c][i]);
                 store8<TYPE>(a.dh, (long long)e * a.d + 8 * (c * kThreads + tid), g);
             }
-        event_loss(a, e, z, dbuf, fbuf);
+        event_loss(a, e, z, loss);
     } else {
         float* out = a.part + ((long long)e * a.splits + part) * 2 * a.d;
 #pragma unroll
@@ -228,42 +282,64 @@ __global__ __launch_bounds__(kThreads) void kd_rows_kernel(KdArgs a) {
     }
 }
 
-// Joins the parts of an event's rows: 2,048 elements of its gradient to a workgroup, the first of which takes the loss as well.
-template <int TYPE>
+// Joins the parts of an event's rows: V elements of its gradient to a thread, whose parts (N at a time) are asked for together; a workgroup
+// of its own takes the loss.
+template <int TYPE, int V, int N>
 __global__ __launch_bounds__(kThreads) void kd_join_kernel(KdArgs a) {
-    __shared__ double dbuf[kWaves];
-    __shared__ float fbuf[kWaves];
-    const int e = blockIdx.x, at = 8 * (blockIdx.y * kThreads + threadIdx.x);
-    const float2* ml = a.part_ml + (long long)e * a.splits;
-    float m = -__builtin_inff();
-    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, ml[s].x);
-    float l = 0.f, o[8] = {}, o2[8] = {};
-    bool none = false;
-    for (int s = 0; s < a.splits; ++s) {
-        const float2 x = ml[s];
-        none |= x.y == -1.f;
-        const bool empty = x.y == 0.f && x.x == -__builtin_inff();           // a part without entries (its sums are zeros)
-        const float f = empty ? 0.f : expf(x.x - m);
-        l += x.y * f;
-        if (at < a.d && !empty) {
-            const float4* p = reinterpret_cast<const float4*>(a.part + ((long long)e * a.splits + s) * 2 * a.d + at);
-            const float4* q = reinterpret_cast<const float4*>(a.part + ((long long)e * a.splits + s) * 2 * a.d + a.d + at);
+    __shared__ LossShared loss;
+    if (blockIdx.y == 0) {
+        event_loss(a, blockIdx.x, a.draft + (long long)blockIdx.x * a.K, loss);
+        return;
+    }
+    typedef float vec __attribute__((ext_vector_type(V)));
+    const int e = blockIdx.x, lane = threadIdx.x & 63, at = V * (((int)blockIdx.y - 1) * kThreads + (int)threadIdx.x);
+    if (at - V * lane >= a.d) return;                            // (whole wavefronts)
+    const float* part = a.part + (long long)e * a.splits * 2 * a.d + min(at, a.d - V);
+    const float inf = __builtin_inff();
+    // lane s has the reference, sum and factor of part s (there are at most 32)
+    const float2 mine = lane < a.splits ? a.part_ml[(long long)e * a.splits + lane] : make_float2(-inf, 0.f);
+    vec u[N], v[N], o = {}, o2 = {};
+    auto load = [&](int s0) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float4 u = p[i], v = q[i];
-                o[4 * i] = fmaf(f, u.x, o[4 * i]); o[4 * i + 1] = fmaf(f, u.y, o[4 * i + 1]);
-                o[4 * i + 2] = fmaf(f, u.z, o[4 * i + 2]); o[4 * i + 3] = fmaf(f, u.w, o[4 * i + 3]);
-                o2[4 * i] += v.x; o2[4 * i + 1] += v.y; o2[4 * i + 2] += v.z; o2[4 * i + 3] += v.w;
+        for (int i = 0; i < N; ++i) {
+            const float* p = part + (long long)min(s0 + i, a.splits - 1) * 2 * a.d;
+            u[i] = *reinterpret_cast<const vec*>(p);
+            v[i] = *reinterpret_cast<const vec*>(p + a.d);
+        }
+    };
+    load(0);
+    const float m = wave_max(mine.x, lane);
+    const bool none = __ballot(mine.y == -1.f) != 0;
+    const bool empty = mine.y == 0.f && mine.x == -inf;          // a part without entries (its sums are zeros)
+    const float factor = empty ? 0.f : expf(mine.x - m);
+    const float l = wave_sum(mine.y * factor, lane);
+    for (int s0 = 0;; load(s0)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            // (without a way past the addition, which would have each part's loads wait for the one before)
+            const bool there = s0 + i < a.splits;
+            const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(factor), (s0 + i) & 63));
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                o[k] = there ? fmaf(f, u[i][k], o[k]) : o[k];
+                o2[k] = there ? o2[k] + v[i][k] : o2[k];
             }
         }
+        if ((s0 += N) >= a.splits) break;
     }
-    const float factor = (a.weight ? a.weight[e] : 1.f) * a.T, li = 1.f / l;
-    if (at < a.d) {
+    if (at >= a.d) return;
+    const float all = (a.weight ? a.weight[e] : 1.f) * a.T, li = 1.f / l;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = none ? 0.f : factor * (o[i] * li - o2[i]);
-        store8<TYPE>(a.dh, (long long)e * a.d + at, o);
+    for (int k = 0; k < V; ++k) o[k] = none ? 0.f : all * (o[k] * li - o2[k]);
+    if constexpr (TYPE == EVOSPEC_FP32) {
+        *reinterpret_cast<vec*>((float*)a.dh + (long long)e * a.d + at) = o;
+    } else {
+        typedef __bf16 out __attribute__((ext_vector_type(V)));
+        out x;
+#pragma unroll
+        for (int k = 0; k < V; ++k) x[k] = (__bf16)o[k];
+        *reinterpret_cast<out*>((__bf16*)a.dh + (long long)e * a.d + at) = x;
     }
-    if (blockIdx.y == 0) event_loss(a, e, a.draft + (long long)e * a.K, dbuf, fbuf);
 }
 
 template <int NC, int RB>
@@ -277,18 +353,24 @@ hipError_t rows_as(const KdArgs& a, hipStream_t stream) {
 }  // namespace
 
 int kd_splits(int E, int K) {
-    int s = 512 / E;
+    int s = 768 / E;
     if (s > K / 8) s = K / 8;
     return s < 1 ? 1 : s > 32 ? 32 : s;
 }
 
 hipError_t launch_kd(const KdArgs& a, hipStream_t stream) {
     const int pieces = (a.d / 8 + kThreads - 1) / kThreads;
-    const hipError_t e = pieces == 1 ? rows_as<1, 8>(a, stream) : pieces == 2 ? rows_as<2, 8>(a, stream) : pieces <= 4 ? rows_as<4, 4>(a, stream) : rows_as<8, 2>(a, stream);
+    const hipError_t e = pieces == 1 ? rows_as<1, 4>(a, stream) : pieces == 2 ? rows_as<2, 4>(a, stream) : pieces <= 4 ? rows_as<4, 2>(a, stream) : rows_as<8, 1>(a, stream);
     if (e != hipSuccess || a.splits == 1) return e;
-    const dim3 grid((unsigned)a.E, (unsigned)pieces);
-    if (a.type == EVOSPEC_FP32) kd_join_kernel<EVOSPEC_FP32><<<grid, kThreads, 0, stream>>>(a);
-    else kd_join_kernel<EVOSPEC_BF16><<<grid, kThreads, 0, stream>>>(a);
+    const int v = a.splits <= 8 ? 4 : 2;
+    const dim3 grid((unsigned)a.E, (unsigned)(1 + (a.d + v * kThreads - 1) / (v * kThreads)));
+    if (v == 4) {
+        if (a.type == EVOSPEC_FP32) kd_join_kernel<EVOSPEC_FP32, 4, 4><<<grid, kThreads, 0, stream>>>(a);
+        else kd_join_kernel<EVOSPEC_BF16, 4, 4><<<grid, kThreads, 0, stream>>>(a);
+    } else {
+        if (a.type == EVOSPEC_FP32) kd_join_kernel<EVOSPEC_FP32, 2, 32><<<grid, kThreads, 0, stream>>>(a);
+        else kd_join_kernel<EVOSPEC_BF16, 2, 32><<<grid, kThreads, 0, stream>>>(a);
+    }
     return hipGetLastError();
 }
 

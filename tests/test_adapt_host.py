@@ -25,7 +25,7 @@ BAD_SIZES = [dict(n=0), dict(n=65536), dict(r=0), dict(r=12), dict(r=72), dict(d
 
 def test_lora_bytes(ev):
     out = ctypes.c_size_t(0)
-    for f in (ev.lib.evospec_lora_workspace_bytes, ev.lib.evospec_lora_backward_workspace_bytes):
+    for f in (ev.lib.evospec_lora_backward_workspace_bytes,):
         assert f(ctypes.byref(lora()), 4, 100, ctypes.byref(out)) == 0 and out.value >= 16 * 100 * 4
         for S, T in ((0, 5), (5, 0)):
             assert f(ctypes.byref(lora()), S, T, ctypes.byref(out)) == 0 and out.value == 0
@@ -35,12 +35,12 @@ def test_lora_bytes(ev):
             assert f(ctypes.byref(lora()), S, T, ctypes.byref(out)) == 2
         assert f(None, 4, 100, ctypes.byref(out)) == 1 and f(ctypes.byref(lora()), 4, 100, None) == 1
     # past 32 bits
-    assert ev.lib.evospec_lora_workspace_bytes(ctypes.byref(lora(r=64)), 1, 1 << 24, ctypes.byref(out)) == 0 and out.value >= 1 << 32
+    assert ev.lib.evospec_lora_backward_workspace_bytes(ctypes.byref(lora(r=64)), 1, 1 << 24, ctypes.byref(out)) == 0 and out.value >= 1 << 32
 
 
 # Addresses below are never dereferenced: every call that is not an error has nothing to do.
-def forward(ev, l=None, x=16, xs=64, off=16, ad=16, S=2, T=5, y=16, ys=32, h=None, ws=16, wb=1 << 30):
-    return ev.lib.evospec_lora_forward(ctypes.byref(l or lora()), x, xs, off, ad, S, T, y, ys, h, ws, wb, None)
+def forward(ev, l=None, x=16, xs=64, off=16, ad=16, S=2, T=5, y=16, ys=32, h=None):
+    return ev.lib.evospec_lora_forward(ctypes.byref(l or lora()), x, xs, off, ad, S, T, y, ys, h, None)
 
 
 def backward(ev, l=None, x=16, xs=64, h=None, dy=16, gs=32, off=16, ad=16, S=2, T=5, dx=None, ds=64, da=16, db=16, ws=16, wb=1 << 30):
@@ -53,11 +53,11 @@ def test_lora_refusals(ev):
             assert f(ev, l=lora(**bad)) == 2, bad
         for bad in (dict(S=-1), dict(T=-1), dict(S=(1 << 16) + 1), dict(T=(1 << 24) + 1), dict(xs=63), dict(xs=(1 << 32) + 8)):
             assert f(ev, **bad) == 2, bad
-        for bad in (dict(x=None), dict(off=None), dict(ad=None), dict(ws=None), dict(l=lora(a=None)), dict(l=lora(b=None))):
+        for bad in (dict(x=None), dict(off=None), dict(ad=None), dict(l=lora(a=None)), dict(l=lora(b=None))):
             assert f(ev, **bad) == 1, bad
-        for bad in (dict(x=24), dict(xs=68), dict(ws=8), dict(l=lora(a=8)), dict(l=lora(b=8)), dict(l=lora(scale=2)), dict(h=2)):
+        for bad in (dict(x=24), dict(xs=68), dict(l=lora(a=8)), dict(l=lora(b=8)), dict(l=lora(scale=2)), dict(h=2)):
             assert f(ev, **bad) == 4, bad
-        assert f(ev, wb=8) == 5
+    assert backward(ev, wb=8) == 5 and backward(ev, ws=None) == 1 and backward(ev, ws=8) == 4
     assert forward(ev, ys=24) == 2 and forward(ev, ys=36) == 4 and forward(ev, y=None) == 1 and forward(ev, y=8) == 4
     assert backward(ev, gs=24) == 2 and backward(ev, gs=36) == 4 and backward(ev, dy=None) == 1 and backward(ev, dy=8) == 4
     assert backward(ev, dx=16, ds=56) == 2 and backward(ev, dx=16, ds=68) == 4 and backward(ev, dx=8) == 4

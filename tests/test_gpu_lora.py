@@ -239,7 +239,7 @@ def test_refusals(ev):
     with pytest.raises(ev.EvospecError):                             # rows that do not begin on 16 bytes
         ev.lora_forward(torch.zeros(11, 68, dtype=torch.bfloat16, device="cuda")[:, 4:], p.bank, p.toff, p.tad, p.ty)
     with pytest.raises(ev.EvospecError):
-        ev.lora_forward(p.tx, p.bank, p.toff, p.tad, p.ty, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))
+        ev.lora_backward(p.tx, p.tdy, p.bank, p.toff, p.tad, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))
     with pytest.raises(ev.EvospecError):
         ev.LoraBank(torch.zeros(1, 12, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(1, 64, 12, dtype=torch.bfloat16, device="cuda"))
     square = Problem(ev, [4], [0], 1, 8, 64, 64)
@@ -270,13 +270,13 @@ def test_streams_and_graphs(ev):
     for a, b in ((y, p.ty), (dx, p.tdx), (das, da), (dbs, db)):
         assert torch.equal(a, b)
     S, T = p.tad.numel(), p.T
-    ws = torch.empty(max(ev.lora_workspace_bytes(p.bank, S, T), ev.lora_workspace_bytes(p.bank, S, T, backward=True)), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(ev.lora_backward_workspace_bytes(p.bank, S, T), dtype=torch.uint8, device="cuda")
     x, dy, h2, da2, db2 = p.tx.clone(), p.tdy.clone(), torch.zeros_like(h), torch.empty_like(da), torch.empty_like(db)
 
     def both():
         y.copy_(y0)
         dx.copy_(dx0)
-        ev.lora_forward(x, p.bank, p.toff, p.tad, y, out_h=h2, workspace=ws)
+        ev.lora_forward(x, p.bank, p.toff, p.tad, y, out_h=h2)
         ev.lora_backward(x, dy, p.bank, p.toff, p.tad, h=h2, dx=dx, out_da=da2, out_db=db2, workspace=ws)
     with torch.cuda.stream(s):
         both()
