@@ -34,7 +34,7 @@ typedef struct evospec_lora {
  *   out_h     dev fp32 [r, T] or NULL: h = x A^T, transposed, for evospec_lora_backward; columns of rows without an adapter
  *             are left as they are
  * Sums are fp32.  h goes into the second product as two bf16 numbers, which keep 2^-16 of it.
- * T at most 2^24, S at most 2^16.
+ * T below 2^24, S at most 2^16, strides at most 2^26.
  */
 int evospec_lora_forward(const evospec_lora *lora, const void *x, long long x_stride, const int32_t *row_off,
                          const int32_t *adapter, int S, int T, void *y, long long y_stride, float *out_h, void *stream);

@@ -19,7 +19,7 @@ int check_lora(const evospec_lora* l, int S, int T) {
     if (!l) return EVOSPEC_NULL_POINTER;
     if (l->n < 1 || l->n > 65535 || l->r < 8 || l->r % 8 || l->r > EVOSPEC_LORA_R_MAX) return EVOSPEC_BAD_SHAPE;
     if (l->d_in < 8 || l->d_in % 8 || l->d_in > (1 << 20) || l->d_out < 8 || l->d_out % 8 || l->d_out > (1 << 20)) return EVOSPEC_BAD_SHAPE;
-    return S < 0 || S > (1 << 16) || T < 0 || T > (1 << 24) ? EVOSPEC_BAD_SHAPE : EVOSPEC_OK;
+    return S < 0 || S > (1 << 16) || T < 0 || T >= (1 << 24) ? EVOSPEC_BAD_SHAPE : EVOSPEC_OK;
 }
 int check_weights(const evospec_lora* l) {
     if (!l->a || !l->b) return EVOSPEC_NULL_POINTER;
@@ -28,7 +28,7 @@ int check_weights(const evospec_lora* l) {
 // Rows of d elements in bf16 that lie `stride` apart.
 int check_matrix(const void* p, long long stride, int d) {
     if (!p) return EVOSPEC_NULL_POINTER;
-    if (stride < d || stride > (1ll << 32)) return EVOSPEC_BAD_SHAPE;
+    if (stride < d || stride > (1ll << 26)) return EVOSPEC_BAD_SHAPE;
     return stride % 8 == 0 && aligned(p, 16) ? EVOSPEC_OK : EVOSPEC_MISALIGNED;
 }
 size_t h_bytes(const evospec_lora* l, int T) { return up_to((size_t)l->r * T * sizeof(float)); }
@@ -68,7 +68,7 @@ int evospec_lora_forward(const evospec_lora* lora, const void* x, long long x_st
     if (!row_off || !adapter) return EVOSPEC_NULL_POINTER;
     if (!aligned(out_h, 4)) return EVOSPEC_MISALIGNED;
     const LoraArgs rows{{row_off, adapter, S, T, lora->n}, x, x_stride, lora->a, lora->d_in, lora->scale, lora->b, lora->d_out, y, y_stride, out_h, lora->r};
-    return failed(launch_lora_rows(rows, lora_plan(S, T, lora->d_out), false, static_cast<hipStream_t>(stream)));
+    return failed(launch_lora_rows(rows, lora_plan(S, T, lora->d_in, lora->d_out), false, static_cast<hipStream_t>(stream)));
 }
 
 int evospec_lora_backward_workspace_bytes(const evospec_lora* lora, int S, int T, size_t* out_bytes) {
@@ -77,7 +77,7 @@ int evospec_lora_backward_workspace_bytes(const evospec_lora* lora, int S, int T
     if (rc) return rc;
     *out_bytes = 0;
     if (S == 0 || T == 0) return EVOSPEC_OK;
-    const int parts = lora_grad_parts(lora->n, T, lora->d_in, lora->d_out);
+    const int parts = lora_grad_parts(lora->n, lora->r, T, lora->d_in, lora->d_out);
     *out_bytes = 2 * h_bytes(lora, T) + (parts > 1 ? (size_t)parts * lora->n * lora->r * ((size_t)lora->d_in + lora->d_out) * sizeof(float) : 0);
     return EVOSPEC_OK;
 }
@@ -104,7 +104,7 @@ int evospec_lora_backward(const evospec_lora* lora, const void* x, long long x_s
     float* g = reinterpret_cast<float*>(ws);
     float* again = reinterpret_cast<float*>(ws + (rows ? h_bytes(lora, T) : 0));
     if (rows) {
-        const LoraPlan p = lora_plan(S, T, lora->d_in);
+        const LoraPlan p = lora_plan(S, T, lora->d_out, lora->d_in);
         if (!h) {
             const LoraArgs down{q, x, x_stride, lora->a, lora->d_in, nullptr, nullptr, 0, nullptr, 0, again, lora->r};
             if ((rc = failed(launch_lora_rows(down, p, false, st)))) return rc;
@@ -117,7 +117,7 @@ int evospec_lora_backward(const evospec_lora* lora, const void* x, long long x_s
     a.job[0] = GradJob{g, nullptr, x, x_stride, lora->d_in, false, out_da};
     a.job[1] = GradJob{h ? h : again, lora->scale, dy, dy_stride, lora->d_out, true, out_db};
     a.r = lora->r;
-    a.parts = rows ? lora_grad_parts(lora->n, T, lora->d_in, lora->d_out) : 1;
+    a.parts = rows ? lora_grad_parts(lora->n, lora->r, T, lora->d_in, lora->d_out) : 1;
     a.partial = reinterpret_cast<float*>(ws + (rows ? 2 * h_bytes(lora, T) : 0));
     return failed(launch_lora_grads(a, st));
 }

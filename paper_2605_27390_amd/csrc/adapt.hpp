@@ -14,13 +14,14 @@ struct Requests {
     int S, T, n;                              // n adapters
 };
 
-// How the products of rows with adapters are laid out: tiles of 16 << shift rows, the columns of the second product in `slices`.
+// How the products of rows with adapters are laid out: tiles of 16 rows, the columns of the second product in `slices`.
 struct LoraPlan {
-    int shift;
     int tiles;                                // workgroups for the rows: every request may begin a tile of its own
     int slices;
+    bool deep;                                // a compute unit has one workgroup at most
+    bool once;                                // y past the caches
 };
-LoraPlan lora_plan(int S, int T, int d_up);
+LoraPlan lora_plan(int S, int T, int d_down, int d_up);
 
 struct LoraArgs {                             // h = x w_down^T (times factor, backward), y += factor h w_up
     Requests q;
@@ -54,7 +55,7 @@ struct GradArgs {
     int r, parts;                             // parts of an adapter's rows
     float* partial;                           // [parts][n r d0 + n r d1] of parts > 1
 };
-int lora_grad_parts(int n, int T, int d0, int d1);
+int lora_grad_parts(int n, int r, int T, int d0, int d1);
 hipError_t launch_lora_grads(const GradArgs& a, hipStream_t stream);
 
 struct KdArgs {

@@ -18,7 +18,7 @@
 namespace evospec {
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kThreads = 256;
 typedef const uint16_t __attribute__((address_space(1))) * gu16;
 
 __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
@@ -54,28 +54,37 @@ __device__ __forceinline__ void columns_of(const u32x2 (&raw)[8], u32x4 (&op)[4]
             op[j][k] = j & 1 ? high_halves(raw[2 * k][j / 2], raw[2 * k + 1][j / 2]) : low_halves(raw[2 * k][j / 2], raw[2 * k + 1][j / 2]);
 }
 
-struct Tile {
+// Neighbouring rows of one adapter.
+struct Run {
     int row0, rows, adapter;
 };
-struct Request {
-    int row0, rows, adapter;
-};
-__device__ __forceinline__ Request request_of(const Requests& q, int s) {
-    Request t{0, 0, -1};
+// Of 64 requests, lane l has request base + l: in the first lane of a run of requests that have the same adapter and follow one another, the
+// run; no rows in the others, or where the adapter is none.
+__device__ __forceinline__ Run runs_of(const Requests& q, int base) {
+    const int lane = threadIdx.x & 63, s = base + lane;
+    Run t{0, 0, -1};
     if (s < q.S) {
         t.row0 = min(max(q.row_off[s], 0), q.T);
         t.rows = min(max(q.row_off[s + 1], t.row0), q.T) - t.row0;
         t.adapter = q.adapter[s];
         if ((unsigned)t.adapter >= (unsigned)q.n) t.rows = 0;
     }
+    if (q.S > 1) {
+        const int end = t.row0 + t.rows;
+        const bool goes_on = __shfl_up(end, 1) == t.row0 && __shfl_up(t.adapter, 1) == t.adapter && __shfl_up(t.rows, 1) > 0 && t.rows > 0 && lane > 0;
+        const u64 on = __ballot(goes_on);
+        const int more = __ffsll((unsigned long long)~(lane < 63 ? on >> (lane + 1) : 0ull)) - 1;        // lanes that go on with this one's
+        const int last = __shfl(end, lane + more);
+        t.rows = goes_on ? 0 : t.rows > 0 ? last - t.row0 : 0;
+    }
     return t;
 }
-// Tile `index` of the requests that have an adapter, in their order; no rows if there are fewer.  64 requests at a time.
-__device__ __forceinline__ Tile find_tile(const Requests& q, int shift, int index) {
+// Tile `index` (16 rows) of the runs, in their order; no rows if there are fewer.
+__device__ __forceinline__ Run find_tile(const Requests& q, int index) {
     const int lane = threadIdx.x & 63;
     for (int base = 0; base < q.S; base += 64) {
-        const Request t = request_of(q, base + lane);
-        const int tiles = (t.rows + (1 << shift) - 1) >> shift;
+        const Run t = runs_of(q, base);
+        const int tiles = (t.rows + 15) >> 4;
         int incl = tiles;
         if (q.S > 1) {
 #pragma unroll
@@ -87,231 +96,259 @@ __device__ __forceinline__ Tile find_tile(const Requests& q, int shift, int inde
         const int total = __builtin_amdgcn_readlane(incl, q.S > 1 ? 63 : 0);
         if (index < total) {
             const int at = __ffsll((unsigned long long)__ballot(incl > index)) - 1;
-            const int first = (index - __builtin_amdgcn_readlane(incl, at) + __builtin_amdgcn_readlane(tiles, at)) << shift;
-            return Tile{__builtin_amdgcn_readlane(t.row0, at) + first, min(__builtin_amdgcn_readlane(t.rows, at) - first, 1 << shift),
-                        __builtin_amdgcn_readlane(t.adapter, at)};
+            const int first = (index - __builtin_amdgcn_readlane(incl, at) + __builtin_amdgcn_readlane(tiles, at)) << 4;
+            return Run{__builtin_amdgcn_readlane(t.row0, at) + first, min(__builtin_amdgcn_readlane(t.rows, at) - first, 16),
+                       __builtin_amdgcn_readlane(t.adapter, at)};
         }
         index -= total;
     }
-    return Tile{0, 0, 0};
+    return Run{0, 0, 0};
 }
 
 // ---------------------------------------------------------------- rows
 
+
 typedef const u32x2 __attribute__((address_space(1))) * gpair;
 typedef const uint32_t __attribute__((address_space(1))) * gword;
+typedef const char __attribute__((address_space(1))) * gbyte;
+typedef const float __attribute__((address_space(1))) * gfloat;
+typedef float f32x4_u __attribute__((ext_vector_type(4), aligned(4)));
+typedef const f32x4_u __attribute__((address_space(1))) * gfloat4;
 
-// One tile of 16 NT rows: h = x W_down^T, then y += h W_up for a slice of the columns.  Forward, W_down = A [r][d] and W_up = B [d][r]; backward
+// One tile of 16 rows: h = x W_down^T, then y += h W_up for a slice of the columns.  Forward, W_down = A [r][d] and W_up = B [d][r]; backward
 // W_down = B^T and W_up = A^T of the same arrays.  The long axis of the first product is split over W wavefronts, whose sums are added
-// in LDS; in the second each takes 64 columns at a time, of which a lane holds 16 in a row of y.  Every slice computes h again: it is
-// launched with slices where tiles are few and the time is that of a launch.
-template <int RT, int NT, bool BACK, int W>
-__global__ __launch_bounds__(64 * W) void lora_rows_kernel(LoraArgs a) {
-    constexpr int KS = (RT + 1) / 2, kRows = 16 * NT;
-    __shared__ __align__(16) f32x4 sums[W][RT * NT][64];
-    __shared__ float hs[16 * RT][kRows + 1];
-    const Tile t = find_tile(a.q, NT == 1 ? 4 : NT == 2 ? 5 : 6, blockIdx.x);
+// in LDS; in the second each takes 64 columns at a time.  Every slice computes h again: it is launched with slices where tiles are
+// few and the time is that of a launch.
+// An operand's neighbouring lanes are neighbouring rows, and a load that follows them touches 64 lines of memory for 1 KB, one a clock: 16 KB of
+// a compute unit's time for 256 KB.  So rows (x, and A forward) are loaded 128 bytes of a row to 8 lanes and change lanes in LDS (a
+// wavefront's own, no barriers; piece c of row m in place c ^ (m mod 8), without bank conflicts), B forward in the order of memory.  Of y a
+// lane has 4 columns in 4 rows, the columns of a row in 16 lanes.
+// DEEP, where tiles and slices leave a compute unit one workgroup at most: 8 wavefronts with 2 KB x 12 on their way each.  Else four
+// workgroups of 4 to a unit, so that some load while others store.  ONCE: y past the caches.
+template <int RT, bool BACK, bool DEEP, bool ONCE>
+__global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lora_rows_kernel(LoraArgs a) {
+    constexpr int W = DEEP ? 8 : 4;
+    constexpr int KS = (RT + 1) / 2;
+    constexpr int kSets = BACK ? 1 : 1 + RT;                     // of 16 rows through LDS: x's, then A's
+    constexpr int kOwn = kSets * 128 > RT * 64 ? kSets * 128 : RT * 64;        // 16-byte pieces of a wavefront (64 columns of B: up to 128 RT)
+    __shared__ __align__(16) u32x4 own[W][kOwn];
+    __shared__ float hs[16 * RT][17];
+    const Run t = find_tile(a.q, blockIdx.x);
     if (t.rows == 0) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, kg = lane >> 4;
     const float factor = a.factor ? a.factor[t.adapter] : 1.f;
-    // 64 columns of the second product: y's, and of the weights what this lane's operands are made of.  Columns 32 b + 8 kg + e of a
-    // row of y are a lane's: row 4 kg + i of tile j is number 4 j + i (forward) or 4 i + j of them, 8 b + e.
+    u32x4* mine = own[wave];
+
+    // 64 columns of the second product: what this lane has of y, and of the weights what operands are made of.  Column 4 m + j of them is
+    // column m of tile j.
     struct Columns {
-        u32x4 y[NT][2];
-        u32x4 w[BACK ? 1 : KS][4];
+        u32x2 y[4];
+        u32x4 w[BACK ? 1 : 2 * RT];
         u32x2 raw[BACK ? KS : 1][8];
     };
     const gu16 w_up = (gu16)a.w_up + (long long)t.adapter * a.r * a.d_up;
     auto load_columns = [&](Columns& col, int g) {
-        const int c0 = 64 * g;
+        const int c = min(64 * g + 4 * m, a.d_up - 4);
 #pragma unroll
-        for (int i = 0; i < NT; ++i)
+        for (int k = 0; k < 4; ++k) {
+            const gpair p = (gpair)((gu16)a.y + (long long)(t.row0 + min(4 * kg + k, t.rows - 1)) * a.y_stride + c);
+            col.y[k] = ONCE ? __builtin_nontemporal_load(p) : *p;
+        }
+        if constexpr (BACK) {                                    // [r][d]
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    col.raw[s][k] = 32 * s + 8 * kg < a.r ? *(gpair)(w_up + (long long)(32 * s + 8 * kg + k) * a.d_up + c) : u32x2{0, 0};
+        } else {                                                 // [d][r]: r / 8 KB
+            const int pieces = min(64, a.d_up - 64 * g) * a.r / 8;
+#pragma unroll
+            for (int k = 0; k < 2 * RT; ++k)
+                if (64 * k < 8 * a.r) col.w[k] = *(gvec_ptr)(w_up + (long long)(64 * g) * a.r + 8 * min(64 * k + lane, pieces - 1));
+        }
+    };
+    // Groups of a slice go round the wavefronts; every tile begins at another one (as in the first product).
+    const int groups = (a.d_up + 63) / 64, g0 = (int)((long long)groups * blockIdx.y / gridDim.y);
+    const int count = a.y ? (int)((long long)groups * (blockIdx.y + 1) / gridDim.y) - g0 : 0, shift = count ? (int)(blockIdx.x * 5u % (unsigned)count) : 0;
+    auto group_of = [&](int n) { return g0 + (n + shift < count ? n + shift : n + shift - count); };
+    Columns first;
+    if (DEEP && wave < count) load_columns(first, group_of(wave));
+    {
+        // Chunks of 64 along the summed axis go round the wavefronts, U at a time; every tile begins at another one, or all workgroups would
+        // ask the same channels of memory at the same time (rows are often a multiple of 4 KB apart).
+        constexpr int U = !DEEP || (RT == 4 && !BACK) ? 1 : RT == 4 ? 2 : 4;
+        const int chunks = (a.d_down + 63) / 64, turn = (int)(blockIdx.x * 5u % (unsigned)chunks);
+        const int row8 = lane >> 3, piece = lane & 7;
+        gu16 from[kSets][2];
+#pragma unroll
+        for (int i = 0; i < kSets; ++i)
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
-                const int c = c0 + 32 * b + 8 * kg;
-                col.y[i][b] = *(gvec_ptr)((gu16)a.y + (long long)(t.row0 + min(16 * i + m, t.rows - 1)) * a.y_stride + min(c, a.d_up - 8));
+                if (i == 0) from[i][b] = (gu16)a.x + (long long)(t.row0 + min(8 * b + row8, t.rows - 1)) * a.x_stride + 8 * piece;
+                else from[i][b] = (gu16)a.w_down + ((long long)t.adapter * a.r + min(16 * (i - 1) + 8 * b + row8, a.r - 1)) * a.d_down + 8 * piece;
             }
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            const int k0 = 32 * s + 8 * kg;
-            if constexpr (BACK) {                                // [r][d]
-                const int c = min(c0 + 32 * ((m >> 1) & 1) + 8 * (m >> 2) + 4 * (m & 1), a.d_up - 4);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) col.raw[s][k] = k0 < a.r ? *(gpair)(w_up + (long long)(k0 + k) * a.d_up + c) : u32x2{0, 0};
-            } else {                                             // [d][r]
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int c = min(c0 + 32 * (j >> 1) + 8 * (m >> 2) + 4 * (j & 1) + (m & 3), a.d_up - 1);
-                    col.w[s][j] = k0 < a.r ? *(gvec_ptr)(w_up + (long long)c * a.r + k0) : u32x4{0, 0, 0, 0};
-                }
-            }
-        }
-    };
-    const int groups = (a.d_up + 63) / 64, parts = gridDim.y * W, part = blockIdx.y * W + wave;
-    const int n0 = (int)((long long)groups * part / parts), n1 = a.y ? (int)((long long)groups * (part + 1) / parts) : 0;
-    // (as the first product's: every tile begins at another place)
-    auto group_of = [&](int n) {
-        const int len = n1 - n0, at = n - n0 + (int)(blockIdx.x % (unsigned)len);
-        return n0 + (at < len ? at : at - len);
-    };
-    Columns first;
-    if (NT == 1 && n0 < n1) load_columns(first, group_of(n0));
-    {
-        const int steps = (a.d_down + 31) / 32;
-        gu16 x[NT];
-#pragma unroll
-        for (int i = 0; i < NT; ++i) x[i] = (gu16)a.x + (long long)(t.row0 + min(16 * i + m, t.rows - 1)) * a.x_stride + 8 * kg;
         const gu16 w = (gu16)a.w_down + (long long)t.adapter * a.r * a.d_down;
-        f32x4 acc[RT][NT] = {};
-        auto load_x = [&](int step, u32x4 (&xs)[NT]) {
-            const bool in = step * 32 + 8 * kg < a.d_down;       // (d ends within a step: zeros on both sides)
-#pragma unroll
-            for (int i = 0; i < NT; ++i) xs[i] = in ? *(gvec_ptr)(x[i] + (long long)step * 32) : u32x4{0, 0, 0, 0};
+        f32x4 acc[RT] = {};
+        struct Chunk {
+            u32x4 rows[kSets][2];
+            uint32_t raw[BACK ? 2 : 1][8][(RT + 1) / 2];
         };
-        auto load_w = [&](int step, u32x4 (&ws)[RT]) {
-            const int k = step * 32 + 8 * kg;
-            const bool in = k < a.d_down;
-            if constexpr (!BACK) {
+        auto load = [&](Chunk& c, int n) {
+            const int at = n < chunks ? n + turn < chunks ? n + turn : n + turn - chunks : chunks;          // (zeros behind the end)
+            const bool in = 64 * at + 8 * piece < a.d_down;
 #pragma unroll
-                for (int j = 0; j < RT; ++j)                     // (ranks from r on: any, they end in nothing)
-                    ws[j] = in ? *(gvec_ptr)(w + (long long)min(16 * j + m, a.r - 1) * a.d_down + k) : u32x4{0, 0, 0, 0};
-            } else {
+            for (int i = 0; i < kSets; ++i)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) c.rows[i][b] = in ? *(gvec_ptr)(from[i][b] + 64 * at) : u32x4{0, 0, 0, 0};
+            if constexpr (BACK) {
                 const int rank = RT * m < a.r ? RT * m : 0;
-                uint32_t raw[8][(RT + 1) / 2];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const gu16 p = w + (long long)(in ? k + i : 0) * a.r + rank;
-                    if constexpr (RT == 1) raw[i][0] = *p;
-                    else if constexpr (RT == 2) raw[i][0] = *(gword)p;
-                    else {
-                        const u32x2 v = *(gpair)p;
-                        raw[i][0] = v[0];
-                        raw[i][1] = v[1];
+                for (int s = 0; s < 2; ++s) {
+                    const int k = 64 * at + 32 * s + 8 * kg;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const gu16 p = w + (long long)(k + i) * a.r + rank;
+                        if constexpr (RT == 1) c.raw[s][i][0] = k < a.d_down ? *p : 0u;
+                        else if constexpr (RT == 2) c.raw[s][i][0] = k < a.d_down ? *(gword)p : 0u;
+                        else {
+                            const u32x2 v = k < a.d_down ? *(gpair)p : u32x2{0, 0};
+                            c.raw[s][i][0] = v[0];
+                            c.raw[s][i][1] = v[1];
+                        }
                     }
                 }
-#pragma unroll
-                for (int j = 0; j < RT; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t v = j & 1 ? high_halves(raw[2 * i][j / 2], raw[2 * i + 1][j / 2]) : low_halves(raw[2 * i][j / 2], raw[2 * i + 1][j / 2]);
-                        ws[j][i] = in ? v : 0u;
-                    }
             }
         };
-        // Chunks of U steps go round the wavefronts; every tile begins at another one, or all workgroups would ask the same
-        // channels of memory at the same time (rows are often a multiple of 4 KB apart).
-        constexpr int U = NT > 1 ? 4 : RT == 4 ? 8 : 16;
-        const int chunks = (steps + U - 1) / U, turn = (int)(blockIdx.x * 5u % (unsigned)chunks);
-        u32x4 xs[U][NT], ws[U][RT];
-        for (int n = wave; n < chunks; n += W) {
-            const int c = n + turn < chunks ? n + turn : n + turn - chunks;
+        auto add = [&](const Chunk& c) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                load_x(c * U + u, xs[u]);                        // (zeros behind the end)
-                load_w(c * U + u, ws[u]);
+            for (int i = 0; i < kSets; ++i)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) mine[128 * i + 64 * b + 8 * row8 + (piece ^ row8)] = c.rows[i][b];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                u32x4 ws[RT];
+#pragma unroll
+                for (int j = 0; j < RT; ++j) {
+                    if constexpr (!BACK) {
+                        ws[j] = mine[128 * (1 + j) + 8 * m + ((4 * s + kg) ^ (m & 7))];
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            ws[j][i] = j & 1 ? high_halves(c.raw[s][2 * i][j / 2], c.raw[s][2 * i + 1][j / 2]) : low_halves(c.raw[s][2 * i][j / 2], c.raw[s][2 * i + 1][j / 2]);
+                    }
+                }
+                const u32x4 x = mine[8 * m + ((4 * s + kg) ^ (m & 7))];
+#pragma unroll
+                for (int j = 0; j < RT; ++j) acc[j] = mfma(ws[j], x, acc[j]);
             }
+        };
+        Chunk even[U], odd[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) load(even[u], wave + W * u);
+        for (int n = wave; n < chunks; n += 2 * W * U) {
 #pragma unroll
-                for (int j = 0; j < RT; ++j)
+            for (int u = 0; u < U; ++u) load(odd[u], n + W * (U + u));
 #pragma unroll
-                    for (int i = 0; i < NT; ++i) acc[j][i] = mfma(ws[u][j], xs[u][i], acc[j][i]);
+            for (int u = 0; u < U; ++u) add(even[u]);
+            if (n + W * U >= chunks) break;
+#pragma unroll
+            for (int u = 0; u < U; ++u) load(even[u], n + W * (2 * U + u));
+#pragma unroll
+            for (int u = 0; u < U; ++u) add(odd[u]);
         }
 #pragma unroll
-        for (int j = 0; j < RT; ++j)
-#pragma unroll
-            for (int i = 0; i < NT; ++i) sums[wave][j * NT + i][lane] = acc[j][i];
+        for (int j = 0; j < RT; ++j) mine[64 * j + lane] = __builtin_bit_cast(u32x4, acc[j]);
     }
-    if (NT > 1 && n0 < n1) load_columns(first, group_of(n0));
+    if (!DEEP && wave < count) load_columns(first, group_of(wave));
     lds_barrier();
-    for (int e = wave; e < RT * NT; e += W) {
-        f32x4 v = sums[0][e][lane];
+    for (int j = wave; j < RT; j += W) {
+        f32x4 v = __builtin_bit_cast(f32x4, own[0][64 * j + lane]);
 #pragma unroll
-        for (int o = 1; o < W; ++o) v += sums[o][e][lane];
-        const int j = e / NT, row = 16 * (e % NT) + m;
+        for (int o = 1; o < W; ++o) v += __builtin_bit_cast(f32x4, own[o][64 * j + lane]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int rank = BACK ? RT * (4 * kg + i) + j : 16 * j + 4 * kg + i;
             const float scaled = v[i] * factor;
-            hs[rank][row] = scaled;
-            if (a.h && blockIdx.y == 0 && rank < a.r && row < t.rows) a.h[(long long)rank * a.q.T + t.row0 + row] = BACK ? scaled : v[i];
+            hs[rank][m] = scaled;
+            if (a.h && blockIdx.y == 0 && rank < a.r && m < t.rows) a.h[(long long)rank * a.q.T + t.row0 + m] = BACK ? scaled : v[i];
         }
     }
     if (!a.y) return;
     lds_barrier();
-    u32x4 h[NT][KS][2];
+    u32x4 h[KS][2];
 #pragma unroll
-    for (int i = 0; i < NT; ++i)
+    for (int s = 0; s < KS; ++s) {
+        float v[8];
 #pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            float v[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = 32 * s + 8 * kg < a.r ? hs[(32 * s + 8 * kg + k) % (16 * RT)][16 * i + m] : 0.f;
-            h[i][s][0] = next_part(v);
-            h[i][s][1] = next_part(v);
-        }
+        for (int k = 0; k < 8; ++k) v[k] = 32 * s + 8 * kg < a.r ? hs[(32 * s + 8 * kg + k) % (16 * RT)][m] : 0.f;
+        h[s][0] = next_part(v);
+        h[s][1] = next_part(v);
+    }
+    // B's 16-byte pieces in LDS: number p, of column p / (r / 8), with its low 4 bits turned by what the columns of a read differ in
+    const int turned = a.r > 32 ? 5 : 4, per = a.r / 8;
     auto add = [&](const Columns& col, int g) {
-        f32x4 acc[4][NT] = {};
+        if constexpr (!BACK) {
+#pragma unroll
+            for (int k = 0; k < 2 * RT; ++k)
+                if (64 * k < 8 * a.r) {
+                    const int p = 64 * k + lane;
+                    mine[p ^ ((p >> turned) & 15)] = col.w[k];
+                }
+        }
+        f32x4 acc[4] = {};
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             u32x4 op[4];
             if constexpr (BACK) {
                 columns_of(col.raw[s], op);
             } else {
+                const bool in = 32 * s + 8 * kg < a.r;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) op[j] = col.w[s][j];
+                for (int j = 0; j < 4; ++j) {
+                    const int p = (4 * m + j) * per + (in ? 4 * s + kg : 0);
+                    const u32x4 v = mine[p ^ ((p >> turned) & 15)];
+                    op[j] = in ? v : u32x4{0, 0, 0, 0};
+                }
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int i = 0; i < NT; ++i) {
-                    acc[j][i] = mfma(op[j], h[i][s][0], acc[j][i]);
-                    acc[j][i] = mfma(op[j], h[i][s][1], acc[j][i]);
-                }
+            for (int j = 0; j < 4; ++j) {
+                acc[j] = mfma(h[s][0], op[j], acc[j]);
+                acc[j] = mfma(h[s][1], op[j], acc[j]);
+            }
         }
+        const int c = 64 * g + 4 * m;
 #pragma unroll
-        for (int i = 0; i < NT; ++i)
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const int c0 = 64 * g + 32 * b + 8 * kg;
-                if (16 * i + m >= t.rows || c0 >= a.d_up) continue;
-                u32x4 v;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t old = col.y[i][b][e];
-                    float z[2];
-#pragma unroll
-                    for (int f = 0; f < 2; ++f) {
-                        const int c = 8 * b + 2 * e + f;         // of the lane's 16: rows 4 kg .. of the tiles
-                        const float up = BACK ? acc[c % 4][i][c / 4] : acc[c / 4][i][c % 4];
-                        z[f] = __uint_as_float(f ? old & 0xffff0000u : old << 16) + up;
-                    }
-                    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-                    v[e] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)z[0], (__bf16)z[1]});
-                }
-                *reinterpret_cast<u32x4*>((uint16_t*)a.y + (long long)(t.row0 + 16 * i + m) * a.y_stride + c0) = v;
-            }
+        for (int k = 0; k < 4; ++k) {
+            if (4 * kg + k >= t.rows || c >= a.d_up) continue;
+            const uint32_t y0 = col.y[k][0], y1 = col.y[k][1];
+            typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+            const bf16x4 v = {(__bf16)(__uint_as_float(y0 << 16) + acc[0][k]), (__bf16)(__uint_as_float(y0 & 0xffff0000u) + acc[1][k]),
+                              (__bf16)(__uint_as_float(y1 << 16) + acc[2][k]), (__bf16)(__uint_as_float(y1 & 0xffff0000u) + acc[3][k])};
+            bf16x4* p = reinterpret_cast<bf16x4*>((uint16_t*)a.y + (long long)(t.row0 + 4 * kg + k) * a.y_stride + c);
+            if constexpr (ONCE) __builtin_nontemporal_store(v, p);
+            else *p = v;
+        }
     };
     // (two sets of registers in turn; the first is on its way since before h was there)
     Columns next;
-    for (int n = n0; n < n1; n += 2) {
-        if (n + 1 < n1) load_columns(next, group_of(n + 1));
+    for (int n = wave; n < count; n += 2 * W) {
+        if (n + W < count) load_columns(next, group_of(n + W));
         add(first, group_of(n));
-        if (n + 1 >= n1) break;
-        if (n + 2 < n1) load_columns(first, group_of(n + 2));
-        add(next, group_of(n + 1));
+        if (n + W >= count) break;
+        if (n + 2 * W < count) load_columns(first, group_of(n + 2 * W));
+        add(next, group_of(n + W));
     }
 }
 
 // ---------------------------------------------------------------- gradients
 
-// The steps of 32 rows of an adapter, request by request.  Everything is the same in all lanes but the 64 requests at hand.
+// The steps of 32 rows of an adapter, run by run.  Everything is the same in all lanes but the 64 requests at hand.
 struct Steps {
     const Requests& q;
     const int adapter;
     int base = -64, row = 0, left = 0;
-    unsigned long long rest = 0;
-    Request mine{};
+    u64 rest = 0;
+    Run mine{};
     __device__ Steps(const Requests& q_, int adapter_) : q(q_), adapter(adapter_) {}
     // Passes over n steps; the next one's first row and how many there are, 0 if there is none.
     __device__ __forceinline__ int skip(int n, int& row0) {
@@ -324,10 +361,10 @@ struct Steps {
                     base = q.S;                                  // (stays at the end)
                     return 0;
                 }
-                mine = request_of(q, base + (int)(threadIdx.x & 63));
+                mine = runs_of(q, base);
                 rest = __ballot(mine.rows > 0 && mine.adapter == adapter);
             }
-            const int at = __ffsll(rest) - 1;
+            const int at = __ffsll((unsigned long long)rest) - 1;
             rest &= rest - 1;
             row = __builtin_amdgcn_readlane(mine.row0, at);
             left = __builtin_amdgcn_readlane(mine.rows, at);
@@ -340,72 +377,94 @@ struct Steps {
     }
 };
 
-// RT tiles of 16 ranks; a workgroup has 64 columns of one adapter, its wavefronts and `parts` workgroups every so many-th step.
-template <int RT>
-__global__ __launch_bounds__(kThreads) void lora_grads_kernel(GradArgs a, int groups0, long long partial_stride) {
-    __shared__ __align__(16) f32x4 sums[kWaves][4 * RT][64];
+// RT tiles of 16 ranks; a workgroup has 64 CG columns of one adapter, its wavefronts and `parts` workgroups every so many-th step.  A step of
+// 64 CG columns and 32 rows is 4 CG KB of x and, from L2, 2 RT KB of h, which becomes an operand in three parts.
+template <int RT, int CG, int W>
+__global__ __launch_bounds__(64 * W, W / 4) void lora_grads_kernel(GradArgs a, int groups0, long long partial_stride) {
+    constexpr int kTiles = 4 * CG * RT;
+    __shared__ __align__(16) f32x4 sums[W / 2][kTiles][64];
+    static_assert(sizeof(sums) >= W * RT * 2048, "h of every wavefront's step");
     const bool second = (int)blockIdx.x >= groups0;
     const GradJob job = second ? a.job[1] : a.job[0];
-    const int c0 = 64 * (blockIdx.x - (second ? groups0 : 0)), adapter = blockIdx.y, part = blockIdx.z;
+    const int c0 = 64 * CG * (blockIdx.x - (second ? groups0 : 0)), adapter = blockIdx.y, part = blockIdx.z;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, kg = lane >> 4;
-    const gu16 x = (gu16)job.x + (c0 + 4 * m < job.d ? c0 + 4 * m : 0);
-    const float* hp[RT];
+    // Places as a uniform address and a lane's 32 bits of offset (row strides are below 2^26, h is smaller than 4 GB): half the registers.
+    const uint32_t down = (uint32_t)(8 * kg * job.x_stride) * 2u;
+    uint32_t x[CG];
 #pragma unroll
-    for (int j = 0; j < RT; ++j) hp[j] = job.h + (long long)min(16 * j + m, a.r - 1) * a.q.T;       // (ranks from r on end in nothing)
-    f32x4 acc[4][RT] = {};
+    for (int g = 0; g < CG; ++g) x[g] = 2u * (c0 + 64 * g + 4 * m < job.d ? c0 + 64 * g + 4 * m : 0);
+    // h goes through LDS as the rows of lora_rows_kernel do: 32 numbers of a rank are 8 pieces, loaded by 8 lanes, the even pieces first
+    const int rank8 = lane >> 3, piece = lane & 7, slot = ((piece >> 1) + 4 * (piece & 1)) ^ rank8;
+    uint32_t hp[2 * RT];
+#pragma unroll
+    for (int j = 0; j < 2 * RT; ++j) hp[j] = 4u * ((uint32_t)min(8 * j + rank8, a.r - 1) * (uint32_t)a.q.T + 4u * piece);    // (ranks from r on end in nothing)
+    f32x4* mine = &sums[0][0][0] + wave * RT * 128;
+    f32x4 acc[CG][4][RT] = {};
     struct Rows {
-        u32x2 raw[8];
-        float h[RT][8];
+        u32x2 raw[CG][8];
+        f32x4 h[2 * RT];
     };
     auto load = [&](Rows& b, int row0, int rows) {
         if (rows == 32) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) b.raw[i] = *(gpair)(x + (long long)(row0 + 8 * kg + i) * job.x_stride);
+            for (int g = 0; g < CG; ++g)
 #pragma unroll
-            for (int j = 0; j < RT; ++j) {
-                typedef float f32x4_u __attribute__((ext_vector_type(4), aligned(4)));
-                const f32x4_u u = *reinterpret_cast<const f32x4_u*>(hp[j] + row0 + 8 * kg), v = *reinterpret_cast<const f32x4_u*>(hp[j] + row0 + 8 * kg + 4);
+                for (int i = 0; i < 8; ++i) b.raw[g][i] = *(gpair)((gbyte)((gu16)job.x + (long long)(row0 + i) * job.x_stride) + (down + x[g]));
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    b.h[j][i] = u[i];
-                    b.h[j][4 + i] = v[i];
-                }
-            }
+            for (int j = 0; j < 2 * RT; ++j) b.h[j] = *(gfloat4)((gbyte)(job.h + row0) + hp[j]);
         } else if (rows > 0) {
-            u32x2 raw[8];
-            float h[RT][8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int row = row0 + min(8 * kg + i, rows - 1);
-                raw[i] = *(gpair)(x + (long long)row * job.x_stride);
+            for (int g = 0; g < CG; ++g)
 #pragma unroll
-                for (int j = 0; j < RT; ++j) h[j][i] = hp[j][row];
-            }
+                for (int i = 0; i < 8; ++i)
+                    b.raw[g][i] = *(gpair)((gbyte)((gu16)job.x + (long long)row0 * job.x_stride) + ((uint32_t)min(8 * kg + i, rows - 1) * (uint32_t)job.x_stride * 2u + x[g]));
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const bool in = 8 * kg + i < rows;
-                b.raw[i] = in ? raw[i] : u32x2{0, 0};
+            for (int j = 0; j < 2 * RT; ++j)
 #pragma unroll
-                for (int j = 0; j < RT; ++j) b.h[j][i] = in ? h[j][i] : 0.f;
-            }
+                for (int i = 0; i < 4; ++i) b.h[j][i] = *(gfloat)((gbyte)(job.h + row0) + (hp[j] + 4u * min(4 * piece + i, rows - 1) - 16u * piece));
+#pragma unroll
+            for (int g = 0; g < CG; ++g)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) b.raw[g][i] = 8 * kg + i < rows ? b.raw[g][i] : u32x2{0, 0};
+#pragma unroll
+            for (int j = 0; j < 2 * RT; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) b.h[j][i] = 4 * piece + i < rows ? b.h[j][i] : 0.f;
         }
     };
-    auto add = [&](Rows& b) {
-        u32x4 op[4];
-        columns_of(b.raw, op);
+    auto add = [&](const Rows& b) {
 #pragma unroll
-        for (int k = 0; k < 3; ++k)
+        for (int j = 0; j < 2 * RT; ++j) mine[64 * j + 8 * rank8 + slot] = b.h[j];
+        // (x's operands of one group at a time, h's of one rank tile or of all: what fewer registers hold)
+        u32x4 op[4], hs[CG > 1 ? RT : 1][3];
+        auto parts_of = [&](int r, u32x4 (&to)[3]) {
+            const f32x4 u = mine[128 * r + 8 * m + (kg ^ (m & 7))], v = mine[128 * r + 8 * m + ((4 + kg) ^ (m & 7))];
+            float h[8] = {u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
+#pragma unroll
+            for (int k = 0; k < 3; ++k) to[k] = next_part(h);
+        };
+        if constexpr (CG > 1) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) parts_of(r, hs[r]);
+        }
+#pragma unroll
+        for (int g = 0; g < CG; ++g) {
+            columns_of(b.raw[g], op);
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                const u32x4 hs = next_part(b.h[r]);
+                if constexpr (CG == 1) parts_of(r, hs[0]);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[j][r] = mfma(op[j], hs, acc[j][r]);
+                for (int k = 0; k < 3; ++k)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[g][j][r] = mfma(op[j], hs[CG > 1 ? r : 0][k], acc[g][j][r]);
             }
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
     Steps steps(a.q, adapter);
-    const int stride = kWaves * a.parts;
+    const int stride = W * a.parts;
     Rows even, odd;
-    int row0 = 0, rows = steps.skip(part * kWaves + wave, row0);
+    int row0 = 0, rows = steps.skip(part * W + wave, row0);
     load(even, row0, rows);
     while (rows) {
         rows = steps.skip(stride - 1, row0);
@@ -416,23 +475,56 @@ __global__ __launch_bounds__(kThreads) void lora_grads_kernel(GradArgs a, int gr
         load(even, row0, rows);
         add(odd);
     }
+    // The upper half of the wavefronts first, whose sums the lower half takes along.
+    __syncthreads();
+    f32x4* own = sums[wave & (W / 2 - 1)][0];
+    if (wave >= W / 2)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+        for (int g = 0; g < CG; ++g)
 #pragma unroll
-        for (int r = 0; r < RT; ++r) sums[wave][j * RT + r][lane] = acc[j][r];
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int r = 0; r < RT; ++r) own[64 * ((g * 4 + j) * RT + r) + lane] = acc[g][j][r];
+    __syncthreads();
+    if (wave < W / 2)
+#pragma unroll
+        for (int g = 0; g < CG; ++g)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int r = 0; r < RT; ++r) own[64 * ((g * 4 + j) * RT + r) + lane] += acc[g][j][r];
     __syncthreads();
     const float factor = job.factor ? job.factor[adapter] : 1.f;
     float* out = a.parts > 1 ? a.partial + part * partial_stride + (second ? (long long)a.q.n * a.r * a.job[0].d : 0ll) : job.out;
     out += (long long)adapter * a.r * job.d;
-    for (int e = wave; e < 4 * RT; e += kWaves) {
-        f32x4 v = sums[0][e][lane];
+    if (job.rank_last) {
+        for (int e = wave; e < kTiles; e += W) {
+            f32x4 v = sums[0][e][lane];
 #pragma unroll
-        for (int w4 = 1; w4 < kWaves; ++w4) v += sums[w4][e][lane];
-        const int j = e / RT, rank = 16 * (e % RT) + m;
+            for (int o = 1; o < W / 2; ++o) v += sums[o][e][lane];
+            const int g = e / (4 * RT), j = e / RT % 4, rank = 16 * (e % RT) + m;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int c = c0 + 4 * (4 * kg + i) + j;
-            if (rank < a.r && c < job.d) out[job.rank_last ? (long long)c * a.r + rank : (long long)rank * job.d + c] = v[i] * factor;
+            for (int i = 0; i < 4; ++i) {
+                const int c = c0 + 64 * g + 4 * (4 * kg + i) + j;
+                if (rank < a.r && c < job.d) out[(long long)c * a.r + rank] = v[i] * factor;
+            }
+        }
+    } else {
+        // (a thread has 16 columns in a row of a rank, its neighbours the next ones)
+        for (int e = threadIdx.x; e < 64 * RT * CG; e += 64 * W) {
+            const int k = e % 4, g = e / 4 % CG, rank = e / (4 * CG), c = c0 + 64 * g + 16 * k;
+            f32x4 v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int at = (g * 4 + j) * RT + rank / 16;
+                v[j] = sums[0][at][16 * k + rank % 16];
+#pragma unroll
+                for (int o = 1; o < W / 2; ++o) v[j] += sums[o][at][16 * k + rank % 16];
+            }
+            if (rank >= a.r) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (c + 4 * i < job.d) *reinterpret_cast<f32x4*>(out + (long long)rank * job.d + c + 4 * i) = f32x4{v[0][i], v[1][i], v[2][i], v[3][i]} * factor;
         }
     }
 }
@@ -450,49 +542,58 @@ __global__ __launch_bounds__(kThreads) void lora_grads_sum_kernel(const float4* 
     else out1[i - count0] = s;
 }
 
-template <int RT, int NT, bool BACK>
-hipError_t rows_as(const LoraArgs& a, const LoraPlan& p, hipStream_t stream) {
-    constexpr int W = 8;
-    lora_rows_kernel<RT, NT, BACK, W><<<dim3((unsigned)p.tiles, (unsigned)(a.y ? p.slices : 1)), 64 * W, 0, stream>>>(a);
-    return hipGetLastError();
-}
 template <int RT, bool BACK>
-hipError_t rows_of(const LoraArgs& a, const LoraPlan& p, hipStream_t stream) {
-    return p.shift == 4 ? rows_as<RT, 1, BACK>(a, p, stream) : rows_as<RT, 2, BACK>(a, p, stream);
+hipError_t rows_as(const LoraArgs& a, const LoraPlan& p, hipStream_t stream) {
+    const dim3 grid((unsigned)p.tiles, (unsigned)(a.y ? p.slices : 1));
+    if (p.deep) lora_rows_kernel<RT, BACK, true, false><<<grid, 512, 0, stream>>>(a);
+    else if (p.once) lora_rows_kernel<RT, BACK, false, true><<<grid, 256, 0, stream>>>(a);
+    else lora_rows_kernel<RT, BACK, false, false><<<grid, 256, 0, stream>>>(a);
+    return hipGetLastError();
 }
 
 }  // namespace
 
-LoraPlan lora_plan(int S, int T, int d_up) {
+// Measured at d = 4,096, rank 32: 64 rows in 1, 4, 8 slices 17.6, 11.3, 10.2 us; 1,024 rows in 1, 2, 4, 8 22.4, 17.5, 15.3, 23.9; 2,048 in
+// 1, 2, 4 23.0, 19.1, 28.6; with smaller workgroups at best 12.4, 19.8, 25.2.  4,096 rows (a tile to a compute unit) 25.4, and 28.7 with smaller
+// workgroups, which win from there on.
+// y past the caches where x and y are 128 MB or more: 8,400 rows of rank 16, other rows between, 67 -> 57 us; 4,096 rows, which are
+// found in the caches, 34.6 -> 43.5.
+LoraPlan lora_plan(int S, int T, int d_down, int d_up) {
     LoraPlan p{};
-    p.shift = T > 16 * S ? 5 : 4;
-    p.tiles = ((T + (1 << p.shift) - 1) >> p.shift) + S;
-    const int whole = p.tiles - S > S ? p.tiles - S : S;         // about as many have rows
+    const int full = (T + 15) / 16, whole = full > S ? full : S;  // about as many have rows
+    p.tiles = full + S;
+    p.deep = whole <= 256;
     const int most = (d_up + 511) / 512;                         // slices that leave a wavefront 64 columns
-    p.slices = 512 / whole < 1 ? 1 : 512 / whole < most ? 512 / whole : most;
+    p.slices = 256 / whole < 1 ? 1 : 256 / whole < most ? 256 / whole : most;
+    p.once = (size_t)T * ((size_t)d_down + d_up) * 2 >= (size_t)128 << 20;
     return p;
 }
 
 hipError_t launch_lora_rows(const LoraArgs& a, const LoraPlan& p, bool back, hipStream_t stream) {
-    if (back) return a.r <= 16 ? rows_of<1, true>(a, p, stream) : a.r <= 32 ? rows_of<2, true>(a, p, stream) : rows_of<4, true>(a, p, stream);
-    return a.r <= 16 ? rows_of<1, false>(a, p, stream) : a.r <= 32 ? rows_of<2, false>(a, p, stream) : rows_of<4, false>(a, p, stream);
+    if (back) return a.r <= 16 ? rows_as<1, true>(a, p, stream) : a.r <= 32 ? rows_as<2, true>(a, p, stream) : rows_as<4, true>(a, p, stream);
+    return a.r <= 16 ? rows_as<1, false>(a, p, stream) : a.r <= 32 ? rows_as<2, false>(a, p, stream) : rows_as<4, false>(a, p, stream);
 }
 
-int lora_grad_parts(int n, int T, int d0, int d1) {
-    const long long groups = (long long)n * ((d0 + 63) / 64 + (d1 + 63) / 64);
-    const int steps = (T + 31) / 32;
-    int parts = (int)(512 / groups);
-    if (parts > (steps + 2 * kWaves - 1) / (2 * kWaves)) parts = (steps + 2 * kWaves - 1) / (2 * kWaves);
+// Columns and wavefronts of a workgroup of the gradients: what 256 registers hold, 512 at rank 64.
+static int grad_columns(int r) { return r <= 16 ? 128 : 64; }
+static int grad_waves(int r) { return r <= 32 ? 8 : 4; }
+
+int lora_grad_parts(int n, int r, int T, int d0, int d1) {
+    const int c = grad_columns(r), w = grad_waves(r);
+    const long long groups = (long long)n * ((d0 + c - 1) / c + (d1 + c - 1) / c);
+    const int steps = (T + 31) / 32, most = (steps + 2 * w - 1) / (2 * w);         // (two steps to a wavefront)
+    int parts = (int)(256 / groups);
+    if (parts > most) parts = most;
     return parts < 1 ? 1 : parts > 16 ? 16 : parts;
 }
 
 hipError_t launch_lora_grads(const GradArgs& a, hipStream_t stream) {
-    const int groups0 = (a.job[0].d + 63) / 64, groups1 = (a.job[1].d + 63) / 64;
+    const int c = grad_columns(a.r), groups0 = (a.job[0].d + c - 1) / c, groups1 = (a.job[1].d + c - 1) / c;
     const long long count0 = (long long)a.q.n * a.r * a.job[0].d, count1 = (long long)a.q.n * a.r * a.job[1].d;
     const dim3 grid((unsigned)(groups0 + groups1), (unsigned)a.q.n, (unsigned)a.parts);
-    if (a.r <= 16) lora_grads_kernel<1><<<grid, kThreads, 0, stream>>>(a, groups0, count0 + count1);
-    else if (a.r <= 32) lora_grads_kernel<2><<<grid, kThreads, 0, stream>>>(a, groups0, count0 + count1);
-    else lora_grads_kernel<4><<<grid, kThreads, 0, stream>>>(a, groups0, count0 + count1);
+    if (a.r <= 16) lora_grads_kernel<1, 2, 8><<<grid, 512, 0, stream>>>(a, groups0, count0 + count1);
+    else if (a.r <= 32) lora_grads_kernel<2, 1, 8><<<grid, 512, 0, stream>>>(a, groups0, count0 + count1);
+    else lora_grads_kernel<4, 1, 4><<<grid, 256, 0, stream>>>(a, groups0, count0 + count1);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.parts == 1) return e;
     lora_grads_sum_kernel<<<dim3((unsigned)(((count0 + count1) / 4 + kThreads - 1) / kThreads)), kThreads, 0, stream>>>(

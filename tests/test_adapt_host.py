@@ -31,11 +31,11 @@ def test_lora_bytes(ev):
             assert f(ctypes.byref(lora()), S, T, ctypes.byref(out)) == 0 and out.value == 0
         for bad in BAD_SIZES:
             assert f(ctypes.byref(lora(**bad)), 4, 100, ctypes.byref(out)) == 2, bad
-        for S, T in ((-1, 5), (5, -1), ((1 << 16) + 1, 5), (5, (1 << 24) + 1)):
+        for S, T in ((-1, 5), (5, -1), ((1 << 16) + 1, 5), (5, 1 << 24)):
             assert f(ctypes.byref(lora()), S, T, ctypes.byref(out)) == 2
         assert f(None, 4, 100, ctypes.byref(out)) == 1 and f(ctypes.byref(lora()), 4, 100, None) == 1
     # past 32 bits
-    assert ev.lib.evospec_lora_backward_workspace_bytes(ctypes.byref(lora(r=64)), 1, 1 << 24, ctypes.byref(out)) == 0 and out.value >= 1 << 32
+    assert ev.lib.evospec_lora_backward_workspace_bytes(ctypes.byref(lora(r=64)), 1, (1 << 24) - 1, ctypes.byref(out)) == 0 and out.value >= 1 << 32
 
 
 # Addresses below are never dereferenced: every call that is not an error has nothing to do.
@@ -51,7 +51,7 @@ def test_lora_refusals(ev):
     for f in (forward, backward):
         for bad in BAD_SIZES:
             assert f(ev, l=lora(**bad)) == 2, bad
-        for bad in (dict(S=-1), dict(T=-1), dict(S=(1 << 16) + 1), dict(T=(1 << 24) + 1), dict(xs=63), dict(xs=(1 << 32) + 8)):
+        for bad in (dict(S=-1), dict(T=-1), dict(S=(1 << 16) + 1), dict(T=1 << 24), dict(xs=63), dict(xs=(1 << 26) + 8)):
             assert f(ev, **bad) == 2, bad
         for bad in (dict(x=None), dict(off=None), dict(ad=None), dict(l=lora(a=None)), dict(l=lora(b=None))):
             assert f(ev, **bad) == 1, bad
