@@ -121,23 +121,13 @@ def _rows_of(x, d, name, dev, T=None):
     return s[0] if x.size(0) > 1 else d
 
 
-def _span(x):
-    """First and last byte of a matrix with strided rows."""
-    at = x.data_ptr()
-    return at, at + 2 * ((x.size(0) - 1) * x.stride(0) + x.size(1)) if x.numel() else at
-
-
-def _apart(out, name, *others):
-    """Refuses an output whose elements are those of an input: rows of one buffer may lie between one another."""
-    lo, hi = _span(out)
-    for x, other in others:
-        a, b = _span(x)
-        if a < hi and lo < b:
-            # beside each other in rows of the same length
-            if out.size(0) > 1 and x.size(0) > 1 and out.stride(0) == x.stride(0):
-                step, by = 2 * out.stride(0), (a - lo) % (2 * out.stride(0))
-                if by >= 2 * out.size(1) and by + 2 * x.size(1) <= step:
-                    continue
+def _apart(out, rows, d, stride, name, x, dx, stride_x, other):
+    """Refuses an output [rows, d] some of whose elements are those of an input [rows, dx]: rows of one buffer may lie between one another.
+    (Strides in elements of bf16; a row's own length where there is one row.)"""
+    lo, a = out.data_ptr(), x.data_ptr()
+    if a < lo + 2 * ((rows - 1) * stride + d) and lo < a + 2 * ((rows - 1) * stride_x + dx) and rows:
+        by = (a - lo) % (2 * stride)
+        if rows == 1 or stride != stride_x or by < 2 * d or by + 2 * dx > 2 * stride:
             raise ValueError(f"{name} overlaps {other}")
 
 
@@ -150,7 +140,7 @@ def lora_forward(x, bank: LoraBank, row_off, adapter, y, keep: bool = False, out
     xs = _rows_of(x, bank.d_in, "x", dev)
     T = x.size(0)
     ys = _rows_of(y, bank.d_out, "y", dev, T)
-    _apart(y, "y", (x, "x"))
+    _apart(y, T, bank.d_out, ys, "y", x, bank.d_in, xs, "x")
     if out_h is not None:
         _expect(out_h, _f32, "out_h", 2)
         _elsewhere(out_h, dev, "out_h")
@@ -179,7 +169,8 @@ def lora_backward(x, dy, bank: LoraBank, row_off, adapter, h=None, dx=None, out_
     ds = 0
     if dx is not None:
         ds = _rows_of(dx, bank.d_in, "dx", dev, T)
-        _apart(dx, "dx", (x, "x"), (dy, "dy"))
+        _apart(dx, T, bank.d_in, ds, "dx", x, bank.d_in, xs, "x")
+        _apart(dx, T, bank.d_in, ds, "dx", dy, bank.d_out, gs, "dy")
     if h is not None:
         _expect(h, _f32, "h", 2)
         _elsewhere(h, dev, "h")

@@ -37,7 +37,7 @@ int check_kd(int E, int K, int d) {
     return E < 0 || E >= (1 << 20) || K < 1 || K > EVOSPEC_KD_K_MAX || d < 8 || d % 8 || d > EVOSPEC_KD_D_MAX ? EVOSPEC_BAD_SHAPE : EVOSPEC_OK;
 }
 size_t kd_workspace(int E, int K, int d) {
-    const int s = E ? kd_splits(E, K) : 1;
+    const int s = E ? kd_splits(E, K, d) : 1;
     return s == 1 ? 0 : up_to((size_t)E * s * 2 * d * sizeof(float)) + (size_t)E * s * sizeof(float2);
 }
 
@@ -145,7 +145,7 @@ int evospec_kd_loss(const void* h, int E, int d, const void* W_lm, int V, const 
     if (workspace_bytes < need) return EVOSPEC_WORKSPACE_TOO_SMALL;
     KdArgs a{};
     a.h = h; a.W = W_lm; a.support = support; a.target = target; a.weight = weight;
-    a.E = E; a.d = d; a.V = V; a.K = K; a.splits = kd_splits(E, K); a.T = T; a.type = type;
+    a.E = E; a.d = d; a.V = V; a.K = K; a.splits = kd_splits(E, K, d); a.T = T; a.type = type;
     a.loss = out_loss; a.dh = out_dh; a.draft = out_draft;
     a.part = static_cast<float*>(workspace);
     if (need) a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + up_to((size_t)E * a.splits * 2 * d * sizeof(float)));

@@ -73,7 +73,7 @@ struct KdArgs {
     float* part;                              // [E][splits][2][d] of splits > 1
     float2* part_ml;                          // [E][splits]: reference and sum
 };
-int kd_splits(int E, int K);
+int kd_splits(int E, int K, int d);
 hipError_t launch_kd(const KdArgs& a, hipStream_t stream);
 
 struct AdamwArgs {

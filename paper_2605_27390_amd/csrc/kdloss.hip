@@ -118,7 +118,7 @@ __device__ __forceinline__ float fold(float a, float b, int lane) {
 
 // NC pieces of 8 elements to a thread, RB rows at a time, the next ones under way meanwhile.
 template <int NC, int RB, int TYPE>
-__global__ __launch_bounds__(kThreads) void kd_rows_kernel(KdArgs a) {
+__global__ __launch_bounds__(kThreads, NC == 2 ? 3 : 1) void kd_rows_kernel(KdArgs a) {
     __shared__ __align__(16) float dots[2][RB][kWaves];
     __shared__ float p[kMost + 16];                                   // of this workgroup's entries
     __shared__ float z[kMost + 16];
@@ -352,15 +352,19 @@ hipError_t rows_as(const KdArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-int kd_splits(int E, int K) {
-    int s = 768 / E;
+// Workgroups that a compute unit has at once: 4, 3, 2 and 1 for 1, 2, 4 and 8 pieces to a thread.  An event's rows are split until they
+// come to one round of them; up to 100 events to two workgroups a unit, whose parts cost less to join than more rows under way gain (256 rows of
+// 4,096; 32 events in 16 and 24 parts 24.0 and 26.3 us, 64 in 8 and 12 35.6 and 38.7, 150 in 3 and 5 72.7 and 65.3, 192 in 2 and 4 99.4 and 79.0).
+int kd_splits(int E, int K, int d) {
+    const int pieces = (d / 8 + kThreads - 1) / kThreads, most = 256 * (pieces == 1 ? 4 : pieces == 2 ? 3 : pieces <= 4 ? 2 : 1);
+    int s = (E <= 100 && most > 512 ? 512 : most) / E;
     if (s > K / 8) s = K / 8;
     return s < 1 ? 1 : s > 32 ? 32 : s;
 }
 
 hipError_t launch_kd(const KdArgs& a, hipStream_t stream) {
     const int pieces = (a.d / 8 + kThreads - 1) / kThreads;
-    const hipError_t e = pieces == 1 ? rows_as<1, 4>(a, stream) : pieces == 2 ? rows_as<2, 4>(a, stream) : pieces <= 4 ? rows_as<4, 2>(a, stream) : rows_as<8, 1>(a, stream);
+    const hipError_t e = pieces == 1 ? rows_as<1, 4>(a, stream) : pieces == 2 ? rows_as<2, 2>(a, stream) : pieces <= 4 ? rows_as<4, 2>(a, stream) : rows_as<8, 1>(a, stream);
     if (e != hipSuccess || a.splits == 1) return e;
     const int v = a.splits <= 8 ? 4 : 2;
     const dim3 grid((unsigned)a.E, (unsigned)(1 + (a.d + v * kThreads - 1) / (v * kThreads)));

@@ -144,15 +144,21 @@ def test_what_overlaps():
     """Rows of one buffer may lie beside each other, and not on one another."""
     import torch
     from paper_2605_27390_amd.adapt import _apart
+
+    def apart(out, x):
+        stride = lambda t: t.stride(0) if t.size(0) > 1 else t.size(1)   # noqa: E731
+        _apart(out, out.size(0), out.size(1), stride(out), "y", x, x.size(1), stride(x), "x")
     both = torch.zeros(6, 96, dtype=torch.bfloat16)
     x, y = both[:, :64], both[:, 64:]
-    _apart(y, "y", (x, "x"))
-    _apart(x, "x", (y, "y"))
-    _apart(both[:2], "y", (both[2:], "x"))
-    for a, b in ((x, x), (both[:, :64], both[:, 56:]), (both[:, 56:], both[:, :64]), (both[:3], both[2:]), (both[:, :32], both[3:, 24:56]),
-                 (both.view(12, 48)[:, :32], both[:, 40:])):
+    apart(y, x)
+    apart(x, y)
+    apart(both[:2], both[2:4])
+    apart(both[:1, :64], both[:1, 64:])
+    apart(both[:0], both[:0])
+    for a, b in ((x, x), (both[:, :64], both[:, 56:]), (both[:, 56:], both[:, :64]), (both[:3], both[2:5]), (both[:3, :32], both[2:5, 24:56]),
+                 (both[:1, :64], both[:1, 56:]), (both.view(12, 48)[:6, :32], both[:, 40:])):
         with pytest.raises(ValueError, match="overlaps"):
-            _apart(a, "y", (b, "x"))
+            apart(a, b)
 
 
 # ---------------------------------------------------------------- the plain implementations
