@@ -68,7 +68,7 @@ int evospec_lora_forward(const evospec_lora* lora, const void* x, long long x_st
     if (!row_off || !adapter) return EVOSPEC_NULL_POINTER;
     if (!aligned(out_h, 4)) return EVOSPEC_MISALIGNED;
     const LoraArgs rows{{row_off, adapter, S, T, lora->n}, x, x_stride, lora->a, lora->d_in, lora->scale, lora->b, lora->d_out, y, y_stride, out_h, lora->r};
-    return failed(launch_lora_rows(rows, lora_plan(S, T, lora->d_in, lora->d_out), false, static_cast<hipStream_t>(stream)));
+    return failed(launch_lora_rows(rows, lora_plan(S, T, lora->r, lora->d_in, lora->d_out), false, static_cast<hipStream_t>(stream)));
 }
 
 int evospec_lora_backward_workspace_bytes(const evospec_lora* lora, int S, int T, size_t* out_bytes) {
@@ -104,7 +104,7 @@ int evospec_lora_backward(const evospec_lora* lora, const void* x, long long x_s
     float* g = reinterpret_cast<float*>(ws);
     float* again = reinterpret_cast<float*>(ws + (rows ? h_bytes(lora, T) : 0));
     if (rows) {
-        const LoraPlan p = lora_plan(S, T, lora->d_out, lora->d_in);
+        const LoraPlan p = lora_plan(S, T, lora->r, lora->d_out, lora->d_in);
         if (!h) {
             const LoraArgs down{q, x, x_stride, lora->a, lora->d_in, nullptr, nullptr, 0, nullptr, 0, again, lora->r};
             if ((rc = failed(launch_lora_rows(down, p, false, st)))) return rc;

@@ -14,14 +14,15 @@ struct Requests {
     int S, T, n;                              // n adapters
 };
 
-// How the products of rows with adapters are laid out: tiles of 16 rows, the columns of the second product in `slices`.
+// How the products of rows with adapters are laid out: tiles of 16 rows, or 32, the columns of the second product in `slices`.
 struct LoraPlan {
+    bool wide;                                // 32
     int tiles;                                // workgroups for the rows: every request may begin a tile of its own
     int slices;
     bool deep;                                // a compute unit has one workgroup at most
     bool once;                                // y past the caches
 };
-LoraPlan lora_plan(int S, int T, int d_down, int d_up);
+LoraPlan lora_plan(int S, int T, int r, int d_down, int d_up);
 
 struct LoraArgs {                             // h = x w_down^T (times factor, backward), y += factor h w_up
     Requests q;

@@ -116,27 +116,21 @@ __device__ __forceinline__ float fold(float a, float b, int lane) {
     return keep + __uint_as_float(xor_lane<STRIDE>(__float_as_uint(give), lane));
 }
 
-// NC pieces of 8 elements to a thread, RB rows at a time, the next ones under way meanwhile.
-template <int NC, int RB, int TYPE>
-__global__ __launch_bounds__(kThreads, NC == 2 ? 3 : 1) void kd_rows_kernel(KdArgs a) {
-    __shared__ __align__(16) float dots[2][RB][kWaves];
-    __shared__ float p[kMost + 16];                                   // of this workgroup's entries
-    __shared__ float z[kMost + 16];
-    __shared__ int32_t ids[kMost + 16];
-    __shared__ LossShared loss;
-    const int e = blockIdx.x, part = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int j0 = (int)((long long)a.K * part / a.splits), j1 = (int)((long long)a.K * (part + 1) / a.splits), n = j1 - j0;
-    const float inv = 1.f / a.T, inf = __builtin_inff();
-    bool in[NC];
-    u32x4 h[NC];
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        in[c] = 8 * (c * kThreads + tid) < a.d;
-        h[c] = in[c] ? *(gvec_ptr)((const uint16_t*)a.h + (long long)e * a.d + 8 * (c * kThreads + tid)) : u32x4{0, 0, 0, 0};
-    }
-    // all entries of the event: p needs their sum
+// What both kernels of the rows begin with: p of this workgroup's entries [j0, j0 + n) of event e and their ids (-1: not in the support), from all
+// entries of the event.  True: nothing is learnt from it (no entry, or no target mass), and p is zero.  `meanwhile` is called when
+// the ids are there.
+struct Entries {
+    float p[kMost + 16];
+    float z[kMost + 16];
+    int32_t ids[kMost + 16];
+    LossShared loss;
+};
+template <typename F>
+__device__ __forceinline__ bool entries_of(const KdArgs& a, int e, int j0, int n, Entries& sh, F meanwhile) {
     constexpr int kPer = kMost / kThreads;
-    float t[kPer], top_t[1] = {-inf};
+    const float inf = __builtin_inff(), inv = 1.f / a.T;
+    const int tid = threadIdx.x;
+    float t[kPer], top[1] = {-inf};
     bool nan = false;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
@@ -144,87 +138,64 @@ __global__ __launch_bounds__(kThreads, NC == 2 ? 3 : 1) void kd_rows_kernel(KdAr
         const int32_t id = j < a.K ? a.support[(long long)e * a.K + j] : -1;
         const bool mine = (unsigned)id < (unsigned)a.V;
         t[i] = mine ? a.target[(long long)e * a.K + j] : -inf;
-        top_t[0] = fmaxf(top_t[0], t[i]);
+        top[0] = fmaxf(top[0], t[i]);
         nan |= t[i] != t[i];
-        if (j >= j0 && j < j1) ids[j - j0] = mine ? id : -1;
+        if (j >= j0 && j < j0 + n) sh.ids[j - j0] = mine ? id : -1;
     }
+    if (tid < 16) sh.ids[n + tid] = -1;                          // (turns may pass the end)
     __syncthreads();
-
-    u32x4 even[RB][NC], odd[RB][NC];
-    auto load = [&](u32x4 (&row)[RB][NC], int at) {
-#pragma unroll
-        for (int r = 0; r < RB; ++r) {
-            const int id = at + r < n ? __builtin_amdgcn_readfirstlane(ids[at + r]) : -1;
-            if (id >= 0) {
-                const uint16_t* w = (const uint16_t*)a.W + (long long)id * a.d;
-#pragma unroll
-                for (int c = 0; c < NC; ++c) row[r][c] = in[c] ? *(gvec_ptr)(w + 8 * (c * kThreads + tid)) : u32x4{0, 0, 0, 0};
-            } else {
-#pragma unroll
-                for (int c = 0; c < NC; ++c) row[r][c] = u32x4{0, 0, 0, 0};
-            }
-        }
-    };
-    load(even, 0);                                               // (on their way during the sum)
-    block_max(top_t, reinterpret_cast<float (*)[1]>(loss.top));
+    meanwhile();
+    block_max(top, reinterpret_cast<float (*)[1]>(sh.loss.top));
     nan = __syncthreads_or(nan);
-    const bool none = top_t[0] == -inf && !nan;
-    float x[kPer], total[1] = {0.f};
+    const bool none = top[0] == -inf && !nan;
+    float total[1] = {0.f};
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-        x[i] = t[i] == -inf ? 0.f : expf((t[i] - top_t[0]) * inv);
-        total[0] += x[i];
+        t[i] = t[i] == -inf ? 0.f : expf((t[i] - top[0]) * inv);
+        total[0] += t[i];
     }
-    block_sums(total, reinterpret_cast<float (*)[1]>(loss.top));
+    block_sums(total, reinterpret_cast<float (*)[1]>(sh.loss.top));
     const float per = none ? 0.f : 1.f / total[0];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int j = i * kThreads + tid;
-        if (j >= j0 && j < j1) p[j - j0] = x[i] * per;
+        if (j >= j0 && j < j0 + n) sh.p[j - j0] = t[i] * per;
     }
     __syncthreads();
+    return none;
+}
 
-    float o1[NC][8] = {}, o2[NC][8] = {};
-    float m = -inf, l = 0.f;
-    const int mod = lane & (RB - 1);                             // the row of a turn whose logit and weights this lane looks after
-    auto add = [&](const u32x4 (&row)[RB][NC], int at, int turn) {
-        float dot[RB];
-#pragma unroll
-        for (int r = 0; r < RB; ++r) {
-            dot[r] = 0.f;
-#pragma unroll
-            for (int c = 0; c < NC; ++c)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const uint32_t w = row[r][c][q], x = h[c][q];        // (a bit_cast of a vector's element takes its first one)
-                    dot[r] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), __builtin_bit_cast(bf16x2, x), dot[r], false);
-                }
-        }
-        // sums of RB rows at once: lanes whose low bits are r end up with row r
-        if constexpr (RB == 4) {
-            const float a0 = fold<1>(dot[0], dot[1], lane), a1 = fold<1>(dot[2], dot[3], lane);
-            dot[0] = fold<2>(a0, a1, lane);
-        } else if constexpr (RB == 2) {
-            dot[0] = fold<1>(dot[0], dot[1], lane);
-            dot[0] += __uint_as_float(xor_lane<2>(__float_as_uint(dot[0]), lane));
-        } else {
-            dot[0] += __uint_as_float(xor_lane<1>(__float_as_uint(dot[0]), lane));
-            dot[0] += __uint_as_float(xor_lane<2>(__float_as_uint(dot[0]), lane));
-        }
-        dot[0] += __uint_as_float(xor_lane<4>(__float_as_uint(dot[0]), lane));
-        dot[0] += __uint_as_float(xor_lane<8>(__float_as_uint(dot[0]), lane));
-        dot[0] += __uint_as_float(xor_lane<16>(__float_as_uint(dot[0]), lane));
-        dot[0] += __uint_as_float(xor_lane<32>(__float_as_uint(dot[0]), lane));
-        if (lane < RB) dots[turn][lane][wave] = dot[0];
-        lds_barrier();                                           // (the rows under way stay so; the two halves of dots take turns)
-        const float4 d = *reinterpret_cast<const float4*>(dots[turn][mod]);
-        float x = (d.x + d.y) + (d.z + d.w);
-        const bool mine = at + mod < n && ids[at + mod] >= 0;
-        if (tid < RB && at + mod < n) z[at + mod] = mine ? x : __builtin_nanf("");
-        x = mine ? x * inv : -inf;
+// The sums over lanes of RB dots at once: lanes whose low bits are r end up with row r's.
+template <int RB>
+__device__ __forceinline__ float lane_sums(float (&dot)[RB], int lane) {
+    if constexpr (RB == 8) {
+        const float a = fold<1>(dot[0], dot[1], lane), b = fold<1>(dot[2], dot[3], lane), c = fold<1>(dot[4], dot[5], lane), d = fold<1>(dot[6], dot[7], lane);
+        dot[0] = fold<4>(fold<2>(a, b, lane), fold<2>(c, d, lane), lane);
+    } else if constexpr (RB == 4) {
+        dot[0] = fold<2>(fold<1>(dot[0], dot[1], lane), fold<1>(dot[2], dot[3], lane), lane);
+    } else if constexpr (RB == 2) {
+        dot[0] = fold<1>(dot[0], dot[1], lane);
+    }
+    if constexpr (RB < 2) dot[0] += __uint_as_float(xor_lane<1>(__float_as_uint(dot[0]), lane));
+    if constexpr (RB < 4) dot[0] += __uint_as_float(xor_lane<2>(__float_as_uint(dot[0]), lane));
+    if constexpr (RB < 8) dot[0] += __uint_as_float(xor_lane<4>(__float_as_uint(dot[0]), lane));
+    dot[0] += __uint_as_float(xor_lane<8>(__float_as_uint(dot[0]), lane));
+    dot[0] += __uint_as_float(xor_lane<16>(__float_as_uint(dot[0]), lane));
+    dot[0] += __uint_as_float(xor_lane<32>(__float_as_uint(dot[0]), lane));
+    return dot[0];
+}
+
+// Running sums of RB rows at a time.  A lane looks after the logit and weights of row `lane % RB` of a turn; all have the same m and l.
+template <int NC>
+struct Sums {
+    float m, l, o1[NC][8], o2[NC][8];
+    template <int RB>
+    __device__ __forceinline__ void add(const u32x4 (&row)[RB][NC], float x, bool mine, float p, int lane) {
+        x = mine ? x : -__builtin_inff();
         float top = x;
         if constexpr (RB >= 2) top = fmaxf(top, __uint_as_float(xor_lane<1>(__float_as_uint(top), lane)));
         if constexpr (RB >= 4) top = fmaxf(top, __uint_as_float(xor_lane<2>(__float_as_uint(top), lane)));
+        if constexpr (RB >= 8) top = fmaxf(top, __uint_as_float(xor_lane<4>(__float_as_uint(top), lane)));
         top = fmaxf(top, m);
         if (__builtin_amdgcn_readfirstlane(top != m)) {          // (the same in all lanes)
             const float back = expf(m - top);
@@ -235,7 +206,7 @@ __global__ __launch_bounds__(kThreads, NC == 2 ? 3 : 1) void kd_rows_kernel(KdAr
                 for (int i = 0; i < 8; ++i) o1[c][i] *= back;
             m = top;
         }
-        const float q = mine ? expf(x - m) : 0.f, w = mine ? p[at + mod] : 0.f;
+        const float q = mine ? expf(x - m) : 0.f, w = mine ? p : 0.f;
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
             const float qr = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(q), r));
@@ -250,6 +221,165 @@ __global__ __launch_bounds__(kThreads, NC == 2 ? 3 : 1) void kd_rows_kernel(KdAr
                     o2[c][i] = fmaf(wr, v, o2[c][i]);
                 }
         }
+    }
+};
+template <int RB, int NC>
+__device__ __forceinline__ void dots_of(const u32x4 (&row)[RB][NC], const u32x4 (&h)[NC], float (&dot)[RB]) {
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        dot[r] = 0.f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t w = row[r][c][q], x = h[c][q];    // (a bit_cast of a vector's element takes its first one)
+                dot[r] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), __builtin_bit_cast(bf16x2, x), dot[r], false);
+            }
+    }
+}
+
+// Rows of up to 512 NC elements: one to a wavefront, RB at a time, the next ones under way meanwhile; the wavefronts meet at the end.
+template <int NC, int RB, int TYPE>
+__global__ __launch_bounds__(kThreads, NC == 4 ? 2 : 3) void kd_rows_kernel(KdArgs a) {
+    __shared__ Entries sh;
+    __shared__ float joined[2][2][NC * 512];
+    __shared__ float2 ml[kWaves];
+    const int e = blockIdx.x, part = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int j0 = (int)((long long)a.K * part / a.splits), j1 = (int)((long long)a.K * (part + 1) / a.splits), n = j1 - j0;
+    const float inv = 1.f / a.T;
+    u32x4 h[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) h[c] = 8 * (64 * c + lane) < a.d ? *(gvec_ptr)((const uint16_t*)a.h + (long long)e * a.d + 8 * (64 * c + lane)) : u32x4{0, 0, 0, 0};
+    u32x4 even[RB][NC], odd[RB][NC];
+    auto load = [&](u32x4 (&row)[RB][NC], int at) {
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            const int id = at < n ? __builtin_amdgcn_readfirstlane(sh.ids[at + r]) : -1;
+            const uint16_t* w = (const uint16_t*)a.W + (long long)(id < 0 ? 0 : id) * a.d;
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                row[r][c] = id >= 0 && 8 * (64 * c + lane) < a.d ? *(gvec_ptr)(w + 8 * (64 * c + lane)) : u32x4{0, 0, 0, 0};
+        }
+    };
+    const bool none = entries_of(a, e, j0, n, sh, [&] { load(even, RB * wave); });
+    Sums<NC> s{};
+    s.m = -__builtin_inff();
+    const int mod = lane & (RB - 1);
+    auto add = [&](const u32x4 (&row)[RB][NC], int at) {
+        if (at >= n) return;                                     // (uniform)
+        float dot[RB];
+        dots_of(row, h, dot);
+        const float x = lane_sums(dot, lane);
+        const bool mine = sh.ids[at + mod] >= 0;
+        if (lane < RB) sh.z[at + mod] = mine ? x : __builtin_nanf("");
+        s.add(row, x * inv, mine, sh.p[at + mod], lane);
+    };
+    for (int at = RB * wave; at < n; at += 2 * RB * kWaves) {
+        load(odd, at + RB * kWaves);
+        add(even, at);
+        load(even, at + 2 * RB * kWaves);
+        add(odd, at + RB * kWaves);
+    }
+    // The wavefronts' sums: two give theirs to the other two, then one to the other.
+    if (lane == 0) ml[wave] = make_float2(s.m, s.l);
+    __syncthreads();
+    float m = -__builtin_inff(), l = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, ml[w].x);
+    auto factor_of = [&](float2 x) { return x.y == 0.f && x.x == -__builtin_inff() ? 0.f : expf(x.x - m); };      // (0: no rows, sums of zero)
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) l += ml[w].y * factor_of(ml[w]);
+    const float mine = factor_of(make_float2(s.m, s.l));
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s.o1[c][i] *= mine;
+#pragma unroll
+    for (int half = kWaves / 2; half > 0; half >>= 1) {
+        if (wave >= half && wave < 2 * half)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                store8<EVOSPEC_FP32>(joined[wave - half][0], 8 * (64 * c + lane), s.o1[c]);
+                store8<EVOSPEC_FP32>(joined[wave - half][1], 8 * (64 * c + lane), s.o2[c]);
+            }
+        __syncthreads();
+        if (wave < half)
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    s.o1[c][i] += joined[wave][0][8 * (64 * c + lane) + i];
+                    s.o2[c][i] += joined[wave][1][8 * (64 * c + lane) + i];
+                }
+        __syncthreads();
+    }
+    for (int j = tid; j < n; j += kThreads) a.draft[(long long)e * a.K + j0 + j] = sh.z[j];
+    if (wave == 0) {
+        if (a.splits == 1) {
+            const float factor = (a.weight ? a.weight[e] : 1.f) * a.T, li = 1.f / l;
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                if (8 * (64 * c + lane) < a.d) {
+                    float g[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) g[i] = none ? 0.f : factor * (s.o1[c][i] * li - s.o2[c][i]);
+                    store8<TYPE>(a.dh, (long long)e * a.d + 8 * (64 * c + lane), g);
+                }
+        } else {
+            float* out = a.part + ((long long)e * a.splits + part) * 2 * a.d;
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                if (8 * (64 * c + lane) < a.d) {
+                    store8<EVOSPEC_FP32>(out, 8 * (64 * c + lane), s.o1[c]);
+                    store8<EVOSPEC_FP32>(out, a.d + 8 * (64 * c + lane), s.o2[c]);
+                }
+            if (lane == 0) a.part_ml[(long long)e * a.splits + part] = make_float2(m, none ? -1.f : l);
+        }
+    }
+    if (a.splits == 1) event_loss(a, e, sh.z, sh.loss);
+}
+
+// Longer rows: one to the workgroup, NC pieces of 8 elements to a thread.
+template <int NC, int RB, int TYPE>
+__global__ __launch_bounds__(kThreads, NC <= 2 ? 3 : 1) void kd_long_rows_kernel(KdArgs a) {
+    __shared__ Entries sh;
+    __shared__ __align__(16) float dots[2][RB][kWaves];
+    const int e = blockIdx.x, part = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int j0 = (int)((long long)a.K * part / a.splits), j1 = (int)((long long)a.K * (part + 1) / a.splits), n = j1 - j0;
+    const float inv = 1.f / a.T;
+    bool in[NC];
+    u32x4 h[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        in[c] = 8 * (c * kThreads + tid) < a.d;
+        h[c] = in[c] ? *(gvec_ptr)((const uint16_t*)a.h + (long long)e * a.d + 8 * (c * kThreads + tid)) : u32x4{0, 0, 0, 0};
+    }
+    u32x4 even[RB][NC], odd[RB][NC];
+    auto load = [&](u32x4 (&row)[RB][NC], int at) {
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            const int id = at < n ? __builtin_amdgcn_readfirstlane(sh.ids[at + r]) : -1;
+            const uint16_t* w = (const uint16_t*)a.W + (long long)(id < 0 ? 0 : id) * a.d;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) row[r][c] = in[c] && id >= 0 ? *(gvec_ptr)(w + 8 * (c * kThreads + tid)) : u32x4{0, 0, 0, 0};
+        }
+    };
+    const bool none = entries_of(a, e, j0, n, sh, [&] { load(even, 0); });
+    Sums<NC> s{};
+    s.m = -__builtin_inff();
+    const int mod = lane & (RB - 1);
+    auto add = [&](const u32x4 (&row)[RB][NC], int at, int turn) {
+        float dot[RB];
+        dots_of(row, h, dot);
+        const float sum = lane_sums(dot, lane);
+        if (lane < RB) dots[turn][lane][wave] = sum;
+        lds_barrier();                                           // (the rows under way stay so; the two halves of dots take turns)
+        if (at >= n) return;                                     // (uniform)
+        const float4 d = *reinterpret_cast<const float4*>(dots[turn][mod]);
+        const float x = (d.x + d.y) + (d.z + d.w);
+        const bool mine = sh.ids[at + mod] >= 0;
+        if (tid < RB) sh.z[at + mod] = mine ? x : __builtin_nanf("");
+        s.add(row, x * inv, mine, sh.p[at + mod], lane);
     };
     for (int at = 0; at < n; at += 2 * RB) {
         load(odd, at + RB);
@@ -258,27 +388,27 @@ __global__ __launch_bounds__(kThreads, NC == 2 ? 3 : 1) void kd_rows_kernel(KdAr
         add(odd, at + RB, 1);
     }
     __syncthreads();
-    for (int j = tid; j < n; j += kThreads) a.draft[(long long)e * a.K + j0 + j] = z[j];
+    for (int j = tid; j < n; j += kThreads) a.draft[(long long)e * a.K + j0 + j] = sh.z[j];
     if (a.splits == 1) {
-        const float factor = (a.weight ? a.weight[e] : 1.f) * a.T, li = 1.f / l;
+        const float factor = (a.weight ? a.weight[e] : 1.f) * a.T, li = 1.f / s.l;
 #pragma unroll
         for (int c = 0; c < NC; ++c)
             if (in[c]) {
                 float g[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) g[i] = none ? 0.f : factor * (o1[c][i] * li - o2[c][i]);
+                for (int i = 0; i < 8; ++i) g[i] = none ? 0.f : factor * (s.o1[c][i] * li - s.o2[c][i]);
                 store8<TYPE>(a.dh, (long long)e * a.d + 8 * (c * kThreads + tid), g);
             }
-        event_loss(a, e, z, loss);
+        event_loss(a, e, sh.z, sh.loss);
     } else {
         float* out = a.part + ((long long)e * a.splits + part) * 2 * a.d;
 #pragma unroll
         for (int c = 0; c < NC; ++c)
             if (in[c]) {
-                store8<EVOSPEC_FP32>(out, 8 * (c * kThreads + tid), o1[c]);
-                store8<EVOSPEC_FP32>(out, a.d + 8 * (c * kThreads + tid), o2[c]);
+                store8<EVOSPEC_FP32>(out, 8 * (c * kThreads + tid), s.o1[c]);
+                store8<EVOSPEC_FP32>(out, a.d + 8 * (c * kThreads + tid), s.o2[c]);
             }
-        if (tid == 0) a.part_ml[(long long)e * a.splits + part] = make_float2(m, none ? -1.f : l);
+        if (tid == 0) a.part_ml[(long long)e * a.splits + part] = make_float2(s.m, none ? -1.f : s.l);
     }
 }
 
@@ -342,29 +472,36 @@ __global__ __launch_bounds__(kThreads) void kd_join_kernel(KdArgs a) {
     }
 }
 
-template <int NC, int RB>
+template <int NC, int RB, bool LONG>
 hipError_t rows_as(const KdArgs& a, hipStream_t stream) {
     const dim3 grid((unsigned)a.E, (unsigned)a.splits);
-    if (a.type == EVOSPEC_FP32) kd_rows_kernel<NC, RB, EVOSPEC_FP32><<<grid, kThreads, 0, stream>>>(a);
-    else kd_rows_kernel<NC, RB, EVOSPEC_BF16><<<grid, kThreads, 0, stream>>>(a);
+    if constexpr (LONG) {
+        if (a.type == EVOSPEC_FP32) kd_long_rows_kernel<NC, RB, EVOSPEC_FP32><<<grid, kThreads, 0, stream>>>(a);
+        else kd_long_rows_kernel<NC, RB, EVOSPEC_BF16><<<grid, kThreads, 0, stream>>>(a);
+    } else {
+        if (a.type == EVOSPEC_FP32) kd_rows_kernel<NC, RB, EVOSPEC_FP32><<<grid, kThreads, 0, stream>>>(a);
+        else kd_rows_kernel<NC, RB, EVOSPEC_BF16><<<grid, kThreads, 0, stream>>>(a);
+    }
     return hipGetLastError();
 }
 
 }  // namespace
 
-// Workgroups that a compute unit has at once: 4, 3, 2 and 1 for 1, 2, 4 and 8 pieces to a thread.  An event's rows are split until they
-// come to one round of them; up to 100 events to two workgroups a unit, whose parts cost less to join than more rows under way gain (256 rows of
-// 4,096; 32 events in 16 and 24 parts 24.0 and 26.3 us, 64 in 8 and 12 35.6 and 38.7, 150 in 3 and 5 72.7 and 65.3, 192 in 2 and 4 99.4 and 79.0).
+// An event's rows are split until the parts come to one round of workgroups, two to a compute unit; three where rows of 2,048 to 4,096 elements
+// are many (256 rows of 4,096; 32 events in 16 and 24 parts 24.0 and 26.3 us, 64 in 8 and 12 35.6 and 38.7, 150 in 3 and 5 69.4 and 65.8, 192 in 2 and 4
+// 94.4 and 78.7), one above 8,192.  Shorter rows gain nothing from three (400 events of 2,048 in 1 and 2 parts 73.6 and 83.3, 338 of 344 20.0 and 21.3).
 int kd_splits(int E, int K, int d) {
-    const int pieces = (d / 8 + kThreads - 1) / kThreads, most = 256 * (pieces == 1 ? 4 : pieces == 2 ? 3 : pieces <= 4 ? 2 : 1);
-    int s = (E <= 100 && most > 512 ? 512 : most) / E;
+    const int most = d > 8192 ? 256 : d > 2048 && d <= 4096 && E > 100 ? 768 : 512;
+    int s = most / E;
     if (s > K / 8) s = K / 8;
     return s < 1 ? 1 : s > 32 ? 32 : s;
 }
 
 hipError_t launch_kd(const KdArgs& a, hipStream_t stream) {
-    const int pieces = (a.d / 8 + kThreads - 1) / kThreads;
-    const hipError_t e = pieces == 1 ? rows_as<1, 4>(a, stream) : pieces == 2 ? rows_as<2, 2>(a, stream) : pieces <= 4 ? rows_as<4, 2>(a, stream) : rows_as<8, 1>(a, stream);
+    // (a row to a wavefront takes half the time of a row to a workgroup at 680 elements and a tenth less at 2,048; at 4,096 its sums and rows
+    // spill: 165 us for 192 events, 79)
+    const hipError_t e = a.d <= 512 ? rows_as<1, 8, false>(a, stream) : a.d <= 1024 ? rows_as<2, 4, false>(a, stream) : a.d <= 2048 ? rows_as<4, 2, false>(a, stream)
+                         : a.d <= 4096 ? rows_as<2, 2, true>(a, stream) : a.d <= 8192 ? rows_as<4, 2, true>(a, stream) : rows_as<8, 1, true>(a, stream);
     if (e != hipSuccess || a.splits == 1) return e;
     const int v = a.splits <= 8 ? 4 : 2;
     const dim3 grid((unsigned)a.E, (unsigned)(1 + (a.d + v * kThreads - 1) / (v * kThreads)));

@@ -79,12 +79,13 @@ __device__ __forceinline__ Run runs_of(const Requests& q, int base) {
     }
     return t;
 }
-// Tile `index` (16 rows) of the runs, in their order; no rows if there are fewer.
+// Tile `index` (1 << SHIFT rows) of the runs, in their order; no rows if there are fewer.
+template <int SHIFT>
 __device__ __forceinline__ Run find_tile(const Requests& q, int index) {
     const int lane = threadIdx.x & 63;
     for (int base = 0; base < q.S; base += 64) {
         const Run t = runs_of(q, base);
-        const int tiles = (t.rows + 15) >> 4;
+        const int tiles = (t.rows + (1 << SHIFT) - 1) >> SHIFT;
         int incl = tiles;
         if (q.S > 1) {
 #pragma unroll
@@ -96,8 +97,8 @@ __device__ __forceinline__ Run find_tile(const Requests& q, int index) {
         const int total = __builtin_amdgcn_readlane(incl, q.S > 1 ? 63 : 0);
         if (index < total) {
             const int at = __ffsll((unsigned long long)__ballot(incl > index)) - 1;
-            const int first = (index - __builtin_amdgcn_readlane(incl, at) + __builtin_amdgcn_readlane(tiles, at)) << 4;
-            return Run{__builtin_amdgcn_readlane(t.row0, at) + first, min(__builtin_amdgcn_readlane(t.rows, at) - first, 16),
+            const int first = (index - __builtin_amdgcn_readlane(incl, at) + __builtin_amdgcn_readlane(tiles, at)) << SHIFT;
+            return Run{__builtin_amdgcn_readlane(t.row0, at) + first, min(__builtin_amdgcn_readlane(t.rows, at) - first, 1 << SHIFT),
                        __builtin_amdgcn_readlane(t.adapter, at)};
         }
         index -= total;
@@ -115,7 +116,7 @@ typedef const float __attribute__((address_space(1))) * gfloat;
 typedef float f32x4_u __attribute__((ext_vector_type(4), aligned(4)));
 typedef const f32x4_u __attribute__((address_space(1))) * gfloat4;
 
-// One tile of 16 rows: h = x W_down^T, then y += h W_up for a slice of the columns.  Forward, W_down = A [r][d] and W_up = B [d][r]; backward
+// One tile of 16 NT rows: h = x W_down^T, then y += h W_up for a slice of the columns.  Forward, W_down = A [r][d] and W_up = B [d][r]; backward
 // W_down = B^T and W_up = A^T of the same arrays.  The long axis of the first product is split over W wavefronts, whose sums are added
 // in LDS; in the second each takes 64 columns at a time.  Every slice computes h again: it is launched with slices where tiles are
 // few and the time is that of a launch.
@@ -125,15 +126,15 @@ typedef const f32x4_u __attribute__((address_space(1))) * gfloat4;
 // lane has 4 columns in 4 rows, the columns of a row in 16 lanes.
 // DEEP, where tiles and slices leave a compute unit one workgroup at most: 8 wavefronts with 2 KB x 12 on their way each.  Else four
 // workgroups of 4 to a unit, so that some load while others store.  ONCE: y past the caches.
-template <int RT, bool BACK, bool DEEP, bool ONCE>
+template <int RT, int NT, bool BACK, bool DEEP, bool ONCE>
 __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lora_rows_kernel(LoraArgs a) {
     constexpr int W = DEEP ? 8 : 4;
     constexpr int KS = (RT + 1) / 2;
-    constexpr int kSets = BACK ? 1 : 1 + RT;                     // of 16 rows through LDS: x's, then A's
-    constexpr int kOwn = kSets * 128 > RT * 64 ? kSets * 128 : RT * 64;        // 16-byte pieces of a wavefront (64 columns of B: up to 128 RT)
+    constexpr int kSets = BACK ? NT : NT + RT;                   // of 16 rows through LDS: x's, then A's
+    constexpr int kOwn = kSets * 128 > RT * NT * 64 ? kSets * 128 : RT * NT * 64;      // 16-byte pieces of a wavefront (64 columns of B: up to 128 RT)
     __shared__ __align__(16) u32x4 own[W][kOwn];
-    __shared__ float hs[16 * RT][17];
-    const Run t = find_tile(a.q, blockIdx.x);
+    __shared__ float hs[16 * RT][16 * NT + 1];
+    const Run t = find_tile<NT == 1 ? 4 : 5>(a.q, blockIdx.x);
     if (t.rows == 0) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, kg = lane >> 4;
     const float factor = a.factor ? a.factor[t.adapter] : 1.f;
@@ -142,7 +143,7 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
     // 64 columns of the second product: what this lane has of y, and of the weights what operands are made of.  Column 4 m + j of them is
     // column m of tile j.
     struct Columns {
-        u32x2 y[4];
+        u32x2 y[NT][4];
         u32x4 w[BACK ? 1 : 2 * RT];
         u32x2 raw[BACK ? KS : 1][8];
     };
@@ -150,10 +151,12 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
     auto load_columns = [&](Columns& col, int g) {
         const int c = min(64 * g + 4 * m, a.d_up - 4);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const gpair p = (gpair)((gu16)a.y + (long long)(t.row0 + min(4 * kg + k, t.rows - 1)) * a.y_stride + c);
-            col.y[k] = ONCE ? __builtin_nontemporal_load(p) : *p;
-        }
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const gpair p = (gpair)((gu16)a.y + (long long)(t.row0 + min(16 * i + 4 * kg + k, t.rows - 1)) * a.y_stride + c);
+                col.y[i][k] = ONCE ? __builtin_nontemporal_load(p) : *p;
+            }
         if constexpr (BACK) {                                    // [r][d]
 #pragma unroll
             for (int s = 0; s < KS; ++s)
@@ -176,7 +179,7 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
     {
         // Chunks of 64 along the summed axis go round the wavefronts, U at a time; every tile begins at another one, or all workgroups would
         // ask the same channels of memory at the same time (rows are often a multiple of 4 KB apart).
-        constexpr int U = !DEEP || (RT == 4 && !BACK) ? 1 : RT == 4 ? 2 : 4;
+        constexpr int U = !DEEP || (RT == 4 && (!BACK || NT > 1)) ? 1 : RT == 4 ? 2 : 4;
         const int chunks = (a.d_down + 63) / 64, turn = (int)(blockIdx.x * 5u % (unsigned)chunks);
         const int row8 = lane >> 3, piece = lane & 7;
         gu16 from[kSets][2];
@@ -184,11 +187,11 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
         for (int i = 0; i < kSets; ++i)
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
-                if (i == 0) from[i][b] = (gu16)a.x + (long long)(t.row0 + min(8 * b + row8, t.rows - 1)) * a.x_stride + 8 * piece;
-                else from[i][b] = (gu16)a.w_down + ((long long)t.adapter * a.r + min(16 * (i - 1) + 8 * b + row8, a.r - 1)) * a.d_down + 8 * piece;
+                if (i < NT) from[i][b] = (gu16)a.x + (long long)(t.row0 + min(16 * i + 8 * b + row8, t.rows - 1)) * a.x_stride + 8 * piece;
+                else from[i][b] = (gu16)a.w_down + ((long long)t.adapter * a.r + min(16 * (i - NT) + 8 * b + row8, a.r - 1)) * a.d_down + 8 * piece;
             }
         const gu16 w = (gu16)a.w_down + (long long)t.adapter * a.r * a.d_down;
-        f32x4 acc[RT] = {};
+        f32x4 acc[RT][NT] = {};
         struct Chunk {
             u32x4 rows[kSets][2];
             uint32_t raw[BACK ? 2 : 1][8][(RT + 1) / 2];
@@ -230,16 +233,19 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
 #pragma unroll
                 for (int j = 0; j < RT; ++j) {
                     if constexpr (!BACK) {
-                        ws[j] = mine[128 * (1 + j) + 8 * m + ((4 * s + kg) ^ (m & 7))];
+                        ws[j] = mine[128 * (NT + j) + 8 * m + ((4 * s + kg) ^ (m & 7))];
                     } else {
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
                             ws[j][i] = j & 1 ? high_halves(c.raw[s][2 * i][j / 2], c.raw[s][2 * i + 1][j / 2]) : low_halves(c.raw[s][2 * i][j / 2], c.raw[s][2 * i + 1][j / 2]);
                     }
                 }
-                const u32x4 x = mine[8 * m + ((4 * s + kg) ^ (m & 7))];
 #pragma unroll
-                for (int j = 0; j < RT; ++j) acc[j] = mfma(ws[j], x, acc[j]);
+                for (int i = 0; i < NT; ++i) {
+                    const u32x4 x = mine[128 * i + 8 * m + ((4 * s + kg) ^ (m & 7))];
+#pragma unroll
+                    for (int j = 0; j < RT; ++j) acc[j][i] = mfma(ws[j], x, acc[j][i]);
+                }
             }
         };
         Chunk even[U], odd[U];
@@ -257,33 +263,38 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
             for (int u = 0; u < U; ++u) add(odd[u]);
         }
 #pragma unroll
-        for (int j = 0; j < RT; ++j) mine[64 * j + lane] = __builtin_bit_cast(u32x4, acc[j]);
+        for (int j = 0; j < RT; ++j)
+#pragma unroll
+            for (int i = 0; i < NT; ++i) mine[64 * (j * NT + i) + lane] = __builtin_bit_cast(u32x4, acc[j][i]);
     }
     if (!DEEP && wave < count) load_columns(first, group_of(wave));
     lds_barrier();
-    for (int j = wave; j < RT; j += W) {
-        f32x4 v = __builtin_bit_cast(f32x4, own[0][64 * j + lane]);
+    for (int e = wave; e < RT * NT; e += W) {
+        f32x4 v = __builtin_bit_cast(f32x4, own[0][64 * e + lane]);
 #pragma unroll
-        for (int o = 1; o < W; ++o) v += __builtin_bit_cast(f32x4, own[o][64 * j + lane]);
+        for (int o = 1; o < W; ++o) v += __builtin_bit_cast(f32x4, own[o][64 * e + lane]);
+        const int j = e / NT, row = 16 * (e % NT) + m;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int rank = BACK ? RT * (4 * kg + i) + j : 16 * j + 4 * kg + i;
             const float scaled = v[i] * factor;
-            hs[rank][m] = scaled;
-            if (a.h && blockIdx.y == 0 && rank < a.r && m < t.rows) a.h[(long long)rank * a.q.T + t.row0 + m] = BACK ? scaled : v[i];
+            hs[rank][row] = scaled;
+            if (a.h && blockIdx.y == 0 && rank < a.r && row < t.rows) a.h[(long long)rank * a.q.T + t.row0 + row] = BACK ? scaled : v[i];
         }
     }
     if (!a.y) return;
     lds_barrier();
-    u32x4 h[KS][2];
+    u32x4 h[NT][KS][2];
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-        float v[8];
+    for (int i = 0; i < NT; ++i)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = 32 * s + 8 * kg < a.r ? hs[(32 * s + 8 * kg + k) % (16 * RT)][m] : 0.f;
-        h[s][0] = next_part(v);
-        h[s][1] = next_part(v);
-    }
+        for (int s = 0; s < KS; ++s) {
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = 32 * s + 8 * kg < a.r ? hs[(32 * s + 8 * kg + k) % (16 * RT)][16 * i + m] : 0.f;
+            h[i][s][0] = next_part(v);
+            h[i][s][1] = next_part(v);
+        }
     // B's 16-byte pieces in LDS: number p, of column p / (r / 8), with its low 4 bits turned by what the columns of a read differ in
     const int turned = a.r > 32 ? 5 : 4, per = a.r / 8;
     auto add = [&](const Columns& col, int g) {
@@ -295,7 +306,7 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
                     mine[p ^ ((p >> turned) & 15)] = col.w[k];
                 }
         }
-        f32x4 acc[4] = {};
+        f32x4 acc[4][NT] = {};
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             u32x4 op[4];
@@ -311,23 +322,28 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
                 }
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                acc[j] = mfma(h[s][0], op[j], acc[j]);
-                acc[j] = mfma(h[s][1], op[j], acc[j]);
-            }
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    acc[j][i] = mfma(h[i][s][0], op[j], acc[j][i]);
+                    acc[j][i] = mfma(h[i][s][1], op[j], acc[j][i]);
+                }
         }
         const int c = 64 * g + 4 * m;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (4 * kg + k >= t.rows || c >= a.d_up) continue;
-            const uint32_t y0 = col.y[k][0], y1 = col.y[k][1];
-            typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-            const bf16x4 v = {(__bf16)(__uint_as_float(y0 << 16) + acc[0][k]), (__bf16)(__uint_as_float(y0 & 0xffff0000u) + acc[1][k]),
-                              (__bf16)(__uint_as_float(y1 << 16) + acc[2][k]), (__bf16)(__uint_as_float(y1 & 0xffff0000u) + acc[3][k])};
-            bf16x4* p = reinterpret_cast<bf16x4*>((uint16_t*)a.y + (long long)(t.row0 + 4 * kg + k) * a.y_stride + c);
-            if constexpr (ONCE) __builtin_nontemporal_store(v, p);
-            else *p = v;
-        }
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int row = 16 * i + 4 * kg + k;
+                if (row >= t.rows || c >= a.d_up) continue;
+                const uint32_t y0 = col.y[i][k][0], y1 = col.y[i][k][1];
+                typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+                const bf16x4 v = {(__bf16)(__uint_as_float(y0 << 16) + acc[0][i][k]), (__bf16)(__uint_as_float(y0 & 0xffff0000u) + acc[1][i][k]),
+                                  (__bf16)(__uint_as_float(y1 << 16) + acc[2][i][k]), (__bf16)(__uint_as_float(y1 & 0xffff0000u) + acc[3][i][k])};
+                bf16x4* p = reinterpret_cast<bf16x4*>((uint16_t*)a.y + (long long)(t.row0 + row) * a.y_stride + c);
+                if constexpr (ONCE) __builtin_nontemporal_store(v, p);
+                else *p = v;
+            }
     };
     // (two sets of registers in turn; the first is on its way since before h was there)
     Columns next;
@@ -377,16 +393,16 @@ struct Steps {
     }
 };
 
-// RT tiles of 16 ranks; a workgroup has 64 CG columns of one adapter, its wavefronts and `parts` workgroups every so many-th step.  A step of
+// RT tiles of 16 ranks (rank 33 and more in two halves); a workgroup has 64 CG columns of one adapter, its wavefronts and `parts` workgroups every so many-th step.  A step of
 // 64 CG columns and 32 rows is 4 CG KB of x and, from L2, 2 RT KB of h, which becomes an operand in three parts.
 template <int RT, int CG, int W>
-__global__ __launch_bounds__(64 * W, W / 4) void lora_grads_kernel(GradArgs a, int groups0, long long partial_stride) {
+__global__ __launch_bounds__(64 * W, 2) void lora_grads_kernel(GradArgs a, int groups0, int halves, long long partial_stride) {
     constexpr int kTiles = 4 * CG * RT;
     __shared__ __align__(16) f32x4 sums[W / 2][kTiles][64];
-    static_assert(sizeof(sums) >= W * RT * 2048, "h of every wavefront's step");
+    static_assert(sizeof(sums) >= (size_t)W * RT * 2048, "h of every wavefront's step");
     const bool second = (int)blockIdx.x >= groups0;
     const GradJob job = second ? a.job[1] : a.job[0];
-    const int c0 = 64 * CG * (blockIdx.x - (second ? groups0 : 0)), adapter = blockIdx.y, part = blockIdx.z;
+    const int c0 = 64 * CG * (blockIdx.x - (second ? groups0 : 0)), adapter = blockIdx.y, part = blockIdx.z / halves, rank0 = 32 * (blockIdx.z % halves);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, kg = lane >> 4;
     // Places as a uniform address and a lane's 32 bits of offset (row strides are below 2^26, h is smaller than 4 GB): half the registers.
     const uint32_t down = (uint32_t)(8 * kg * job.x_stride) * 2u;
@@ -397,7 +413,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void lora_grads_kernel(GradArgs a, i
     const int rank8 = lane >> 3, piece = lane & 7, slot = ((piece >> 1) + 4 * (piece & 1)) ^ rank8;
     uint32_t hp[2 * RT];
 #pragma unroll
-    for (int j = 0; j < 2 * RT; ++j) hp[j] = 4u * ((uint32_t)min(8 * j + rank8, a.r - 1) * (uint32_t)a.q.T + 4u * piece);    // (ranks from r on end in nothing)
+    for (int j = 0; j < 2 * RT; ++j) hp[j] = 4u * ((uint32_t)min(rank0 + 8 * j + rank8, a.r - 1) * (uint32_t)a.q.T + 4u * piece);    // (ranks from r on end in nothing)
     f32x4* mine = &sums[0][0][0] + wave * RT * 128;
     f32x4 acc[CG][4][RT] = {};
     struct Rows {
@@ -461,10 +477,24 @@ __global__ __launch_bounds__(64 * W, W / 4) void lora_grads_kernel(GradArgs a, i
             __builtin_amdgcn_sched_barrier(0);
         }
     };
+    float* out = a.parts > 1 ? a.partial + part * partial_stride + (second ? (long long)a.q.n * a.r * a.job[0].d : 0ll) : job.out;
+    out += (long long)adapter * a.r * job.d;
     Steps steps(a.q, adapter);
     const int stride = W * a.parts;
     Rows even, odd;
-    int row0 = 0, rows = steps.skip(part * W + wave, row0);
+    int row0 = 0, rows = steps.skip(part * W, row0);
+    if (rows == 0) {                                             // (the same in all wavefronts) nothing to add: an adapter without rows, often
+        const int ranks = min(a.r - rank0, 16 * RT) / 4, columns = min(64 * CG, job.d - c0);
+        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+        if (job.rank_last)
+            for (int e = threadIdx.x; e < columns * ranks; e += 64 * W)
+                *reinterpret_cast<f32x4*>(out + (long long)(c0 + e / ranks) * a.r + rank0 + 4 * (e % ranks)) = zero;
+        else
+            for (int e = threadIdx.x; e < columns * ranks; e += 64 * W)
+                *reinterpret_cast<f32x4*>(out + (long long)(rank0 + e / (columns / 4)) * job.d + c0 + 4 * (e % (columns / 4))) = zero;
+        return;
+    }
+    if (wave > 0) rows = steps.skip(wave - 1, row0);
     load(even, row0, rows);
     while (rows) {
         rows = steps.skip(stride - 1, row0);
@@ -495,14 +525,12 @@ __global__ __launch_bounds__(64 * W, W / 4) void lora_grads_kernel(GradArgs a, i
                 for (int r = 0; r < RT; ++r) own[64 * ((g * 4 + j) * RT + r) + lane] += acc[g][j][r];
     __syncthreads();
     const float factor = job.factor ? job.factor[adapter] : 1.f;
-    float* out = a.parts > 1 ? a.partial + part * partial_stride + (second ? (long long)a.q.n * a.r * a.job[0].d : 0ll) : job.out;
-    out += (long long)adapter * a.r * job.d;
     if (job.rank_last) {
         for (int e = wave; e < kTiles; e += W) {
             f32x4 v = sums[0][e][lane];
 #pragma unroll
             for (int o = 1; o < W / 2; ++o) v += sums[o][e][lane];
-            const int g = e / (4 * RT), j = e / RT % 4, rank = 16 * (e % RT) + m;
+            const int g = e / (4 * RT), j = e / RT % 4, rank = rank0 + 16 * (e % RT) + m;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int c = c0 + 64 * g + 4 * (4 * kg + i) + j;
@@ -521,10 +549,10 @@ __global__ __launch_bounds__(64 * W, W / 4) void lora_grads_kernel(GradArgs a, i
 #pragma unroll
                 for (int o = 1; o < W / 2; ++o) v[j] += sums[o][at][16 * k + rank % 16];
             }
-            if (rank >= a.r) continue;
+            if (rank0 + rank >= a.r) continue;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (c + 4 * i < job.d) *reinterpret_cast<f32x4*>(out + (long long)rank * job.d + c + 4 * i) = f32x4{v[0][i], v[1][i], v[2][i], v[3][i]} * factor;
+                if (c + 4 * i < job.d) *reinterpret_cast<f32x4*>(out + (long long)(rank0 + rank) * job.d + c + 4 * i) = f32x4{v[0][i], v[1][i], v[2][i], v[3][i]} * factor;
         }
     }
 }
@@ -542,13 +570,19 @@ __global__ __launch_bounds__(kThreads) void lora_grads_sum_kernel(const float4* 
     else out1[i - count0] = s;
 }
 
-template <int RT, bool BACK>
+template <int RT, int NT, bool BACK>
 hipError_t rows_as(const LoraArgs& a, const LoraPlan& p, hipStream_t stream) {
     const dim3 grid((unsigned)p.tiles, (unsigned)(a.y ? p.slices : 1));
-    if (p.deep) lora_rows_kernel<RT, BACK, true, false><<<grid, 512, 0, stream>>>(a);
-    else if (p.once) lora_rows_kernel<RT, BACK, false, true><<<grid, 256, 0, stream>>>(a);
-    else lora_rows_kernel<RT, BACK, false, false><<<grid, 256, 0, stream>>>(a);
+    if (p.deep) lora_rows_kernel<RT, NT, BACK, true, false><<<grid, 512, 0, stream>>>(a);
+    else if (p.once) lora_rows_kernel<RT, NT, BACK, false, true><<<grid, 256, 0, stream>>>(a);
+    else lora_rows_kernel<RT, NT, BACK, false, false><<<grid, 256, 0, stream>>>(a);
     return hipGetLastError();
+}
+template <bool BACK>
+hipError_t rows_of(const LoraArgs& a, const LoraPlan& p, hipStream_t stream) {
+    if (a.r <= 16) return rows_as<1, 1, BACK>(a, p, stream);
+    if (a.r <= 32) return rows_as<2, 1, BACK>(a, p, stream);
+    return p.wide ? rows_as<4, 2, BACK>(a, p, stream) : rows_as<4, 1, BACK>(a, p, stream);
 }
 
 }  // namespace
@@ -558,42 +592,48 @@ hipError_t rows_as(const LoraArgs& a, const LoraPlan& p, hipStream_t stream) {
 // workgroups, which win from there on.
 // y past the caches where x and y are 128 MB or more: 8,400 rows of rank 16, other rows between, 67 -> 57 us; 4,096 rows, which are
 // found in the caches, 34.6 -> 43.5.
-LoraPlan lora_plan(int S, int T, int d_down, int d_up) {
+LoraPlan lora_plan(int S, int T, int r, int d_down, int d_up) {
     LoraPlan p{};
-    const int full = (T + 15) / 16, whole = full > S ? full : S;  // about as many have rows
+    p.wide = r > 32 && T > 16 * S;
+    const int size = p.wide ? 32 : 16, full = (T + size - 1) / size, whole = full > S ? full : S;    // about as many have rows
     p.tiles = full + S;
     p.deep = whole <= 256;
     const int most = (d_up + 511) / 512;                         // slices that leave a wavefront 64 columns
     p.slices = 256 / whole < 1 ? 1 : 256 / whole < most ? 256 / whole : most;
-    p.once = (size_t)T * ((size_t)d_down + d_up) * 2 >= (size_t)128 << 20;
+    p.once = !p.deep && (size_t)T * ((size_t)d_down + d_up) * 2 >= (size_t)128 << 20;
     return p;
 }
 
 hipError_t launch_lora_rows(const LoraArgs& a, const LoraPlan& p, bool back, hipStream_t stream) {
-    if (back) return a.r <= 16 ? rows_as<1, true>(a, p, stream) : a.r <= 32 ? rows_as<2, true>(a, p, stream) : rows_as<4, true>(a, p, stream);
-    return a.r <= 16 ? rows_as<1, false>(a, p, stream) : a.r <= 32 ? rows_as<2, false>(a, p, stream) : rows_as<4, false>(a, p, stream);
+    return back ? rows_of<true>(a, p, stream) : rows_of<false>(a, p, stream);
 }
 
-// Columns and wavefronts of a workgroup of the gradients: what 256 registers hold, 512 at rank 64.
+// Columns of a workgroup of the gradients, and halves of the ranks: what 256 registers hold without spilling.  (Rank 64 in one, four wavefronts of
+// 400 registers: VX us against VY.)
 static int grad_columns(int r) { return r <= 16 ? 128 : 64; }
-static int grad_waves(int r) { return r <= 32 ? 8 : 4; }
+static int grad_halves(int r) { return r <= 32 ? 1 : 2; }
+
+static long long grad_groups(int n, int r, int d0, int d1) {
+    const int c = grad_columns(r);
+    return (long long)n * grad_halves(r) * ((d0 + c - 1) / c + (d1 + c - 1) / c);
+}
 
 int lora_grad_parts(int n, int r, int T, int d0, int d1) {
-    const int c = grad_columns(r), w = grad_waves(r);
-    const long long groups = (long long)n * ((d0 + c - 1) / c + (d1 + c - 1) / c);
-    const int steps = (T + 31) / 32, most = (steps + 2 * w - 1) / (2 * w);         // (two steps to a wavefront)
-    int parts = (int)(256 / groups);
+    const int steps = (T + 31) / 32, most = (steps + 15) / 16;   // (two steps to a wavefront)
+    int parts = (int)(256 / grad_groups(n, r, d0, d1));
     if (parts > most) parts = most;
     return parts < 1 ? 1 : parts > 16 ? 16 : parts;
 }
 
 hipError_t launch_lora_grads(const GradArgs& a, hipStream_t stream) {
-    const int c = grad_columns(a.r), groups0 = (a.job[0].d + c - 1) / c, groups1 = (a.job[1].d + c - 1) / c;
+    const int c = grad_columns(a.r), groups0 = (a.job[0].d + c - 1) / c, groups1 = (a.job[1].d + c - 1) / c, halves = grad_halves(a.r);
     const long long count0 = (long long)a.q.n * a.r * a.job[0].d, count1 = (long long)a.q.n * a.r * a.job[1].d;
-    const dim3 grid((unsigned)(groups0 + groups1), (unsigned)a.q.n, (unsigned)a.parts);
-    if (a.r <= 16) lora_grads_kernel<1, 2, 8><<<grid, 512, 0, stream>>>(a, groups0, count0 + count1);
-    else if (a.r <= 32) lora_grads_kernel<2, 1, 8><<<grid, 512, 0, stream>>>(a, groups0, count0 + count1);
-    else lora_grads_kernel<4, 1, 4><<<grid, 256, 0, stream>>>(a, groups0, count0 + count1);
+    const dim3 grid((unsigned)(groups0 + groups1), (unsigned)a.q.n, (unsigned)(a.parts * halves));
+    // Many workgroups with few rows each: four of two wavefronts to a compute unit.
+    const bool few = grad_groups(a.q.n, a.r, a.job[0].d, a.job[1].d) > 512 && a.q.T <= 256 * (a.q.n < a.q.S ? a.q.n : a.q.S);
+    auto go = [&](auto kernel, int threads) { kernel<<<grid, threads, 0, stream>>>(a, groups0, halves, count0 + count1); };
+    if (a.r <= 16) few ? go(lora_grads_kernel<1, 2, 2>, 128) : go(lora_grads_kernel<1, 2, 8>, 512);
+    else few ? go(lora_grads_kernel<2, 1, 2>, 128) : go(lora_grads_kernel<2, 1, 8>, 512);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.parts == 1) return e;
     lora_grads_sum_kernel<<<dim3((unsigned)(((count0 + count1) / 4 + kThreads - 1) / kThreads)), kThreads, 0, stream>>>(
