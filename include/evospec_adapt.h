@@ -48,6 +48,7 @@ int evospec_lora_forward(const evospec_lora *lora, const void *x, long long x_st
  *   out_da    dev fp32 [n][r][d_in], 16-B aligned      out_db dev fp32 [n][d_out][r], 16-B aligned: written whole (zeros where an
  *             adapter has no rows)
  *   workspace dev, 16-B aligned, at least evospec_lora_backward_workspace_bytes(...) bytes, scratch
+ * n (d_in + d_out) / 64 below 2^22 (rank 33 and more) or 2^23.
  * Sums are fp32 in an order that depends on the sizes only: the same inputs give the same bits.
  */
 int evospec_lora_backward_workspace_bytes(const evospec_lora *lora, int S, int T, size_t *out_bytes /*host*/);

@@ -116,8 +116,8 @@ def _rows_of(x, d, name, dev, T=None):
     if x.dim() != 2 or x.size(1) != d or (T is not None and x.size(0) != T):
         raise ValueError(f"{name} must be [{'rows' if T is None else T}, {d}], got {tuple(x.shape)}")
     s = x.stride()
-    if s[1] != 1:
-        raise ValueError(f"{name}: elements of a row must be contiguous")
+    if s[1] != 1 or (s[0] < d and x.size(0) > 1):
+        raise ValueError(f"{name}: elements of a row must be contiguous, and rows apart")
     return s[0] if x.size(0) > 1 else d
 
 
@@ -242,7 +242,8 @@ class AdamW:
     tensors into which every step's gradients are written) and the moments, state "fp32" or "8bit", in flat buffers in which the
     tensors follow one another, each from a multiple of 256 elements on: m and v (fp32, or uint8 codes with scales fp32 [blocks, 2]).
     master: True or a flat fp32 buffer, from which parameters of 16 bits are rounded; True takes the parameters as they are now.
-    Buffers that are not given are allocated here, as zeros.  `offsets` says where each tensor begins."""
+    Buffers that are not given are allocated here, as zeros.  `offsets` says where each tensor begins.  The handle keeps the tensors and their
+    addresses: their memory must stay theirs (no `.data = ...`, no `set_`), and parameters must not share any."""
 
     def __init__(self, params, grads, state: str = "fp32", m=None, v=None, scales=None, master=None):
         if state not in _MOMENTS:
@@ -265,6 +266,9 @@ class AdamW:
             table[i] = _Tensor(p.data_ptr(), g.data_ptr(), p.numel())
             self.offsets.append(at)
             at += -(-p.numel() // ADAMW_BLOCK) * ADAMW_BLOCK
+        spans = sorted((p.data_ptr(), p.data_ptr() + p.numel() * p.element_size()) for p in params if p.numel())
+        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+            raise ValueError("two of params are the same memory")
         blocks = _ll(0)
         _check(lib.evospec_adamw_blocks(table, len(params), ctypes.byref(blocks)), "evospec_adamw_blocks")
         self.blocks, self.state, self._device = blocks.value, state, dev

@@ -31,6 +31,8 @@ int check_matrix(const void* p, long long stride, int d) {
     if (stride < d || stride > (1ll << 26)) return EVOSPEC_BAD_SHAPE;
     return stride % 8 == 0 && aligned(p, 16) ? EVOSPEC_OK : EVOSPEC_MISALIGNED;
 }
+// (a launch takes fewer than 2^32 threads, of 512 here; more than a part of the rows only where workgroups are few)
+bool grads_fit(const evospec_lora* l) { return lora_grad_groups(l->n, l->r, l->d_in, l->d_out) < (1ll << 23); }
 size_t h_bytes(const evospec_lora* l, int T) { return up_to((size_t)l->r * T * sizeof(float)); }
 
 int check_kd(int E, int K, int d) {
@@ -75,6 +77,7 @@ int evospec_lora_backward_workspace_bytes(const evospec_lora* lora, int S, int T
     if (!out_bytes) return EVOSPEC_NULL_POINTER;
     const int rc = check_lora(lora, S, T);
     if (rc) return rc;
+    if (!grads_fit(lora)) return EVOSPEC_BAD_SHAPE;
     *out_bytes = 0;
     if (S == 0 || T == 0) return EVOSPEC_OK;
     const int parts = lora_grad_parts(lora->n, lora->r, T, lora->d_in, lora->d_out);
@@ -87,6 +90,7 @@ int evospec_lora_backward(const evospec_lora* lora, const void* x, long long x_s
                           float* out_db, void* workspace, size_t workspace_bytes, void* stream) {
     int rc = check_lora(lora, S, T);
     if (rc) return rc;
+    if (!grads_fit(lora)) return EVOSPEC_BAD_SHAPE;
     const bool rows = S > 0 && T > 0;                            // (without any the gradients are zeros)
     if ((rc = check_weights(lora))) return rc;
     if (rows && ((rc = check_matrix(x, x_stride, lora->d_in)) || (rc = check_matrix(dy, dy_stride, lora->d_out)) ||

@@ -58,52 +58,81 @@ __device__ __forceinline__ void columns_of(const u32x2 (&raw)[8], u32x4 (&op)[4]
 struct Run {
     int row0, rows, adapter;
 };
-// Of 64 requests, lane l has request base + l: in the first lane of a run of requests that have the same adapter and follow one another, the
-// run; no rows in the others, or where the adapter is none.
-__device__ __forceinline__ Run runs_of(const Requests& q, int base) {
-    const int lane = threadIdx.x & 63, s = base + lane;
+// No rows of a request that has no adapter, or is none.
+__device__ __forceinline__ Run request_of(const Requests& q, int s) {
     Run t{0, 0, -1};
-    if (s < q.S) {
+    if (s >= 0 && s < q.S) {
         t.row0 = min(max(q.row_off[s], 0), q.T);
         t.rows = min(max(q.row_off[s + 1], t.row0), q.T) - t.row0;
         t.adapter = q.adapter[s];
         if ((unsigned)t.adapter >= (unsigned)q.n) t.rows = 0;
     }
+    return t;
+}
+// Whether a lane's request goes on with the run of the lane before it.  (All lanes take part in all exchanges: a lane that is switched off has
+// nothing to give.)
+__device__ __forceinline__ bool goes_on(const Run& t) {
+    const int end = __shfl_up(t.row0 + t.rows, 1), adapter = __shfl_up(t.adapter, 1), rows = __shfl_up(t.rows, 1);
+    return (threadIdx.x & 63) > 0 && t.rows > 0 && rows > 0 && end == t.row0 && adapter == t.adapter;
+}
+// Of 64 requests, lane l has request base + l: in the first lane of a run, the run; no rows in the others, or where the adapter is none.
+__device__ __forceinline__ Run runs_of(const Requests& q, int base) {
+    const int lane = threadIdx.x & 63;
+    Run t = request_of(q, base + lane);
     if (q.S > 1) {
-        const int end = t.row0 + t.rows;
-        const bool goes_on = __shfl_up(end, 1) == t.row0 && __shfl_up(t.adapter, 1) == t.adapter && __shfl_up(t.rows, 1) > 0 && t.rows > 0 && lane > 0;
-        const u64 on = __ballot(goes_on);
+        const bool mine = goes_on(t);
+        const u64 on = __ballot(mine);
         const int more = __ffsll((unsigned long long)~(lane < 63 ? on >> (lane + 1) : 0ull)) - 1;        // lanes that go on with this one's
-        const int last = __shfl(end, lane + more);
-        t.rows = goes_on ? 0 : t.rows > 0 ? last - t.row0 : 0;
+        const int last = __shfl(t.row0 + t.rows, lane + more);
+        t.rows = mine ? 0 : t.rows > 0 ? last - t.row0 : 0;
     }
     return t;
 }
-// Tile `index` (1 << SHIFT rows) of the runs, in their order; no rows if there are fewer.
+// Work item `index` of up to 1 << SHIFT rows: how many, their adapter, and in `where` (LDS; every wavefront writes the same) which.  Request s has the numbers
+// from row0 / size + s on, one for each block of rows that it touches (the call's rows, blocks begin at multiples of size), so that the last request
+// whose first number is not larger is found by looking at 64 of them at a time, however many there are.  Of 64 requests:
+// with one row each, as in a decode step, those with one adapter are an item together, wherever they are, of the first one's number;
+// otherwise what a run has in a block, of the number of its first request there.
 template <int SHIFT>
-__device__ __forceinline__ Run find_tile(const Requests& q, int index) {
+__device__ __forceinline__ Run find_rows(const Requests& q, int index, int* where) {
+    constexpr int kSize = 1 << SHIFT;
     const int lane = threadIdx.x & 63;
-    for (int base = 0; base < q.S; base += 64) {
-        const Run t = runs_of(q, base);
-        const int tiles = (t.rows + (1 << SHIFT) - 1) >> SHIFT;
-        int incl = tiles;
-        if (q.S > 1) {
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int up = __shfl_up(incl, o);
-                if (lane >= o) incl += up;
-            }
+    int lo = 0;
+    if (q.S > 1) {
+        int hi = q.S;
+        while (hi - lo > 1) {
+            const int step = (hi - lo + 63) >> 6, s = lo + lane * step;
+            const bool at_most = s < hi && (min(max(q.row_off[s], 0), q.T) >> SHIFT) + s <= index;
+            const int n = __popcll(__ballot(at_most));
+            if (n == 0) return Run{0, 0, 0};
+            lo += (n - 1) * step;
+            hi = min(lo + step, hi);
         }
-        const int total = __builtin_amdgcn_readlane(incl, q.S > 1 ? 63 : 0);
-        if (index < total) {
-            const int at = __ffsll((unsigned long long)__ballot(incl > index)) - 1;
-            const int first = (index - __builtin_amdgcn_readlane(incl, at) + __builtin_amdgcn_readlane(tiles, at)) << SHIFT;
-            return Run{__builtin_amdgcn_readlane(t.row0, at) + first, min(__builtin_amdgcn_readlane(t.rows, at) - first, 1 << SHIFT),
-                       __builtin_amdgcn_readlane(t.adapter, at)};
-        }
-        index -= total;
     }
-    return Run{0, 0, 0};
+    const int at = lo & 63;
+    const Run t = request_of(q, lo - at + lane);
+    const int row0 = __builtin_amdgcn_readlane(t.row0, at), rows = __builtin_amdgcn_readlane(t.rows, at), adapter = __builtin_amdgcn_readlane(t.adapter, at);
+    const int first = max(row0, (index - lo) << SHIFT), past = (index - lo + 1) << SHIFT, last = row0 + rows;
+    if (first >= last) return Run{0, 0, 0};                      // (a number that no block of the request has, or no rows)
+    int count;
+    if (__ballot(t.rows > 1) == 0) {
+        const bool mine = t.rows > 0 && t.adapter == adapter;
+        const u64 same = __ballot(mine);
+        const int before = __popcll(same & ((1ull << at) - 1));
+        if (before & (kSize - 1)) return Run{0, 0, 0};
+        const int rank = __popcll(same & ((1ull << lane) - 1)) - before;
+        count = min((int)__popcll(same) - before, kSize);
+        if (lane >= count && lane < kSize) where[lane] = row0;
+        if (mine && rank >= 0 && rank < kSize) where[rank] = t.row0;
+    } else {
+        const u64 on = __ballot(goes_on(t));
+        if ((on >> at & 1) && first == row0 && (row0 & (kSize - 1))) return Run{0, 0, 0};
+        const int more = __ffsll((unsigned long long)~(at < 63 ? on >> (at + 1) : 0ull)) - 1;         // requests that go on with this one's
+        const int end = min(__builtin_amdgcn_readlane(t.row0 + t.rows, at + more), past);
+        count = (last < past ? end : past) - first;
+        if (lane < kSize) where[lane] = min(first + lane, first + count - 1);
+    }
+    return Run{first, count, adapter};
 }
 
 // ---------------------------------------------------------------- rows
@@ -134,12 +163,18 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
     constexpr int kOwn = kSets * 128 > RT * NT * 64 ? kSets * 128 : RT * NT * 64;      // 16-byte pieces of a wavefront (64 columns of B: up to 128 RT)
     __shared__ __align__(16) u32x4 own[W][kOwn];
     __shared__ float hs[16 * RT][16 * NT + 1];
-    const Run t = find_tile<NT == 1 ? 4 : 5>(a.q, blockIdx.x);
+    __shared__ int where[16 * NT];
+    const Run t = find_rows<NT == 1 ? 4 : 5>(a.q, blockIdx.x, where);
     if (t.rows == 0) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, kg = lane >> 4;
     const float factor = a.factor ? a.factor[t.adapter] : 1.f;
     u32x4* mine = own[wave];
 
+    int row_of[NT][4];                                           // this lane's rows of y
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) row_of[i][k] = where[16 * i + 4 * kg + k];
     // 64 columns of the second product: what this lane has of y, and of the weights what operands are made of.  Column 4 m + j of them is
     // column m of tile j.
     struct Columns {
@@ -154,7 +189,7 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
         for (int i = 0; i < NT; ++i)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const gpair p = (gpair)((gu16)a.y + (long long)(t.row0 + min(16 * i + 4 * kg + k, t.rows - 1)) * a.y_stride + c);
+                const gpair p = (gpair)((gu16)a.y + (long long)row_of[i][k] * a.y_stride + c);
                 col.y[i][k] = ONCE ? __builtin_nontemporal_load(p) : *p;
             }
         if constexpr (BACK) {                                    // [r][d]
@@ -187,7 +222,7 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
         for (int i = 0; i < kSets; ++i)
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
-                if (i < NT) from[i][b] = (gu16)a.x + (long long)(t.row0 + min(16 * i + 8 * b + row8, t.rows - 1)) * a.x_stride + 8 * piece;
+                if (i < NT) from[i][b] = (gu16)a.x + (long long)where[16 * i + 8 * b + row8] * a.x_stride + 8 * piece;
                 else from[i][b] = (gu16)a.w_down + ((long long)t.adapter * a.r + min(16 * (i - NT) + 8 * b + row8, a.r - 1)) * a.d_down + 8 * piece;
             }
         const gu16 w = (gu16)a.w_down + (long long)t.adapter * a.r * a.d_down;
@@ -279,7 +314,7 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
             const int rank = BACK ? RT * (4 * kg + i) + j : 16 * j + 4 * kg + i;
             const float scaled = v[i] * factor;
             hs[rank][row] = scaled;
-            if (a.h && blockIdx.y == 0 && rank < a.r && row < t.rows) a.h[(long long)rank * a.q.T + t.row0 + row] = BACK ? scaled : v[i];
+            if (a.h && blockIdx.y == 0 && rank < a.r && row < t.rows) a.h[(long long)rank * a.q.T + where[row]] = BACK ? scaled : v[i];
         }
     }
     if (!a.y) return;
@@ -340,7 +375,7 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
                 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
                 const bf16x4 v = {(__bf16)(__uint_as_float(y0 << 16) + acc[0][i][k]), (__bf16)(__uint_as_float(y0 & 0xffff0000u) + acc[1][i][k]),
                                   (__bf16)(__uint_as_float(y1 << 16) + acc[2][i][k]), (__bf16)(__uint_as_float(y1 & 0xffff0000u) + acc[3][i][k])};
-                bf16x4* p = reinterpret_cast<bf16x4*>((uint16_t*)a.y + (long long)(t.row0 + row) * a.y_stride + c);
+                bf16x4* p = reinterpret_cast<bf16x4*>((uint16_t*)a.y + (long long)row_of[i][k] * a.y_stride + c);
                 if constexpr (ONCE) __builtin_nontemporal_store(v, p);
                 else *p = v;
             }
@@ -376,6 +411,14 @@ struct Steps {
                     left = 0;
                     base = q.S;                                  // (stays at the end)
                     return 0;
+                }
+                if (q.S - base > 256) {                          // many: groups of 64 without the adapter are passed over four at a time
+                    u64 there[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) there[i] = __ballot(q.adapter[base + 64 * i + (int)(threadIdx.x & 63)] == adapter);
+                    const int at = there[0] ? 0 : there[1] ? 1 : there[2] ? 2 : 3;
+                    base += 64 * at;
+                    if (!there[at]) continue;
                 }
                 mine = runs_of(q, base);
                 rest = __ballot(mine.rows > 0 && mine.adapter == adapter);
@@ -613,14 +656,14 @@ hipError_t launch_lora_rows(const LoraArgs& a, const LoraPlan& p, bool back, hip
 static int grad_columns(int r) { return r <= 16 ? 128 : 64; }
 static int grad_halves(int r) { return r <= 32 ? 1 : 2; }
 
-static long long grad_groups(int n, int r, int d0, int d1) {
+long long lora_grad_groups(int n, int r, int d0, int d1) {
     const int c = grad_columns(r);
     return (long long)n * grad_halves(r) * ((d0 + c - 1) / c + (d1 + c - 1) / c);
 }
 
 int lora_grad_parts(int n, int r, int T, int d0, int d1) {
     const int steps = (T + 31) / 32, most = (steps + 15) / 16;   // (two steps to a wavefront)
-    int parts = (int)(256 / grad_groups(n, r, d0, d1));
+    int parts = (int)(256 / lora_grad_groups(n, r, d0, d1));
     if (parts > most) parts = most;
     return parts < 1 ? 1 : parts > 16 ? 16 : parts;
 }
@@ -629,11 +672,15 @@ hipError_t launch_lora_grads(const GradArgs& a, hipStream_t stream) {
     const int c = grad_columns(a.r), groups0 = (a.job[0].d + c - 1) / c, groups1 = (a.job[1].d + c - 1) / c, halves = grad_halves(a.r);
     const long long count0 = (long long)a.q.n * a.r * a.job[0].d, count1 = (long long)a.q.n * a.r * a.job[1].d;
     const dim3 grid((unsigned)(groups0 + groups1), (unsigned)a.q.n, (unsigned)(a.parts * halves));
-    // Many workgroups with few rows each: four of two wavefronts to a compute unit.
-    const bool few = grad_groups(a.q.n, a.r, a.job[0].d, a.job[1].d) > 512 && a.q.T <= 256 * (a.q.n < a.q.S ? a.q.n : a.q.S);
-    auto go = [&](auto kernel, int threads) { kernel<<<grid, threads, 0, stream>>>(a, groups0, halves, count0 + count1); };
-    if (a.r <= 16) few ? go(lora_grads_kernel<1, 2, 2>, 128) : go(lora_grads_kernel<1, 2, 8>, 512);
-    else few ? go(lora_grads_kernel<2, 1, 2>, 128) : go(lora_grads_kernel<2, 1, 8>, 512);
+    // One workgroup of 8 wavefronts to a compute unit; where there are more than units that have rows, two of 4, or four of 2 with few rows each, so that
+    // some load while others store (9,000 rows of 2 adapters, rank 32, 8 / 4 / 2 wavefronts 44.8 / 47.7 / 49.3 us; rank 64, twice as many
+    // workgroups, 76.8 / 71.2 / 75.5; 6,400 rows of 16 adapters 62.0 / 47.0 / 45.6; 64 rows of 16 24.7 / 15.5 / 14.2).
+    const int used = a.q.n < a.q.S ? a.q.n : a.q.S;
+    const long long full = lora_grad_groups(used, a.r, a.job[0].d, a.job[1].d);
+    const int waves = full <= 256 ? 8 : a.q.T <= 32 * used ? 2 : 4;
+    auto go = [&](auto kernel) { kernel<<<grid, 64 * waves, 0, stream>>>(a, groups0, halves, count0 + count1); };
+    if (a.r <= 16) waves == 8 ? go(lora_grads_kernel<1, 2, 8>) : waves == 4 ? go(lora_grads_kernel<1, 2, 4>) : go(lora_grads_kernel<1, 2, 2>);
+    else waves == 8 ? go(lora_grads_kernel<2, 1, 8>) : waves == 4 ? go(lora_grads_kernel<2, 1, 4>) : go(lora_grads_kernel<2, 1, 2>);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.parts == 1) return e;
     lora_grads_sum_kernel<<<dim3((unsigned)(((count0 + count1) / 4 + kThreads - 1) / kThreads)), kThreads, 0, stream>>>(

@@ -47,6 +47,15 @@ def backward(ev, l=None, x=16, xs=64, h=None, dy=16, gs=32, off=16, ad=16, S=2, 
     return ev.lib.evospec_lora_backward(ctypes.byref(l or lora()), x, xs, h, dy, gs, off, ad, S, T, dx, ds, da, db, ws, wb, None)
 
 
+def test_lora_launch_limits(ev):
+    out = ctypes.c_size_t(0)
+    f = ev.lib.evospec_lora_backward_workspace_bytes
+    assert f(ctypes.byref(lora(n=65535, r=64, d_in=4096, d_out=4096)), 1, 5, ctypes.byref(out)) == 2
+    assert backward(ev, l=lora(n=65535, r=64, d_in=4096, d_out=4096)) == 2
+    assert f(ctypes.byref(lora(n=65535, r=32, d_in=4096, d_out=4160)), 1, 5, ctypes.byref(out)) == 2
+    assert f(ctypes.byref(lora(n=65535, r=32, d_in=4096, d_out=2048)), 1, 5, ctypes.byref(out)) == 0
+
+
 def test_lora_refusals(ev):
     for f in (forward, backward):
         for bad in BAD_SIZES:

@@ -261,6 +261,11 @@ def test_refusals(ev):
         ev.AdamW([w(4)], [w(4)], m=torch.zeros(4, device="cuda"))
     with pytest.raises(TypeError):
         ev.AdamW([w(4)], [w(4)], state="8bit", m=torch.zeros(256, device="cuda"))
+    both = w(512)
+    for pair in ([both, both], [both[:300], both[256:]]):
+        with pytest.raises(ValueError, match="same memory"):
+            ev.AdamW(pair, [torch.zeros_like(p) for p in pair])
+    ev.AdamW([both[:256], both[256:]], [w(256), w(256)])
     opt = ev.AdamW([w(4)], [w(4)])
     for bad in (dict(t=0), dict(eps=0.0), dict(betas=(1.0, 0.9)), dict(lr=float("nan"))):
         with pytest.raises(ev.EvospecError):

@@ -127,6 +127,31 @@ def test_many_requests_and_rows(ev):
     p.check_backward(da, db, p.tdx)
 
 
+@pytest.mark.parametrize("seed", range(6))
+def test_requests_that_follow_one_another(ev, seed):
+    """Runs of requests with one adapter, that begin and end at and between multiples of 16 and 32 rows, with empty ones among them."""
+    rng = np.random.default_rng(seed)
+    S = [40, 64, 65, 130, 200, 500][seed]
+    rows = rng.choice([0, 1, 1, 2, 3, 5, 15, 16, 17, 32, 48], size=S) if seed % 2 else rng.choice([0, 1, 1, 1, 2, 16, 32], size=S)
+    adapter = np.repeat(rng.integers(-1, 3, size=S), rng.integers(1, 20, size=S))[:S]
+    p = Problem(ev, [int(v) for v in rows], [int(v) for v in adapter], 3, [16, 40][seed // 3], 64, 72, seed=20 + seed, lead=int(rng.integers(0, 40)),
+                tail=seed)
+    h = ev.lora_forward(p.tx, p.bank, p.toff, p.tad, p.ty, keep=True)
+    p.check_forward(p.ty, h)
+    da, db = ev.lora_backward(p.tx, p.tdy, p.bank, p.toff, p.tad, h=h, dx=p.tdx)
+    p.check_backward(da, db, p.tdx)
+
+
+def test_thousands_of_requests(ev):
+    rng = np.random.default_rng(30)
+    for S, adapters in ((5000, rng.integers(-1, 5, size=5000)), (4200, np.where(np.arange(4200) % 700 == 699, 1, -1)), (4097, np.zeros(4097, int))):
+        p = Problem(ev, [int(v) for v in rng.integers(0, 4, size=S)], [int(v) for v in adapters], 5, 8, 16, 24, seed=31, lead=3)
+        h = ev.lora_forward(p.tx, p.bank, p.toff, p.tad, p.ty, keep=True)
+        p.check_forward(p.ty, h)
+        da, db = ev.lora_backward(p.tx, p.tdy, p.bank, p.toff, p.tad, h=h, dx=p.tdx)
+        p.check_backward(da, db, p.tdx)
+
+
 def test_rows_far_into_memory(ev):
     """Rows whose place passes 2^31 elements and 2^32 bytes: only the last ones belong to a request."""
     import torch
@@ -234,6 +259,10 @@ def test_refusals(ev):
         ev.lora_forward(p.tx[:5], p.bank, p.toff, p.tad, p.ty)
     with pytest.raises(ValueError):
         ev.lora_forward(p.tx.t().contiguous().t(), p.bank, p.toff, p.tad, p.ty)
+    with pytest.raises(ValueError):
+        ev.lora_forward(p.tx, p.bank, p.toff, p.tad, p.ty[:1].expand(11, 72))
+    with pytest.raises(ValueError):
+        ev.lora_forward(p.tx[:1].expand(11, 64), p.bank, p.toff, p.tad, p.ty)
     with pytest.raises(ValueError):
         ev.lora_forward(p.tx, p.bank, p.toff, p.tad, p.ty, out_h=torch.zeros(11, 16, device="cuda"))
     with pytest.raises(ev.EvospecError):                             # rows that do not begin on 16 bytes
