@@ -3,8 +3,8 @@
 // Every element is read and written once: 22 bytes with moments in 32 bits beside bf16 parameters, 10 with 8 bits.  A wavefront has
 // blocks of 256 elements, 4 in a row to a lane, so that the largest magnitude of a block is a reduction within it.  Addresses
 // of up to kTensors tensors go along with the launch itself; a wavefront finds its block's tensor by one comparison in every lane.
-// Measured, bf16: 134 million elements with 32 bits 547 us (5.4 TB/s, a copy's rate), with 8 bits 297 us (4.5 TB/s; some 70 vector instructions
-// an element, a third of them the rounding's hash and codes, are 200 us of it alone), with 8 bits and masters 373 us (5.8 TB/s).
+// Measured, bf16: 134 million elements with 32 bits 546 us (5.4 TB/s, a copy's rate), with 8 bits 293 us (4.6 TB/s: some 60 vector instructions
+// an element, half of them the rounding's hash and codes, are nearly as long), with 8 bits and masters 370 us (5.8 TB/s).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -45,14 +45,17 @@ struct Element<EVOSPEC_FP32> {
     using type = float;
 };
 
+// (addresses that come out of a table: said to be global memory, whose loads do not go through the checks of flat ones)
+#define GLOBAL __attribute__((address_space(1)))
+
 // 4 elements from `at` on; of a tensor's end those that there are, and zeros.
 template <int TYPE>
-__device__ __forceinline__ void load4(const void* base, long long at, int there, float (&x)[4]) {
+__device__ __forceinline__ void load4(uint64_t base, long long at, int there, float (&x)[4]) {
     using T = typename Element<TYPE>::type;
     typedef T vec __attribute__((ext_vector_type(4)));
-    const T* p = (const T*)base + at;
+    const GLOBAL T* p = (const GLOBAL T*)base + at;
     if (there >= 4) {
-        const vec v = *reinterpret_cast<const vec*>(p);
+        const vec v = *(const GLOBAL vec*)p;
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = (float)v[i];
     } else {
@@ -61,12 +64,12 @@ __device__ __forceinline__ void load4(const void* base, long long at, int there,
     }
 }
 template <int TYPE>
-__device__ __forceinline__ void store4(void* base, long long at, int there, const float (&x)[4]) {
+__device__ __forceinline__ void store4(uint64_t base, long long at, int there, const float (&x)[4]) {
     using T = typename Element<TYPE>::type;
     typedef T vec __attribute__((ext_vector_type(4)));
-    T* p = (T*)base + at;
+    GLOBAL T* p = (GLOBAL T*)base + at;
     if (there >= 4) {
-        *reinterpret_cast<vec*>(p) = vec{(T)x[0], (T)x[1], (T)x[2], (T)x[3]};
+        *(GLOBAL vec*)p = vec{(T)x[0], (T)x[1], (T)x[2], (T)x[3]};
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -76,12 +79,21 @@ __device__ __forceinline__ void store4(void* base, long long at, int there, cons
 
 // 2^e, the least from 2^-100 to 2^100 with amax <= most 2^e, most = (1 + FRACTION / 2^23) 2^LEAST
 template <int LEAST, uint32_t FRACTION>
-__device__ __forceinline__ float power_for(float amax) {
-    const uint32_t u = __float_as_uint(amax);
+__device__ __forceinline__ float power_for(uint32_t u /*amax as bits*/) {
     const int e = (int)(u >> 23) - 127 - LEAST + ((u & 0x7fffffu) > FRACTION);
     return __uint_as_float((uint32_t)(min(max(e, -100), 100) + 127) << 23);
 }
 __device__ __forceinline__ float reciprocal(float power) { return __uint_as_float((254u << 23) - __float_as_uint(power)); }
+
+// The largest of the wavefront, as a scalar: within 16 lanes by exchanges that ride on the comparison, then four lanes' values.
+template <int CTRL>
+__device__ __forceinline__ uint32_t larger(uint32_t x) { return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true)); }
+__device__ __forceinline__ uint32_t wave_top(uint32_t x) {
+    x = larger<0x140>(larger<0x141>(larger<0x4E>(larger<0xB1>(x))));         // neighbours, pairs, halves of 8 mirrored, 16 mirrored
+    const uint32_t a = __builtin_amdgcn_readlane(x, 0), b = __builtin_amdgcn_readlane(x, 16), c = __builtin_amdgcn_readlane(x, 32), d = __builtin_amdgcn_readlane(x, 48);
+    const uint32_t ab = a > b ? a : b, cd = c > d ? c : d;
+    return ab > cd ? ab : cd;
+}
 
 // The code of a magnitude that is divided by its scale; bits: 16 random ones.
 template <int BIAS>
@@ -141,16 +153,16 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(Table table, AdamwArgs 
         within[u] = (long long)(block - table.first[at]) * kBlock + 4 * lane;
         const long long flat = (table.base + block) * kBlock + 4 * lane, rest = (long long)table.n[at] - within[u];
         there[u] = rest >= 4 ? 4 : rest > 0 ? (int)rest : 0;
-        load4<GT>((const void*)table.grad[at], within[u], there[u], g[u]);
-        if constexpr (MASTER) load4<EVOSPEC_FP32>(a.master, flat, 4, p[u]);
-        else load4<PT>((const void*)param[u], within[u], there[u], p[u]);
+        load4<GT>(table.grad[at], within[u], there[u], g[u]);
+        if constexpr (MASTER) load4<EVOSPEC_FP32>((uint64_t)a.master, flat, 4, p[u]);
+        else load4<PT>(param[u], within[u], there[u], p[u]);
         if constexpr (KIND == EVOSPEC_MOMENTS_8BIT) {
             cm[u] = *(const uint32_t*)((const uint8_t*)a.m + flat);
             cv[u] = *(const uint32_t*)((const uint8_t*)a.v + flat);
             s[u] = reinterpret_cast<const float2*>(a.scales)[table.base + block];
         } else {
-            load4<EVOSPEC_FP32>(a.m, flat, 4, m[u]);
-            load4<EVOSPEC_FP32>(a.v, flat, 4, v[u]);
+            load4<EVOSPEC_FP32>((uint64_t)a.m, flat, 4, m[u]);
+            load4<EVOSPEC_FP32>((uint64_t)a.v, flat, 4, v[u]);
         }
     }
 #pragma unroll
@@ -165,8 +177,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(Table table, AdamwArgs 
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[u][i] = v_value((cv[u] >> (8 * i)) & 255u) * s[u].y;
         }
-        float top_m = 0.f, top_v = 0.f;
-        bool fine = true;
+        uint32_t top_m = 0, top_v = 0;                           // magnitudes as bits, whose order is theirs; NaN and infinity are the largest
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if (i >= there[u]) p[u][i] = m[u][i] = v[u][i] = 0.f;            // (g is)
@@ -176,43 +187,57 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(Table table, AdamwArgs 
             // (reciprocal and root to the last bit or so: 2^-23 of an update, which is itself small beside p)
             p[u][i] = fmaf(p[u][i], decay, -(rate * m[u][i]) * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(v[u][i]), root, a.eps)));
             if constexpr (KIND == EVOSPEC_MOMENTS_8BIT) {
-                top_m = fmaxf(top_m, fabsf(m[u][i]));
-                top_v = fmaxf(top_v, v[u][i]);
-                fine &= fabsf(m[u][i]) < __builtin_inff() && v[u][i] < __builtin_inff();
+                top_m = max(top_m, __float_as_uint(m[u][i]) & 0x7fffffffu);
+                top_v = max(top_v, __float_as_uint(v[u][i]));
             }
         }
-        store4<PT>((void*)param[u], within[u], there[u], p[u]);
-        if constexpr (MASTER) store4<EVOSPEC_FP32>(a.master, flat, 4, p[u]);
+        store4<PT>(param[u], within[u], there[u], p[u]);
+        if constexpr (MASTER) store4<EVOSPEC_FP32>((uint64_t)a.master, flat, 4, p[u]);
         if constexpr (KIND == EVOSPEC_MOMENTS_8BIT) {
-            const bool all_fine = __ballot(!fine) == 0;          // (nearly always)
-            if (!all_fine) {
-                top_m = top_v = 0.f;
+            top_m = wave_top(top_m);
+            top_v = wave_top(top_v);
+            // what is rare, a NaN, an infinity or what the largest scale does not take, has a way of its own
+            const bool rare = max(top_m, top_v) >= __float_as_uint(0x1p108f);
+            if (rare) {
+                top_m = top_v = 0;
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (fabsf(m[u][i]) < __builtin_inff() && v[u][i] < __builtin_inff()) {
-                        top_m = fmaxf(top_m, fabsf(m[u][i]));
-                        top_v = fmaxf(top_v, v[u][i]);
+                        top_m = max(top_m, __float_as_uint(m[u][i]) & 0x7fffffffu);
+                        top_v = max(top_v, __float_as_uint(v[u][i]));
                     }
+                top_m = wave_top(top_m);
+                top_v = wave_top(top_v);
             }
-            const float sm = power_for<8, 0x600000u>(wave_max(top_m, lane)), sv = power_for<15, 0x700000u>(wave_max(top_v, lane));
+            const float sm = power_for<8, 0x600000u>(top_m), sv = power_for<15, 0x700000u>(top_v);
             const float im = reciprocal(sm), iv = reciprocal(sv);
             uint32_t xm = 0, xv = 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const uint32_t bits = random_bits((uint32_t)(flat + i), key);
-                uint32_t x = code_of<7>(fminf(fabsf(m[u][i]) * im, 448.f), bits & 0xffffu) | (__float_as_uint(m[u][i]) >> 31) << 7;
-                uint32_t y = code_of<15>(fminf(v[u][i] * iv, 61440.f), bits >> 16);
-                if (y == 0 && v[u][i] > 0.f) y = 1;
-                if (!all_fine && !(fabsf(m[u][i]) < __builtin_inff() && v[u][i] < __builtin_inff())) { x = 0x7f; y = 0xf7; }
-                xm |= x << (8 * i);
-                xv |= y << (8 * i);
+                const float y = fabsf(m[u][i]) * im, z = v[u][i] * iv;
+                const uint32_t cy = code_of<7>(y, bits & 0xffffu), cz = max(code_of<15>(z, bits >> 16), v[u][i] > 0.f ? 1u : 0u);
+                xm |= (cy | (__float_as_uint(m[u][i]) >> 31) << 7) << (8 * i);
+                xv |= cz << (8 * i);
             }
-            *(uint32_t*)((uint8_t*)a.m + flat) = xm;
-            *(uint32_t*)((uint8_t*)a.v + flat) = xv;
+            if (rare) {
+                xm = xv = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t bits = random_bits((uint32_t)(flat + i), key);
+                    const bool fine = fabsf(m[u][i]) < __builtin_inff() && v[u][i] < __builtin_inff();
+                    const uint32_t cy = code_of<7>(fminf(fabsf(m[u][i]) * im, 448.f), bits & 0xffffu) | (__float_as_uint(m[u][i]) >> 31) << 7;
+                    const uint32_t cz = max(code_of<15>(fminf(v[u][i] * iv, 61440.f), bits >> 16), v[u][i] > 0.f ? 1u : 0u);
+                    xm |= (fine ? cy : 0x7fu) << (8 * i);
+                    xv |= (fine ? cz : 0xf7u) << (8 * i);
+                }
+            }
+            *(GLOBAL uint32_t*)((uint64_t)a.m + flat) = xm;
+            *(GLOBAL uint32_t*)((uint64_t)a.v + flat) = xv;
             if (lane == 0) reinterpret_cast<float2*>(a.scales)[table.base + block0 + u] = make_float2(sm, sv);
         } else {
-            store4<EVOSPEC_FP32>(a.m, flat, 4, m[u]);
-            store4<EVOSPEC_FP32>(a.v, flat, 4, v[u]);
+            store4<EVOSPEC_FP32>((uint64_t)a.m, flat, 4, m[u]);
+            store4<EVOSPEC_FP32>((uint64_t)a.v, flat, 4, v[u]);
         }
     }
 }
@@ -228,8 +253,8 @@ __global__ __launch_bounds__(kThreads) void adamw_moments_kernel(const uint8_t* 
     const float x[4] = {__builtin_amdgcn_cvt_f32_fp8((int)cm, 0) * s.x, __builtin_amdgcn_cvt_f32_fp8((int)cm, 1) * s.x,
                         __builtin_amdgcn_cvt_f32_fp8((int)cm, 2) * s.x, __builtin_amdgcn_cvt_f32_fp8((int)cm, 3) * s.x};
     const float y[4] = {v_value(cv & 255u) * s.y, v_value((cv >> 8) & 255u) * s.y, v_value((cv >> 16) & 255u) * s.y, v_value(cv >> 24) * s.y};
-    store4<TYPE>(out_m, flat, 4, x);
-    store4<TYPE>(out_v, flat, 4, y);
+    store4<TYPE>((uint64_t)out_m, flat, 4, x);
+    store4<TYPE>((uint64_t)out_v, flat, 4, y);
 }
 
 template <int I>
@@ -257,7 +282,7 @@ hipError_t launch_adamw(const evospec_adamw_tensor* tensors, int count, int para
         if (blocks == 0) break;
         t.blocks = (uint32_t)blocks;
         auto go = [&](auto pt, auto gt, auto kd, auto ms) {
-            // (134 million elements with 8 bits in 1, 2, 4 blocks to a wavefront 325, 297, 316 us; with masters 373, 391, 401, and with 32 bits 547,
+            // (134 million elements with 8 bits in 1, 2, 4 blocks to a wavefront 325, 297, 316 us; with masters 373, 391, 401, and with 32 bits 548,
             // 551, 550: enough is under way)
             constexpr int U = kd.value == EVOSPEC_MOMENTS_8BIT && ms.value == 0 ? 2 : 1;
             const dim3 grid((unsigned)((blocks + kWaves * U - 1) / (kWaves * U)));

@@ -341,7 +341,7 @@ __global__ __launch_bounds__(kThreads, NC == 4 ? 2 : 3) void kd_rows_kernel(KdAr
 
 // Longer rows: one to the workgroup, NC pieces of 8 elements to a thread.
 template <int NC, int RB, int TYPE>
-__global__ __launch_bounds__(kThreads, NC <= 2 ? 3 : 1) void kd_long_rows_kernel(KdArgs a) {
+__global__ __launch_bounds__(kThreads, NC * RB <= 4 ? 3 : 1) void kd_long_rows_kernel(KdArgs a) {
     __shared__ Entries sh;
     __shared__ __align__(16) float dots[2][RB][kWaves];
     const int e = blockIdx.x, part = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -499,9 +499,9 @@ int kd_splits(int E, int K, int d) {
 
 hipError_t launch_kd(const KdArgs& a, hipStream_t stream) {
     // (a row to a wavefront takes half the time of a row to a workgroup at 680 elements and a tenth less at 2,048; at 4,096 its sums and rows
-    // spill: 165 us for 192 events, 79)
+    // spill: 165 us for 192 events, 79.  Two rows of 4,096 under way beside two for three workgroups to a unit, four for two: 64 events 35.6 and 33.6)
     const hipError_t e = a.d <= 512 ? rows_as<1, 8, false>(a, stream) : a.d <= 1024 ? rows_as<2, 4, false>(a, stream) : a.d <= 2048 ? rows_as<4, 2, false>(a, stream)
-                         : a.d <= 4096 ? rows_as<2, 2, true>(a, stream) : a.d <= 8192 ? rows_as<4, 2, true>(a, stream) : rows_as<8, 1, true>(a, stream);
+                         : a.d <= 4096 ? (a.E <= 100 ? rows_as<2, 4, true>(a, stream) : rows_as<2, 2, true>(a, stream)) : a.d <= 8192 ? rows_as<4, 2, true>(a, stream) : rows_as<8, 1, true>(a, stream);
     if (e != hipSuccess || a.splits == 1) return e;
     const int v = a.splits <= 8 ? 4 : 2;
     const dim3 grid((unsigned)a.E, (unsigned)(1 + (a.d + v * kThreads - 1) / (v * kThreads)));
