@@ -196,13 +196,11 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
 #pragma unroll
             for (int s = 0; s < KS; ++s)
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    col.raw[s][k] = 32 * s + 8 * kg < a.r ? *(gpair)(w_up + (long long)(32 * s + 8 * kg + k) * a.d_up + c) : u32x2{0, 0};
+                for (int k = 0; k < 8; ++k) col.raw[s][k] = *(gpair)(w_up + (long long)((32 * s + 8 * kg < a.r ? 32 * s + 8 * kg : 0) + k) * a.d_up + c);
         } else {                                                 // [d][r]: r / 8 KB
             const int pieces = min(64, a.d_up - 64 * g) * a.r / 8;
 #pragma unroll
-            for (int k = 0; k < 2 * RT; ++k)
-                if (64 * k < 8 * a.r) col.w[k] = *(gvec_ptr)(w_up + (long long)(64 * g) * a.r + 8 * min(64 * k + lane, pieces - 1));
+            for (int k = 0; k < 2 * RT; ++k) col.w[k] = *(gvec_ptr)(w_up + (long long)(64 * g) * a.r + 8 * min(64 * k + lane, pieces - 1));
         }
     };
     // Groups of a slice go round the wavefronts; every tile begins at another one (as in the first product).
@@ -214,7 +212,7 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
     {
         // Chunks of 64 along the summed axis go round the wavefronts, U at a time; every tile begins at another one, or all workgroups would
         // ask the same channels of memory at the same time (rows are often a multiple of 4 KB apart).
-        constexpr int U = !DEEP || (RT == 4 && (!BACK || NT > 1)) ? 1 : RT == 4 ? 2 : 4;
+        constexpr int U = !DEEP || RT == 4 ? 1 : BACK || RT == 2 ? 3 : 4;
         const int chunks = (a.d_down + 63) / 64, turn = (int)(blockIdx.x * 5u % (unsigned)chunks);
         const int row8 = lane >> 3, piece = lane & 7;
         gu16 from[kSets][2];
@@ -231,25 +229,27 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
             u32x4 rows[kSets][2];
             uint32_t raw[BACK ? 2 : 1][8][(RT + 1) / 2];
         };
+        // Behind the end, and in the lanes of the last chunk that have nothing, loads go to places that are there and zeros are put in
+        // later: a load under a condition leaves the compiler without a count of those on their way, and it waits for all.
+        auto chunk_of = [&](int n) { return n < chunks ? n + turn < chunks ? n + turn : n + turn - chunks : chunks; };
         auto load = [&](Chunk& c, int n) {
-            const int at = n < chunks ? n + turn < chunks ? n + turn : n + turn - chunks : chunks;          // (zeros behind the end)
-            const bool in = 64 * at + 8 * piece < a.d_down;
+            const int at = chunk_of(n), k0 = 64 * at + 8 * piece < a.d_down ? 64 * at : 0;
 #pragma unroll
             for (int i = 0; i < kSets; ++i)
 #pragma unroll
-                for (int b = 0; b < 2; ++b) c.rows[i][b] = in ? *(gvec_ptr)(from[i][b] + 64 * at) : u32x4{0, 0, 0, 0};
+                for (int b = 0; b < 2; ++b) c.rows[i][b] = *(gvec_ptr)(from[i][b] + k0);
             if constexpr (BACK) {
                 const int rank = RT * m < a.r ? RT * m : 0;
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
-                    const int k = 64 * at + 32 * s + 8 * kg;
+                    const int k = 64 * at + 32 * s + 8 * kg < a.d_down ? 64 * at + 32 * s + 8 * kg : 0;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const gu16 p = w + (long long)(k + i) * a.r + rank;
-                        if constexpr (RT == 1) c.raw[s][i][0] = k < a.d_down ? *p : 0u;
-                        else if constexpr (RT == 2) c.raw[s][i][0] = k < a.d_down ? *(gword)p : 0u;
+                        if constexpr (RT == 1) c.raw[s][i][0] = *p;
+                        else if constexpr (RT == 2) c.raw[s][i][0] = *(gword)p;
                         else {
-                            const u32x2 v = k < a.d_down ? *(gpair)p : u32x2{0, 0};
+                            const u32x2 v = *(gpair)p;
                             c.raw[s][i][0] = v[0];
                             c.raw[s][i][1] = v[1];
                         }
@@ -257,7 +257,23 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
                 }
             }
         };
-        auto add = [&](const Chunk& c) {
+        auto add = [&](Chunk& c, int n) {
+            const int at = chunk_of(n);
+            if (64 * at + 64 > a.d_down) {
+                if (at == chunks) return;
+#pragma unroll
+                for (int i = 0; i < kSets; ++i)
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) c.rows[i][b] = 64 * at + 8 * piece < a.d_down ? c.rows[i][b] : u32x4{0, 0, 0, 0};
+                if constexpr (BACK) {
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+#pragma unroll
+                            for (int e = 0; e < (RT + 1) / 2; ++e) c.raw[s][i][e] = 64 * at + 32 * s + 8 * kg < a.d_down ? c.raw[s][i][e] : 0u;
+                }
+            }
 #pragma unroll
             for (int i = 0; i < kSets; ++i)
 #pragma unroll
@@ -290,12 +306,12 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
 #pragma unroll
             for (int u = 0; u < U; ++u) load(odd[u], n + W * (U + u));
 #pragma unroll
-            for (int u = 0; u < U; ++u) add(even[u]);
+            for (int u = 0; u < U; ++u) add(even[u], n + W * u);
             if (n + W * U >= chunks) break;
 #pragma unroll
             for (int u = 0; u < U; ++u) load(even[u], n + W * (2 * U + u));
 #pragma unroll
-            for (int u = 0; u < U; ++u) add(odd[u]);
+            for (int u = 0; u < U; ++u) add(odd[u], n + W * (U + u));
         }
 #pragma unroll
         for (int j = 0; j < RT; ++j)
@@ -332,7 +348,7 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
         }
     // B's 16-byte pieces in LDS: number p, of column p / (r / 8), with its low 4 bits turned by what the columns of a read differ in
     const int turned = a.r > 32 ? 5 : 4, per = a.r / 8;
-    auto add = [&](const Columns& col, int g) {
+    auto add = [&](Columns& col, int g) {
         if constexpr (!BACK) {
 #pragma unroll
             for (int k = 0; k < 2 * RT; ++k)
@@ -346,6 +362,11 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
         for (int s = 0; s < KS; ++s) {
             u32x4 op[4];
             if constexpr (BACK) {
+                if (a.r < 32 * s + 32) {
+                    const bool in = 32 * s + 8 * kg < a.r;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) col.raw[s][k] = in ? col.raw[s][k] : u32x2{0, 0};
+                }
                 columns_of(col.raw[s], op);
             } else {
                 const bool in = 32 * s + 8 * kg < a.r;
@@ -380,14 +401,22 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
                 else *p = v;
             }
     };
-    // (two sets of registers in turn; the first is on its way since before h was there)
+    // (two sets of registers in turn; the first is on its way since before h was there.  A load under a condition would leave the compiler without
+    // a count of those on their way, and it would wait for all: 55.3 -> 51.1 us for 8,400 rows of rank 16.)
     Columns next;
-    for (int n = wave; n < count; n += 2 * W) {
-        if (n + W < count) load_columns(next, group_of(n + W));
+    int n = wave;
+    for (; n + 2 * W < count; n += 2 * W) {
+        load_columns(next, group_of(n + W));
         add(first, group_of(n));
-        if (n + W >= count) break;
-        if (n + 2 * W < count) load_columns(first, group_of(n + 2 * W));
+        load_columns(first, group_of(n + 2 * W));
         add(next, group_of(n + W));
+    }
+    if (n + W < count) {
+        load_columns(next, group_of(n + W));
+        add(first, group_of(n));
+        add(next, group_of(n + W));
+    } else if (n < count) {
+        add(first, group_of(n));
     }
 }
 
@@ -471,16 +500,21 @@ __global__ __launch_bounds__(64 * W, 2) void lora_grads_kernel(GradArgs a, int g
                 for (int i = 0; i < 8; ++i) b.raw[g][i] = *(gpair)((gbyte)((gu16)job.x + (long long)(row0 + i) * job.x_stride) + (down + x[g]));
 #pragma unroll
             for (int j = 0; j < 2 * RT; ++j) b.h[j] = *(gfloat4)((gbyte)(job.h + row0) + hp[j]);
-        } else if (rows > 0) {
+        } else {                                                 // a run's end; 0 rows: loads for nothing (see lora_rows_kernel) from where the last were
+            const int last = max(rows - 1, 0);
 #pragma unroll
             for (int g = 0; g < CG; ++g)
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    b.raw[g][i] = *(gpair)((gbyte)((gu16)job.x + (long long)row0 * job.x_stride) + ((uint32_t)min(8 * kg + i, rows - 1) * (uint32_t)job.x_stride * 2u + x[g]));
+                    b.raw[g][i] = *(gpair)((gbyte)((gu16)job.x + (long long)row0 * job.x_stride) + ((uint32_t)min(8 * kg + i, last) * (uint32_t)job.x_stride * 2u + x[g]));
 #pragma unroll
             for (int j = 0; j < 2 * RT; ++j)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) b.h[j][i] = *(gfloat)((gbyte)(job.h + row0) + (hp[j] + 4u * min(4 * piece + i, rows - 1) - 16u * piece));
+                for (int i = 0; i < 4; ++i) b.h[j][i] = *(gfloat)((gbyte)(job.h + row0) + (hp[j] + 4u * min(4 * piece + i, last) - 16u * piece));
+        }
+    };
+    auto add = [&](Rows& b, int rows) {
+        if (rows < 32) {
 #pragma unroll
             for (int g = 0; g < CG; ++g)
 #pragma unroll
@@ -490,8 +524,6 @@ __global__ __launch_bounds__(64 * W, 2) void lora_grads_kernel(GradArgs a, int g
 #pragma unroll
                 for (int i = 0; i < 4; ++i) b.h[j][i] = 4 * piece + i < rows ? b.h[j][i] : 0.f;
         }
-    };
-    auto add = [&](const Rows& b) {
 #pragma unroll
         for (int j = 0; j < 2 * RT; ++j) mine[64 * j + 8 * rank8 + slot] = b.h[j];
         // (x's operands of one group at a time, h's of one rank tile or of all: what fewer registers hold)
@@ -540,13 +572,13 @@ __global__ __launch_bounds__(64 * W, 2) void lora_grads_kernel(GradArgs a, int g
     if (wave > 0) rows = steps.skip(wave - 1, row0);
     load(even, row0, rows);
     while (rows) {
-        rows = steps.skip(stride - 1, row0);
-        load(odd, row0, rows);
-        add(even);
-        if (!rows) break;
+        const int then = steps.skip(stride - 1, row0);
+        load(odd, row0, then);
+        add(even, rows);
+        if (!then) break;
         rows = steps.skip(stride - 1, row0);
         load(even, row0, rows);
-        add(odd);
+        add(odd, then);
     }
     // The upper half of the wavefronts first, whose sums the lower half takes along.
     __syncthreads();
@@ -633,14 +665,18 @@ hipError_t rows_of(const LoraArgs& a, const LoraPlan& p, hipStream_t stream) {
 // Measured at d = 4,096, rank 32: 64 rows in 1, 4, 8 slices 17.6, 11.3, 10.2 us; 1,024 rows in 1, 2, 4, 8 22.4, 17.5, 15.3, 23.9; 2,048 in
 // 1, 2, 4 23.0, 19.1, 28.6; with smaller workgroups at best 12.4, 19.8, 25.2.  4,096 rows (a tile to a compute unit) 25.4, and 28.7 with smaller
 // workgroups, which win from there on.
+// As many tiles as T rows and half a tile for every request have: with more than units, the last ones begin when the others end (2,000 rows of 23
+// requests, rank 64, 7,392 -> 3,760: 61.8 us in 4 slices, 34.2 in 3).
+// Rank 56 and 64 in tiles of 32 rows, 6,100 rows and more (6,554, 6,208 columns: 57.4 us, 65.3 in tiles of 16; ranks 40 and 48 have a rank tile for
+// nothing: 72.7 and 64.0), in smaller workgroups from 128 tiles on (63.2 -> 57.4).
 // y past the caches where x and y are 128 MB or more: 8,400 rows of rank 16, other rows between, 67 -> 57 us; 4,096 rows, which are
 // found in the caches, 34.6 -> 43.5.
 LoraPlan lora_plan(int S, int T, int r, int d_down, int d_up) {
     LoraPlan p{};
-    p.wide = r > 32 && T > 16 * S;
-    const int size = p.wide ? 32 : 16, full = (T + size - 1) / size, whole = full > S ? full : S;    // about as many have rows
+    p.wide = r > 48 && T > 16 * S;
+    const int size = p.wide ? 32 : 16, full = (T + size - 1) / size, whole = full + S / 2 > S ? full + S / 2 : S;      // about as many have rows
     p.tiles = full + S;
-    p.deep = whole <= 256;
+    p.deep = whole <= (p.wide ? 128 : 256);
     const int most = (d_up + 511) / 512;                         // slices that leave a wavefront 64 columns
     p.slices = 256 / whole < 1 ? 1 : 256 / whole < most ? 256 / whole : most;
     p.once = !p.deep && (size_t)T * ((size_t)d_down + d_up) * 2 >= (size_t)128 << 20;
@@ -651,8 +687,7 @@ hipError_t launch_lora_rows(const LoraArgs& a, const LoraPlan& p, bool back, hip
     return back ? rows_of<true>(a, p, stream) : rows_of<false>(a, p, stream);
 }
 
-// Columns of a workgroup of the gradients, and halves of the ranks: what 256 registers hold without spilling.  (Rank 64 in one, four wavefronts of
-// 400 registers: VX us against VY.)
+// Columns of a workgroup of the gradients, and halves of the ranks: what 256 registers hold without spilling.
 static int grad_columns(int r) { return r <= 16 ? 128 : 64; }
 static int grad_halves(int r) { return r <= 32 ? 1 : 2; }
 
