@@ -12,6 +12,8 @@
 // three (all 24 bits) where the result is fp32.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "adapt.hpp"
 #include "common.hpp"
 
@@ -465,6 +467,29 @@ struct Steps {
     }
 };
 
+// How many of `parts` an adapter's rows are split into: its share of the call's rows, so that workgroups are as many wherever the rows are.
+// (All threads of a workgroup; every workgroup finds the same.)
+__device__ int parts_of(const Requests& q, int adapter, int parts) {
+    __shared__ unsigned found[kThreads / 64 * 2];
+    if (parts == 1) return 1;
+    const unsigned all = (unsigned)q.T;
+    unsigned rows = 0;                                           // (up to T, if offsets are not in order)
+    const int step = q.S <= 64 ? 64 : blockDim.x;                // (few: every wavefront by itself)
+    for (int s = threadIdx.x & (step - 1); s < q.S; s += step) {
+        const Run t = request_of(q, s);
+        rows = min(rows + (t.adapter == adapter ? (unsigned)t.rows : 0u), all);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) rows = min(rows + __shfl_xor(rows, o), all);
+    if (q.S > 64) {
+        if ((threadIdx.x & 63) == 0) found[threadIdx.x >> 6] = rows;
+        __syncthreads();
+        rows = 0;
+        for (unsigned w = 0; w < blockDim.x / 64; ++w) rows = min(rows + found[w], all);
+    }
+    return max(1, (int)((rows * (unsigned)parts + all / 2) / all));
+}
+
 // RT tiles of 16 ranks (rank 33 and more in two halves); a workgroup has 64 CG columns of one adapter, its wavefronts and `parts` workgroups every so many-th step.  A step of
 // 64 CG columns and 32 rows is 4 CG KB of x and, from L2, 2 RT KB of h, which becomes an operand in three parts.
 template <int RT, int CG, int W>
@@ -552,10 +577,12 @@ __global__ __launch_bounds__(64 * W, 2) void lora_grads_kernel(GradArgs a, int g
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    float* out = a.parts > 1 ? a.partial + part * partial_stride + (second ? (long long)a.q.n * a.r * a.job[0].d : 0ll) : job.out;
+    const int parts = parts_of(a.q, adapter, a.parts);
+    if (part >= parts) return;
+    float* out = parts > 1 ? a.partial + part * partial_stride + (second ? (long long)a.q.n * a.r * a.job[0].d : 0ll) : job.out;
     out += (long long)adapter * a.r * job.d;
     Steps steps(a.q, adapter);
-    const int stride = W * a.parts;
+    const int stride = W * parts;
     Rows even, odd;
     int row0 = 0, rows = steps.skip(part * W, row0);
     if (rows == 0) {                                             // (the same in all wavefronts) nothing to add: an adapter without rows, often
@@ -632,17 +659,18 @@ __global__ __launch_bounds__(64 * W, 2) void lora_grads_kernel(GradArgs a, int g
     }
 }
 
-__global__ __launch_bounds__(kThreads) void lora_grads_sum_kernel(const float4* partial, int parts, long long count0, long long count1,
-                                                                  float4* out0, float4* out1) {
-    const long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
-    if (i >= count0 + count1) return;
-    float4 s = partial[i];
-    for (int p = 1; p < parts; ++p) {
-        const float4 v = partial[p * (count0 + count1) + i];
-        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+__global__ __launch_bounds__(kThreads) void lora_grads_sum_kernel(GradArgs a, long long partial_stride) {
+    const int parts = parts_of(a.q, blockIdx.y, a.parts);
+    if (parts == 1) return;
+    const long long of0 = (long long)a.r * a.job[0].d / 4, of1 = (long long)a.r * a.job[1].d / 4;
+    for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < of0 + of1; i += (long long)gridDim.x * kThreads) {
+        const bool second = i >= of0;
+        const long long at = second ? blockIdx.y * of1 + i - of0 : blockIdx.y * of0 + i;         // (in its output, and, behind the first output's, in a part)
+        const f32x4* partial = reinterpret_cast<const f32x4*>(a.partial) + (second ? a.q.n * of0 : 0ll) + at;
+        f32x4 s = *partial;
+        for (int p = 1; p < parts; ++p) s += partial[p * (partial_stride / 4)];
+        reinterpret_cast<f32x4*>(a.job[second].out)[at] = s;
     }
-    if (i < count0) out0[i] = s;
-    else out1[i - count0] = s;
 }
 
 template <int RT, int NT, bool BACK>
@@ -696,11 +724,15 @@ long long lora_grad_groups(int n, int r, int d0, int d1) {
     return (long long)n * grad_halves(r) * ((d0 + c - 1) / c + (d1 + c - 1) / c);
 }
 
+// Parts that fill the card if all rows are of one adapter, where the most that an adapter has (parts_of shares them out) are four steps to a wavefront (two, if there is one adapter)
+// and, as the sum is a launch more that the rows may not need, one adapter alone would have a third of the card: 8 adapters' columns, all rows
+// of one of them, 7,000 rows of rank 8 39.1 -> 24.5 us, 5,900 of rank 16 55.9 -> 42.5; rows of all alike 33 -> 34, 12 adapters 19.1 -> 21.3 (with two
+// parts, rank 32, 42.9 -> 45.1).  A workspace of 128 MB at most.
 int lora_grad_parts(int n, int r, int T, int d0, int d1) {
-    const int steps = (T + 31) / 32, most = (steps + 15) / 16;   // (two steps to a wavefront)
-    int parts = (int)(256 / lora_grad_groups(n, r, d0, d1));
-    if (parts > most) parts = most;
-    return parts < 1 ? 1 : parts > 16 ? 16 : parts;
+    const int each = n > 1 ? 32 : 16;
+    const long long most = ((T + 31) / 32 + each - 1) / each, fit = (128 << 20) / ((long long)n * r * (d0 + d1) * 4);
+    const long long parts = std::min(std::min(256 / lora_grad_groups(1, r, d0, d1), 16ll), std::min(most, fit));
+    return parts < (n > 1 ? 3 : 2) ? 1 : (int)parts;
 }
 
 hipError_t launch_lora_grads(const GradArgs& a, hipStream_t stream) {
@@ -718,8 +750,8 @@ hipError_t launch_lora_grads(const GradArgs& a, hipStream_t stream) {
     else waves == 8 ? go(lora_grads_kernel<2, 1, 8>) : waves == 4 ? go(lora_grads_kernel<2, 1, 4>) : go(lora_grads_kernel<2, 1, 2>);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.parts == 1) return e;
-    lora_grads_sum_kernel<<<dim3((unsigned)(((count0 + count1) / 4 + kThreads - 1) / kThreads)), kThreads, 0, stream>>>(
-        reinterpret_cast<const float4*>(a.partial), a.parts, count0 / 4, count1 / 4, reinterpret_cast<float4*>(a.job[0].out), reinterpret_cast<float4*>(a.job[1].out));
+    const unsigned blocks = (unsigned)(((count0 + count1) / a.q.n / 4 + kThreads - 1) / kThreads);
+    lora_grads_sum_kernel<<<dim3(std::min(blocks, 256u), (unsigned)a.q.n), kThreads, 0, stream>>>(a, count0 + count1);
     return hipGetLastError();
 }
 
