@@ -37,6 +37,7 @@ struct LoraArgs {                             // h = x w_down^T (times factor, b
     long long y_stride;
     float* h;                                 // [r][T] or NULL
     int r;
+    int slices = 1;                           // of y's columns (set by the launch)
 };
 // back: w_down is [n][d][r] and w_up [n][r][d], else the other way round
 hipError_t launch_lora_rows(const LoraArgs& a, const LoraPlan& p, bool back, hipStream_t stream);
