@@ -183,10 +183,10 @@ typedef const f32x4_u __attribute__((address_space(1))) * gfloat4;
 // a compute unit's time for 256 KB.  So rows (x, and A forward) are loaded 128 bytes of a row to 8 lanes and change lanes in LDS (a
 // wavefront's own, no barriers; piece c of row m in place c ^ (m mod 8), without bank conflicts), B forward in the order of memory.  Of y a
 // lane has 4 columns in 4 rows, the columns of a row in 16 lanes.
-// DEEP, where tiles and slices leave a compute unit one workgroup at most: 8 wavefronts with 2 KB x 12 on their way each.  Else four
-// workgroups of 4 to a unit, so that some load while others store.  ONCE: y past the caches.
+// DEEP, where tiles and slices leave a compute unit one workgroup at most: 8 wavefronts.  Else four workgroups of 4 to a unit (two of rank 40 and
+// more), so that some load while others store.  ONCE: y past the caches.
 template <int RT, int NT, bool BACK, bool DEEP, bool ONCE>
-__global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lora_rows_kernel(LoraArgs a) {
+__global__ __launch_bounds__(DEEP ? 512 : 256, RT == 4 ? 2 : 4) void lora_rows_kernel(LoraArgs a) {
     constexpr int W = DEEP ? 8 : 4;
     constexpr int KS = (RT + 1) / 2;
     constexpr int kSets = BACK ? NT : NT + RT;                   // of 16 rows through LDS: x's, then A's
@@ -239,11 +239,12 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
     const int count = a.y ? (int)((long long)groups * (slice + 1) / a.slices) - g0 : 0, shift = count ? (int)(tile * 5u % (unsigned)count) : 0;
     auto group_of = [&](int n) { return g0 + (n + shift < count ? n + shift : n + shift - count); };
     Columns first;
-    if (DEEP && wave < count) load_columns(first, group_of(wave));
+    if (DEEP && RT < 4 && wave < count) load_columns(first, group_of(wave));
     {
-        // Chunks of 64 along the summed axis go round the wavefronts, U at a time; every tile begins at another one, or all workgroups would
-        // ask the same channels of memory at the same time (rows are often a multiple of 4 KB apart).
-        constexpr int U = !DEEP || RT == 4 ? 1 : BACK || RT == 2 ? 3 : 4;
+        // Chunks of 64 along the summed axis go round the wavefronts; every tile begins at another one, or all workgroups would ask the same
+        // channels of memory at the same time (rows are often a multiple of 4 KB apart).  One chunk at a time: the next one's loads ahead, or three
+        // and four chunks in registers, cost more in instructions, which every launch has to bring in, than they hide (1, 2, 3 chunks ahead at one row
+        // of 4,096, rank 32: 8.3, 9.1, 9.8 us, none ahead 8.1; 9,000 rows 57.5, none ahead 55.5).
         const int chunks = (a.d_down + 63) / 64, turn = (int)(tile * 5u % (unsigned)chunks);
         const int row8 = lane >> 3, piece = lane & 7;
         gu16 from[kSets][2];
@@ -256,19 +257,14 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
             }
         const gu16 w = (gu16)a.w_down + (long long)t.adapter * a.r * a.d_down;
         f32x4 acc[RT][NT] = {};
-        struct Chunk {
+        for (int n = wave; n < chunks; n += W) {
+            const int at = n + turn < chunks ? n + turn : n + turn - chunks, here = 64 * at + 8 * piece < a.d_down ? 64 * at : 0;
             u32x4 rows[kSets][2];
             uint32_t raw[BACK ? 2 : 1][8][(RT + 1) / 2];
-        };
-        // Behind the end, and in the lanes of the last chunk that have nothing, loads go to places that are there and zeros are put in
-        // later: a load under a condition leaves the compiler without a count of those on their way, and it waits for all.
-        auto chunk_of = [&](int n) { return n < chunks ? n + turn < chunks ? n + turn : n + turn - chunks : chunks; };
-        auto load = [&](Chunk& c, int n) {
-            const int at = chunk_of(n), k0 = 64 * at + 8 * piece < a.d_down ? 64 * at : 0;
 #pragma unroll
             for (int i = 0; i < kSets; ++i)
 #pragma unroll
-                for (int b = 0; b < 2; ++b) c.rows[i][b] = *(gvec_ptr)(from[i][b] + k0);
+                for (int b = 0; b < 2; ++b) rows[i][b] = *(gvec_ptr)(from[i][b] + here);
             if constexpr (BACK) {
                 const int rank = RT * m < a.r ? RT * m : 0;
 #pragma unroll
@@ -277,38 +273,34 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const gu16 p = w + (long long)(k + i) * a.r + rank;
-                        if constexpr (RT == 1) c.raw[s][i][0] = *p;
-                        else if constexpr (RT == 2) c.raw[s][i][0] = *(gword)p;
+                        if constexpr (RT == 1) raw[s][i][0] = *p;
+                        else if constexpr (RT == 2) raw[s][i][0] = *(gword)p;
                         else {
                             const u32x2 v = *(gpair)p;
-                            c.raw[s][i][0] = v[0];
-                            c.raw[s][i][1] = v[1];
+                            raw[s][i][0] = v[0];
+                            raw[s][i][1] = v[1];
                         }
                     }
                 }
             }
-        };
-        auto add = [&](Chunk& c, int n) {
-            const int at = chunk_of(n);
-            if (64 * at + 64 > a.d_down) {
-                if (at == chunks) return;
+            if (64 * at + 64 > a.d_down) {                       // zeros for what the last chunk does not have
 #pragma unroll
                 for (int i = 0; i < kSets; ++i)
 #pragma unroll
-                    for (int b = 0; b < 2; ++b) c.rows[i][b] = 64 * at + 8 * piece < a.d_down ? c.rows[i][b] : u32x4{0, 0, 0, 0};
+                    for (int b = 0; b < 2; ++b) rows[i][b] = 64 * at + 8 * piece < a.d_down ? rows[i][b] : u32x4{0, 0, 0, 0};
                 if constexpr (BACK) {
 #pragma unroll
                     for (int s = 0; s < 2; ++s)
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
 #pragma unroll
-                            for (int e = 0; e < (RT + 1) / 2; ++e) c.raw[s][i][e] = 64 * at + 32 * s + 8 * kg < a.d_down ? c.raw[s][i][e] : 0u;
+                            for (int e = 0; e < (RT + 1) / 2; ++e) raw[s][i][e] = 64 * at + 32 * s + 8 * kg < a.d_down ? raw[s][i][e] : 0u;
                 }
             }
 #pragma unroll
             for (int i = 0; i < kSets; ++i)
 #pragma unroll
-                for (int b = 0; b < 2; ++b) mine[128 * i + 64 * b + 8 * row8 + (piece ^ row8)] = c.rows[i][b];
+                for (int b = 0; b < 2; ++b) mine[128 * i + 64 * b + 8 * row8 + (piece ^ row8)] = rows[i][b];
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 u32x4 ws[RT];
@@ -319,7 +311,7 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
                     } else {
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            ws[j][i] = j & 1 ? high_halves(c.raw[s][2 * i][j / 2], c.raw[s][2 * i + 1][j / 2]) : low_halves(c.raw[s][2 * i][j / 2], c.raw[s][2 * i + 1][j / 2]);
+                            ws[j][i] = j & 1 ? high_halves(raw[s][2 * i][j / 2], raw[s][2 * i + 1][j / 2]) : low_halves(raw[s][2 * i][j / 2], raw[s][2 * i + 1][j / 2]);
                     }
                 }
 #pragma unroll
@@ -329,27 +321,13 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
                     for (int j = 0; j < RT; ++j) acc[j][i] = mfma(ws[j], x, acc[j][i]);
                 }
             }
-        };
-        Chunk even[U], odd[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) load(even[u], wave + W * u);
-        for (int n = wave; n < chunks; n += 2 * W * U) {
-#pragma unroll
-            for (int u = 0; u < U; ++u) load(odd[u], n + W * (U + u));
-#pragma unroll
-            for (int u = 0; u < U; ++u) add(even[u], n + W * u);
-            if (n + W * U >= chunks) break;
-#pragma unroll
-            for (int u = 0; u < U; ++u) load(even[u], n + W * (2 * U + u));
-#pragma unroll
-            for (int u = 0; u < U; ++u) add(odd[u], n + W * (U + u));
         }
 #pragma unroll
         for (int j = 0; j < RT; ++j)
 #pragma unroll
             for (int i = 0; i < NT; ++i) mine[64 * (j * NT + i) + lane] = __builtin_bit_cast(u32x4, acc[j][i]);
     }
-    if (!DEEP && wave < count) load_columns(first, group_of(wave));
+    if ((!DEEP || RT == 4) && wave < count) load_columns(first, group_of(wave));
     lds_barrier();
     for (int e = wave; e < RT * NT; e += W) {
         f32x4 v = __builtin_bit_cast(f32x4, own[0][64 * e + lane]);
@@ -432,8 +410,8 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, DEEP || RT == 4 ? 2 : 4) void lor
                 else *p = v;
             }
     };
-    // (two sets of registers in turn; the first is on its way since before h was there.  A load under a condition would leave the compiler without
-    // a count of those on their way, and it would wait for all: 55.3 -> 51.1 us for 8,400 rows of rank 16.)
+    // (two sets of registers in turn; the first is on its way since before h was there, or, where registers are few, since the sums are.  A load under a
+    // condition would leave the compiler without a count of those on their way, and it would wait for all: 55.3 -> 51.1 us for 8,400 rows of rank 16.)
     Columns next;
     int n = wave;
     for (; n + 2 * W < count; n += 2 * W) {
@@ -554,7 +532,7 @@ __global__ __launch_bounds__(64 * W, 2) void lora_grads_kernel(GradArgs a, int g
                 for (int i = 0; i < 8; ++i) b.raw[g][i] = *(gpair)((gbyte)((gu16)job.x + (long long)(row0 + i) * job.x_stride) + (down + x[g]));
 #pragma unroll
             for (int j = 0; j < 2 * RT; ++j) b.h[j] = *(gfloat4)((gbyte)(job.h + row0) + hp[j]);
-        } else {                                                 // a run's end; 0 rows: loads for nothing (see lora_rows_kernel) from where the last were
+        } else {                                                 // a run's end; 0 rows: loads for nothing from where the last were
             const int last = max(rows - 1, 0);
 #pragma unroll
             for (int g = 0; g < CG; ++g)
