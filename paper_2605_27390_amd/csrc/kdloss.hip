@@ -238,7 +238,24 @@ __device__ __forceinline__ void dots_of(const u32x4 (&row)[RB][NC], const u32x4 
     }
 }
 
-// Rows of up to 512 NC elements: one to a wavefront, RB at a time, the next ones under way meanwhile; the wavefronts meet at the end.
+// Zeros for rows that are not in the support and for what is behind a row's end, which are loaded like the others, from places that are there: a load
+// under a condition leaves the compiler without a count of those on their way, and it waits for all (64 events of 4,096 34.0 -> 32.3 us).
+template <int RB, int NC>
+__device__ __forceinline__ void zeros_in(u32x4 (&row)[RB][NC], const Entries& sh, int at, bool ends, int column, int step, int d) {
+    if (ends)
+#pragma unroll
+        for (int r = 0; r < RB; ++r)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) row[r][c] = column + step * c < d ? row[r][c] : u32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int r = 0; r < RB; ++r)
+        if (__builtin_amdgcn_readfirstlane(sh.ids[at + r]) < 0)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) row[r][c] = u32x4{0, 0, 0, 0};
+}
+
+// Rows of up to 512 NC elements: one to a wavefront, RB at a time; the wavefronts meet at the end.  The other wavefronts' loads are enough: with the next
+// rows under way 842 events of 656 elements take 63.8 us, 59.7 without, 400 of 2,048 74.5 and 70.5 (900 of 128 rows 79.4 and 82.9).
 template <int NC, int RB, int TYPE>
 __global__ __launch_bounds__(kThreads, NC == 4 ? 2 : 3) void kd_rows_kernel(KdArgs a) {
     __shared__ Entries sh;
@@ -250,23 +267,23 @@ __global__ __launch_bounds__(kThreads, NC == 4 ? 2 : 3) void kd_rows_kernel(KdAr
     u32x4 h[NC];
 #pragma unroll
     for (int c = 0; c < NC; ++c) h[c] = 8 * (64 * c + lane) < a.d ? *(gvec_ptr)((const uint16_t*)a.h + (long long)e * a.d + 8 * (64 * c + lane)) : u32x4{0, 0, 0, 0};
-    u32x4 even[RB][NC], odd[RB][NC];
+    u32x4 row[RB][NC];
     auto load = [&](u32x4 (&row)[RB][NC], int at) {
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
             const int id = at < n ? __builtin_amdgcn_readfirstlane(sh.ids[at + r]) : -1;
             const uint16_t* w = (const uint16_t*)a.W + (long long)(id < 0 ? 0 : id) * a.d;
 #pragma unroll
-            for (int c = 0; c < NC; ++c)
-                row[r][c] = id >= 0 && 8 * (64 * c + lane) < a.d ? *(gvec_ptr)(w + 8 * (64 * c + lane)) : u32x4{0, 0, 0, 0};
+            for (int c = 0; c < NC; ++c) row[r][c] = *(gvec_ptr)(w + min(8 * (64 * c + lane), a.d - 8));
         }
     };
-    const bool none = entries_of(a, e, j0, n, sh, [&] { load(even, RB * wave); });
+    const bool none = entries_of(a, e, j0, n, sh, [&] { load(row, RB * wave); });
     Sums<NC> s{};
     s.m = -__builtin_inff();
     const int mod = lane & (RB - 1);
-    auto add = [&](const u32x4 (&row)[RB][NC], int at) {
+    auto add = [&](u32x4 (&row)[RB][NC], int at) {
         if (at >= n) return;                                     // (uniform)
+        zeros_in(row, sh, at, a.d % (512 * NC) != 0, 8 * lane, 512, a.d);
         float dot[RB];
         dots_of(row, h, dot);
         const float x = lane_sums(dot, lane);
@@ -274,11 +291,10 @@ __global__ __launch_bounds__(kThreads, NC == 4 ? 2 : 3) void kd_rows_kernel(KdAr
         if (lane < RB) sh.z[at + mod] = mine ? x : __builtin_nanf("");
         s.add(row, x * inv, mine, sh.p[at + mod], lane);
     };
-    for (int at = RB * wave; at < n; at += 2 * RB * kWaves) {
-        load(odd, at + RB * kWaves);
-        add(even, at);
-        load(even, at + 2 * RB * kWaves);
-        add(odd, at + RB * kWaves);
+#pragma unroll 1
+    for (int at = RB * wave; at < n; at += RB * kWaves) {
+        if (at >= RB * kWaves) load(row, at);
+        add(row, at);
     }
     // The wavefronts' sums: two give theirs to the other two, then one to the other.
     if (lane == 0) ml[wave] = make_float2(s.m, s.l);
@@ -354,21 +370,22 @@ __global__ __launch_bounds__(kThreads, NC * RB <= 4 ? 3 : 1) void kd_long_rows_k
         in[c] = 8 * (c * kThreads + tid) < a.d;
         h[c] = in[c] ? *(gvec_ptr)((const uint16_t*)a.h + (long long)e * a.d + 8 * (c * kThreads + tid)) : u32x4{0, 0, 0, 0};
     }
-    u32x4 even[RB][NC], odd[RB][NC];
+    u32x4 row[RB][NC], next[RB][NC];
     auto load = [&](u32x4 (&row)[RB][NC], int at) {
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
             const int id = at < n ? __builtin_amdgcn_readfirstlane(sh.ids[at + r]) : -1;
             const uint16_t* w = (const uint16_t*)a.W + (long long)(id < 0 ? 0 : id) * a.d;
 #pragma unroll
-            for (int c = 0; c < NC; ++c) row[r][c] = in[c] && id >= 0 ? *(gvec_ptr)(w + 8 * (c * kThreads + tid)) : u32x4{0, 0, 0, 0};
+            for (int c = 0; c < NC; ++c) row[r][c] = *(gvec_ptr)(w + min(8 * (c * kThreads + tid), a.d - 8));
         }
     };
-    const bool none = entries_of(a, e, j0, n, sh, [&] { load(even, 0); });
+    const bool none = entries_of(a, e, j0, n, sh, [&] { load(row, 0); });
     Sums<NC> s{};
     s.m = -__builtin_inff();
     const int mod = lane & (RB - 1);
-    auto add = [&](const u32x4 (&row)[RB][NC], int at, int turn) {
+    auto add = [&](u32x4 (&row)[RB][NC], int at, int turn) {
+        zeros_in(row, sh, at, a.d % (8 * NC * kThreads) != 0, 8 * tid, 8 * kThreads, a.d);
         float dot[RB];
         dots_of(row, h, dot);
         const float sum = lane_sums(dot, lane);
@@ -381,11 +398,16 @@ __global__ __launch_bounds__(kThreads, NC * RB <= 4 ? 3 : 1) void kd_long_rows_k
         if (tid < RB) sh.z[at + mod] = mine ? x : __builtin_nanf("");
         s.add(row, x * inv, mine, sh.p[at + mod], lane);
     };
-    for (int at = 0; at < n; at += 2 * RB) {
-        load(odd, at + RB);
-        add(even, at, 0);
-        load(even, at + 2 * RB);
-        add(odd, at + RB, 1);
+    // (the next rows are under way; one loop with rows handed on, not two rows' sets in turn: a launch has half the instructions to bring in.  192 events
+    // 76.5 and 76.2 us, 300 123 and 115, 64 alike)
+#pragma unroll 1
+    for (int at = 0, turn = 0; at < n; at += RB, turn ^= 1) {
+        load(next, at + RB);
+        add(row, at, turn);
+#pragma unroll
+        for (int r = 0; r < RB; ++r)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) row[r][c] = next[r][c];
     }
     __syncthreads();
     for (int j = tid; j < n; j += kThreads) a.draft[(long long)e * a.K + j0 + j] = sh.z[j];
