@@ -532,7 +532,7 @@ __global__ __launch_bounds__(64 * W, 2) void lora_grads_kernel(GradArgs a, int g
                 for (int i = 0; i < 8; ++i) b.raw[g][i] = *(gpair)((gbyte)((gu16)job.x + (long long)(row0 + i) * job.x_stride) + (down + x[g]));
 #pragma unroll
             for (int j = 0; j < 2 * RT; ++j) b.h[j] = *(gfloat4)((gbyte)(job.h + row0) + hp[j]);
-        } else {                                                 // a run's end; 0 rows: loads for nothing from where the last were
+        } else {                                                 // a run's end
             const int last = max(rows - 1, 0);
 #pragma unroll
             for (int g = 0; g < CG; ++g)
@@ -590,7 +590,7 @@ __global__ __launch_bounds__(64 * W, 2) void lora_grads_kernel(GradArgs a, int g
     out += (long long)adapter * a.r * job.d;
     Steps steps(a.q, adapter);
     const int stride = W * parts;
-    Rows even, odd;
+    Rows now;
     int row0 = 0, rows = steps.skip(part * W, row0);
     if (rows == 0) {                                             // (the same in all wavefronts) nothing to add: an adapter without rows, often
         const int ranks = min(a.r - rank0, 16 * RT) / 4, columns = min(64 * CG, job.d - c0);
@@ -604,15 +604,14 @@ __global__ __launch_bounds__(64 * W, 2) void lora_grads_kernel(GradArgs a, int g
         return;
     }
     if (wave > 0) rows = steps.skip(wave - 1, row0);
-    load(even, row0, rows);
+    load(now, row0, rows);
+    // (one step's registers: the next one's loads ahead double the instructions that a launch brings in and leave fewer wavefronts; 64 rows of 16 adapters
+    // 14.5 us, 11.1 without, 6,400 of 16 46.0 and 40.1, 9,000 of 2 43.0 and 42.5; where few workgroups have rows 24.2 and 27.7, 72.6 and 79.5)
+#pragma unroll 1
     while (rows) {
-        const int then = steps.skip(stride - 1, row0);
-        load(odd, row0, then);
-        add(even, rows);
-        if (!then) break;
+        add(now, rows);
         rows = steps.skip(stride - 1, row0);
-        load(even, row0, rows);
-        add(odd, then);
+        if (rows) load(now, row0, rows);
     }
     // The upper half of the wavefronts first, whose sums the lower half takes along.
     __syncthreads();
@@ -747,9 +746,9 @@ hipError_t launch_lora_grads(const GradArgs& a, hipStream_t stream) {
     const int c = grad_columns(a.r), groups0 = (a.job[0].d + c - 1) / c, groups1 = (a.job[1].d + c - 1) / c, halves = grad_halves(a.r);
     const long long count0 = (long long)a.q.n * a.r * a.job[0].d, count1 = (long long)a.q.n * a.r * a.job[1].d;
     const dim3 grid((unsigned)(groups0 + groups1), (unsigned)a.q.n, (unsigned)(a.parts * halves));
-    // One workgroup of 8 wavefronts to a compute unit; where there are more than units that have rows, two of 4, or four of 2 with few rows each, so that
-    // some load while others store (9,000 rows of 2 adapters, rank 32, 8 / 4 / 2 wavefronts 44.8 / 47.7 / 49.3 us; rank 64, twice as many
-    // workgroups, 76.8 / 71.2 / 75.5; 6,400 rows of 16 adapters 62.0 / 47.0 / 45.6; 64 rows of 16 24.7 / 15.5 / 14.2).
+    // One workgroup of 8 wavefronts to a compute unit; where there are more than units that have rows, of 4, or of 2 with few rows each, so that some
+    // load while others store (9,000 rows of 2 adapters, rank 32, 8 / 4 / 2 wavefronts 42.6 / 44.5 / 72.7 us; rank 64, twice as many workgroups,
+    // 73.0 / 67.7 / 99.9; 6,400 rows of 16 adapters 55.6 / 40.2 / 44.0; 64 rows of 16 21.9 / 15.9 / 11.2).
     const int used = a.q.n < a.q.S ? a.q.n : a.q.S;
     const long long full = lora_grad_groups(used, a.r, a.job[0].d, a.job[1].d);
     const int waves = full <= 256 ? 8 : a.q.T <= 32 * used ? 2 : 4;
