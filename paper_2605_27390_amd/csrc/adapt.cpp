@@ -80,7 +80,7 @@ int evospec_lora_backward_workspace_bytes(const evospec_lora* lora, int S, int T
     if (!grads_fit(lora)) return EVOSPEC_BAD_SHAPE;
     *out_bytes = 0;
     if (S == 0 || T == 0) return EVOSPEC_OK;
-    const int parts = lora_grad_parts(lora->n, lora->r, T, lora->d_in, lora->d_out);
+    const int parts = lora_grad_parts(lora->n, lora->r, 1, T, lora->d_in, lora->d_out);          // (the most that fewer rows or other requests need)
     *out_bytes = 2 * h_bytes(lora, T) + (parts > 1 ? (size_t)parts * lora->n * lora->r * ((size_t)lora->d_in + lora->d_out) * sizeof(float) : 0);
     return EVOSPEC_OK;
 }
@@ -121,7 +121,7 @@ int evospec_lora_backward(const evospec_lora* lora, const void* x, long long x_s
     a.job[0] = GradJob{g, nullptr, x, x_stride, lora->d_in, false, out_da};
     a.job[1] = GradJob{h ? h : again, lora->scale, dy, dy_stride, lora->d_out, true, out_db};
     a.r = lora->r;
-    a.parts = rows ? lora_grad_parts(lora->n, lora->r, T, lora->d_in, lora->d_out) : 1;
+    a.parts = rows ? lora_grad_parts(lora->n, lora->r, S, T, lora->d_in, lora->d_out) : 1;
     a.partial = reinterpret_cast<float*>(ws + (rows ? 2 * h_bytes(lora, T) : 0));
     return failed(launch_lora_grads(a, st));
 }

@@ -58,7 +58,7 @@ struct GradArgs {
     float* partial;                           // [parts][n r d0 + n r d1] of parts > 1
 };
 long long lora_grad_groups(int n, int r, int d0, int d1);      // workgroups of a part
-int lora_grad_parts(int n, int r, int T, int d0, int d1);
+int lora_grad_parts(int n, int r, int S, int T, int d0, int d1);
 hipError_t launch_lora_grads(const GradArgs& a, hipStream_t stream);
 
 struct KdArgs {

@@ -731,15 +731,17 @@ long long lora_grad_groups(int n, int r, int d0, int d1) {
     return (long long)n * grad_halves(r) * ((d0 + c - 1) / c + (d1 + c - 1) / c);
 }
 
-// Parts that fill the card if all rows are of one adapter, where the most that an adapter has (parts_of shares them out) are four steps to a wavefront (two, if there is one adapter)
-// and, as the sum is a launch more that the rows may not need, one adapter alone would have a third of the card: 8 adapters' columns, all rows
-// of one of them, 7,000 rows of rank 8 39.1 -> 24.5 us, 5,900 of rank 16 55.9 -> 42.5; rows of all alike 33 -> 34, 12 adapters 19.1 -> 21.3 (with two
-// parts, rank 32, 42.9 -> 45.1).  A workspace of 128 MB at most.
-int lora_grad_parts(int n, int r, int T, int d0, int d1) {
-    const int each = n > 1 ? 32 : 16;
+// Parts that fill the card if all rows are of one adapter, of at least two steps to a wavefront (parts_of shares them out).  Where there are several
+// adapters the parts, and the launch that adds them, may turn out not to be needed: four steps, and one adapter alone would have a third of the
+// card.  (5 adapters, all rows of one, 7,000 rows of rank 8 39.1 -> 20.7 us, 5,900 of rank 16 55.9 -> 43.5; 9,000 rows of 2, which then have as
+// many parts as before, 32.9 -> 33.6, 12 adapters 19.1 -> 21.0; with two parts, rank 32, 42.9 -> 45.1.  One request of 8,735 rows, 73.3 -> 46.7.)
+// A workspace of 128 MB at most.
+int lora_grad_parts(int n, int r, int S, int T, int d0, int d1) {
+    const bool several = n > 1 && S > 1;                         // adapters, among which the rows may lie anyhow
+    const int each = several ? 32 : 16;
     const long long most = ((T + 31) / 32 + each - 1) / each, fit = (128 << 20) / ((long long)n * r * (d0 + d1) * 4);
     const long long parts = std::min(std::min(256 / lora_grad_groups(1, r, d0, d1), 16ll), std::min(most, fit));
-    return parts < (n > 1 ? 3 : 2) ? 1 : (int)parts;
+    return parts < (several ? 3 : 2) ? 1 : (int)parts;
 }
 
 hipError_t launch_lora_grads(const GradArgs& a, hipStream_t stream) {

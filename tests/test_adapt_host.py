@@ -38,6 +38,18 @@ def test_lora_bytes(ev):
     assert ev.lib.evospec_lora_backward_workspace_bytes(ctypes.byref(lora(r=64)), 1, (1 << 24) - 1, ctypes.byref(out)) == 0 and out.value >= 1 << 32
 
 
+def test_lora_bytes_of_fewer(ev):
+    """A workspace is enough for fewer rows, whatever the requests."""
+    for n, r, d in ((1, 8, 64), (1, 32, 4096), (5, 16, 1024), (16, 64, 2048), (300, 32, 4096)):
+        before = 0
+        for T in (1, 31, 500, 1025, 2049, 9000, 70000):
+            out = [ctypes.c_size_t(0) for _ in range(3)]
+            for o, S in zip(out, (1, 2, T)):
+                assert ev.lib.evospec_lora_backward_workspace_bytes(ctypes.byref(lora(n=n, r=r, d_in=d, d_out=d)), min(S, 1 << 16), T, ctypes.byref(o)) == 0
+            assert out[0].value == out[1].value == out[2].value >= before
+            before = out[0].value
+
+
 # Addresses below are never dereferenced: every call that is not an error has nothing to do.
 def forward(ev, l=None, x=16, xs=64, off=16, ad=16, S=2, T=5, y=16, ys=32, h=None):
     return ev.lib.evospec_lora_forward(ctypes.byref(l or lora()), x, xs, off, ad, S, T, y, ys, h, None)

@@ -142,6 +142,36 @@ def test_requests_that_follow_one_another(ev, seed):
     p.check_backward(da, db, p.tdx)
 
 
+@pytest.mark.parametrize("seed", range(3))
+def test_requests_that_follow_one_another_at_rank_64(ev, seed):
+    """The same in tiles of 32 rows."""
+    rng = np.random.default_rng(40 + seed)
+    S = [30, 64, 90][seed]
+    rows = rng.choice([0, 1, 16, 31, 32, 33, 64, 70], size=S)
+    adapter = np.repeat(rng.integers(-1, 3, size=S), rng.integers(1, 20, size=S))[:S]
+    p = Problem(ev, [int(v) for v in rows], [int(v) for v in adapter], 3, 64, 72, 136, seed=43 + seed, lead=int(rng.integers(0, 40)), tail=seed)
+    h = ev.lora_forward(p.tx, p.bank, p.toff, p.tad, p.ty, keep=True)
+    p.check_forward(p.ty, h)
+    da, db = ev.lora_backward(p.tx, p.tdy, p.bank, p.toff, p.tad, h=h, dx=p.tdx)
+    p.check_backward(da, db, p.tdx)
+
+
+@pytest.mark.parametrize("r", [8, 24, 64])
+@pytest.mark.parametrize("adapter", [[1] * 6, [1, 1, 1, 1, 4, 0], [0, 1, 2, 3, 4, -1], [-1] * 6, [2, 9, -1, -1, 2, 9]])
+def test_shares_of_adapters(ev, adapter, r):
+    """Rows enough for an adapter's to be split, by its share of them: all of them, most, alike, none; twice the same."""
+    import torch
+    p = Problem(ev, [600, 500, 601, 433, 37, 700], adapter, 5, r, 136, 200, seed=60, lead=2, tail=1)
+    h = ev.lora_forward(p.tx, p.bank, p.toff, p.tad, p.ty, keep=True)
+    da, db = ev.lora_backward(p.tx, p.tdy, p.bank, p.toff, p.tad, h=h)
+    p.check_backward(da, db)
+    outs = [torch.full_like(t, float("nan")) for t in (da, db)]
+    need = ev.lora_backward_workspace_bytes(p.bank, 6, p.T)
+    ev.lora_backward(p.tx, p.tdy, p.bank, p.toff, p.tad, h=h, out_da=outs[0], out_db=outs[1],
+                     workspace=torch.full((need,), 255, dtype=torch.uint8, device="cuda"))
+    assert torch.equal(da, outs[0]) and torch.equal(db, outs[1])
+
+
 def test_thousands_of_requests(ev):
     rng = np.random.default_rng(30)
     for S, adapters in ((5000, rng.integers(-1, 5, size=5000)), (4200, np.where(np.arange(4200) % 700 == 699, 1, -1)), (4097, np.zeros(4097, int))):
