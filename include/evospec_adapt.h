@@ -47,9 +47,10 @@ int evospec_lora_forward(const evospec_lora *lora, const void *x, long long x_st
  *   dx        dev bf16 [T, d_in], rows dx_stride elements apart, 16-B aligned, or NULL; rounded once; no overlap with x or dy
  *   out_da    dev fp32 [n][r][d_in], 16-B aligned      out_db dev fp32 [n][d_out][r], 16-B aligned: written whole (zeros where an
  *             adapter has no rows)
- *   workspace dev, 16-B aligned, at least evospec_lora_backward_workspace_bytes(...) bytes, scratch
+ *   workspace dev, 16-B aligned, at least evospec_lora_backward_workspace_bytes(...) bytes, scratch: enough for every call of
+ *             as many rows or fewer, whatever the requests
  * n (d_in + d_out) / 64 below 2^22 (rank 33 and more) or 2^23.
- * Sums are fp32 in an order that depends on the sizes only: the same inputs give the same bits.
+ * Sums are fp32 in an order that depends on the sizes, row_off and adapter only: the same inputs give the same bits.
  */
 int evospec_lora_backward_workspace_bytes(const evospec_lora *lora, int S, int T, size_t *out_bytes /*host*/);
 int evospec_lora_backward(const evospec_lora *lora, const void *x, long long x_stride, const float *h, const void *dy,
@@ -98,7 +99,8 @@ int evospec_adamw_blocks(const evospec_adamw_tensor *tensors /*host [count]*/, i
  * One step of AdamW over `count` tensors, for every element, with g = grad * grad_scale:
  *   m = beta1 m + (1 - beta1) g      v = beta2 v + (1 - beta2) g^2
  *   p = p (1 - lr weight_decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
- * in fp32, from the moments before they are rounded.  (A v below 2^-126 may count as 0.)
+ * in fp32, from the moments before they are rounded.  (A v below 2^-126 may count as 0.)  The moments' products and sums are rounded one by one,
+ * so that their codes are the same wherever the formulas are computed in that order.
  *   param_type  of all parameters (fp16, bf16, fp32); grad_type: the same, or EVOSPEC_FP32
  *   kind        EVOSPEC_MOMENTS_FP32: m and v dev fp32 [blocks * 256], scales NULL
  *               EVOSPEC_MOMENTS_8BIT: m and v dev uint8 [blocks * 256], scales dev fp32 [blocks][2], of m and of v

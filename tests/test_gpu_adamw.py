@@ -129,6 +129,31 @@ def test_steps(ev, sizes, ptype, gtype, master, state):
     p.check_step(ev, 0.0, 12345678, seed=9, betas=(0.95, 0.9999))
 
 
+@pytest.mark.parametrize("state", ["fp32", "8bit"])
+def test_moments_to_the_bit(ev, state):
+    """Those of the formulas computed one operation after the other in fp32, and their codes, step after step."""
+    p = Problem(ev, [70000, 300, 256, 1], "bf16", "bf16", state, False, seed=90)
+    b1, b2, g = 0.9, 0.98, p.flat(p.grads).astype(np.float32)
+    f = np.float32
+    for t in (1, 2, 3):
+        m, v = (x.astype(np.float32) for x in p.moments())
+        m, v = f(b1) * m + f(1 - b1) * g, f(b2) * v + f(1 - b2) * (g * g)
+        ev.adamw_step(p.opt, 1e-3, t, betas=(b1, b2), seed=77)
+        if state == "fp32":
+            gm, gv = p.moments()
+            assert np.array_equal(gm, m) and np.array_equal(gv, v)
+            continue
+        s = host(p.opt.scales).reshape(-1, 2)
+        r = ref.random_bits(np.arange(p.total), 77, t)
+        for codes, x, col, bias, largest, bits in ((p.opt.m, m, 0, 7, 448.0, r & 0xffff), (p.opt.v, v, 1, 15, 61440.0, r >> 16)):
+            assert [ref.scale_for(float(top), largest) for top in np.abs(x).reshape(-1, BLOCK).max(1)] == list(s[:, col])
+            y, least = np.abs(x) / s[:, col].repeat(BLOCK).astype(np.float32), f(2.0 ** (1 - bias))
+            y = np.where(y < least, (y + least).astype(np.float64) - least, y)
+            want = ref.grid(y, bits, bias, largest)
+            want = np.where(x > 0, np.maximum(want, 1), want) if bias == 15 else want + np.where(np.signbit(x), 128, 0)
+            assert np.array_equal(codes.cpu().numpy(), want)
+
+
 def test_gradients_of_zero_and_far_apart(ev):
     """A block of zeros; magnitudes from 1e-18 to 1e6 within one: those that do not fit a block's codes become the smallest, not zero, for v."""
     for state in ("fp32", "8bit"):
