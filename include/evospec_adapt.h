@@ -31,8 +31,8 @@ typedef struct evospec_lora {
  *   x         dev bf16 [T, d_in], rows x_stride elements apart, 16-B aligned
  *   row_off   dev int32 [S + 1], non-decreasing, values clamped to [0, T]       adapter dev int32 [S]
  *   y         dev bf16 [T, d_out], rows y_stride elements apart, 16-B aligned; no overlap with x.  Rounded once.
- *   out_h     dev fp32 [r, T] or NULL: h = x A^T, transposed, for evospec_lora_backward; columns of rows without an adapter
- *             are left as they are
+ *   out_h     dev fp32 [r, T] or NULL: h = x A^T, transposed, for evospec_lora_backward; zeros in columns of rows without an
+ *             adapter
  * Sums are fp32.  h goes into the second product as two bf16 numbers, which keep 2^-16 of it.
  * T below 2^24, S at most 2^16, strides at most 2^26.
  */
@@ -67,8 +67,9 @@ int evospec_lora_backward(const evospec_lora *lora, const void *x, long long x_s
  *   h         dev bf16 [E, d]         W_lm dev bf16 [V, d], both 16-B aligned; d a multiple of 8, at most EVOSPEC_KD_D_MAX
  *   support   dev int32 [E, K], K at most EVOSPEC_KD_K_MAX         target dev fp32 [E, K]         weight dev fp32 [E] or NULL (1)
  *   out_loss  dev fp32 [E]            out_dh dev `type` (EVOSPEC_BF16 or EVOSPEC_FP32) [E, d], 16-B aligned
- *   out_draft dev fp32 [E, K]: z, NaN where the entry is not in the support
- *   workspace dev, 16-B aligned, at least evospec_kd_loss_workspace_bytes(E, K, d) bytes, scratch
+ *   out_draft dev fp32 [E, K]: z, NaN where the entry is not in the support.  No output overlaps an input.
+ *   workspace dev, 16-B aligned, at least evospec_kd_loss_workspace_bytes(E, K, d) bytes, scratch (fewer events can need more: their rows
+ *             are split)
  * T > 0 and finite.  Logits and gradients are summed in fp32, the loss in 64 bits from the logits.  E < 2^20.
  */
 #define EVOSPEC_KD_K_MAX 1024

@@ -64,10 +64,10 @@ int evospec_lora_forward(const evospec_lora* lora, const void* x, long long x_st
                          int S, int T, void* y, long long y_stride, float* out_h, void* stream) {
     int rc = check_lora(lora, S, T);
     if (rc) return rc;
-    if (S == 0 || T == 0) return EVOSPEC_OK;
+    if (T == 0 || (S == 0 && !out_h)) return EVOSPEC_OK;          // (without requests out_h is zeros)
     if ((rc = check_weights(lora))) return rc;
     if ((rc = check_matrix(x, x_stride, lora->d_in)) || (rc = check_matrix(y, y_stride, lora->d_out))) return rc;
-    if (!row_off || !adapter) return EVOSPEC_NULL_POINTER;
+    if (!row_off || (!adapter && S)) return EVOSPEC_NULL_POINTER;
     if (!aligned(out_h, 4)) return EVOSPEC_MISALIGNED;
     const LoraArgs rows{{row_off, adapter, S, T, lora->n}, x, x_stride, lora->a, lora->d_in, lora->scale, lora->b, lora->d_out, y, y_stride, out_h, lora->r};
     return failed(launch_lora_rows(rows, lora_plan(S, T, lora->r, lora->d_in, lora->d_out), false, static_cast<hipStream_t>(stream)));

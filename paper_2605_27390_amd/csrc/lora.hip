@@ -165,8 +165,35 @@ __device__ __forceinline__ Run find_rows(const Requests& q, int index, int* wher
     return Run{first, count, adapter};
 }
 
-// ---------------------------------------------------------------- rows
+// Zeros for what h has in columns [base, base + size) of rows that no adapter is for.  (All of a workgroup of W wavefronts.)
+template <int W>
+__device__ __forceinline__ void zeros_of_none(const Requests& q, int base, int size, float* h, int r) {
+    const int lane = threadIdx.x & 63, end = min(base + size, q.T);
+    int lo = 0;                                                  // the last request, of those at multiples of 64, that begins at or before base
+    for (int hi = (q.S + 63) >> 6; hi - lo > 1;) {
+        const int step = (hi - lo + 63) >> 6, s = lo + lane * step;
+        const bool at_most = s < hi && min(max(q.row_off[64 * s], 0), q.T) <= base;
+        const int n = max((int)__popcll(__ballot(at_most)), 1);
+        lo += (n - 1) * step;
+        hi = min(lo + step, hi);
+    }
+    u64 there = 0;
+    for (int s = 64 * lo; s < q.S; s += 64) {
+        const Run t = request_of(q, s + lane);
+        const int from = max(t.row0, base) - base, to = min(t.row0 + t.rows, end) - base;
+        u64 mine = to > from ? ((1ull << (to - from)) - 1) << from : 0;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) mine |= __shfl_xor(mine, o);
+        there |= mine;
+        if (s + 64 < q.S && q.row_off[s + 64] >= end) break;
+    }
+    for (int e = threadIdx.x; e < size * r; e += 64 * W) {
+        const int row = e % size;
+        if (base + row < end && !(there >> row & 1)) h[(long long)(e / size) * q.T + base + row] = 0.f;
+    }
+}
 
+// ---------------------------------------------------------------- rows
 
 typedef const u32x2 __attribute__((address_space(1))) * gpair;
 typedef const uint32_t __attribute__((address_space(1))) * gword;
@@ -196,6 +223,8 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, RT == 4 ? 2 : 4) void lora_rows_k
     __shared__ int where[16 * NT];
     const int tile = blockIdx.x / 8 / a.slices * 8 + blockIdx.x % 8, slice = blockIdx.x / 8 % a.slices;        // a tile's slices on one of the 8 dies
     const Run t = find_rows<NT == 1 ? 4 : 5>(a.q, tile, where);
+    if constexpr (!BACK)
+        if (a.h && a.y && slice == 0 && 16 * NT * tile < a.q.T) zeros_of_none<W>(a.q, 16 * NT * tile, 16 * NT, a.h, a.r);
     if (t.rows == 0) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, kg = lane >> 4;
     const float factor = a.factor ? a.factor[t.adapter] : 1.f;

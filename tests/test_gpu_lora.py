@@ -88,7 +88,7 @@ def test_forward(ev, case, wide):
     assert ev.lora_forward(p.tx, p.bank, p.toff, p.tad, p.ty, out_h=h) is h
     p.check_forward(p.ty, h)
     none = np.isnan(ref.lora_forward(p.x, p.A, p.B, p.scale, p.off, p.adapter, p.y)[2][0])
-    assert (h.cpu().numpy()[:, none] == 9.0).all()
+    assert not h.cpu().numpy()[:, none].any()
     again = p.rows_of(p.y)
     assert ev.lora_forward(p.tx, p.bank, p.toff, p.tad, again) is again
     assert torch.equal(again, p.ty)                                  # the same bits, whether h is kept or not
@@ -154,6 +154,22 @@ def test_requests_that_follow_one_another_at_rank_64(ev, seed):
     p.check_forward(p.ty, h)
     da, db = ev.lora_backward(p.tx, p.tdy, p.bank, p.toff, p.tad, h=h, dx=p.tdx)
     p.check_backward(da, db, p.tdx)
+
+
+@pytest.mark.parametrize("S", [0, 1, 9, 64, 70, 300, 5000])
+@pytest.mark.parametrize("r", [8, 64])
+def test_kept_columns_of_rows_without_an_adapter(ev, S, r):
+    """h is written whole: zeros for requests without an adapter, and before, between and behind the requests' rows."""
+    import torch
+    rng = np.random.default_rng(S)
+    adapter = [-1 if s % 9 == 8 or s % 64 == 63 else s // 3 % 2 for s in range(S)]
+    for rows in ([int(v) for v in rng.integers(0, 40 if S < 1000 else 3, size=S)], [1] * S):
+        p = Problem(ev, rows, adapter, 2, r, 64, 72, seed=70 + S, lead=37, tail=50)
+        h = torch.full((r, p.T), float("nan"), device="cuda")
+        ev.lora_forward(p.tx, p.bank, p.toff, p.tad, p.ty, out_h=h)
+        p.check_forward(p.ty, h)
+        none = np.isnan(ref.lora_forward(p.x, p.A, p.B, p.scale, p.off, p.adapter, p.y)[2][0])
+        assert not h.cpu().numpy()[:, none].any()
 
 
 @pytest.mark.parametrize("r", [8, 24, 64])
