@@ -64,9 +64,16 @@ def _workspace_of(workspace, need, dev, device):
     return _new((need,), (1,), dtype=torch.uint8, device=device) if need else None
 
 
+def _fixed(name):
+    """A handle's tensor: its address went to the library, so another one cannot take its place."""
+    return property(lambda self: getattr(self, name))
+
+
 class LoraBank:
     """Adapters of one projection: a bf16 [n, r, d_in], b bf16 [n, d_out, r], scale fp32 [n] or None (1).  r is a multiple of 8 up to
-    64; adapters of a smaller rank are padded with zeros.  The tensors are used as they are at each call."""
+    64; adapters of a smaller rank are padded with zeros.  The tensors' values are used as they are at each call; the handle keeps the tensors
+    and their addresses, so that their memory must stay theirs (no `.data = ...`, no `set_`)."""
+    a, b, scale = _fixed("_a"), _fixed("_b"), _fixed("_scale")
 
     def __init__(self, a, b, scale=None):
         _expect(a, _bf16, "a", 3)
@@ -83,7 +90,7 @@ class LoraBank:
             if scale.numel() != self.n:
                 raise ValueError("scale needs a value for every adapter")
         _lora_bytes(self.n, self.r, self.d_in, self.d_out, 0, 0)      # (refuses the sizes that no call takes)
-        self.a, self.b, self.scale = a, b, scale
+        self._a, self._b, self._scale = a, b, scale
         self._c = _Lora(a.data_ptr(), b.data_ptr(), _ptr(scale), self.n, self.r, self.d_in, self.d_out)
         self._ref = ctypes.byref(self._c)
 
@@ -134,7 +141,8 @@ def _apart(out, rows, d, stride, name, x, dx, stride_x, other):
 def lora_forward(x, bank: LoraBank, row_off, adapter, y, keep: bool = False, out_h=None):
     """y[t] += scale (x[t] A^T) B^T in place, with the adapter of the request that row t belongs to: rows row_off[s] .. row_off[s + 1] have
     adapter[s] (int32, both on the GPU); rows of a request whose adapter is not in 0 .. n - 1, and rows of none, stay as they are.
-    x [T, d_in], y [T, d_out] in bf16.  Returns h = x A^T, transposed, fp32 [r, T] (with keep, or as out_h), for lora_backward, else y."""
+    x [T, d_in], y [T, d_out] in bf16.  Returns h = x A^T, transposed, fp32 [r, T] (with keep, or as out_h; zeros for rows without an
+    adapter), for lora_backward, else y."""
     dev = bank._device
     S = _requests(row_off, adapter, dev)
     xs = _rows_of(x, bank.d_in, "x", dev)
@@ -227,6 +235,9 @@ def kd_loss(h, W_lm, support, target, weight=None, T: float = 1.0, dtype=torch.b
             _elsewhere(t, dev, name)
             if tuple(t.shape) != shape:
                 raise ValueError(f"{name} must be {shape}, got {tuple(t.shape)}")
+            for x, other in ((h, "h"), (W_lm, "W_lm"), (support, "support"), (target, "target"), (weight, "weight")):
+                if x is not None and t.data_ptr() < x.data_ptr() + x.nbytes and x.data_ptr() < t.data_ptr() + t.nbytes:
+                    raise ValueError(f"{name} overlaps {other}")
     out_loss = _new((E,), (1,), dtype=_f32, device=h.device) if out_loss is None else out_loss
     out_dh = _new((E, d), (d, 1), dtype=dtype, device=h.device) if out_dh is None else out_dh
     out_draft = _new((E, K), (K, 1), dtype=_f32, device=h.device) if out_draft is None else out_draft
@@ -243,7 +254,9 @@ class AdamW:
     tensors follow one another, each from a multiple of 256 elements on: m and v (fp32, or uint8 codes with scales fp32 [blocks, 2]).
     master: True or a flat fp32 buffer, from which parameters of 16 bits are rounded; True takes the parameters as they are now.
     Buffers that are not given are allocated here, as zeros.  `offsets` says where each tensor begins.  The handle keeps the tensors and their
-    addresses: their memory must stay theirs (no `.data = ...`, no `set_`), and parameters must not share any."""
+    addresses: their memory must stay theirs (no `.data = ...`, no `set_`), and parameters must not share any.  A state that was saved is copied
+    into m, v, scales and master."""
+    params, grads, m, v, scales, master = (_fixed("_" + n) for n in ("params", "grads", "m", "v", "scales", "master"))
 
     def __init__(self, params, grads, state: str = "fp32", m=None, v=None, scales=None, master=None):
         if state not in _MOMENTS:
@@ -289,11 +302,11 @@ class AdamW:
                 _elsewhere(t, dev, name)
                 if tuple(t.shape) != shape:
                     raise ValueError(f"{name} must be {shape}, got {tuple(t.shape)}")
-            setattr(self, name, t)
+            setattr(self, "_" + name, t)
         if master is True:
             for p, o in zip(params, self.offsets):
                 self.master[o:o + p.numel()] = p.detach().reshape(-1)
-        self.params, self.grads = params, grads
+        self._params, self._grads = tuple(params), tuple(grads)
         self._table, self._types = table, (_TYPES[kind], _TYPES[gkind], _MOMENTS[state])
         self._buffers = (self.m.data_ptr(), self.v.data_ptr(), _ptr(self.scales), _ptr(self.master))
 

@@ -304,6 +304,21 @@ def test_refusals(ev):
         ev.adamw_step(ev.AdamW([odd], [w(19)]), 1e-3, 1)
 
 
+def test_tensors_of_a_handle_stay(ev):
+    """Their addresses went to the library: another tensor in their place would not be seen."""
+    import torch
+    p = Problem(ev, [300, 5], "bf16", "bf16", "8bit", True)
+    for name in ("params", "grads", "m", "v", "scales", "master"):
+        with pytest.raises(AttributeError):
+            setattr(p.opt, name, getattr(p.opt, name))
+    with pytest.raises(TypeError):
+        p.opt.grads[0] = torch.zeros_like(p.grads[0])
+    bank = ev.LoraBank(torch.zeros(2, 8, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(2, 32, 8, dtype=torch.bfloat16, device="cuda"))
+    for name in ("a", "b", "scale"):
+        with pytest.raises(AttributeError):
+            setattr(bank, name, getattr(bank, name))
+
+
 def test_another_gpu_than_the_current_one(ev, monkeypatch):
     """Played: there is one GPU here."""
     from paper_2605_27390_amd import decode

@@ -161,6 +161,15 @@ def test_refusals(ev):
     assert [tuple(t.shape) for t in none] == [(0,), (0, 64), (0, 20)]
 
 
+def test_outputs_that_are_inputs(ev):
+    import torch
+    h, W, support, target, weight = problem(4, 20, 64, 50)
+    ok = dict(h=dev(h, torch.bfloat16), W_lm=dev(W, torch.bfloat16), support=dev(support), target=dev(target, torch.float32))
+    for bad in (dict(out_draft=ok["target"]), dict(out_draft=ok["support"].view(torch.float32)), dict(out_dh=ok["h"]), dict(out_dh=ok["W_lm"][46:])):
+        with pytest.raises(ValueError, match="overlaps"):
+            ev.kd_loss(**{**ok, **bad})
+
+
 @pytest.mark.parametrize("E", [3, 520])
 def test_streams_and_graphs(ev, E):
     import torch
