@@ -288,7 +288,7 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, RT == 4 ? 2 : 4) void lora_rows_k
         f32x4 acc[RT][NT] = {};
         // (8 rows that a tile does not have are not loaded: what their lanes find in LDS ends in rows that are not stored.  8.1 -> 7.7 us for one row.)
         for (int n = wave; n < chunks; n += W) {
-            const int at = n + turn < chunks ? n + turn : n + turn - chunks, here = 64 * at + 8 * piece < a.d_down ? 64 * at : 0;
+            const int at = n + turn < chunks ? n + turn : n + turn - chunks, here = 64 * at + 8 * piece < a.d_down ? 64 * at : -8 * piece;
             u32x4 rows[kSets][2];
             uint32_t raw[BACK ? 2 : 1][8][(RT + 1) / 2];
 #pragma unroll
