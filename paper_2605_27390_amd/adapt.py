@@ -184,12 +184,13 @@ def lora_backward(x, dy, bank: LoraBank, row_off, adapter, h=None, dx=None, out_
         _elsewhere(h, dev, "h")
         if tuple(h.shape) != (bank.r, T):
             raise ValueError(f"h must be [{bank.r}, {T}], got {tuple(h.shape)}")
-    for t, shape, name in ((out_da, (bank.n, bank.r, bank.d_in), "out_da"), (out_db, (bank.n, bank.d_out, bank.r), "out_db")):
-        if t is not None:
-            _expect(t, _f32, name, 3)
-            _elsewhere(t, dev, name)
-            if tuple(t.shape) != shape:
-                raise ValueError(f"{name} must be {shape}, got {tuple(t.shape)}")
+    if out_da is not None or out_db is not None:
+        for t, shape, name in ((out_da, (bank.n, bank.r, bank.d_in), "out_da"), (out_db, (bank.n, bank.d_out, bank.r), "out_db")):
+            if t is not None:
+                _expect(t, _f32, name, 3)
+                _elsewhere(t, dev, name)
+                if tuple(t.shape) != shape:
+                    raise ValueError(f"{name} must be {shape}, got {tuple(t.shape)}")
     if out_da is None:
         out_da = _new((bank.n, bank.r, bank.d_in), (bank.r * bank.d_in, bank.d_in, 1), dtype=_f32, device=x.device)
     if out_db is None:
