@@ -64,13 +64,21 @@ __device__ __forceinline__ void event_loss(const KdArgs& a, int e, const float* 
     constexpr int kPer = kMost / kThreads;
     const float inf = __builtin_inff();
     float t[kPer], z[kPer], top[2] = {-inf, -inf};
+    int32_t id[kPer];
     bool mine[kPer];
+    // (all loads together, of entries that there are not the last one's)
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-        const int j = i * kThreads + threadIdx.x;
-        mine[i] = j < a.K && (unsigned)a.support[(long long)e * a.K + j] < (unsigned)a.V;
-        t[i] = mine[i] ? a.target[(long long)e * a.K + j] : -inf;
-        z[i] = mine[i] ? draft[j] : -inf;
+        const int j = min(i * kThreads + (int)threadIdx.x, a.K - 1);
+        id[i] = a.support[(long long)e * a.K + j];
+        t[i] = a.target[(long long)e * a.K + j];
+        z[i] = draft[j];
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        mine[i] = i * kThreads + (int)threadIdx.x < a.K && (unsigned)id[i] < (unsigned)a.V;
+        t[i] = mine[i] ? t[i] : -inf;
+        z[i] = mine[i] ? z[i] : -inf;
         top[0] = fmaxf(top[0], t[i]);
         top[1] = fmaxf(top[1], z[i]);
     }
@@ -131,16 +139,22 @@ __device__ __forceinline__ bool entries_of(const KdArgs& a, int e, int j0, int n
     const float inf = __builtin_inff(), inv = 1.f / a.T;
     const int tid = threadIdx.x;
     float t[kPer], top[1] = {-inf};
+    int32_t id[kPer];
     bool nan = false;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {                             // (all loads together, as above)
+        const int j = min(i * kThreads + tid, a.K - 1);
+        id[i] = a.support[(long long)e * a.K + j];
+        t[i] = a.target[(long long)e * a.K + j];
+    }
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int j = i * kThreads + tid;
-        const int32_t id = j < a.K ? a.support[(long long)e * a.K + j] : -1;
-        const bool mine = (unsigned)id < (unsigned)a.V;
-        t[i] = mine ? a.target[(long long)e * a.K + j] : -inf;
+        const bool mine = j < a.K && (unsigned)id[i] < (unsigned)a.V;
+        t[i] = mine ? t[i] : -inf;
         top[0] = fmaxf(top[0], t[i]);
         nan |= t[i] != t[i];
-        if (j >= j0 && j < j0 + n) sh.ids[j - j0] = mine ? id : -1;
+        if (j >= j0 && j < j0 + n) sh.ids[j - j0] = mine ? id[i] : -1;
     }
     if (tid < 16) sh.ids[n + tid] = -1;                          // (turns may pass the end)
     __syncthreads();
@@ -257,7 +271,7 @@ __device__ __forceinline__ void zeros_in(u32x4 (&row)[RB][NC], const Entries& sh
 // Rows of up to 512 NC elements: one to a wavefront, RB at a time; the wavefronts meet at the end.  The other wavefronts' loads are enough: with the next
 // rows under way 842 events of 656 elements take 63.8 us, 59.7 without, 400 of 2,048 74.5 and 70.5 (900 of 128 rows 79.4 and 82.9).
 template <int NC, int RB, int TYPE>
-__global__ __launch_bounds__(kThreads, NC == 4 ? 2 : 3) void kd_rows_kernel(KdArgs a) {
+__global__ __launch_bounds__(kThreads, NC == 4 ? 2 : 4) void kd_rows_kernel(KdArgs a) {
     __shared__ Entries sh;
     __shared__ float joined[2][2][NC * 512];
     __shared__ float2 ml[kWaves];
