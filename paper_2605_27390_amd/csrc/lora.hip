@@ -729,21 +729,21 @@ hipError_t rows_of(const LoraArgs& a, const LoraPlan& p, hipStream_t stream) {
 
 }  // namespace
 
-// Measured at d = 4,096, rank 32: 64 rows in 1, 4, 8 slices 17.6, 11.3, 10.2 us; 1,024 rows in 1, 2, 4, 8 22.4, 17.5, 15.3, 23.9; 2,048 in
-// 1, 2, 4 23.0, 19.1, 28.6; with smaller workgroups at best 12.4, 19.8, 25.2.  4,096 rows (a tile to a compute unit) 25.4, and 28.7 with smaller
-// workgroups, which win from there on.
+// Measured at d = 4,096, rank 32: 64 rows in 1, 4, 8 slices 14.3, 9.6, 9.0 us; 1,024 rows in 1, 2, 4, 8 16.7, 13.6, 12.1, 15.5; 2,048 in
+// 1, 2, 4 17.2, 14.7, 17.5; with smaller workgroups at best 11.0, 16.2, 19.1.  4,096 rows (a tile to a compute unit) 19.3, and 24.7 with smaller
+// workgroups, which win from there on (4,500 rows of rank 64, 141 tiles of 32 rows, 29.9, and 39.6 with smaller ones).
 // As many tiles as T rows and half a tile for every request have: with more than units, the last ones begin when the others end (2,000 rows of 23
 // requests, rank 64, 7,392 -> 3,760: 61.8 us in 4 slices, 34.2 in 3).
-// Rank 56 and 64 in tiles of 32 rows, 6,100 rows and more (6,554, 6,208 columns: 57.4 us, 65.3 in tiles of 16; ranks 40 and 48 have a rank tile for
-// nothing: 72.7 and 64.0), in smaller workgroups from 128 tiles on (63.2 -> 57.4).
-// y past the caches where x and y are 128 MB or more: 8,400 rows of rank 16, other rows between, 67 -> 57 us; 4,096 rows, which are
-// found in the caches, 34.6 -> 43.5.
+// Rank 40 and more in tiles of 32 rows where tiles of 16 are many: backward, 9,000 rows of 4,096, rank 40 83.3 -> 69.6 us, 6,554 of 6,208, rank 64,
+// 92.7 -> 73.9; 600 rows of 4,096, rank 64, 18.1, and 15.8 in tiles of 16, 2,000 20.7 and 19.9, 3,000 25.0 and 25.8.
+// y past the caches where x and y are 128 MB or more: 8,400 rows of rank 16, other rows between, 58.3 -> 50.0 us; 4,096 rows of rank 32, which are
+// found in the caches, 24.7 -> 29.7.
 LoraPlan lora_plan(int S, int T, int r, int d_down, int d_up) {
     LoraPlan p{};
-    p.wide = r > 48 && T > 16 * S;
+    p.wide = r > 32 && T > 16 * S && (T + 15) / 16 + S / 2 > 128;
     const int size = p.wide ? 32 : 16, full = (T + size - 1) / size, whole = full + S / 2 > S ? full + S / 2 : S;      // about as many have rows
     p.tiles = full + S;
-    p.deep = whole <= (p.wide ? 128 : 256);
+    p.deep = whole <= 256;
     const int most = (d_up + 511) / 512;                         // slices that leave a wavefront 64 columns
     p.slices = std::max(1, std::min(32 / ((whole + 7) / 8), most));      // (of 32 units on a die)
     p.once = !p.deep && (size_t)T * ((size_t)d_down + d_up) * 2 >= (size_t)128 << 20;

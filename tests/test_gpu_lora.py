@@ -156,6 +156,16 @@ def test_requests_that_follow_one_another_at_rank_64(ev, seed):
     p.check_backward(da, db, p.tdx)
 
 
+@pytest.mark.parametrize("r,d", [(8, 4096), (32, 4096), (64, 4096), (16, 64), (40, 72), (64, 64)])
+def test_more_tiles_than_units(ev, r, d):
+    """Rows so many that a compute unit has several tiles, and (4,096) so large that they do not fit the caches."""
+    p = Problem(ev, [4000, 5001, 17], [1, 0, 1], 2, r, d, d, seed=80 + r, lead=3)
+    h = ev.lora_forward(p.tx, p.bank, p.toff, p.tad, p.ty, keep=True)
+    p.check_forward(p.ty, h)
+    da, db = ev.lora_backward(p.tx, p.tdy, p.bank, p.toff, p.tad, h=h, dx=p.tdx)
+    p.check_backward(da, db, p.tdx)
+
+
 @pytest.mark.parametrize("S", [0, 1, 9, 64, 70, 300, 5000])
 @pytest.mark.parametrize("r", [8, 64])
 def test_kept_columns_of_rows_without_an_adapter(ev, S, r):
