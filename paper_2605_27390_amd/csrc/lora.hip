@@ -90,24 +90,25 @@ __device__ __forceinline__ Run runs_of(const Requests& q, int base) {
     }
     return t;
 }
-// Work item `index` of up to 1 << SHIFT rows: how many, their adapter, and in `where` (LDS; every wavefront writes the same) which.  Request s has the numbers
-// from row0 / size + s on, one for each block of rows that it touches (the call's rows, blocks begin at multiples of size), so that the last request
-// whose first number is not larger is found by looking at 64 of them at a time, however many there are.  Of 64 requests:
-// with one row each, as in a decode step, those with one adapter are an item together, wherever they are, of the first one's number;
-// otherwise what a run has in a block, of the number of its first request there.  These, of up to 64 requests, are counted instead and have
-// numbers without gaps: workgroups go round the card's parts by number, and where the ones without rows lay badly some parts had twice what others had
-// (23 requests of up to 95 rows, 7,392 -> 3,760, rank 64, 55.7 us, of up to 100 33.1).
+// Work item `index` of up to 1 << SHIFT rows: how many, their adapter, and in `where` (LDS; every wavefront writes the same) which.  Of 64 requests
+// with one row each, as in a decode step, those with one adapter are an item together, wherever they are; otherwise runs are cut into items.
+// Up to 64 requests with more rows: the items are counted, and have numbers without gaps.  Workgroups go round the card's parts by number, and
+// where ones without rows lay badly some parts had twice what others had (23 requests of up to 95 rows, 7,392 -> 3,760, rank 64, 55.7 us, of up
+// to 100 33.1).
+// Else request s has the numbers from row0 / size + s on, one for each block of rows that it touches (the call's rows, blocks begin at multiples of
+// size), so that the last request whose first number is not larger is found by looking at 64 of them at a time, however many there are; an
+// item of several requests has the number of its first one there.
 template <int SHIFT>
 __device__ __forceinline__ Run find_rows(const Requests& q, int index, int* where) {
     constexpr int kSize = 1 << SHIFT;
     const int lane = threadIdx.x & 63;
-    const auto first_row = [&](int s) { return min(max(q.row_off[s], 0), q.T); };
+    const auto first_number = [&](int s) { return (min(max(q.row_off[s], 0), q.T) >> SHIFT) + s; };
     int lo = 0;
     if (q.S > 64) {
         int hi = q.S;
         while (hi - lo > 1) {
             const int step = (hi - lo + 63) >> 6, s = lo + lane * step;
-            const bool at_most = s < hi && (first_row(s) >> SHIFT) + s <= index;
+            const bool at_most = s < hi && first_number(s) <= index;
             const int n = __popcll(__ballot(at_most));
             if (n == 0) return Run{0, 0, 0};
             lo += (n - 1) * step;
@@ -117,31 +118,32 @@ __device__ __forceinline__ Run find_rows(const Requests& q, int index, int* wher
     const Run t = request_of(q, (lo & ~63) + lane);
     const bool one_each = __ballot(t.rows > 1) == 0;
     const u64 on = __ballot(goes_on(t));
-    int block = index - lo;                                      // of the call's rows
-    if (q.S <= 64) {
-        const int begin = t.row0 >> SHIFT;
-        if (one_each) {
-            const u64 before = __ballot(lane < q.S && begin + lane <= index);
-            if (before == 0) return Run{0, 0, 0};
-            lo = 63 - __clzll((long long)before);
-            block = index - lo;
-        } else {
-            const int shared = (on >> lane & 1) && (t.row0 & (kSize - 1)) ? 1 : 0;               // a block that an earlier request of the run has
-            const int own = t.rows > 0 ? ((t.row0 + t.rows - 1) >> SHIFT) + 1 - begin - shared : 0;
-            int number = own;
+    if (q.S <= 64 && !one_each) {
+        const int more = __ffsll((unsigned long long)~(lane < 63 ? on >> (lane + 1) : 0ull)) - 1;    // lanes that go on with this one's
+        const int end = __shfl(t.row0 + t.rows, lane + more);
+        const int own = t.rows > 0 && !(on >> lane & 1) ? (end - t.row0 + kSize - 1) >> SHIFT : 0;
+        int number = own;
 #pragma unroll
-            for (int o = 1; o < 64; o *= 2) {
-                const int v = __shfl_up(number, o);
-                number += lane >= o ? v : 0;
-            }
-            number -= own;
-            const u64 before = __ballot(own > 0 && number <= index);
-            if (before == 0) return Run{0, 0, 0};
-            lo = 63 - __clzll((long long)before);
-            block = __builtin_amdgcn_readlane(begin + shared - number, lo) + index;
+        for (int o = 1; o < 64; o *= 2) {
+            const int v = __shfl_up(number, o);
+            number += lane >= o ? v : 0;
         }
+        number -= own;
+        const u64 before = __ballot(own > 0 && number <= index);
+        if (before == 0) return Run{0, 0, 0};
+        const int at = 63 - __clzll((long long)before);
+        const int first = __builtin_amdgcn_readlane(t.row0 - (number << SHIFT), at) + (index << SHIFT);
+        const int count = min(__builtin_amdgcn_readlane(end, at) - first, kSize);
+        if (count <= 0) return Run{0, 0, 0};
+        if (lane < kSize) where[lane] = first + min(lane, count - 1);
+        return Run{first, count, __builtin_amdgcn_readlane(t.adapter, at)};
     }
-    const int at = lo & 63;
+    if (q.S <= 64) {
+        const u64 before = __ballot(lane < q.S && (t.row0 >> SHIFT) + lane <= index);
+        if (before == 0) return Run{0, 0, 0};
+        lo = 63 - __clzll((long long)before);
+    }
+    const int at = lo & 63, block = index - lo;                  // of the call's rows
     const int row0 = __builtin_amdgcn_readlane(t.row0, at), rows = __builtin_amdgcn_readlane(t.rows, at), adapter = __builtin_amdgcn_readlane(t.adapter, at);
     const int first = max(row0, block << SHIFT), past = (block + 1) << SHIFT, last = row0 + rows;
     if (first >= last) return Run{0, 0, 0};                      // (a number that no block of the request has, or no rows)
@@ -157,7 +159,7 @@ __device__ __forceinline__ Run find_rows(const Requests& q, int index, int* wher
         if (mine && rank >= 0 && rank < kSize) where[rank] = t.row0;
     } else {
         if ((on >> at & 1) && first == row0 && (row0 & (kSize - 1))) return Run{0, 0, 0};
-        const int more = __ffsll((unsigned long long)~(at < 63 ? on >> (at + 1) : 0ull)) - 1;         // requests that go on with this one's
+        const int more = __ffsll((unsigned long long)~(at < 63 ? on >> (at + 1) : 0ull)) - 1;
         const int end = min(__builtin_amdgcn_readlane(t.row0 + t.rows, at + more), past);
         count = (last < past ? end : past) - first;
         if (lane < kSize) where[lane] = min(first + lane, first + count - 1);
