@@ -523,21 +523,23 @@ hipError_t rows_as(const KdArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-// An event's rows are split until the parts come to one round of workgroups, two to a compute unit; three where rows of 2,048 to 4,096 elements
-// are many (256 rows of 4,096; 32 events in 16 and 24 parts 24.0 and 26.3 us, 64 in 8 and 12 35.6 and 38.7, 150 in 3 and 5 69.4 and 65.8, 192 in 2 and 4
-// 94.4 and 78.7), one above 8,192.  Shorter rows gain nothing from three (400 events of 2,048 in 1 and 2 parts 73.6 and 83.3, 338 of 344 20.0 and 21.3).
+// An event's rows are split until the parts come to one round of workgroups, two to a compute unit; three where two leave a seventh of the card empty and
+// rows have 2,048 to 4,096 elements (256 rows of 4,096; 110 events in 4 and 6 parts 45.7 and 50.4 us, 150 in 3 and 5 59.0 and 63.4, 192 in 2 and 4 79.8
+// and 76.4, 256 in 2 and 3 93.3 and 97.1, 300 in 1 and 2 138 and 115), one above 8,192.  Shorter rows gain nothing from three (400 events of 2,048 in 1 and 2
+// parts 73.6 and 83.3, 338 of 344 20.0 and 21.3).
 int kd_splits(int E, int K, int d) {
-    const int most = d > 8192 ? 256 : d > 2048 && d <= 4096 && E > 100 ? 768 : 512;
+    int most = d > 8192 ? 256 : 512;
+    if (d > 2048 && d <= 4096 && E > 100 && most / E * E < most - most / 7) most = 768;
     int s = most / E;
     if (s > K / 8) s = K / 8;
     return s < 1 ? 1 : s > 32 ? 32 : s;
 }
 
 hipError_t launch_kd(const KdArgs& a, hipStream_t stream) {
-    // (a row to a wavefront takes half the time of a row to a workgroup at 680 elements and a tenth less at 2,048; at 4,096 its sums and rows
-    // spill: 165 us for 192 events, 79.  Two rows of 4,096 under way beside two for three workgroups to a unit, four for two: 64 events 35.6 and 33.6)
+    // (a row to a wavefront takes a quarter of the time of a row to a workgroup at 680 elements, 548 events 47 and 179 us, and half at 2,048; at 4,096 its sums and rows
+    // spill: 165 us for 192 events, 79.  Two rows of 4,096 at a time, four where a part has 8 rows at most: one event 12.2 and 11.6, 48 events 28.4 and 29.9)
     const hipError_t e = a.d <= 512 ? rows_as<1, 8, false>(a, stream) : a.d <= 1024 ? rows_as<2, 4, false>(a, stream) : a.d <= 2048 ? rows_as<4, 2, false>(a, stream)
-                         : a.d <= 4096 ? (a.E <= 100 ? rows_as<2, 4, true>(a, stream) : rows_as<2, 2, true>(a, stream)) : a.d <= 8192 ? rows_as<4, 2, true>(a, stream) : rows_as<8, 1, true>(a, stream);
+                         : a.d <= 4096 ? (a.K <= 8 * a.splits ? rows_as<2, 4, true>(a, stream) : rows_as<2, 2, true>(a, stream)) : a.d <= 8192 ? rows_as<4, 2, true>(a, stream) : rows_as<8, 1, true>(a, stream);
     if (e != hipSuccess || a.splits == 1) return e;
     const int v = a.splits <= 8 ? 4 : 2;
     const dim3 grid((unsigned)a.E, (unsigned)(1 + (a.d + v * kThreads - 1) / (v * kThreads)));
