@@ -33,7 +33,8 @@ typedef struct evospec_lora {
  *   y         dev bf16 [T, d_out], rows y_stride elements apart, 16-B aligned; no overlap with x.  Rounded once.
  *   out_h     dev fp32 [r, T] or NULL: h = x A^T, transposed, for evospec_lora_backward; zeros in columns of rows without an
  *             adapter
- * Sums are fp32.  h goes into the second product as two bf16 numbers, which keep 2^-16 of it.
+ * Sums are fp32.  h goes into the second product as three bf16 numbers, which are all of its 24 bits.  (So a product of an infinity and a
+ * finite number may be NaN, not infinite; the same in the backward pass.)
  * T below 2^24, S at most 2^16, strides at most 2^26.
  */
 int evospec_lora_forward(const evospec_lora *lora, const void *x, long long x_stride, const int32_t *row_off,

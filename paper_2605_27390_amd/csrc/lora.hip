@@ -8,8 +8,9 @@
 // g A, the rows' elements in the gradients), a lane takes 2, 4 or 8 bytes of 8 neighbours along the summed axis and puts halves of
 // dwords together (one v_perm_b32 for two numbers): its 1, 2 or 4 columns belong to as many tiles, so that column RT m + j is
 // row m of tile j.  No LDS, and whole lines of memory.
-// h stays in fp32 between the kernels.  As an operand it is a sum of bf16 numbers, two (2^-16 of it) where the result is rounded to bf16,
-// three (all 24 bits) where the result is fp32.
+// h stays in fp32 between the kernels.  As an operand it is a sum of three bf16 numbers, which are all of its 24 bits.  (Two, cut off, leave up to
+// 2^-15 of it, always towards zero, which shows where ranks' shares of y cancel; y of 8,386 rows differed by 1.1e-4 of its size from fp32's, by 1.2e-5 now.  One row of
+// 4,096, rank 32, 7.1 -> 7.3 us, 8,386 rows of rank 16 51.0 -> 51.1; 9,229 of rank 32, backward, 110.7 -> 112.1.)
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -217,7 +218,7 @@ typedef const f32x4_u __attribute__((address_space(1))) * gfloat4;
 // DEEP, where tiles and slices leave a compute unit one workgroup at most: 8 wavefronts.  Else four workgroups of 4 to a unit (two of rank 40 and
 // more), so that some load while others store.  ONCE: y past the caches.
 template <int RT, int NT, bool BACK, bool DEEP, bool ONCE>
-__global__ __launch_bounds__(DEEP ? 512 : 256, RT == 4 ? 2 : 4) void lora_rows_kernel(LoraArgs a) {
+__global__ __launch_bounds__(DEEP ? 512 : 256, RT < 4 ? 4 : NT == 1 && !DEEP ? 3 : 2) void lora_rows_kernel(LoraArgs a) {
     constexpr int W = DEEP ? 8 : 4;
     constexpr int KS = (RT + 1) / 2;
     constexpr int kSets = BACK ? NT : NT + RT;                   // of 16 rows through LDS: x's, then A's
@@ -247,7 +248,7 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, RT == 4 ? 2 : 4) void lora_rows_k
         u32x4 w[BACK ? 1 : 2 * RT];
         u32x2 raw[BACK ? KS : 1][8];
     };
-    const gu16 w_up = (gu16)a.w_up + (long long)t.adapter * a.r * a.d_up;
+    const gu16 w_up = (gu16)a.w_up + (long long)__builtin_amdgcn_readfirstlane(t.adapter) * a.r * a.d_up;
     auto load_columns = [&](Columns& col, int g) {
         const int c = min(64 * g + 4 * m, a.d_up - 4);
 #pragma unroll
@@ -259,9 +260,12 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, RT == 4 ? 2 : 4) void lora_rows_k
             }
         if constexpr (BACK) {                                    // [r][d]
 #pragma unroll
-            for (int s = 0; s < KS; ++s)
+            for (int s = 0; s < KS; ++s) {
+                // (a uniform address and a lane's 32 bits of offset: 16 registers less than a place of its own for each load)
+                const uint32_t at = 2u * ((uint32_t)(32 * s + 8 * kg < a.r ? 32 * s + 8 * kg : 0) * (uint32_t)a.d_up + (uint32_t)c);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) col.raw[s][k] = *(gpair)(w_up + (long long)((32 * s + 8 * kg < a.r ? 32 * s + 8 * kg : 0) + k) * a.d_up + c);
+                for (int k = 0; k < 8; ++k) col.raw[s][k] = *(gpair)((gbyte)(w_up + (long long)k * a.d_up) + at);
+            }
         } else {                                                 // [d][r]: r / 8 KB
             const int pieces = min(64, a.d_up - 64 * g) * a.r / 8;
 #pragma unroll
@@ -427,7 +431,7 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, RT == 4 ? 2 : 4) void lora_rows_k
     }
     if (!a.y) return;
     lds_barrier();
-    u32x4 h[NT][KS][2];
+    u32x4 h[NT][KS][3];
 #pragma unroll
     for (int i = 0; i < NT; ++i)
 #pragma unroll
@@ -435,8 +439,8 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, RT == 4 ? 2 : 4) void lora_rows_k
             float v[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = 32 * s + 8 * kg < a.r ? hs[(32 * s + 8 * kg + k) % (16 * RT)][16 * i + m] : 0.f;
-            h[i][s][0] = next_part(v);
-            h[i][s][1] = next_part(v);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) h[i][s][k] = next_part(v);
         }
     // B's 16-byte pieces in LDS: number p, of column p / (r / 8), with its low 4 bits turned by what the columns of a read differ in
     const int turned = a.r > 32 ? 5 : 4, per = a.r / 8;
@@ -472,10 +476,9 @@ __global__ __launch_bounds__(DEEP ? 512 : 256, RT == 4 ? 2 : 4) void lora_rows_k
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int i = 0; i < NT; ++i) {
-                    acc[j][i] = mfma(h[i][s][0], op[j], acc[j][i]);
-                    acc[j][i] = mfma(h[i][s][1], op[j], acc[j][i]);
-                }
+                for (int i = 0; i < NT; ++i)
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) acc[j][i] = mfma(h[i][s][k], op[j], acc[j][i]);
         }
         const int c = 64 * g + 4 * m;
 #pragma unroll
