@@ -108,7 +108,7 @@ int evospec_adamw_blocks(const evospec_adamw_tensor *tensors /*host [count]*/, i
  *               EVOSPEC_MOMENTS_8BIT: m and v dev uint8 [blocks * 256], scales dev fp32 [blocks][2], of m and of v
  *   master      dev fp32 [blocks * 256] or NULL: what p is read from and written to; the parameters become its rounded values.
  *               NULL: p is the parameter.
- *   t           >= 1, the number of this step
+ *   t           >= 1, the number of this step            eps at least 2^-126, as fp32
  *   schedule    dev fp32 [2] or NULL: {lr, t} read on the GPU in place of the arguments, for a captured graph that is replayed
  *   grad_scale  dev fp32 [1] or NULL (1).  If it is infinite or NaN, the step changes nothing.
  * 8 bits: a value is code * scale, the scale of a block the least power of two from 2^-100 to 2^100 that takes its largest finite

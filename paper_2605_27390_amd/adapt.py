@@ -326,7 +326,7 @@ def adamw_step(opt: AdamW, lr: float, t: int, betas=(0.9, 0.999), eps: float = 1
                schedule=None, grad_scale=None) -> None:
     """Step number t (from 1 on) of AdamW with the gradients as they are in opt.grads.  grad_scale (fp32 [1] on the GPU) multiplies them, and a
     value that is infinite or NaN leaves everything as it is.  schedule (fp32 [2] on the GPU: lr, t) takes the place of the two
-    arguments, for a captured graph.  seed: moments of 8 bits are rounded at random, by a hash of seed, t and an element's place."""
+    arguments, for a captured graph.  eps: 2^-126 (1.2e-38) or more.  seed: moments of 8 bits are rounded at random, by a hash of seed, t and an element's place."""
     at, gs = _scalars(schedule, 2, "schedule", opt._device), _scalars(grad_scale, 1, "grad_scale", opt._device)
     _check(lib.evospec_adamw_step(opt._table, len(opt.params), *opt._types, *opt._buffers, lr, betas[0], betas[1], eps, weight_decay, t,
                                   seed & 0xffffffff, at, gs, _stream_of(opt._device)), "evospec_adamw_step")

@@ -2,6 +2,7 @@
 // and the launches.
 #include <hip/hip_runtime.h>
 
+#include <cfloat>
 #include <cmath>
 
 #include "adapt.hpp"
@@ -170,7 +171,8 @@ int evospec_adamw_step(const evospec_adamw_tensor* tensors, int count, int param
     if (param_type < EVOSPEC_BF16 || param_type > EVOSPEC_FP32 || (grad_type != param_type && grad_type != EVOSPEC_FP32) ||
         (kind != EVOSPEC_MOMENTS_FP32 && kind != EVOSPEC_MOMENTS_8BIT))
         return EVOSPEC_BAD_TYPE;
-    if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps > 0.0) || !std::isfinite(eps) || !std::isfinite(lr) ||
+    // (eps as the kernel has it: below the normal numbers its reciprocal is infinite, and an update of nothing, 0 x infinity, NaN)
+    if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !((float)eps >= FLT_MIN) || !std::isfinite((float)eps) || !std::isfinite(lr) ||
         !std::isfinite(weight_decay) || t < 1)
         return EVOSPEC_BAD_SHAPE;
     if (blocks == 0) return EVOSPEC_OK;

@@ -1,0 +1,15 @@
+"""Refusals of include/evospec_adapt.h at the ends of what fp32 holds, before anything touches the GPU."""
+import pytest
+
+from test_adapt_host import ev, step  # noqa: F401
+
+
+@pytest.mark.parametrize("eps", [1e-40, 1e-50, 1.17e-38, 5e-324, 3.5e38, 1e300])
+def test_eps_that_fp32_does_not_have(ev, eps):  # noqa: F811
+    """Its reciprocal would be infinite: elements that never had a gradient became 0 x infinity."""
+    assert step(ev, eps=eps) == 2
+
+
+def test_the_least_and_the_largest_eps(ev):  # noqa: F811
+    nothing = ((None, None, 0),)
+    assert step(ev, rows=nothing, eps=2.0 ** -126) == 0 and step(ev, rows=nothing, eps=3e38) == 0
