@@ -71,7 +71,8 @@ int evospec_lora_backward(const evospec_lora *lora, const void *x, long long x_s
  *   out_draft dev fp32 [E, K]: z, NaN where the entry is not in the support.  No output overlaps an input.
  *   workspace dev, 16-B aligned, at least evospec_kd_loss_workspace_bytes(E, K, d) bytes, scratch (fewer events can need more: their rows
  *             are split)
- * T > 0 and finite.  Logits and gradients are summed in fp32, the loss in 64 bits from the logits.  E < 2^20.
+ * T at least 2^-126 and finite.  Logits and gradients are summed in fp32, the loss in 64 bits from the logits.  A logit of -inf (a sum past fp32's range)
+ * is a share of zero; one of +inf makes its event's loss and gradient NaN.  E < 2^20.
  */
 #define EVOSPEC_KD_K_MAX 1024
 #define EVOSPEC_KD_D_MAX 16384

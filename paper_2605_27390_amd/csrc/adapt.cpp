@@ -141,7 +141,7 @@ int evospec_kd_loss(const void* h, int E, int d, const void* W_lm, int V, const 
     const int rc = check_kd(E, K, d);
     if (rc) return rc;
     if (type != EVOSPEC_BF16 && type != EVOSPEC_FP32) return EVOSPEC_BAD_TYPE;
-    if (V < 1 || !(T > 0.f) || !std::isfinite(T)) return EVOSPEC_BAD_SHAPE;
+    if (V < 1 || !(T >= FLT_MIN) || !std::isfinite(T)) return EVOSPEC_BAD_SHAPE;        // (1 / T is finite)
     if (E == 0) return EVOSPEC_OK;
     if (!h || !W_lm || !support || !target || !out_loss || !out_dh || !out_draft) return EVOSPEC_NULL_POINTER;
     if (!aligned(h, 16) || !aligned(W_lm, 16) || !aligned(out_dh, 16) || !aligned(workspace, 16)) return EVOSPEC_MISALIGNED;

@@ -8,6 +8,8 @@
 // registers.  The loss is taken from the K logits in 64 bits at the end: near its minimum it is a small difference of large terms.
 #include <hip/hip_runtime.h>
 
+#include <cfloat>
+
 #include "adapt.hpp"
 #include "common.hpp"
 
@@ -200,11 +202,13 @@ __device__ __forceinline__ float lane_sums(float (&dot)[RB], int lane) {
 }
 
 // Running sums of RB rows at a time.  A lane looks after the logit and weights of row `lane % RB` of a turn; all have the same m and l.
+// m is a logit, and distances from it are divided by T: logits over T have errors of their own size, or are infinite where T is small.  It begins
+// with the least finite number, so that a logit of -inf is a share of zero also before any other.
 template <int NC>
 struct Sums {
-    float m, l, o1[NC][8], o2[NC][8];
+    float m = -FLT_MAX, l = 0.f, o1[NC][8] = {}, o2[NC][8] = {};
     template <int RB>
-    __device__ __forceinline__ void add(const u32x4 (&row)[RB][NC], float x, bool mine, float p, int lane) {
+    __device__ __forceinline__ void add(const u32x4 (&row)[RB][NC], float x, bool mine, float p, float inv, int lane) {
         x = mine ? x : -__builtin_inff();
         float top = x;
         if constexpr (RB >= 2) top = fmaxf(top, __uint_as_float(xor_lane<1>(__float_as_uint(top), lane)));
@@ -212,7 +216,7 @@ struct Sums {
         if constexpr (RB >= 8) top = fmaxf(top, __uint_as_float(xor_lane<4>(__float_as_uint(top), lane)));
         top = fmaxf(top, m);
         if (__builtin_amdgcn_readfirstlane(top != m)) {          // (the same in all lanes)
-            const float back = expf(m - top);
+            const float back = expf((m - top) * inv);
             l *= back;
 #pragma unroll
             for (int c = 0; c < NC; ++c)
@@ -220,7 +224,7 @@ struct Sums {
                 for (int i = 0; i < 8; ++i) o1[c][i] *= back;
             m = top;
         }
-        const float q = mine ? expf(x - m) : 0.f, w = mine ? p : 0.f;
+        const float q = mine ? expf((x - m) * inv) : 0.f, w = mine ? p : 0.f;
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
             const float qr = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(q), r));
@@ -292,8 +296,7 @@ __global__ __launch_bounds__(kThreads, NC == 4 ? 2 : 4) void kd_rows_kernel(KdAr
         }
     };
     const bool none = entries_of(a, e, j0, n, sh, [&] { load(row, RB * wave); });
-    Sums<NC> s{};
-    s.m = -__builtin_inff();
+    Sums<NC> s;
     const int mod = lane & (RB - 1);
     auto add = [&](u32x4 (&row)[RB][NC], int at) {
         if (at >= n) return;                                     // (uniform)
@@ -303,7 +306,7 @@ __global__ __launch_bounds__(kThreads, NC == 4 ? 2 : 4) void kd_rows_kernel(KdAr
         const float x = lane_sums(dot, lane);
         const bool mine = sh.ids[at + mod] >= 0;
         if (lane < RB) sh.z[at + mod] = mine ? x : __builtin_nanf("");
-        s.add(row, x * inv, mine, sh.p[at + mod], lane);
+        s.add(row, x, mine, sh.p[at + mod], inv, lane);
     };
 #pragma unroll 1
     for (int at = RB * wave; at < n; at += RB * kWaves) {
@@ -313,13 +316,12 @@ __global__ __launch_bounds__(kThreads, NC == 4 ? 2 : 4) void kd_rows_kernel(KdAr
     // The wavefronts' sums: two give theirs to the other two, then one to the other.
     if (lane == 0) ml[wave] = make_float2(s.m, s.l);
     __syncthreads();
-    float m = -__builtin_inff(), l = 0.f;
+    float m = -FLT_MAX, l = 0.f;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) m = fmaxf(m, ml[w].x);
-    auto factor_of = [&](float2 x) { return x.y == 0.f && x.x == -__builtin_inff() ? 0.f : expf(x.x - m); };      // (0: no rows, sums of zero)
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) l += ml[w].y * factor_of(ml[w]);
-    const float mine = factor_of(make_float2(s.m, s.l));
+    for (int w = 0; w < kWaves; ++w) l += ml[w].y * expf((ml[w].x - m) * inv);
+    const float mine = expf((s.m - m) * inv);
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -395,8 +397,7 @@ __global__ __launch_bounds__(kThreads, NC * RB <= 4 ? 3 : 1) void kd_long_rows_k
         }
     };
     const bool none = entries_of(a, e, j0, n, sh, [&] { load(row, 0); });
-    Sums<NC> s{};
-    s.m = -__builtin_inff();
+    Sums<NC> s;
     const int mod = lane & (RB - 1);
     auto add = [&](u32x4 (&row)[RB][NC], int at, int turn) {
         zeros_in(row, sh, at, a.d % (8 * NC * kThreads) != 0, 8 * tid, 8 * kThreads, a.d);
@@ -410,7 +411,7 @@ __global__ __launch_bounds__(kThreads, NC * RB <= 4 ? 3 : 1) void kd_long_rows_k
         const float x = (d.x + d.y) + (d.z + d.w);
         const bool mine = sh.ids[at + mod] >= 0;
         if (tid < RB) sh.z[at + mod] = mine ? x : __builtin_nanf("");
-        s.add(row, x * inv, mine, sh.p[at + mod], lane);
+        s.add(row, x, mine, sh.p[at + mod], inv, lane);
     };
     // (the next rows are under way; one loop with rows handed on, not two rows' sets in turn: a launch has half the instructions to bring in.  192 events
     // 76.5 and 76.2 us, 300 123 and 115, 64 alike)
@@ -476,8 +477,7 @@ __global__ __launch_bounds__(kThreads) void kd_join_kernel(KdArgs a) {
     load(0);
     const float m = wave_max(mine.x, lane);
     const bool none = __ballot(mine.y == -1.f) != 0;
-    const bool empty = mine.y == 0.f && mine.x == -inf;          // a part without entries (its sums are zeros)
-    const float factor = empty ? 0.f : expf(mine.x - m);
+    const float factor = expf((mine.x - m) * (1.f / a.T));       // (a part without entries has sums of zero)
     const float l = wave_sum(mine.y * factor, lane);
     for (int s0 = 0;; load(s0)) {
 #pragma unroll

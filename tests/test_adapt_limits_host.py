@@ -1,7 +1,7 @@
 """Refusals of include/evospec_adapt.h at the ends of what fp32 holds, before anything touches the GPU."""
 import pytest
 
-from test_adapt_host import ev, step  # noqa: F401
+from test_adapt_host import ev, kd, step  # noqa: F401
 
 
 @pytest.mark.parametrize("eps", [1e-40, 1e-50, 1.17e-38, 5e-324, 3.5e38, 1e300])
@@ -13,3 +13,8 @@ def test_eps_that_fp32_does_not_have(ev, eps):  # noqa: F811
 def test_the_least_and_the_largest_eps(ev):  # noqa: F811
     nothing = ((None, None, 0),)
     assert step(ev, rows=nothing, eps=2.0 ** -126) == 0 and step(ev, rows=nothing, eps=3e38) == 0
+
+
+@pytest.mark.parametrize("T", [1e-39, 1e-45, 1.17e-38])
+def test_temperatures_whose_reciprocal_is_infinite(ev, T):  # noqa: F811
+    assert kd(ev, T=T) == 2 and kd(ev, T=2.0 ** -126, E=0) == 0 and kd(ev, T=3e38, E=0) == 0
