@@ -2,7 +2,9 @@
  * evospec_adapt.h -- what the draft model learns from the events that evospec_kl_gate admits (Path B of the EvoSpec paper,
  * Sec. "Online parameter update"): low-rank adapters beside a projection, forward and backward, for the requests of a batch
  * at once; the distillation loss on the retained support (Eq. 5) with its gradient; and an AdamW step over many tensors.
- * Conventions (errors, pointers, streams, workspaces) are those of evospec.h.
+ * Conventions (errors, pointers, streams, workspaces) are those of evospec.h.  What a call writes (outputs, tensors updated in place, its
+ * workspace) shares no memory with what it reads, nor one with another; rows of one buffer may lie between one another.  The entries below do not
+ * look for that; the Python binding does.
  */
 #ifndef EVOSPEC_ADAPT_H
 #define EVOSPEC_ADAPT_H

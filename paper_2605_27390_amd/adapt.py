@@ -91,6 +91,8 @@ class LoraBank:
                 raise ValueError("scale needs a value for every adapter")
         _lora_bytes(self.n, self.r, self.d_in, self.d_out, 0, 0)      # (refuses the sizes that no call takes)
         self._a, self._b, self._scale = a, b, scale
+        self._places = tuple(_place(t, n) for t, n in ((a, "the adapters' a"), (b, "the adapters' b"), (scale, "the adapters' scale")) if t is not None)
+        self._lo, self._hi = min(p[0] for p in self._places), max(p[1] for p in self._places)
         self._c = _Lora(a.data_ptr(), b.data_ptr(), _ptr(scale), self.n, self.r, self.d_in, self.d_out)
         self._ref = ctypes.byref(self._c)
 
@@ -128,14 +130,45 @@ def _rows_of(x, d, name, dev, T=None):
     return s[0] if x.size(0) > 1 else d
 
 
+# A place in memory: from, to, bytes of a row, bytes from one row to the next, name.
+def _place(t, name):
+    lo, n = t.data_ptr(), t.nbytes
+    return lo, lo + n, n, n, name
+
+
+def _meet(a, b):
+    """Whether two places share a byte.  Rows of one buffer may lie between one another; with different strides they are taken to meet."""
+    lo, hi, row, step, _ = a
+    at, end, other, per, _ = b
+    if lo >= end or at >= hi or lo == hi or at == end:
+        return False
+    if row == hi - lo:                                               # (one row)
+        if other == end - at:
+            return True
+        lo, row, step, at, other = at, other, per, lo, row
+    elif other != end - at and step != per:
+        return True
+    by = (at - lo) % step
+    return by < row or by + other > step
+
+
+def _refuse(out, *others):
+    """No byte of an output is one of an input, or of another output."""
+    lo, hi = out[0], out[1]
+    for x in others:
+        if x[0] < hi and lo < x[1] and _meet(out, x):
+            raise ValueError(f"{out[4]} overlaps {x[4]}")
+
+
 def _apart(out, rows, d, stride, name, x, dx, stride_x, other):
-    """Refuses an output [rows, d] some of whose elements are those of an input [rows, dx]: rows of one buffer may lie between one another.
-    (Strides in elements of bf16; a row's own length where there is one row.)"""
-    lo, a = out.data_ptr(), x.data_ptr()
-    if a < lo + 2 * ((rows - 1) * stride + d) and lo < a + 2 * ((rows - 1) * stride_x + dx) and rows:
-        by = (a - lo) % (2 * stride)
-        if rows == 1 or stride != stride_x or by < 2 * d or by + 2 * dx > 2 * stride:
-            raise ValueError(f"{name} overlaps {other}")
+    """Refuses an output [rows, d] some of whose elements are those of an input [rows, dx], both in bf16.  (Strides in elements; a row's own length
+    where there is one row.)"""
+    _refuse(_rows_place(out, rows, d, stride, name), _rows_place(x, rows, dx, stride_x, other))
+
+
+def _rows_place(x, rows, d, stride, name):
+    lo = x.data_ptr()
+    return lo, lo + 2 * ((rows - 1) * stride + d) if rows else lo, 2 * d, 2 * stride, name
 
 
 def lora_forward(x, bank: LoraBank, row_off, adapter, y, keep: bool = False, out_h=None):
@@ -148,15 +181,23 @@ def lora_forward(x, bank: LoraBank, row_off, adapter, y, keep: bool = False, out
     xs = _rows_of(x, bank.d_in, "x", dev)
     T = x.size(0)
     ys = _rows_of(y, bank.d_out, "y", dev, T)
-    _apart(y, T, bank.d_out, ys, "y", x, bank.d_in, xs, "x")
+    px, py, po, pa = x.data_ptr(), y.data_ptr(), row_off.data_ptr(), adapter.data_ptr()
+    end = py + 2 * ((T - 1) * ys + bank.d_out)
+    # (written out: a function for each check costs as much as all of them)
+    if out_h is not None or (px < end and py < px + 2 * ((T - 1) * xs + bank.d_in)) or (bank._lo < end and py < bank._hi) or po < end and py < po + 4 * S + 4 \
+            or pa < end and py < pa + 4 * S:
+        mine = _rows_place(x, T, bank.d_in, xs, "x"), _place(row_off, "row_off"), _place(adapter, "adapter"), *bank._places
+        out = _rows_place(y, T, bank.d_out, ys, "y")
+        _refuse(out, *mine)
     if out_h is not None:
         _expect(out_h, _f32, "out_h", 2)
         _elsewhere(out_h, dev, "out_h")
         if tuple(out_h.shape) != (bank.r, T):
             raise ValueError(f"out_h must be [{bank.r}, {T}], got {tuple(out_h.shape)}")
+        _refuse(_place(out_h, "out_h"), out, *mine)
     elif keep:
         out_h = _new((bank.r, T), (T, 1), dtype=_f32, device=x.device)
-    _check(lib.evospec_lora_forward(bank._ref, x.data_ptr(), xs, row_off.data_ptr(), adapter.data_ptr(), S, T, y.data_ptr(), ys,
+    _check(lib.evospec_lora_forward(bank._ref, px, xs, po, pa, S, T, py, ys,
                                     _ptr(out_h), _stream_of(dev)), "evospec_lora_forward")
     return y if out_h is None else out_h
 
@@ -177,13 +218,26 @@ def lora_backward(x, dy, bank: LoraBank, row_off, adapter, h=None, dx=None, out_
     ds = 0
     if dx is not None:
         ds = _rows_of(dx, bank.d_in, "dx", dev, T)
-        _apart(dx, T, bank.d_in, ds, "dx", x, bank.d_in, xs, "x")
-        _apart(dx, T, bank.d_in, ds, "dx", dy, bank.d_out, gs, "dy")
     if h is not None:
         _expect(h, _f32, "h", 2)
         _elsewhere(h, dev, "h")
         if tuple(h.shape) != (bank.r, T):
             raise ValueError(f"h must be [{bank.r}, {T}], got {tuple(h.shape)}")
+    px, pg, po, pa = x.data_ptr(), dy.data_ptr(), row_off.data_ptr(), adapter.data_ptr()
+    near = out_da is not None or out_db is not None or workspace is not None
+    if dx is not None and not near:
+        at = dx.data_ptr()
+        end = at + 2 * ((T - 1) * ds + bank.d_in)
+        near = (px < end and at < px + 2 * ((T - 1) * xs + bank.d_in)) or (pg < end and at < pg + 2 * ((T - 1) * gs + bank.d_out)) or (bank._lo < end and at < bank._hi) \
+            or po < end and at < po + 4 * S + 4 or pa < end and at < pa + 4 * S or h is not None and h.data_ptr() < end and at < h.data_ptr() + 4 * bank.r * T
+    if near:
+        mine = [_rows_place(x, T, bank.d_in, xs, "x"), _rows_place(dy, T, bank.d_out, gs, "dy"), _place(row_off, "row_off"), _place(adapter, "adapter"), *bank._places]
+        if h is not None:
+            mine.append(_place(h, "h"))
+        if dx is not None:
+            out = _rows_place(dx, T, bank.d_in, ds, "dx")
+            _refuse(out, *mine)
+            mine.append(out)
     if out_da is not None or out_db is not None:
         for t, shape, name in ((out_da, (bank.n, bank.r, bank.d_in), "out_da"), (out_db, (bank.n, bank.d_out, bank.r), "out_db")):
             if t is not None:
@@ -191,12 +245,19 @@ def lora_backward(x, dy, bank: LoraBank, row_off, adapter, h=None, dx=None, out_
                 _elsewhere(t, dev, name)
                 if tuple(t.shape) != shape:
                     raise ValueError(f"{name} must be {shape}, got {tuple(t.shape)}")
+                out = _place(t, name)
+                _refuse(out, *mine)
+                mine.append(out)
+    if workspace is not None:
+        workspace = _workspace_of(workspace, 0, dev, None)
+        _refuse(_place(workspace, "workspace"), *mine)
     if out_da is None:
         out_da = _new((bank.n, bank.r, bank.d_in), (bank.r * bank.d_in, bank.d_in, 1), dtype=_f32, device=x.device)
     if out_db is None:
         out_db = _new((bank.n, bank.d_out, bank.r), (bank.r * bank.d_out, bank.r, 1), dtype=_f32, device=x.device)
-    workspace = _workspace_of(workspace, _lora_bytes(bank.n, bank.r, bank.d_in, bank.d_out, S, T), dev, x.device)
-    _check(lib.evospec_lora_backward(bank._ref, x.data_ptr(), xs, _ptr(h), dy.data_ptr(), gs, row_off.data_ptr(), adapter.data_ptr(), S, T,
+    if workspace is None:
+        workspace = _workspace_of(None, _lora_bytes(bank.n, bank.r, bank.d_in, bank.d_out, S, T), dev, x.device)
+    _check(lib.evospec_lora_backward(bank._ref, px, xs, _ptr(h), pg, gs, po, pa, S, T,
                                      _ptr(dx), ds, out_da.data_ptr(), out_db.data_ptr(), _ptr(workspace),
                                      0 if workspace is None else workspace.numel(), _stream_of(dev)), "evospec_lora_backward")
     return out_da, out_db
@@ -230,23 +291,42 @@ def kd_loss(h, W_lm, support, target, weight=None, T: float = 1.0, dtype=torch.b
         _elsewhere(weight, dev, "weight")
         if weight.numel() != E:
             raise ValueError("weight needs a value for every event")
-    for t, kind, shape, name in ((out_loss, _f32, (E,), "out_loss"), (out_dh, dtype, (E, d), "out_dh"), (out_draft, _f32, (E, K), "out_draft")):
-        if t is not None:
-            _expect(t, kind, name, len(shape))
-            _elsewhere(t, dev, name)
-            if tuple(t.shape) != shape:
-                raise ValueError(f"{name} must be {shape}, got {tuple(t.shape)}")
-            for x, other in ((h, "h"), (W_lm, "W_lm"), (support, "support"), (target, "target"), (weight, "weight")):
-                if x is not None and t.data_ptr() < x.data_ptr() + x.nbytes and x.data_ptr() < t.data_ptr() + t.nbytes:
-                    raise ValueError(f"{name} overlaps {other}")
+    if out_loss is not None or out_dh is not None or out_draft is not None or workspace is not None:
+        mine = [_place(t, n) for t, n in ((h, "h"), (W_lm, "W_lm"), (support, "support"), (target, "target"), (weight, "weight")) if t is not None]
+        for t, kind, shape, name in ((out_loss, _f32, (E,), "out_loss"), (out_dh, dtype, (E, d), "out_dh"), (out_draft, _f32, (E, K), "out_draft")):
+            if t is not None:
+                _expect(t, kind, name, len(shape))
+                _elsewhere(t, dev, name)
+                if tuple(t.shape) != shape:
+                    raise ValueError(f"{name} must be {shape}, got {tuple(t.shape)}")
+                out = _place(t, name)
+                _refuse(out, *mine)
+                mine.append(out)
+        if workspace is not None:
+            workspace = _workspace_of(workspace, 0, dev, None)
+            _refuse(_place(workspace, "workspace"), *mine)
     out_loss = _new((E,), (1,), dtype=_f32, device=h.device) if out_loss is None else out_loss
     out_dh = _new((E, d), (d, 1), dtype=dtype, device=h.device) if out_dh is None else out_dh
     out_draft = _new((E, K), (K, 1), dtype=_f32, device=h.device) if out_draft is None else out_draft
-    workspace = _workspace_of(workspace, _kd_bytes(E, K, d), dev, h.device)
+    if workspace is None:
+        workspace = _workspace_of(None, _kd_bytes(E, K, d), dev, h.device)
     _check(lib.evospec_kd_loss(h.data_ptr(), E, d, W_lm.data_ptr(), W_lm.shape[0], support.data_ptr(), target.data_ptr(), _ptr(weight), K, T,
                                _TYPES[dtype], out_loss.data_ptr(), out_dh.data_ptr(), out_draft.data_ptr(), _ptr(workspace),
                                0 if workspace is None else workspace.numel(), _stream_of(dev)), "evospec_kd_loss")
     return out_loss, out_dh, out_draft
+
+
+def _refuse_all(written, read):
+    """No byte of what is written is another's, among many places without gaps."""
+    end = last = 0                                                   # of all places so far, and of those that are written
+    by = of = None
+    for place, writes in sorted([(p, True) for p in written if p[2]] + [(p, False) for p in read if p[2]], key=lambda x: x[0][0]):
+        if place[0] < (end if writes else last):
+            raise ValueError(f"{(by if writes else of)[4]} overlaps {place[4]}")
+        if place[1] > end:
+            end, by = place[1], place
+        if writes and place[1] > last:
+            last, of = place[1], place
 
 
 class AdamW:
@@ -255,7 +335,7 @@ class AdamW:
     tensors follow one another, each from a multiple of 256 elements on: m and v (fp32, or uint8 codes with scales fp32 [blocks, 2]).
     master: True or a flat fp32 buffer, from which parameters of 16 bits are rounded; True takes the parameters as they are now.
     Buffers that are not given are allocated here, as zeros.  `offsets` says where each tensor begins.  The handle keeps the tensors and their
-    addresses: their memory must stay theirs (no `.data = ...`, no `set_`), and parameters must not share any.  A state that was saved is copied
+    addresses: their memory must stay theirs (no `.data = ...`, no `set_`), and what a step writes must not share any with the rest.  A state that was saved is copied
     into m, v, scales and master."""
     params, grads, m, v, scales, master = (_fixed("_" + n) for n in ("params", "grads", "m", "v", "scales", "master"))
 
@@ -304,6 +384,9 @@ class AdamW:
                 if tuple(t.shape) != shape:
                     raise ValueError(f"{name} must be {shape}, got {tuple(t.shape)}")
             setattr(self, "_" + name, t)
+        written = [_place(p, f"params[{i}]") for i, p in enumerate(params)] + [
+            _place(t, n) for t, n in ((self.m, "m"), (self.v, "v"), (self.scales, "scales"), (self.master, "master")) if t is not None]
+        _refuse_all(written, [_place(g, f"grads[{i}]") for i, g in enumerate(grads)])
         if master is True:
             for p, o in zip(params, self.offsets):
                 self.master[o:o + p.numel()] = p.detach().reshape(-1)
@@ -339,12 +422,16 @@ def adamw_moments(opt: AdamW, dtype=torch.bfloat16, out_m=None, out_v=None):
     if dtype not in (_bf16, _f32):
         raise TypeError(f"dtype must be {_bf16} or {_f32}")
     n = opt.blocks * ADAMW_BLOCK
+    mine = [] if out_m is None and out_v is None else [_place(t, name) for t, name in ((opt.m, "m"), (opt.v, "v"), (opt.scales, "scales"))]
     for t, name in ((out_m, "out_m"), (out_v, "out_v")):
         if t is not None:
             _expect(t, dtype, name, 1)
             _elsewhere(t, opt._device, name)
             if t.numel() != n:
                 raise ValueError(f"{name} must have {n} elements")
+            out = _place(t, name)
+            _refuse(out, *mine)
+            mine.append(out)
     out_m = _new((n,), (1,), dtype=dtype, device=opt.m.device) if out_m is None else out_m
     out_v = _new((n,), (1,), dtype=dtype, device=opt.m.device) if out_v is None else out_v
     _check(lib.evospec_adamw_moments(opt._buffers[0], opt._buffers[1], opt._buffers[2], opt.blocks, _TYPES[dtype], out_m.data_ptr(),
