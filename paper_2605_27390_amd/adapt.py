@@ -1,12 +1,14 @@
 """ctypes binding of include/evospec_adapt.h: low-rank adapters of many requests, the distillation loss on the retained support and
 AdamW.  Argument marshalling only; tensors are torch tensors on the GPU, work goes to torch's current HIP stream.  Gradients are outputs of
-the calls: nothing here takes part in autograd."""
+the calls: nothing here takes part in autograd.  What a call changes in place is a new version to torch, so that a graph that saved the old one says so,
+and y, dx or an output that requires a gradient is refused while gradients are recorded, since what the call adds would be missing from them."""
 from __future__ import annotations
 
 import ctypes
 import functools
 
 import torch
+from torch.autograd.graph import increment_version as _changed
 
 from .binding import _check, _expect, _ptr, lib
 from .decode import _TYPES, _elsewhere, _new, _stream_of
@@ -62,6 +64,12 @@ def _workspace_of(workspace, need, dev, device):
         _elsewhere(workspace, dev, "workspace")
         return workspace
     return _new((need,), (1,), dtype=torch.uint8, device=device) if need else None
+
+
+def _recorded(t, name):
+    """Refuses a tensor that is written where torch records gradients and t has one."""
+    if torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient, and the call takes no part in autograd: detach it, or call under torch.no_grad()")
 
 
 def _fixed(name):
@@ -181,6 +189,8 @@ def lora_forward(x, bank: LoraBank, row_off, adapter, y, keep: bool = False, out
     xs = _rows_of(x, bank.d_in, "x", dev)
     T = x.size(0)
     ys = _rows_of(y, bank.d_out, "y", dev, T)
+    if y.requires_grad:
+        _recorded(y, "y")
     px, py, po, pa = x.data_ptr(), y.data_ptr(), row_off.data_ptr(), adapter.data_ptr()
     end = py + 2 * ((T - 1) * ys + bank.d_out)
     # (written out: a function for each check costs as much as all of them)
@@ -195,10 +205,14 @@ def lora_forward(x, bank: LoraBank, row_off, adapter, y, keep: bool = False, out
         if tuple(out_h.shape) != (bank.r, T):
             raise ValueError(f"out_h must be [{bank.r}, {T}], got {tuple(out_h.shape)}")
         _refuse(_place(out_h, "out_h"), out, *mine)
+        if out_h.requires_grad:
+            _recorded(out_h, "out_h")
+        _changed(out_h)
     elif keep:
         out_h = _new((bank.r, T), (T, 1), dtype=_f32, device=x.device)
     _check(lib.evospec_lora_forward(bank._ref, px, xs, po, pa, S, T, py, ys,
                                     _ptr(out_h), _stream_of(dev)), "evospec_lora_forward")
+    _changed(y)
     return y if out_h is None else out_h
 
 
@@ -218,6 +232,8 @@ def lora_backward(x, dy, bank: LoraBank, row_off, adapter, h=None, dx=None, out_
     ds = 0
     if dx is not None:
         ds = _rows_of(dx, bank.d_in, "dx", dev, T)
+        if dx.requires_grad:
+            _recorded(dx, "dx")
     if h is not None:
         _expect(h, _f32, "h", 2)
         _elsewhere(h, dev, "h")
@@ -248,6 +264,9 @@ def lora_backward(x, dy, bank: LoraBank, row_off, adapter, h=None, dx=None, out_
                 out = _place(t, name)
                 _refuse(out, *mine)
                 mine.append(out)
+                if t.requires_grad:
+                    _recorded(t, name)
+                _changed(t)
     if workspace is not None:
         workspace = _workspace_of(workspace, 0, dev, None)
         _refuse(_place(workspace, "workspace"), *mine)
@@ -260,6 +279,8 @@ def lora_backward(x, dy, bank: LoraBank, row_off, adapter, h=None, dx=None, out_
     _check(lib.evospec_lora_backward(bank._ref, px, xs, _ptr(h), pg, gs, po, pa, S, T,
                                      _ptr(dx), ds, out_da.data_ptr(), out_db.data_ptr(), _ptr(workspace),
                                      0 if workspace is None else workspace.numel(), _stream_of(dev)), "evospec_lora_backward")
+    if dx is not None:
+        _changed(dx)
     return out_da, out_db
 
 
@@ -302,6 +323,9 @@ def kd_loss(h, W_lm, support, target, weight=None, T: float = 1.0, dtype=torch.b
                 out = _place(t, name)
                 _refuse(out, *mine)
                 mine.append(out)
+                if t.requires_grad:
+                    _recorded(t, name)
+                _changed(t)
         if workspace is not None:
             workspace = _workspace_of(workspace, 0, dev, None)
             _refuse(_place(workspace, "workspace"), *mine)
@@ -392,17 +416,16 @@ class AdamW:
                 self.master[o:o + p.numel()] = p.detach().reshape(-1)
         self._params, self._grads = tuple(params), tuple(grads)
         self._table, self._types = table, (_TYPES[kind], _TYPES[gkind], _MOMENTS[state])
+        self._written = [*params, *(t for t in (self.m, self.v, self.scales, self.master) if t is not None)]
         self._buffers = (self.m.data_ptr(), self.v.data_ptr(), _ptr(self.scales), _ptr(self.master))
 
 
 def _scalars(t, n, name, dev):
-    if t is not None:
-        _expect(t, _f32, name, 1)
-        _elsewhere(t, dev, name)
-        if t.numel() != n:
-            raise ValueError(f"{name} must have {n} elements")
-        return t.data_ptr()
-    return None
+    _expect(t, _f32, name, 1)
+    _elsewhere(t, dev, name)
+    if t.numel() != n:
+        raise ValueError(f"{name} must have {n} elements")
+    return t.data_ptr()
 
 
 def adamw_step(opt: AdamW, lr: float, t: int, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01, seed: int = 0,
@@ -410,9 +433,11 @@ def adamw_step(opt: AdamW, lr: float, t: int, betas=(0.9, 0.999), eps: float = 1
     """Step number t (from 1 on) of AdamW with the gradients as they are in opt.grads.  grad_scale (fp32 [1] on the GPU) multiplies them, and a
     value that is infinite or NaN leaves everything as it is.  schedule (fp32 [2] on the GPU: lr, t) takes the place of the two
     arguments, for a captured graph.  eps: 2^-126 (1.2e-38) or more.  seed: moments of 8 bits are rounded at random, by a hash of seed, t and an element's place."""
-    at, gs = _scalars(schedule, 2, "schedule", opt._device), _scalars(grad_scale, 1, "grad_scale", opt._device)
-    _check(lib.evospec_adamw_step(opt._table, len(opt.params), *opt._types, *opt._buffers, lr, betas[0], betas[1], eps, weight_decay, t,
+    at = None if schedule is None else _scalars(schedule, 2, "schedule", opt._device)
+    gs = None if grad_scale is None else _scalars(grad_scale, 1, "grad_scale", opt._device)
+    _check(lib.evospec_adamw_step(opt._table, len(opt._params), *opt._types, *opt._buffers, lr, betas[0], betas[1], eps, weight_decay, t,
                                   seed & 0xffffffff, at, gs, _stream_of(opt._device)), "evospec_adamw_step")
+    _changed(opt._written)
 
 
 def adamw_moments(opt: AdamW, dtype=torch.bfloat16, out_m=None, out_v=None):
@@ -432,6 +457,9 @@ def adamw_moments(opt: AdamW, dtype=torch.bfloat16, out_m=None, out_v=None):
             out = _place(t, name)
             _refuse(out, *mine)
             mine.append(out)
+            if t.requires_grad:
+                _recorded(t, name)
+            _changed(t)
     out_m = _new((n,), (1,), dtype=dtype, device=opt.m.device) if out_m is None else out_m
     out_v = _new((n,), (1,), dtype=dtype, device=opt.m.device) if out_v is None else out_v
     _check(lib.evospec_adamw_moments(opt._buffers[0], opt._buffers[1], opt._buffers[2], opt.blocks, _TYPES[dtype], out_m.data_ptr(),
