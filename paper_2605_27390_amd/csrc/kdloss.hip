@@ -273,7 +273,8 @@ __device__ __forceinline__ void zeros_in(u32x4 (&row)[RB][NC], const Entries& sh
 }
 
 // Rows of up to 512 NC elements: one to a wavefront, RB at a time; the wavefronts meet at the end.  The other wavefronts' loads are enough: with the next
-// rows under way 842 events of 656 elements take 63.8 us, 59.7 without, 400 of 2,048 74.5 and 70.5 (900 of 128 rows 79.4 and 82.9).
+// rows under way 842 events of 656 elements take 63.8 us, 59.7 without, 400 of 2,048 74.5 and 70.5 (900 of 128 rows 79.4 and 82.9).  Of 513 to 1,024 elements with a
+// gradient in bf16 two registers do not fit the four wavefronts to a SIMD and are kept in memory (outside the loop).
 template <int NC, int RB, int TYPE>
 __global__ __launch_bounds__(kThreads, NC == 4 ? 2 : 4) void kd_rows_kernel(KdArgs a) {
     __shared__ Entries sh;
@@ -414,7 +415,7 @@ __global__ __launch_bounds__(kThreads, NC * RB <= 4 ? 3 : 1) void kd_long_rows_k
         s.add(row, x, mine, sh.p[at + mod], inv, lane);
     };
     // (the next rows are under way; one loop with rows handed on, not two rows' sets in turn: a launch has half the instructions to bring in.  192 events
-    // 76.5 and 76.2 us, 300 123 and 115, 64 alike)
+    // 76.5 and 76.2 us, 300 123 and 115, 64 alike; here and below the launches alone, one after the other: in a pass over other inputs each time 192 events take 79)
 #pragma unroll 1
     for (int at = 0, turn = 0; at < n; at += RB, turn ^= 1) {
         load(next, at + RB);
@@ -523,13 +524,19 @@ hipError_t rows_as(const KdArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-// An event's rows are split until the parts come to one round of workgroups, two to a compute unit; three where two leave a seventh of the card empty and
-// rows have 2,048 to 4,096 elements (256 rows of 4,096; 110 events in 4 and 6 parts 45.7 and 50.4 us, 150 in 3 and 5 59.0 and 63.4, 192 in 2 and 4 79.8
-// and 76.4, 256 in 2 and 3 93.3 and 97.1, 300 in 1 and 2 138 and 115), one above 8,192.  Shorter rows gain nothing from three (400 events of 2,048 in 1 and 2
-// parts 73.6 and 83.3, 338 of 344 20.0 and 21.3).
+// An event's rows are split until the parts come to one round of workgroups, two to a compute unit, one above 8,192 elements.  Three to a unit where rows
+// have 2,048 to 4,096 elements and two would leave a seventh of the card empty; of more than 3,600, where it takes more than four parts, which have to be joined, a
+// fifth.  256 rows, us with two and with three:
+//             109 events in 4 and 7 parts   129 in 3 and 5   146 in 3 and 5   192 in 2 and 4   205 in 2 and 3
+//   of 3,200          44.6   39.8             55.7   47.4      56.3   49.2      79.0   59.5      79.6   70.2
+//   of 3,600          45.5   45.4             56.8   51.0      57.7   55.6      80.7   67.9      81.4   74.0
+//   of 3,800          46.1   47.3             57.2   53.6      58.7   59.0      81.6   71.7      82.3   78.1
+//   of 4,096          45.7   49.7             56.3   56.1      58.4   61.7      80.5   76.4      82.1   82.5
+// (of 4,096, 102 events in 4 and 5 44.8 and 44.1, 256 in 2 and 3 93.3 and 97.1, 300 in 1 and 2 139 and 115, 400 143 and 159.)  Shorter rows gain nothing from three (400
+// events of 2,048 in 1 and 2 parts 73.6 and 83.3, 338 of 344 20.0 and 21.3).
 int kd_splits(int E, int K, int d) {
     int most = d > 8192 ? 256 : 512;
-    if (d > 2048 && d <= 4096 && E > 100 && most / E * E < most - most / 7) most = 768;
+    if (d > 2048 && d <= 4096 && E > 100 && most / E * E < most - most / (d > 3600 && 768 / E > 4 ? 5 : 7)) most = 768;
     int s = most / E;
     if (s > K / 8) s = K / 8;
     return s < 1 ? 1 : s > 32 ? 32 : s;
