@@ -95,7 +95,7 @@ typedef struct evospec_adamw_tensor {
 } evospec_adamw_tensor;
 
 /*
- * Blocks of EVOSPEC_ADAMW_BLOCK elements of the flat buffers below, in which the tensors follow one another, each from a block
+ * (A tensor has at most 2^33 elements.)  Blocks of EVOSPEC_ADAMW_BLOCK elements of the flat buffers below, in which the tensors follow one another, each from a block
  * of its own on (elements behind a tensor's last are zeros once a step has run).
  */
 int evospec_adamw_blocks(const evospec_adamw_tensor *tensors /*host [count]*/, int count, long long *out_blocks /*host*/);

@@ -311,11 +311,18 @@ hipError_t launch_adamw(const evospec_adamw_tensor* tensors, int count, int para
 
 hipError_t launch_adamw_moments(const void* m, const void* v, const float* scales, long long blocks, int type, void* out_m, void* out_v,
                                 hipStream_t stream) {
-    const dim3 grid((unsigned)((blocks + kWaves - 1) / kWaves));
-    const float2* s = reinterpret_cast<const float2*>(scales);
-    if (type == EVOSPEC_FP32) adamw_moments_kernel<EVOSPEC_FP32><<<grid, kThreads, 0, stream>>>((const uint8_t*)m, (const uint8_t*)v, s, blocks, out_m, out_v);
-    else adamw_moments_kernel<EVOSPEC_BF16><<<grid, kThreads, 0, stream>>>((const uint8_t*)m, (const uint8_t*)v, s, blocks, out_m, out_v);
-    return hipGetLastError();
+    constexpr long long kMost = 1ll << 25;                       // (a launch has fewer than 2^32 threads)
+    for (long long at = 0; at < blocks; at += kMost) {
+        const long long count = std::min(blocks - at, kMost), place = at * kBlock;
+        const dim3 grid((unsigned)((count + kWaves - 1) / kWaves));
+        const float2* s = reinterpret_cast<const float2*>(scales) + at;
+        const uint8_t *cm = (const uint8_t*)m + place, *cv = (const uint8_t*)v + place;
+        if (type == EVOSPEC_FP32) adamw_moments_kernel<EVOSPEC_FP32><<<grid, kThreads, 0, stream>>>(cm, cv, s, count, (float*)out_m + place, (float*)out_v + place);
+        else adamw_moments_kernel<EVOSPEC_BF16><<<grid, kThreads, 0, stream>>>(cm, cv, s, count, (__bf16*)out_m + place, (__bf16*)out_v + place);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace evospec

@@ -201,7 +201,7 @@ int evospec_adamw_step(const evospec_adamw_tensor* tensors, int count, int param
 int evospec_adamw_moments(const void* m, const void* v, const float* scales, long long blocks, int type, void* out_m, void* out_v,
                           void* stream) {
     if (type != EVOSPEC_BF16 && type != EVOSPEC_FP32) return EVOSPEC_BAD_TYPE;
-    if (blocks < 0 || blocks > (1ll << 25)) return EVOSPEC_BAD_SHAPE;
+    if (blocks < 0 || blocks > (1ll << 40)) return EVOSPEC_BAD_SHAPE;
     if (blocks == 0) return EVOSPEC_OK;
     if (!m || !v || !scales || !out_m || !out_v) return EVOSPEC_NULL_POINTER;
     if (!aligned(m, 16) || !aligned(v, 16) || !aligned(scales, 8) || !aligned(out_m, 16) || !aligned(out_v, 16)) return EVOSPEC_MISALIGNED;
