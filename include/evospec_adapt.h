@@ -66,14 +66,15 @@ int evospec_lora_backward(const evospec_lora *lora, const void *x, long long x_s
  * p = softmax(target[e] / T) and q = softmax(z / T) over the event's support:
  *   loss[e] = weight[e] T^2 sum_j p_j (log p_j - log q_j)          d loss[e] / d h[e] = weight[e] T sum_j (q_j - p_j) W_lm[support[e, j]]
  * An entry whose id is not in [0, V) is not in the support (evospec_kl_gate leaves -1).  An event without an entry, or whose
- * target logits are all -inf, has loss 0 and gradient 0; a NaN among an event's numbers makes both NaN.
+ * target logits are all -inf, has loss 0 and gradient 0; a NaN among another event's numbers makes both NaN.
  *   h         dev bf16 [E, d]         W_lm dev bf16 [V, d], both 16-B aligned; d a multiple of 8, at most EVOSPEC_KD_D_MAX
  *   support   dev int32 [E, K], K at most EVOSPEC_KD_K_MAX         target dev fp32 [E, K]         weight dev fp32 [E] or NULL (1)
  *   out_loss  dev fp32 [E]            out_dh dev `type` (EVOSPEC_BF16 or EVOSPEC_FP32) [E, d], 16-B aligned
  *   out_draft dev fp32 [E, K]: z, NaN where the entry is not in the support.  No output overlaps an input.
  *   workspace dev, 16-B aligned, at least evospec_kd_loss_workspace_bytes(E, K, d) bytes, scratch (fewer events can need more: their rows
  *             are split)
- * T at least 2^-126 and finite.  Logits and gradients are summed in fp32, the loss in 64 bits from the logits.  A logit of -inf (a sum past fp32's range)
+ * T at least 2^-126 and finite.  Logits and gradients are summed in fp32, the loss in 64 bits from the logits.  (The gradient
+ * is a difference of two such sums: its error is relative to sum (p + q) |W|, also where p is nearly q.)  A logit of -inf (a sum past fp32's range)
  * is a share of zero; one of +inf makes its event's loss and gradient NaN.  E < 2^20.
  */
 #define EVOSPEC_KD_K_MAX 1024
@@ -104,8 +105,8 @@ int evospec_adamw_blocks(const evospec_adamw_tensor *tensors /*host [count]*/, i
  * One step of AdamW over `count` tensors, for every element, with g = grad * grad_scale:
  *   m = beta1 m + (1 - beta1) g      v = beta2 v + (1 - beta2) g^2
  *   p = p (1 - lr weight_decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
- * in fp32, from the moments before they are rounded.  (A v below 2^-126 may count as 0.)  The moments' products and sums are rounded one by one,
- * so that their codes are the same wherever the formulas are computed in that order.
+ * in fp32, from the moments before they are rounded.  (A v below 2^-126 may count as 0; root and reciprocal are right to about the last bit.)
+ * The moments' products and sums are rounded one by one, so that their codes are the same wherever the formulas are computed in that order.
  *   param_type  of all parameters (fp16, bf16, fp32); grad_type: the same, or EVOSPEC_FP32
  *   kind        EVOSPEC_MOMENTS_FP32: m and v dev fp32 [blocks * 256], scales NULL
  *               EVOSPEC_MOMENTS_8BIT: m and v dev uint8 [blocks * 256], scales dev fp32 [blocks][2], of m and of v

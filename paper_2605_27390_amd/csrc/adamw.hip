@@ -3,7 +3,7 @@
 // Every element is read and written once: 22 bytes with moments in 32 bits beside bf16 parameters, 10 with 8 bits.  A wavefront has
 // blocks of 256 elements, 4 in a row to a lane, so that the largest magnitude of a block is a reduction within it.  Addresses
 // of up to kTensors tensors go along with the launch itself; a wavefront finds its block's tensor by one comparison in every lane.
-// Measured, bf16: 134 million elements with 32 bits 546 us (5.4 TB/s, a copy's rate), with 8 bits 293 us (4.6 TB/s: some 60 vector instructions
+// Measured, bf16: 134 million elements with 32 bits 546 us (5.4 TB/s; a copy of 1 GiB reaches 5.14), with 8 bits 293 us (4.6 TB/s: some 60 vector instructions
 // an element, half of them the rounding's hash and codes, are nearly as long), with 8 bits and masters 370 us (5.8 TB/s).
 #include <hip/hip_runtime.h>
 
